@@ -306,6 +306,107 @@ pq_status pq_rope_kv4_append(pq_ctx* ctx, const pq_kv4_cache* cache, int32_t seq
                              double theta, int32_t rotate, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Paged KV4 cache (the cache of Sec. 4.2 for a server whose requests come and go: the paper has no counterpart of the paging).
+ * Sequences take pages of `page` tokens from one pool; the pool's block table is shared by all layers, each layer has codes of
+ * its own for every page. The same code, step and prefix rules as in the contiguous cache above hold.
+ *
+ *   table      int32 [B, max_pages]  page ids of each sequence in order; entries behind its last page are neither read nor written
+ *   len        int32 [B]             cached tokens of each sequence
+ *   free_list  int32 [n_pages]       entries 0 .. *n_free - 1 are the ids of the free pages (a stack, taken from its end)
+ *   n_free     int32 [1]
+ *   page in {16, 32, 64, 128}; B <= 8192; max_pages * page < 2^31.
+ * All on the device; a page id outside [0, n_pages) is never followed (PQ_ERR_SHAPE in the status word). */
+typedef struct pq_pages {
+  int32_t* table;
+  int32_t* len;
+  int32_t* free_list;
+  int32_t* n_free;
+  int32_t B, max_pages, page, n_pages;
+} pq_pages;
+
+/* Block tables, slots and positions of one step, built on the device from the request lengths: sequence b gets n_new[b] >= 0 tokens.
+ *     need[b] = ceil((len[b] + n_new[b]) / page) - ceil(len[b] / page)    pages are taken sequence by sequence, in ascending order:
+ *               the k-th page of the step is free_list[*n_free - 1 - k]; it is entered into table behind the pages the sequence has
+ *     q_begin[b] = n_new[0] + .. + n_new[b - 1], q_begin[B] = their sum   rows of the step, sequence by sequence
+ *     row r = q_begin[b] + t is the token at place c = len[b] + t of its sequence:
+ *               slot[r] = table[b, c / page] * page + c % page,  pos[r] = pos0 + c   (pos0: the number of prefixed tokens, usually)
+ *     rows behind the last token (a step padded to n_rows rows): slot -1, pos 0
+ *     len_out[b] = len[b] + n_new[b],  *n_free_out = *n_free - sum need
+ *   n_new int32 [B]; q_begin int32 [B + 1]; slot int64 [n_rows]; pos int32 [n_rows] (slot and pos 16-byte aligned); len_out int32 [B] and
+ *   n_free_out int32 [1] may be len and n_free themselves (a captured decode loop advances in place).
+ * If the step cannot be served as a whole (a negative length or count, a sequence past max_pages, more rows than n_rows, too few free
+ * pages), no page is taken: q_begin is 0 everywhere, every slot -1, len_out = len, *n_free_out = *n_free, and PQ_ERR_SHAPE is left in
+ * the status word; the calls that follow then have no rows. */
+pq_status pq_page_plan(pq_ctx* ctx, const pq_pages* pages, const int32_t* n_new, int32_t pos0, int64_t n_rows, int32_t* q_begin, int64_t* slot,
+                       int32_t* pos, int32_t* len_out, int32_t* n_free_out, void* stream);
+/* The pages of the sequences with done[b] != 0 go back, sequence by sequence in the order of the table: they follow the free ids,
+ * *n_free_out = *n_free + their number, len_out[b] = 0 (len[b] for the others). The table is left as it is. len_out and n_free_out may
+ * be len and n_free. If the list cannot hold them (n_pages entries) or a length is no length, nothing changes and PQ_ERR_SHAPE is reported. */
+pq_status pq_page_release(pq_ctx* ctx, const pq_pages* pages, const int32_t* done, int32_t* len_out, int32_t* n_free_out, void* stream);
+
+/* Norm of every query and key head and rotary embedding in one pass over x bf16 [N, Hq + Hk, 128], ld elements between rows:
+ *     v = x / sqrt(mean(x^2) + eps) * g          g = gq bf16 [128] for the heads 0 .. Hq - 1, gk for the next Hk; gq and gk both null: v = x
+ *     y[i] = v[i] cos - v[i+64] sin,  y[i+64] = v[i+64] cos + v[i] sin,  angle = pos[a(i)][row] * theta^(-2i/128)     i < 64
+ *     and, when rotate != 0, y H_128 / sqrt(128) (R3, as in pq_rope_rotate)
+ *   pos       int32 [n_axes, N] with ld_pos elements between axes: every row has positions of its own, on 1 to 3 axes (a token of an
+ *             image: time, row, column)
+ *   sections  host array of n_axes counts with sum 64: the first sections[0] frequencies follow axis 0, the next sections[1] axis 1, ..
+ *             (null with n_axes = 1)
+ *   y         bf16 [N, Hq + Hk, 128], ldy elements between rows; may be x (with ldy == ld)
+ * fp32 arithmetic, angles reduced in 64 bits, one rounding. D = 128; x, y, gq, gk 16-byte aligned; ld, ldy multiples of 8. Hk may be 0. */
+pq_status pq_qk_norm_rope(pq_ctx* ctx, const void* x, int64_t N, int32_t Hq, int32_t Hk, int32_t D, int64_t ld, const void* gq, const void* gk,
+                          float eps, const int32_t* pos, int32_t n_axes, int64_t ld_pos, const int32_t* sections, double theta, int32_t rotate,
+                          void* y, int64_t ldy, void* stream);
+
+/* One layer's paged cache.
+ *   codes     u8 [n_pages, Hkv, 2, page, D/2]   packed codes, keys then values of a (page, head)
+ *   steps     f32 [n_pages, Hkv, 2, page]       the own step of every cached vector, or null: the static steps
+ *   s_k, s_v  f32 [Hkv]                         static steps per head (not used, and may be null, when steps is given)
+ *   prefix_k, prefix_v  fp16 [Hkv, n_prefix, D] shared by all sequences
+ * D = 128; Hq a multiple of Hkv with Hq / Hkv <= 8; n_prefix <= 64; codes, steps and the prefix 16-byte aligned. Steps are positive and
+ * lie in [2^-60, 2^60]. */
+typedef struct pq_kv4_paged {
+  pq_pages pages;
+  const void* prefix_k;
+  const void* prefix_v;
+  uint8_t* codes;
+  float* steps;
+  const float* s_k;
+  const float* s_v;
+  int32_t Hq, Hkv, D, n_prefix;
+} pq_kv4_paged;
+
+/* The same pass over a projection output qkv bf16 [N, (Hq + 2 Hkv) * 128] with the quantize-on-write into the paged cache: the query heads
+ * go to q_out bf16 [N, Hq, 128] (ldq elements between rows), the key and value heads to the row's slot,
+ *     code = clamp(round_half_even(fp32(y / s)), -8, 7)
+ * where y of a key head is formed in 64 bits and not rounded in between (no code depends on how a sum was ordered), y of a value head is the
+ * projection's bf16 value, and s is the head's static step or, with steps, max|y| / 7 of the vector (1 where max|y| < 2^-57), which is written
+ * beside the codes.
+ * Rows with a negative slot (padding) are neither read nor written; a slot past the cache is skipped and PQ_ERR_SHAPE reported. The slots of
+ * a call are distinct. q_out may be qkv itself (with ldq == ld), else it must not overlap it. pos, sections, theta, rotate, gq, gk as above;
+ * qkv, q_out 16-byte aligned, ld, ldq multiples of 8. */
+pq_status pq_qk_norm_rope_kv4_paged_append(pq_ctx* ctx, const pq_kv4_paged* cache, const void* qkv, int64_t N, int64_t ld, const void* gq,
+                                           const void* gk, float eps, const int32_t* pos, int32_t n_axes, int64_t ld_pos, const int32_t* sections,
+                                           double theta, int32_t rotate, const int64_t* slot, void* q_out, int64_t ldq, void* stream);
+/* What a reader of the cache finds at the given slots: out bf16 [N, 2, Hkv, 128] = bf16(step * code), keys then values; rows with a negative
+ * slot are left as they are, a slot past the cache is skipped and PQ_ERR_SHAPE reported. out 16-byte aligned. */
+pq_status pq_kv4_paged_read(pq_ctx* ctx, const pq_kv4_paged* cache, const int64_t* slot, int64_t N, void* out, void* stream);
+
+/* Attention over [prefix || paged 4-bit cache] for a ragged batch (decode steps, prompts, chunks of prompts, any mixture): the rows
+ * q_begin[b] .. q_begin[b + 1] - 1 of q are the last n = q_begin[b + 1] - q_begin[b] tokens of the len[b] cached ones of sequence b
+ * (pq_page_plan has advanced len, the append has written them). Row t of them sees every prefixed key and the cached keys 0 .. len[b] - n + t:
+ *     out[row, g, :] = softmax_j(q[row, g, :] . K_j * sm_scale) . V      (zeros where nothing is visible)
+ *   q        bf16 [n_rows, Hq, 128] with ldq elements between rows (a multiple of 8), out bf16 [n_rows, Hq, 128] dense, both 16-byte aligned
+ *   q_begin  int32 [B + 1], ascending, on the device; rows from q_begin[B] on (padding) are neither read nor written
+ *   max_new  at least the largest n (a host bound); sequences with more rows are left out and PQ_ERR_SHAPE is reported
+ *   max_len  at least the largest len (a host bound that only chooses how the work is split; 0: the capacity max_pages * page)
+ *   ws       scratch of pq_attn_kv4_paged_workspace_bytes(ctx, cache, n_rows, max_new) bytes, 16-byte aligned
+ *   sm_scale > 0. */
+size_t pq_attn_kv4_paged_workspace_bytes(const pq_ctx* ctx, const pq_kv4_paged* cache, int64_t n_rows, int32_t max_new);
+pq_status pq_attn_kv4_paged(pq_ctx* ctx, const pq_kv4_paged* cache, const void* q, int64_t ldq, const int32_t* q_begin, int64_t n_rows,
+                            int32_t max_new, int32_t max_len, void* out, float sm_scale, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Decode attention for callers that may not allocate. (The paper has no counterpart: this is a
  * packaging variant of pq_decode_attn_kv4_prefix, same kernel, same arguments and result.)
  *

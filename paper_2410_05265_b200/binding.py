@@ -7,6 +7,7 @@ torch; there is no CPU fallback: without the compiled library every call fails.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from ctypes import POINTER, Structure, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_void_p
 
@@ -29,6 +30,8 @@ EXPORTS = [
     "pq_dyn_act_scale", "pq_dyn_hadamard_quant_act", "pq_hadamard_quant_act_rows", "pq_w4a4_gemm_rows", "pq_outlier_tokens",
     "pq_calib_act_asym", "pq_hadamard_quant_act_asym", "pq_weight_code_sums", "pq_w4a4_gemm_asym",
     "pq_swiglu_hadamard_quant_act", "pq_kv4_append_decode_attn", "pq_set_wait_limit", "pq_probe_i8_mma", "pq_grid_search_act_asym", "pq_grid_search_clip_dyn", "pq_rmsnorm_hadamard_quant_act", "pq_rope_kv4_append", "pq_selftest_wait",
+    "pq_page_plan", "pq_page_release", "pq_qk_norm_rope", "pq_qk_norm_rope_kv4_paged_append", "pq_kv4_paged_read",
+    "pq_attn_kv4_paged_workspace_bytes", "pq_attn_kv4_paged",
 ]
 
 
@@ -44,6 +47,20 @@ class KV4CacheStruct(Structure):
         ("s_k", c_void_p), ("s_v", c_void_p), ("len", c_void_p),
         ("B", c_int32), ("Hq", c_int32), ("Hkv", c_int32), ("D", c_int32), ("n_prefix", c_int32), ("Tmax", c_int32),
         ("sk_tok", c_void_p), ("sv_tok", c_void_p),
+    ]
+
+
+class PagesStruct(Structure):
+    _fields_ = [
+        ("table", c_void_p), ("len", c_void_p), ("free_list", c_void_p), ("n_free", c_void_p),
+        ("B", c_int32), ("max_pages", c_int32), ("page", c_int32), ("n_pages", c_int32),
+    ]
+
+
+class KV4PagedStruct(Structure):
+    _fields_ = [
+        ("pages", PagesStruct), ("prefix_k", c_void_p), ("prefix_v", c_void_p), ("codes", c_void_p), ("steps", c_void_p),
+        ("s_k", c_void_p), ("s_v", c_void_p), ("Hq", c_int32), ("Hkv", c_int32), ("D", c_int32), ("n_prefix", c_int32),
     ]
 
 
@@ -120,9 +137,22 @@ def load_library() -> ctypes.CDLL:
                                                  c_void_p, c_void_p]
     lib.pq_kv4_append_decode_attn.argtypes = [c_void_p, POINTER(KV4CacheStruct), c_void_p, c_void_p, c_void_p, c_void_p, c_float,
                                               c_void_p, c_size_t, c_void_p]
+    lib.pq_page_plan.argtypes = [c_void_p, POINTER(PagesStruct), c_void_p, c_int32, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                 c_void_p]
+    lib.pq_page_release.argtypes = [c_void_p, POINTER(PagesStruct), c_void_p, c_void_p, c_void_p, c_void_p]
+    lib.pq_qk_norm_rope.argtypes = [c_void_p, c_void_p, c_int64, c_int32, c_int32, c_int32, c_int64, c_void_p, c_void_p, c_float, c_void_p, c_int32,
+                                    c_int64, POINTER(c_int32), c_double, c_int32, c_void_p, c_int64, c_void_p]
+    lib.pq_qk_norm_rope_kv4_paged_append.argtypes = [c_void_p, POINTER(KV4PagedStruct), c_void_p, c_int64, c_int64, c_void_p, c_void_p, c_float,
+                                                     c_void_p, c_int32, c_int64, POINTER(c_int32), c_double, c_int32, c_void_p, c_void_p, c_int64,
+                                                     c_void_p]
+    lib.pq_kv4_paged_read.argtypes = [c_void_p, POINTER(KV4PagedStruct), c_void_p, c_int64, c_void_p, c_void_p]
+    lib.pq_attn_kv4_paged_workspace_bytes.restype = c_size_t
+    lib.pq_attn_kv4_paged_workspace_bytes.argtypes = [c_void_p, POINTER(KV4PagedStruct), c_int64, c_int32]
+    lib.pq_attn_kv4_paged.argtypes = [c_void_p, POINTER(KV4PagedStruct), c_void_p, c_int64, c_void_p, c_int64, c_int32, c_int32, c_void_p, c_float,
+                                      c_void_p, c_size_t, c_void_p]
     for name in EXPORTS:
         getattr(lib, name)
-        if name not in ("pq_status_string", "pq_w4a4_gemm_workspace_bytes", "pq_decode_attn_workspace_bytes"):
+        if name not in ("pq_status_string", "pq_w4a4_gemm_workspace_bytes", "pq_decode_attn_workspace_bytes", "pq_attn_kv4_paged_workspace_bytes"):
             getattr(lib, name).restype = c_int32
     _lib = lib
     return lib
@@ -142,6 +172,11 @@ def _stream():
 def _ok(status: int, where: str):
     if status != 0:
         raise PQError(status, where)
+
+
+def _row_stride(t: torch.Tensor) -> int:
+    """Elements between the rows of t; of a single row, whose stride says nothing, its own width."""
+    return t.stride(0) if t.shape[0] > 1 else math.prod(t.shape[1:])
 
 
 def _dev(t: torch.Tensor, dtype, name: str):
@@ -177,6 +212,50 @@ class KV4Cache:
         )
 
 
+class Pages:
+    """Caller-owned block table of a paged KV4 cache, shared by all layers: table int32 [B, max_pages], length int32 [B], the stack of
+    free page ids int32 [n_pages] with its count int32 [1], tokens per page (16, 32, 64 or 128)."""
+
+    def __init__(self, table, length, free_list, n_free, page: int):
+        for t, name in ((table, "table"), (length, "length"), (free_list, "free_list"), (n_free, "n_free")):
+            _dev(t, torch.int32, name)
+            assert t.is_contiguous() and t.device == table.device, name
+        B, max_pages = table.shape
+        assert length.shape == (B,) and free_list.dim() == 1 and n_free.numel() == 1
+        self.table, self.length, self.free_list, self.n_free = table, length, free_list, n_free
+        self.B, self.max_pages, self.page, self.n_pages = B, max_pages, int(page), free_list.numel()
+        self.struct = PagesStruct(table.data_ptr(), length.data_ptr(), free_list.data_ptr(), n_free.data_ptr(), B, max_pages, self.page, self.n_pages)
+
+
+class KV4PagedCache:
+    """One layer's paged cache: codes u8 [n_pages, Hkv, 2, page, 64] (keys, then values), static steps s_k, s_v f32 [Hkv] or the own step of every
+    vector in steps f32 [n_pages, Hkv, 2, page], fp16 prefix [Hkv, n_prefix, 128] (or None) shared by all sequences."""
+
+    def __init__(self, pages: Pages, prefix_k, prefix_v, codes, Hq: int, s_k=None, s_v=None, steps=None):
+        _dev(codes, torch.uint8, "codes")
+        n_pages, Hkv, two, page, D2 = codes.shape
+        assert (n_pages, two, page) == (pages.n_pages, 2, pages.page) and codes.is_contiguous()
+        if steps is not None:
+            _dev(steps, torch.float32, "steps")
+            assert steps.shape == (n_pages, Hkv, 2, page) and steps.is_contiguous()
+        else:
+            for t, name in ((s_k, "s_k"), (s_v, "s_v")):
+                _dev(t, torch.float32, name)
+                assert t.shape == (Hkv,) and t.is_contiguous(), name
+        n_prefix = 0 if prefix_k is None else prefix_k.shape[1]
+        if n_prefix:
+            for t, name in ((prefix_k, "prefix_k"), (prefix_v, "prefix_v")):
+                _dev(t, torch.float16, name)
+                assert t.shape == (Hkv, n_prefix, 2 * D2) and t.is_contiguous(), name
+        for t in (codes, steps, s_k, s_v, prefix_k, prefix_v):
+            assert t is None or t.device == pages.table.device
+        self.pages, self.prefix_k, self.prefix_v, self.codes, self.steps, self.s_k, self.s_v = pages, prefix_k, prefix_v, codes, steps, s_k, s_v
+        self.Hq, self.Hkv, self.D, self.n_prefix = int(Hq), Hkv, 2 * D2, n_prefix
+        at = lambda t: t.data_ptr() if t is not None else 0
+        self.struct = KV4PagedStruct(pages.struct, at(prefix_k) if n_prefix else 0, at(prefix_v) if n_prefix else 0, codes.data_ptr(), at(steps), at(s_k),
+                                     at(s_v), self.Hq, Hkv, 2 * D2, n_prefix)
+
+
 class Context:
     """Owns one pq_ctx on the current CUDA device."""
 
@@ -189,6 +268,7 @@ class Context:
         h = c_void_p()
         _ok(self.lib.pq_create(ctypes.byref(h)), "pq_create")
         self.h = h
+        self.device = torch.cuda.current_device()
 
     def close(self):
         if getattr(self, "h", None):
@@ -562,6 +642,126 @@ class Context:
         assert qkv.dim() == 2 and qkv.stride(1) == 1 and qkv.shape[1] == (cache.Hq + 2 * cache.Hkv) * cache.D
         _ok(self.lib.pq_rope_kv4_append(self.h, ctypes.byref(cache.struct), int(seq), _ptr(qkv), T, qkv.stride(0), int(pos0), float(theta),
                                         1 if rotate else 0, _stream()), "pq_rope_kv4_append")
+
+    # ---- paged KV4 cache ------------------------------------------------------------------------
+    def page_plan(self, pages: Pages, n_new: torch.Tensor, n_rows: int | None = None, pos0: int = 0, out=None, len_out=None, n_free_out=None):
+        """Pages, slots and positions of a step in which sequence b gets n_new[b] tokens; n_rows is the number of rows of the (padded) step.
+        Returns (q_begin int32 [B + 1], slot int64 [n_rows], pos int32 [n_rows]), which may be given as `out`. The lengths and the count
+        of free pages advance in place unless len_out, n_free_out are given."""
+        _dev(n_new, torch.int32, "n_new")
+        assert n_new.shape == (pages.B,) and n_new.is_contiguous()
+        if out is None:
+            out = (torch.empty((pages.B + 1,), dtype=torch.int32, device=n_new.device), torch.empty((n_rows,), dtype=torch.int64, device=n_new.device),
+                   torch.empty((n_rows,), dtype=torch.int32, device=n_new.device))
+        q_begin, slot, pos = out
+        len_out, n_free_out = pages.length if len_out is None else len_out, pages.n_free if n_free_out is None else n_free_out
+        _dev(q_begin, torch.int32, "q_begin"), _dev(slot, torch.int64, "slot"), _dev(pos, torch.int32, "pos")
+        _dev(len_out, torch.int32, "len_out"), _dev(n_free_out, torch.int32, "n_free_out")
+        assert q_begin.shape == (pages.B + 1,) and slot.dim() == 1 and slot.shape == pos.shape and (n_rows is None or slot.shape[0] == n_rows)
+        assert len_out.shape == (pages.B,) and n_free_out.numel() == 1 and all(t.is_contiguous() for t in (q_begin, slot, pos, len_out))
+        self._here(pages.table, n_new, q_begin, slot, pos, len_out, n_free_out)
+        _ok(self.lib.pq_page_plan(self.h, ctypes.byref(pages.struct), _ptr(n_new), int(pos0), slot.shape[0], _ptr(q_begin), _ptr(slot), _ptr(pos),
+                                  _ptr(len_out), _ptr(n_free_out), _stream()), "pq_page_plan")
+        return out
+
+    def page_release(self, pages: Pages, done: torch.Tensor, len_out=None, n_free_out=None) -> None:
+        """The pages of the sequences with done[b] != 0 (int32 [B]) go back to the free list; lengths and count change in place by default."""
+        len_out, n_free_out = pages.length if len_out is None else len_out, pages.n_free if n_free_out is None else n_free_out
+        _dev(done, torch.int32, "done"), _dev(len_out, torch.int32, "len_out"), _dev(n_free_out, torch.int32, "n_free_out")
+        assert done.shape == (pages.B,) == len_out.shape and done.is_contiguous() and len_out.is_contiguous() and n_free_out.numel() == 1
+        self._here(pages.table, done, len_out, n_free_out)
+        _ok(self.lib.pq_page_release(self.h, ctypes.byref(pages.struct), _ptr(done), _ptr(len_out), _ptr(n_free_out), _stream()), "pq_page_release")
+
+    def _here(self, *tensors):
+        """The tensors of a call live on the context's device, which is the current one: its stream is the one that is used."""
+        current = torch._C._cuda_getDevice()
+        for t in tensors:
+            if t is not None and (t.device.index != self.device or current != self.device):
+                raise ValueError(f"a tensor on {t.device} with cuda:{current} current in a context of cuda:{self.device}")
+
+    @staticmethod
+    def _rope_args(N, gq, gk, pos, sections):
+        """(axes, distance of the axes, sections) as the C calls take them; pos int32 [N] or [axes, N]."""
+        _dev(pos, torch.int32, "pos")
+        for g, name in ((gq, "gq"), (gk, "gk")):
+            if g is not None:
+                _dev(g, torch.bfloat16, name)
+                assert g.shape == (128,) and g.is_contiguous(), name
+        assert (gq is None) == (gk is None)
+        axes = 1 if pos.dim() == 1 else pos.shape[0]
+        assert pos.shape[-1] == N and (N <= 1 or pos.stride(-1) == 1)
+        if sections is not None:
+            assert len(sections) == axes
+        return axes, pos.stride(0) if pos.dim() == 2 else N, (c_int32 * axes)(*sections) if sections is not None else None
+
+    def qk_norm_rope(self, x: torch.Tensor, Hq: int, gq, gk, eps: float, pos: torch.Tensor, theta: float, sections=None, rotate: bool = False,
+                     out: torch.Tensor | None = None):
+        """RMSNorm of every head (gains gq for the first Hq heads of x [N, H, 128], gk for the others; both None: no norm), rotary embedding with the
+        positions pos int32 [N] or [axes, N] (frequencies dealt to the axes by `sections`), with rotate=True followed by R3. out may be x."""
+        _dev(x, torch.bfloat16, "x")
+        N, H, D = x.shape
+        assert x.stride(2) == 1 and (H == 1 or x.stride(1) == D)
+        axes, ld_pos, sec = self._rope_args(N, gq, gk, pos, sections)
+        if out is None:
+            out = torch.empty((N, H, D), dtype=x.dtype, device=x.device)
+        _dev(out, torch.bfloat16, "out")
+        assert out.shape == x.shape and out.stride(2) == 1 and (H == 1 or out.stride(1) == D)
+        self._here(x, gq, gk, pos, out)
+        _ok(self.lib.pq_qk_norm_rope(self.h, _ptr(x), N, int(Hq), H - int(Hq), D, _row_stride(x), _ptr(gq), _ptr(gk), float(eps), _ptr(pos), axes, ld_pos,
+                                     sec, float(theta), 1 if rotate else 0, _ptr(out), _row_stride(out), _stream()), "pq_qk_norm_rope")
+        return out
+
+    def qk_norm_rope_kv4_paged_append(self, cache: KV4PagedCache, qkv: torch.Tensor, gq, gk, eps: float, pos: torch.Tensor, slot: torch.Tensor,
+                                      theta: float, sections=None, rotate: bool = False, q_out: torch.Tensor | None = None):
+        """qk_norm_rope of a projection output qkv [N, (Hq + 2 Hkv) * 128]: the query heads to q_out [N, Hq, 128] (returned), the key and value
+        heads, quantized, to the slots of the paged cache. Rows with slot -1 are neither read nor written."""
+        _dev(qkv, torch.bfloat16, "qkv"), _dev(slot, torch.int64, "slot")
+        N = qkv.shape[0]
+        assert qkv.dim() == 2 and qkv.stride(1) == 1 and qkv.shape[1] == (cache.Hq + 2 * cache.Hkv) * cache.D
+        assert slot.shape == (N,) and slot.is_contiguous()
+        axes, ld_pos, sec = self._rope_args(N, gq, gk, pos, sections)
+        if q_out is None:
+            q_out = torch.empty((N, cache.Hq, cache.D), dtype=qkv.dtype, device=qkv.device)
+        _dev(q_out, torch.bfloat16, "q_out")
+        assert q_out.shape == (N, cache.Hq, cache.D) and q_out.stride(2) == 1 and (cache.Hq == 1 or q_out.stride(1) == cache.D)
+        self._here(cache.codes, qkv, gq, gk, pos, slot, q_out)
+        _ok(self.lib.pq_qk_norm_rope_kv4_paged_append(self.h, ctypes.byref(cache.struct), _ptr(qkv), N, _row_stride(qkv), _ptr(gq), _ptr(gk), float(eps),
+                                                      _ptr(pos), axes, ld_pos, sec, float(theta), 1 if rotate else 0, _ptr(slot), _ptr(q_out),
+                                                      _row_stride(q_out), _stream()), "pq_qk_norm_rope_kv4_paged_append")
+        return q_out
+
+    def kv4_paged_read(self, cache: KV4PagedCache, slot: torch.Tensor, out: torch.Tensor | None = None):
+        """Keys and values at the given slots as a reader of the cache finds them, bf16 [N, 2, Hkv, 128]; rows with slot -1 keep what out holds."""
+        _dev(slot, torch.int64, "slot")
+        N = slot.shape[0]
+        if out is None:
+            out = torch.zeros((N, 2, cache.Hkv, cache.D), dtype=torch.bfloat16, device=slot.device)
+        _dev(out, torch.bfloat16, "out")
+        assert slot.dim() == 1 and slot.is_contiguous() and out.shape == (N, 2, cache.Hkv, cache.D) and out.is_contiguous()
+        self._here(cache.codes, slot, out)
+        _ok(self.lib.pq_kv4_paged_read(self.h, ctypes.byref(cache.struct), _ptr(slot), N, _ptr(out), _stream()), "pq_kv4_paged_read")
+        return out
+
+    def attn_kv4_paged_workspace(self, cache: KV4PagedCache, n_rows: int, max_new: int) -> torch.Tensor:
+        n = int(self.lib.pq_attn_kv4_paged_workspace_bytes(self.h, ctypes.byref(cache.struct), int(n_rows), int(max_new)))
+        return torch.empty((max(n, 16),), dtype=torch.uint8, device=cache.codes.device)
+
+    def attn_kv4_paged(self, cache: KV4PagedCache, q: torch.Tensor, q_begin: torch.Tensor, max_new: int, sm_scale: float, ws: torch.Tensor,
+                       max_len: int = 0, out: torch.Tensor | None = None):
+        """Causal attention of the rows q [N, Hq, 128] of a ragged batch (sequence b: rows q_begin[b] .. q_begin[b + 1] - 1, its last tokens) over
+        [prefix || paged cache]. max_new bounds the rows of a sequence, max_len (0: the capacity) the lengths; rows behind the last stay as they are."""
+        _dev(q, torch.bfloat16, "q"), _dev(q_begin, torch.int32, "q_begin"), _dev(ws, torch.uint8, "ws")
+        N = q.shape[0]
+        assert q.shape == (N, cache.Hq, cache.D) and q.stride(2) == 1 and (cache.Hq == 1 or q.stride(1) == cache.D)
+        assert q_begin.shape == (cache.pages.B + 1,) and q_begin.is_contiguous()
+        if out is None:
+            out = torch.zeros((N, cache.Hq, cache.D), dtype=q.dtype, device=q.device)
+        _dev(out, torch.bfloat16, "out")
+        assert out.shape == q.shape and out.is_contiguous()
+        self._here(cache.codes, q, q_begin, ws, out)
+        _ok(self.lib.pq_attn_kv4_paged(self.h, ctypes.byref(cache.struct), _ptr(q), _row_stride(q), _ptr(q_begin), N, int(max_new), int(max_len), _ptr(out),
+                                       float(sm_scale), _ptr(ws), ws.numel(), _stream()), "pq_attn_kv4_paged")
+        return out
 
     # ---- transformer-block glue -----------------------------------------------------------------
     def rmsnorm(self, x: torch.Tensor, g: torch.Tensor, eps: float = 1e-5, out: torch.Tensor | None = None):
