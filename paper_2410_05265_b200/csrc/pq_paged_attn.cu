@@ -2,39 +2,18 @@
 //
 // One CTA per (row, KV head): a thread scores one key of a chunk of 128 for all query heads of the group in fp32, then takes one head dim of
 // the output over the chunk's keys; running maximum and sum per head.
-#include <math.h>
-
-#include "pq_paged.cuh"
+#include "pq_paged_attn.cuh"
 
 namespace {
 
 constexpr int SA_THREADS = 128;
-
-struct SimpleParams {
-  const __nv_bfloat16* q;
-  int64_t ldq;
-  __nv_bfloat16* out;
-  const int32_t* q_begin;
-  const int32_t* len;
-  const int32_t* table;
-  const __half* prefix_k;
-  const __half* prefix_v;
-  const uint8_t* codes;
-  const float* steps;
-  const float* s_k;
-  const float* s_v;
-  int32_t* status;
-  int64_t n_rows;
-  float scale2;  // sm_scale log2(e)
-  int32_t B, max_pages, page_log2, n_pages, Hq, Hkv, G, n_prefix, max_new;
-};
 
 __device__ __forceinline__ float nibble(const uint8_t* row, int d) {
   const int b = row[d >> 1];
   return static_cast<float>((d & 1) ? static_cast<int8_t>(b) >> 4 : static_cast<int8_t>(b << 4) >> 4);
 }
 
-__global__ void __launch_bounds__(SA_THREADS) attn_simple_kernel(const SimpleParams p) {
+__global__ void __launch_bounds__(SA_THREADS) attn_simple_kernel(const PagedAttnParams p) {
   __shared__ float sq[PQ_PAGED_MAX_GROUP][128];
   __shared__ float sp[PQ_PAGED_MAX_GROUP][SA_THREADS];
   __shared__ float red[SA_THREADS / 32];
@@ -48,6 +27,7 @@ __global__ void __launch_bounds__(SA_THREADS) attn_simple_kernel(const SimplePar
   const int n = p.q_begin[b + 1] - p.q_begin[b];
   const int64_t capacity = static_cast<int64_t>(p.max_pages) << p.page_log2;
   int len = p.len[b];
+  if (n == 1) return;  // the other kernel's
   if (n > p.max_new || len < 0 || len > capacity) {
     if (tid == 0) pq::report(p.status, PQ_ERR_SHAPE);
     if (n > p.max_new) return;
@@ -116,27 +96,32 @@ __global__ void __launch_bounds__(SA_THREADS) attn_simple_kernel(const SimplePar
 }  // namespace
 
 extern "C" size_t pq_attn_kv4_paged_workspace_bytes(const pq_ctx* ctx, const pq_kv4_paged* cache, int64_t n_rows, int32_t max_new) {
-  if (!ctx || !cache || cache->Hkv <= 0 || n_rows <= 0 || max_new <= 0) return 0;
-  return 16;
+  if (!ctx || pq_check_paged(cache) != PQ_OK || n_rows <= 0 || max_new <= 0) return 0;
+  return pq_paged_decode_ws_bytes(ctx, cache);
 }
 
 extern "C" pq_status pq_attn_kv4_paged(pq_ctx* ctx, const pq_kv4_paged* c, const void* q, int64_t ldq, const int32_t* q_begin, int64_t n_rows,
                                        int32_t max_new, int32_t max_len, void* out, float sm_scale, void* ws, size_t ws_bytes, void* stream) {
-  if (!ctx || n_rows < 0 || max_new < 0 || max_len < 0 || !(sm_scale > 0.0f)) return PQ_ERR_INVALID_ARG;
-  const pq_status st = pq_check_paged(c);
+  if (!ctx || n_rows < 0 || max_new < 0 || max_len < 0 || !(sm_scale > 0.0f) || !isfinite(sm_scale)) return PQ_ERR_INVALID_ARG;
+  pq_status st = pq_check_paged(c);
   if (st != PQ_OK) return st;
   if (n_rows == 0 || c->pages.B == 0 || max_new == 0) return PQ_OK;
   if (!q || !out || !q_begin || ldq < static_cast<int64_t>(c->Hq) * 128) return PQ_ERR_INVALID_ARG;
   if (n_rows > 0x7fffffffll) return PQ_ERR_SHAPE;
   if (pq_misaligned16(q) || pq_misaligned16(out) || pq_misaligned16(ws) || ldq % 8 != 0) return PQ_ERR_ALIGN;
   if (!ws || ws_bytes < pq_attn_kv4_paged_workspace_bytes(ctx, c, n_rows, max_new)) return PQ_ERR_WORKSPACE;
-  SimpleParams p{};
+  PagedAttnParams p{};
   p.q = static_cast<const __nv_bfloat16*>(q), p.ldq = ldq, p.out = static_cast<__nv_bfloat16*>(out), p.q_begin = q_begin;
   p.len = c->pages.len, p.table = c->pages.table;
   p.prefix_k = static_cast<const __half*>(c->prefix_k), p.prefix_v = static_cast<const __half*>(c->prefix_v);
-  p.codes = c->codes, p.steps = c->steps, p.s_k = c->s_k, p.s_v = c->s_v, p.status = ctx->d_status;
-  p.n_rows = n_rows, p.scale2 = sm_scale * 1.4426950408889634f;
+  p.codes = c->codes, p.steps = c->steps, p.s_k = c->s_k, p.s_v = c->s_v, p.tickets = ctx->d_tickets, p.status = ctx->d_status;
+  p.wait_clocks = ctx->wait_clocks;
+  p.n_rows = static_cast<int32_t>(n_rows), p.scale2 = sm_scale * 1.4426950408889634f;
   p.B = c->pages.B, p.max_pages = c->pages.max_pages, p.page_log2 = pq_page_log2(c->pages.page), p.n_pages = c->pages.n_pages;
   p.Hq = c->Hq, p.Hkv = c->Hkv, p.G = c->Hq / c->Hkv, p.n_prefix = c->n_prefix, p.max_new = max_new;
+  const int64_t capacity = static_cast<int64_t>(p.max_pages) << p.page_log2;
+  const int64_t bound = max_len > 0 && max_len < capacity ? max_len : capacity;
+  st = pq_paged_decode_launch(ctx, c, p, bound, ws, static_cast<cudaStream_t>(stream));
+  if (st != PQ_OK || max_new == 1) return st;
   return pq_launch_pdl(attn_simple_kernel, dim3(static_cast<unsigned>(n_rows), c->Hkv), SA_THREADS, 0, static_cast<cudaStream_t>(stream), p);
 }

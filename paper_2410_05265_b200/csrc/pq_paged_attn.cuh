@@ -1,0 +1,80 @@
+// Parameters and small device helpers of the two kernels behind pq_attn_kv4_paged: the one for single tokens (pq_paged_decode.cu) and
+// the one for sequences of several rows (pq_paged_prefill.cu).
+#pragma once
+
+#include <math.h>
+
+#include "pq_paged.cuh"
+
+struct PagedAttnParams {
+  const __nv_bfloat16* q;
+  int64_t ldq;
+  __nv_bfloat16* out;
+  const int32_t* q_begin;
+  const int32_t* len;
+  const int32_t* table;
+  const __half* prefix_k;
+  const __half* prefix_v;
+  const uint8_t* codes;
+  const float* steps;  // null: the static steps
+  const float* s_k;
+  const float* s_v;
+  float* ws_o;   // partial outputs in value units: [2 * workers] x rows x 128
+  float* ws_ml;  // their reference exponents (log2 units) and denominators
+  uint32_t* tickets;
+  int32_t* status;
+  long long wait_clocks;
+  float scale2;  // sm_scale log2(e)
+  int32_t n_rows, B, max_pages, page_log2, n_pages, Hq, Hkv, G, n_prefix, max_new;
+  int32_t csize;    // decode: CTAs of a worker (one cluster)
+  int32_t workers;  // 0: one worker per (sequence, KV head)
+};
+
+// Tickets 0 .. 15 belong to the appends, those from PQ_N_TICKETS / 2 on to the one-launch decode step.
+#define PQ_PAGED_TICKET0 16
+#define PQ_PAGED_MAX_WORKERS 4096
+
+size_t pq_paged_decode_ws_bytes(const pq_ctx* ctx, const pq_kv4_paged* c);
+pq_status pq_paged_decode_launch(pq_ctx* ctx, const pq_kv4_paged* c, PagedAttnParams p, int64_t max_len, void* ws, cudaStream_t st);
+
+namespace pq {
+
+__device__ __forceinline__ float lg2_approx(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// (a & M) ^ C in one LOP3; the constants are immediates
+template <uint32_t M, uint32_t C>
+__device__ __forceinline__ uint32_t and_xor(uint32_t a) {
+  uint32_t d;
+  asm("lop3.b32 %0, %1, %2, %3, 0x6A;" : "=r"(d) : "r"(a), "n"(M), "n"(C));
+  return d;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// 1-D bulk copy global -> shared, completion counted in bytes on an mbarrier.
+__device__ __forceinline__ void bulk_load(uint32_t dst_smem, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst_smem), "l"(src), "r"(bytes),
+               "r"(smem_u32(bar))
+               : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ float lds32f(uint32_t a) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(a));
+  return v;
+}
+
+}  // namespace pq
