@@ -117,7 +117,7 @@ extern "C" pq_status pq_attn_kv4_paged(pq_ctx* ctx, const pq_kv4_paged* c, const
   p.codes = c->codes, p.steps = c->steps, p.s_k = c->s_k, p.s_v = c->s_v, p.tickets = ctx->d_tickets, p.status = ctx->d_status;
   p.wait_clocks = ctx->wait_clocks;
   p.n_rows = static_cast<int32_t>(n_rows), p.scale2 = sm_scale * 1.4426950408889634f;
-  p.B = c->pages.B, p.max_pages = c->pages.max_pages, p.page_log2 = pq_page_log2(c->pages.page), p.n_pages = c->pages.n_pages;
+  p.B = c->pages.B, p.max_pages = c->pages.n_pages > 0 ? c->pages.max_pages : 0, p.page_log2 = pq_page_log2(c->pages.page), p.n_pages = c->pages.n_pages;
   p.Hq = c->Hq, p.Hkv = c->Hkv, p.G = c->Hq / c->Hkv, p.n_prefix = c->n_prefix, p.max_new = max_new;
   const int64_t capacity = static_cast<int64_t>(p.max_pages) << p.page_log2;
   const int64_t bound = max_len > 0 && max_len < capacity ? max_len : capacity;

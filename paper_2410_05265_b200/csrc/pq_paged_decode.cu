@@ -12,13 +12,16 @@
 // Warps work alone: warp w of the worker takes every 4 * csize-th block of 32 keys, brings it into its own ring of staging slots
 // by bulk copies (16 rows of keys or values each, page by page; the ids of the pages of the next block are loaded one block ahead), and no
 // CTA barrier stands in the key loop. The ring runs on across the pairs of a stretch.
-//   scores   S^T[key, head] with the fp16 MMA, keys on the 16-row side; codes become exact fp16 integers in place (nibbles 0 and 2 of a 16-bit
-//            half under the exponent of 1024, nibbles 1 and 3 stay four bits up under that of 1024: 16 x code, with q / 16). The query is
-//            scaled by a power of two per head, so that every bf16 query fits fp16.
+//   scores   S^T[key, head] with the fp16 MMA, keys on the 16-row side. code + 8 is taken as the fp16 number whose bits it is (a subnormal, (code + 8) 2^-24;
+//            the odd nibbles four bits up, with q / 16): one LOP3 for two codes, and 8 sum(q) is taken off each score. The offset is of
+//            the codes' own size, so fp32 sums lose nothing by it. The query is scaled by a power of two per head, so that every bf16
+//            query fits fp16.
 //   softmax  in log2 units against a reference exponent per head that moves only when a score exceeds it by more than DP_HEADROOM
-//   output   O^T = V^T P^T with the fp16 MMA, head dims on the 16-row side; static steps: codes, times s_v at the end, the denominator from one more MMA
-//            over the same rounded P. Own steps: the exponent of a weight takes log2 of the value's step with it, w = 2^(s + log2 step - m), so
+//   output   O^T = V^T P^T with the fp16 MMA, head dims on the 16-row side, codes + 8 as above; one more MMA over codes of zero gives what the offset adds
+//            and, for static steps, the denominator, both from the same rounded P. Own steps: the exponent of a weight takes log2 of the value's step with it, w = 2^(s + log2 step - m), so
 //            that fp16 holds the largest of what enters the sum whatever the steps are; the denominator is the sum of w / step in fp32.
+#include <atomic>
+
 #include "pq_paged_attn.cuh"
 
 namespace {
@@ -35,24 +38,28 @@ constexpr int DP_MAX_CLUSTER = 8;
 
 // Bytes of a staging slot: 32 rows of keys, 32 rows of values, with own steps 32 + 32 floats.
 __host__ __device__ constexpr int slot_bytes(bool dyn) { return DP_BLOCK * 128 + (dyn ? DP_BLOCK * 8 : 0); }
-constexpr int fixed_smem(bool dyn) { return DP_WARPS * DP_SLOTS * slot_bytes(dyn) + DP_WARPS * DP_ROWS * DP_SO_STRIDE * 4 + DP_ROWS * 128 * 4; }
+// Dynamic shared memory: staging, the warps' partial outputs, prefix scores, and (equal stretches) rounds and lengths of the sequences.
+size_t dynamic_smem(bool dyn, int G, int n_prefix, int seqs) {
+  return DP_WARPS * DP_SLOTS * slot_bytes(dyn) + static_cast<size_t>(DP_WARPS) * G * DP_SO_STRIDE * 4 + static_cast<size_t>(G) * n_prefix * 4 +
+         (seqs > 0 ? (3 * static_cast<size_t>(seqs) + 1) * 4 : 0);
+}
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint32_t hsub2(uint32_t a, uint32_t b) {
-  uint32_t d;
-  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-  return d;
-}
-// Two codes of a word as fp16: nibbles 0 and 4 (1032 + code less 1032), nibbles 1 and 5 (1152 + 16 code less 1152: sixteen times the code).
-__device__ __forceinline__ uint32_t codes_lo(uint32_t w) { return hsub2(pq::and_xor<0x000F000Fu, 0x64086408u>(w), 0x64086408u); }
-__device__ __forceinline__ uint32_t codes_hi16(uint32_t w) { return hsub2(pq::and_xor<0x00F000F0u, 0x64806480u>(w), 0x64806480u); }
+// Two codes of a word as (code + 8) 2^-24 (nibbles 0 and 4) and (code + 8) 2^-20 (nibbles 1 and 5), fp16 subnormals: their bits are the numbers.
+__device__ __forceinline__ uint32_t codes_lo(uint32_t w) { return pq::and_xor<0x000F000Fu, 0x00080008u>(w); }
+__device__ __forceinline__ uint32_t codes_hi(uint32_t w) { return pq::and_xor<0x00F000F0u, 0x00800080u>(w); }
 __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t a) {
   uint32_t d;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
 __device__ __forceinline__ uint32_t map_cta(uint32_t smem_addr, int rank) {
@@ -82,15 +89,20 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
   constexpr int SLOT = slot_bytes(DYN);
   extern __shared__ __align__(128) uint8_t dp_smem[];
   float* sm_o = reinterpret_cast<float*>(dp_smem + DP_WARPS * DP_SLOTS * SLOT);  // [warp][head][DP_SO_STRIDE]; dim 16a + 2b + c at 16b + 2a + c
-  float* cl_o = sm_o + DP_WARPS * DP_ROWS * DP_SO_STRIDE;                        // [head][128]: this CTA's partial of a cluster
-  int32_t* scan = reinterpret_cast<int32_t*>(cl_o + DP_ROWS * 128);              // [B + 1] rounds before a sequence (workers > 0)
-  int32_t* lens = scan + p.B + 1;                                                // [B]
+  float* cl_o = sm_o;  // [head] rows of the first warp, once they have been read: this CTA's partial of a cluster, dims in order
+  float* sm_pre = sm_o + DP_WARPS * p.G * DP_SO_STRIDE;                     // [head][n_prefix]
+  int32_t* scan = reinterpret_cast<int32_t*>(sm_pre + p.G * p.n_prefix);    // [B + 1] rounds before a sequence (workers > 0)
+  int32_t* lens = scan + p.B + 1;                                           // [B]
+  int32_t* rows = lens + p.B;                                               // [B] the row of a sequence that has exactly one
   __shared__ __align__(8) uint64_t full[DP_WARPS][DP_SLOTS];
   __shared__ float sm_ml[DP_WARPS][DP_ROWS][2];
   __shared__ float2 cl_ml[DP_ROWS];
-  __shared__ float sm_pre[DP_ROWS][PQ_PAGED_MAX_PREFIX];
+  __shared__ uint4 sm_q[DP_ROWS][17];  // the queries as MMA operand; a padded row keeps the eight heads of a load apart
+  __shared__ float2 sm_f[DP_ROWS];
   __shared__ int64_t part[DP_WARPS];
-  __shared__ int sm_last;
+  __shared__ float4 sm_step[DYN ? DP_WARPS : 1][DYN ? DP_BLOCK : 1];
+  __shared__ int sm_last[2];
+  __shared__ int4 sm_shared[2];  // (row, KV head, first and last worker)
 
   const int csize = p.csize, worker = blockIdx.x / csize, rank = blockIdx.x % csize;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -103,14 +115,9 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
   }
   const int64_t capacity = static_cast<int64_t>(p.max_pages) << page_log2;
   auto clip_len = [&](int l) { return l < 0 ? 0 : l > capacity ? static_cast<int>(capacity) : l; };
-  // The row of a sequence that has exactly one; -1 for the others (the other kernel's, or none).
-  auto row_of = [&](int b) {
-    const int r0 = pq::ld_dep(p.q_begin + b), r1 = pq::ld_dep(p.q_begin + b + 1);
-    return r1 - r0 == 1 && r0 >= 0 && r0 < p.n_rows ? r0 : -1;
-  };
 
   // ---- this worker's stretch of units [u0, u1)
-  int u0 = 0, u1 = 0, b_direct = 0, h_direct = 0, len_direct = 0, n_workers = 1, U = 0;
+  int u0 = 0, u1 = 0, b_direct = 0, h_direct = 0, len_direct = 0, row_direct = 0, n_workers = 1, U = 0;
   const bool direct = p.workers == 0;
   if (direct) {
     b_direct = worker / p.Hkv, h_direct = worker % p.Hkv;
@@ -119,6 +126,7 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
     const int r0 = pq::ld_dep(p.q_begin + b_direct), r1 = pq::ld_dep(p.q_begin + b_direct + 1);
     if (threadIdx.x == 0 && (r1 - r0 > p.max_new || (l != len_direct && r1 > r0))) pq::report(p.status, PQ_ERR_SHAPE);
     if (r1 - r0 != 1 || r0 < 0 || r0 >= p.n_rows) return;  // the whole cluster alike
+    row_direct = r0;
     u1 = max(1, (len_direct + DP_ROUND - 1) / DP_ROUND);
     __syncwarp();
   } else {
@@ -128,7 +136,7 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
       const int r0 = pq::ld_dep(p.q_begin + b), r1 = pq::ld_dep(p.q_begin + b + 1);
       const bool mine = r1 - r0 == 1 && r0 >= 0 && r0 < p.n_rows;
       odd |= r1 - r0 > p.max_new || (l != lc && r1 > r0);
-      lens[b] = lc;
+      lens[b] = lc, rows[b] = r0;
       scan[b] = mine ? max(1, (lc + DP_ROUND - 1) / DP_ROUND) : 0;
     }
     __syncthreads();
@@ -145,64 +153,84 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
   struct Piece {
     int b, h, r0, r1, rounds, len;  // rounds r0 .. r1 - 1 of the `rounds` of the pair
   };
-  auto piece_at = [&](int u) {
+  auto first_piece = [&]() {
     Piece x;
     if (direct) {
       x.b = b_direct, x.h = h_direct, x.r0 = 0, x.r1 = x.rounds = u1, x.len = len_direct;
       return x;
     }
-    x.b = pq::find_segment(scan, p.B, u / p.Hkv);
+    x.b = pq::find_segment(scan, p.B, u0 / p.Hkv);
     const int before = scan[x.b];
     x.rounds = scan[x.b + 1] - before;
-    const int rel = u - before * p.Hkv;
+    const int rel = u0 - before * p.Hkv;
     x.h = rel / x.rounds;
     x.r0 = rel - x.h * x.rounds;
-    x.r1 = min(x.rounds, x.r0 + (u1 - u));
+    x.r1 = min(x.rounds, x.r0 + (u1 - u0));
     x.len = lens[x.b];
     return x;
+  };
+  auto advance = [&](Piece& x, int u) {  // to the piece that begins at unit u < u1
+    if (++x.h == p.Hkv) {
+      x.h = 0;
+      do ++x.b;
+      while (scan[x.b + 1] == scan[x.b]);
+      x.rounds = scan[x.b + 1] - scan[x.b];
+      x.len = lens[x.b];
+    }
+    x.r0 = 0, x.r1 = min(x.rounds, u1 - u);
   };
 
   // ---- staging: the cursor of what is requested runs ahead of the computation, across the pieces of the stretch
   const int first_key = (rank * DP_WARPS + warp) * DP_BLOCK, stride = csize * DP_WARPS * DP_BLOCK;
-  int is_u = u0, is_key = 0, is_end = 0, is_h = 0, is_b = 0, is_id = -1;
+  Piece is_piece = first_piece();
+  int is_u = u0, is_key = 0, is_end = 0, is_id = -1;
   bool is_ok = false, timed_out = false;
-  const uint32_t stage0 = pq::smem_u32(dp_smem) + warp * DP_SLOTS * SLOT;
+  const uint8_t* const stage = dp_smem + warp * DP_SLOTS * SLOT;
+  const uint32_t stage0 = pq::smem_u32(stage);
   // lanes 0 .. 3 copy rows (group of 16 keys = bit 1, keys or values = bit 0), lanes 4 .. 7 the steps of the same
-  const int cp_group = (lane >> 1) & 1, cp_kv = lane & 1;
+  const int cp_group = (lane >> 1) & 1, cp_kv = lane & 1, page_mask = (1 << page_log2) - 1;
+  const bool cp_steps = DYN && (lane & 4), cp_lane = lane < (DYN ? 8 : 4);
+  const int cp_unit = cp_steps ? 4 : 64;  // bytes of a row
+  const uint32_t cp_bytes = cp_steps ? 64 : 1024;
+  const uint32_t cp_dst = stage0 + (cp_steps ? DP_BLOCK * 128 + cp_kv * (DP_BLOCK * 4) + cp_group * 64 : cp_kv * (DP_BLOCK * 64) + cp_group * 1024);
+  const uint8_t* const cp_base = cp_steps ? reinterpret_cast<const uint8_t*>(p.steps) : p.codes;
+  const int64_t page_bytes = static_cast<int64_t>(p.Hkv * 2 * cp_unit) << page_log2;
+  const uint8_t* is_src = cp_base;  // the head's rows inside a page
+  const int32_t* is_row = p.table;
+  // The page of this lane's group of the cursor's block. An id that is none is reported and page 0 read in its place.
   auto fetch_id = [&]() {
     const int k = is_key + 16 * cp_group;
-    is_id = is_ok && lane < (DYN ? 8 : 4) && k < is_end ? pq::ld_dep(p.table + static_cast<int64_t>(is_b) * p.max_pages + (k >> page_log2)) : -2;
+    is_id = cp_lane && k < is_end ? pq::ld_dep(is_row + (k >> page_log2)) : -1;
   };
   auto next_piece = [&]() {
     is_ok = false;
     while (is_u < u1) {
-      const Piece x = piece_at(is_u);
+      if (is_u != u0) advance(is_piece, is_u);
+      const Piece& x = is_piece;
       is_u += x.r1 - x.r0;
-      is_key = x.r0 * DP_ROUND + first_key, is_end = min(x.len, x.r1 * DP_ROUND), is_b = x.b, is_h = x.h;
+      is_key = x.r0 * DP_ROUND + first_key, is_end = min(x.len, x.r1 * DP_ROUND);
       if (is_key < is_end) {
         is_ok = true;
+        is_row = p.table + static_cast<int64_t>(x.b) * p.max_pages;
+        is_src = cp_base + ((static_cast<int64_t>(2 * x.h + cp_kv) * cp_unit) << page_log2);
+        fetch_id();
         break;
       }
     }
-    fetch_id();
   };
   int n_issued = 0, n_done = 0;
   auto issue = [&]() {  // the cursor's block into the next slot; the whole warp
     if (!is_ok) return;
-    const int s = n_issued % DP_SLOTS;
-    const bool good = is_id >= 0 && is_id < p.n_pages;
-    if (is_id != -2 && !good) pq::report(p.status, PQ_ERR_SHAPE);
-    const uint32_t mask = __ballot_sync(0xffffffffu, good);
-    if (lane == 0) pq::mbar_arrive_expect_tx(&full[warp][s], __popc(mask & 0xFu) * 1024u + __popc(mask & 0xF0u) * 64u);
-    __syncwarp();
-    if (good) {
-      const int k = is_key + 16 * cp_group;
-      const int64_t vec = (((static_cast<int64_t>(is_id) * p.Hkv + is_h) * 2 + cp_kv) << page_log2) + (k & ((1 << page_log2) - 1));
-      const uint32_t slot = stage0 + s * SLOT;
-      if (!DYN || lane < 4)
-        pq::bulk_load(slot + cp_kv * (DP_BLOCK * 64) + cp_group * 1024, p.codes + vec * 64, 1024, &full[warp][s]);
-      else
-        pq::bulk_load(slot + DP_BLOCK * 128 + cp_kv * (DP_BLOCK * 4) + cp_group * 64, p.steps + vec, 64, &full[warp][s]);
+    const int s = n_issued % DP_SLOTS, k = is_key + 16 * cp_group;
+    uint64_t* bar = &full[warp][s];
+    const bool both = is_key + 16 < is_end;
+    if (lane == 0) pq::mbar_arrive_expect_tx(bar, (both ? 2u : 1u) * (2 * 1024 + (DYN ? 2 * 64 : 0)));
+    if (cp_lane && k < is_end) {
+      if (static_cast<uint32_t>(is_id) >= static_cast<uint32_t>(p.n_pages)) {
+        pq::report(p.status, PQ_ERR_SHAPE);
+        is_id = 0;
+      }
+      pq::bulk_load(cp_dst + s * SLOT, is_src + is_id * page_bytes + (k & page_mask) * cp_unit, cp_bytes, bar);
     }
     ++n_issued;
     is_key += stride;
@@ -214,23 +242,29 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
   next_piece();
   for (int s = 0; s < DP_SLOTS; ++s) issue();
 
+  // What a piece needs first, requested while the piece before it is merged: 8 dims of a query head (sixteen threads to a head) and the steps.
+  Piece x = first_piece();
+  int row = 0;
+  uint4 q_raw;
+  float s_k_h, s_v_h;
+  auto request = [&]() {
+    row = direct ? row_direct : rows[x.b];
+    const int head = threadIdx.x >> 4;
+    const __nv_bfloat16* q0 = p.q + row * p.ldq + static_cast<int64_t>(x.h) * G * 128;
+    q_raw = head < G ? pq::ld_dep(reinterpret_cast<const uint4*>(q0 + head * 128) + (threadIdx.x & 15)) : make_uint4(0, 0, 0, 0);
+    s_k_h = DYN ? 1.0f : pq::ld_dep(p.s_k + x.h), s_v_h = DYN ? 1.0f : pq::ld_dep(p.s_v + x.h);
+  };
+  request();
+  int n_shared = 0;  // pairs this worker shares with others: its first and its last
   for (int u = u0; u < u1;) {
-    const Piece x = piece_at(u);
-    const int row = row_of(x.b), kend = min(x.len, x.r1 * DP_ROUND);
+    const int kend = min(x.len, x.r1 * DP_ROUND);
     const bool whole = x.r0 == 0 && x.r1 == x.rounds;
     const bool has_prefix = x.r0 == 0 && rank == csize - 1 && p.n_prefix > 0;  // the CTA with the fewest blocks of the pair's first stretch
     const __nv_bfloat16* q0 = p.q + row * p.ldq + static_cast<int64_t>(x.h) * G * 128;
-    const bool row_ok = g < G;
-    uint4 q_raw[4];  // 32 bf16 of query head g: dims 32t .. 32t+31
-    {
-      const uint4* q4 = reinterpret_cast<const uint4*>(q0 + (row_ok ? g : 0) * 128 + 32 * t);
-#pragma unroll
-      for (int w = 0; w < 4; ++w) q_raw[w] = row_ok ? pq::ld_dep(q4 + w) : make_uint4(0, 0, 0, 0);
-    }
-    const float s_k_h = DYN ? 1.0f : pq::ld_dep(p.s_k + x.h), s_v_h = DYN ? 1.0f : pq::ld_dep(p.s_v + x.h);
+    const float value_unit = s_v_h;
+    __syncthreads();  // what the warps read of the piece before, they have read
     // ---- prefix keys in fp32: eight lanes per (head, key) pair, 16 dims each
     if (has_prefix) {
-      __syncthreads();  // the scores of the pair before have been read
       const int n_pairs = G * p.n_prefix, sub = threadIdx.x & 7;
       for (int pair0 = 0; pair0 < n_pairs; pair0 += DP_THREADS / 8) {
         const int pair = pair0 + (threadIdx.x >> 3);
@@ -253,97 +287,121 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
         acc += __shfl_xor_sync(0xffffffffu, acc, 1);
         acc += __shfl_xor_sync(0xffffffffu, acc, 2);
         acc += __shfl_xor_sync(0xffffffffu, acc, 4);
-        if (ok && sub == 0) sm_pre[r][j] = acc * p.scale2;
+        if (ok && sub == 0) sm_pre[r * p.n_prefix + j] = acc * p.scale2;
       }
     }
-    // ---- query fragments. A 32-bit word of a packed key row holds the codes of dims 8W..8W+7; nibble i of its low half is dim 8W+i, nibble i of
-    // its high half dim 8W+4+i. Fragment j of a lane holds (q[D], q[D+4]) in its first and (q[D+1], q[D+5]) / 16 in its second register
-    // with D = 32t + 8(j>>1) + 2(j&1), of head g: the k rows 2t, 2t+1 and 2t+8, 2t+9 of score MMA j.
-    uint32_t qb[8][2];
-    float f_lo, f_hi;  // what a raw score of heads 2t, 2t + 1 is multiplied with: log2 units (DYN: times the key's step)
+    // ---- the query as B operand, made once per CTA: sixteen threads to a head, eight dims each. A 32-bit word of a packed key row holds the codes of dims
+    // 8W..8W+7; nibble i of its low half is dim 8W+i, nibble i of its high half dim 8W+4+i. Fragment j of a lane holds (q[D], q[D+4]) in its
+    // first and (q[D+1], q[D+5]) / 16 in its second register with D = 32t + 8(j>>1) + 2(j&1), of head g: the k rows 2t, 2t+1 and 2t+8,
+    // 2t+9 of score MMA j.
     {
+      const int head = threadIdx.x >> 4, part8 = threadIdx.x & 15;
+      const uint32_t ww[4] = {q_raw.x, q_raw.y, q_raw.z, q_raw.w};
       uint32_t top = 0;  // largest magnitude of the head as bits
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const uint32_t ww[4] = {q_raw[w].x, q_raw[w].y, q_raw[w].z, q_raw[w].w};
+      for (int e = 0; e < 4; ++e) top = max(top, max(ww[e] & 0x7FFF0000u, (ww[e] << 16) & 0x7FFF0000u));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) top = max(top, max(ww[e] & 0x7FFF0000u, (ww[e] << 16) & 0x7FFF0000u));
-      }
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      for (int m = 1; m < 16; m <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, m));
       // a power of two that brings the largest value to [2^8, 2^9); the scale and its inverse are normal numbers
       int ex = static_cast<int>(top >> 23);
       ex = ex < 10 ? 10 : ex > 254 ? 254 : ex;  // (a head of zeros, subnormals, infinities or NaN)
-      const float up = __uint_as_float(static_cast<uint32_t>(127 + 8 + 127 - ex) << 23);
-      const float down = 1.0f / up;
+      const float up = __uint_as_float(static_cast<uint32_t>(127 + 8 + 127 - ex) << 23), down = 1.0f / up;
+      float f[8], sum = 0.0f;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const uint32_t ww[4] = {q_raw[w].x, q_raw[w].y, q_raw[w].z, q_raw[w].w};
-        float f[8];
+      for (int e = 0; e < 8; ++e) f[e] = __uint_as_float((e & 1) ? (ww[e >> 1] & 0xFFFF0000u) : (ww[e >> 1] << 16)) * up;
+      uint32_t frag[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = __uint_as_float((e & 1) ? (ww[e >> 1] & 0xFFFF0000u) : (ww[e >> 1] << 16)) * up;
-#pragma unroll
-        for (int jj = 0; jj < 2; ++jj) {  // score MMA j = 2w + jj uses nibbles 2jj and 2jj + 1
-          qb[2 * w + jj][0] = pq::pack_f16(f[2 * jj], f[2 * jj + 4]);
-          qb[2 * w + jj][1] = pq::pack_f16(f[2 * jj + 1] * 0.0625f, f[2 * jj + 5] * 0.0625f);
-        }
+      for (int jj = 0; jj < 2; ++jj) {  // score MMA j = 2 (dims / 8) + jj uses nibbles 2jj and 2jj + 1
+        frag[2 * jj] = pq::pack_f16(f[2 * jj], f[2 * jj + 4]);
+        frag[2 * jj + 1] = pq::pack_f16(f[2 * jj + 1] * 0.0625f, f[2 * jj + 5] * 0.0625f);
+        // the offset is that of the values the MMA multiplies with
+        const float2 e0 = __half22float2(*reinterpret_cast<const __half2*>(&frag[2 * jj])), e1 = __half22float2(*reinterpret_cast<const __half2*>(&frag[2 * jj + 1]));
+        sum += (e0.x + e0.y) + 16.0f * (e1.x + e1.y);
       }
-      const float factor = down * s_k_h * p.scale2;
-      f_lo = __shfl_sync(0xffffffffu, factor, 8 * t), f_hi = __shfl_sync(0xffffffffu, factor, 8 * t + 4);
+#pragma unroll
+      for (int m = 1; m < 16; m <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
+      const float unit = down * s_k_h * p.scale2;
+      sm_q[head][part8] = make_uint4(frag[0], frag[1], frag[2], frag[3]);
+      if (part8 == 0) sm_f[head] = make_float2(unit * 16777216.0f, -8.0f * sum * unit);
     }
+    __syncthreads();
+    uint32_t qb[8][2];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const uint4 v = sm_q[g][4 * t + w];
+      qb[2 * w][0] = v.x, qb[2 * w][1] = v.y, qb[2 * w + 1][0] = v.z, qb[2 * w + 1][1] = v.w;
+    }
+    // a raw score r of heads 2t, 2t + 1 is r f + n in log2 units (DYN: times the key's step)
+    const float2 fn0 = sm_f[2 * t], fn1 = sm_f[2 * t + 1];
+    const float f_lo = fn0.x, f_hi = fn1.x, n_lo = fn0.y, n_hi = fn1.y;
     // Reference exponents of heads 2t and 2t + 1 (the same in all lanes of equal t). A head that does not exist keeps a huge one: its
     // weights are zero and it never asks for a move.
     float m0 = 2 * t < G ? -INFINITY : 1e30f, m1 = 2 * t + 1 < G ? -INFINITY : 1e30f;
-    float o[8][4];  // tile m: o[m][0], o[m][1] = dim 16g+2m of heads 2t, 2t+1, o[m][2], o[m][3] = 16 x dim 16g+2m+1
+    float z0 = m0 == -INFINITY ? 0.0f : m0, z1 = m1 == -INFINITY ? 0.0f : m1;  // what is subtracted (-inf less -inf would be no number)
+    // Tile m, times 2^24: o[m][0], o[m][1] = dim 16g+2m of heads 2t, 2t+1, o[m][2], o[m][3] = 16 x dim 16g+2m+1, each with 8 sum(weight) too much:
+    // that is `zero`, summed by the same instructions in the same order over codes of zero, so that the two carry the same bias of
+    // the accumulation. It also is the denominator (static steps).
+    float o[8][4];
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
-    float lacc[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // [0], [1]: denominators of heads 2t, 2t+1
+    float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    float den0 = 0.0f, den1 = 0.0f;  // DYN: this lane's shares of the denominators of heads 2t, 2t+1
 
     const uint32_t k_off = g * 64 + 16 * t;      // key g (and g + 8): 32 codes at dims 32t..32t+31
     const uint32_t v_off = (2 * t) * 64 + 8 * g;  // keys 2t, 2t+1, 2t+8, 2t+9: 16 codes at dims 16g..16g+15
     for (int key0 = x.r0 * DP_ROUND + first_key; key0 < kend; key0 += stride) {
       const int s = n_done % DP_SLOTS;
-      if (timed_out || n_done >= n_issued ||
-          __any_sync(0xffffffffu, !pq::mbar_wait_for(&full[warp][s], (n_done / DP_SLOTS) & 1, p.wait_clocks))) {
+      bool late = !__all_sync(0xffffffffu, pq::mbar_try_wait(&full[warp][s], (n_done / DP_SLOTS) & 1));
+      if (late) late = timed_out || n_done >= n_issued || __any_sync(0xffffffffu, !pq::mbar_wait_for(&full[warp][s], (n_done / DP_SLOTS) & 1, p.wait_clocks));
+      if (late) {
         timed_out = true;  // nothing more is requested; the pieces run out without work
         is_ok = false;
         break;
       }
-      const uint32_t slot = stage0 + s * SLOT;
-      float c[2][4];  // scores: [0], [1] = key g x heads 2t, 2t+1; [2], [3] = key g + 8 x the same heads
+      const uint8_t* const slot = stage + s * SLOT;
       float rs[2][2];  // DYN: 1 / step of the values of keys g, g + 8
+      float c[2][4];  // scores: [0], [1] = key g x heads 2t, 2t+1; [2], [3] = key g + 8 x the same heads
+      if (DYN) {
+        // lane j turns the steps of key j into what all lanes need, once: (step of the key, log2 and reciprocal of the step of the value); a key past the
+        // end has the score -inf
+        const float* st = reinterpret_cast<const float*>(slot + DP_BLOCK * 128) + lane;
+        const float k_step = st[0], v_step = st[DP_BLOCK];
+        const bool dead = key0 + lane >= kend;
+        sm_step[warp][lane] = dead ? make_float4(0.0f, -INFINITY, 0.0f, 0.0f) : make_float4(k_step, pq::lg2_approx(v_step), pq::rcp_approx(v_step), 0.0f);
+        __syncwarp();
+      }
 #pragma unroll
       for (int v = 0; v < 2; ++v) {
-        const uint32_t kb = slot + v * 1024;
-        const uint4 kc0 = pq::lds128(kb + k_off), kc1 = pq::lds128(kb + k_off + 8 * 64);
+        const uint8_t* kb = slot + v * 1024 + k_off;
+        const uint4 kc0 = *reinterpret_cast<const uint4*>(kb), kc1 = *reinterpret_cast<const uint4*>(kb + 8 * 64);
         float ca[4] = {0.0f, 0.0f, 0.0f, 0.0f}, cb[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         const uint32_t wl[4] = {kc0.x, kc0.y, kc0.z, kc0.w}, wh[4] = {kc1.x, kc1.y, kc1.z, kc1.w};
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           const uint32_t wl8 = wl[w] >> 8, wh8 = wh[w] >> 8;
-          mma_f16(ca, codes_lo(wl[w]), codes_lo(wh[w]), codes_hi16(wl[w]), codes_hi16(wh[w]), qb[2 * w][0], qb[2 * w][1]);
-          mma_f16(cb, codes_lo(wl8), codes_lo(wh8), codes_hi16(wl8), codes_hi16(wh8), qb[2 * w + 1][0], qb[2 * w + 1][1]);
+          mma_f16(ca, codes_lo(wl[w]), codes_lo(wh[w]), codes_hi(wl[w]), codes_hi(wh[w]), qb[2 * w][0], qb[2 * w][1]);
+          mma_f16(cb, codes_lo(wl8), codes_lo(wh8), codes_hi(wl8), codes_hi(wh8), qb[2 * w + 1][0], qb[2 * w + 1][1]);
         }
-        const bool dead_lo = key0 + 16 * v + g >= kend, dead_hi = key0 + 16 * v + 8 + g >= kend;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c[v][i] = fmaf(ca[i] + cb[i], i & 1 ? f_hi : f_lo, i & 1 ? n_hi : n_lo);
         if (DYN) {
-          const uint32_t st = slot + DP_BLOCK * 128 + (16 * v + g) * 4;
-          const float k_lo = pq::lds32f(st), k_hi = pq::lds32f(st + 32);
-          const float v_lo = dead_lo ? 1.0f : pq::lds32f(st + DP_BLOCK * 4), v_hi = dead_hi ? 1.0f : pq::lds32f(st + DP_BLOCK * 4 + 32);
-          const float b_lo = pq::lg2_approx(v_lo), b_hi = pq::lg2_approx(v_hi);
-          rs[v][0] = pq::rcp_approx(v_lo), rs[v][1] = pq::rcp_approx(v_hi);
-          c[v][0] = fmaf(ca[0] + cb[0], f_lo * k_lo, b_lo), c[v][1] = fmaf(ca[1] + cb[1], f_hi * k_lo, b_lo);
-          c[v][2] = fmaf(ca[2] + cb[2], f_lo * k_hi, b_hi), c[v][3] = fmaf(ca[3] + cb[3], f_hi * k_hi, b_hi);
-        } else {
-          c[v][0] = (ca[0] + cb[0]) * f_lo, c[v][1] = (ca[1] + cb[1]) * f_hi;
-          c[v][2] = (ca[2] + cb[2]) * f_lo, c[v][3] = (ca[3] + cb[3]) * f_hi;
+          const float4 a = sm_step[warp][16 * v + g], b = sm_step[warp][16 * v + 8 + g];
+          c[v][0] = fmaf(c[v][0], a.x, a.y), c[v][1] = fmaf(c[v][1], a.x, a.y);
+          c[v][2] = fmaf(c[v][2], b.x, b.y), c[v][3] = fmaf(c[v][3], b.x, b.y);
+          rs[v][0] = a.z, rs[v][1] = b.z;
         }
-        if (dead_lo) c[v][0] = c[v][1] = -INFINITY;
-        if (dead_hi) c[v][2] = c[v][3] = -INFINITY;
+      }
+      if (!DYN && key0 + DP_BLOCK > kend) {  // the last block of a sequence
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          if (key0 + 16 * v + g >= kend) c[v][0] = c[v][1] = -INFINITY;
+          if (key0 + 16 * v + 8 + g >= kend) c[v][2] = c[v][3] = -INFINITY;
+        }
       }
       // maxima of heads 2t, 2t+1 over this lane's keys; a reference moves only when one exceeds it by more than the headroom (the first
       // block of a warp always takes this path)
-      float x0 = fmaxf(fmaxf(c[0][0], c[0][2]), fmaxf(c[1][0], c[1][2])), x1 = fmaxf(fmaxf(c[0][1], c[0][3]), fmaxf(c[1][1], c[1][3]));
-      if (__any_sync(0xffffffffu, x0 - DP_HEADROOM > m0 || x1 - DP_HEADROOM > m1)) {
+      float x0 = max3(c[0][0], c[0][2], fmaxf(c[1][0], c[1][2])), x1 = max3(c[0][1], c[0][3], fmaxf(c[1][1], c[1][3]));
+      if (__any_sync(0xffffffffu, x0 > m0 + DP_HEADROOM || x1 > m1 + DP_HEADROOM)) {
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) {
           x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, d));
@@ -352,36 +410,35 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
         const float n0 = fmaxf(m0, x0), n1 = fmaxf(m1, x1);
         const float a_lo = n0 == -INFINITY ? 1.0f : pq::ex2_approx(m0 - n0), a_hi = n1 == -INFINITY ? 1.0f : pq::ex2_approx(m1 - n1);
         m0 = n0, m1 = n1;
-        lacc[0] *= a_lo, lacc[1] *= a_hi, lacc[2] *= a_lo, lacc[3] *= a_hi;
+        zero[0] *= a_lo, zero[1] *= a_hi, zero[2] *= a_lo, zero[3] *= a_hi;
+        den0 *= a_lo, den1 *= a_hi;
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[i][0] *= a_lo, o[i][1] *= a_hi, o[i][2] *= a_lo, o[i][3] *= a_hi;
+        z0 = m0 == -INFINITY ? 0.0f : m0, z1 = m1 == -INFINITY ? 0.0f : m1;
       }
-      const float z0 = m0 == -INFINITY ? 0.0f : m0, z1 = m1 == -INFINITY ? 0.0f : m1;  // (-inf less -inf would be no number)
 #pragma unroll
       for (int v = 0; v < 2; ++v) {
-        const uint32_t vb = slot + DP_BLOCK * 64 + v * 1024;
-        const uint2 vc0 = pq::lds64(vb + v_off), vc1 = pq::lds64(vb + v_off + 64);
-        const uint2 vc2 = pq::lds64(vb + v_off + 8 * 64), vc3 = pq::lds64(vb + v_off + 9 * 64);
+        const uint8_t* vb = slot + DP_BLOCK * 64 + v * 1024 + v_off;
+        const uint2 vc0 = *reinterpret_cast<const uint2*>(vb), vc1 = *reinterpret_cast<const uint2*>(vb + 64);
+        const uint2 vc2 = *reinterpret_cast<const uint2*>(vb + 8 * 64), vc3 = *reinterpret_cast<const uint2*>(vb + 9 * 64);
         const float w0 = pq::ex2_approx(c[v][0] - z0), w1 = pq::ex2_approx(c[v][1] - z1);
         const float w2 = pq::ex2_approx(c[v][2] - z0), w3 = pq::ex2_approx(c[v][3] - z1);
         // weights in fp16, transposed from (key, head pair) to the (key pair, head) layout of an MMA B operand
         const uint32_t pb0 = movmatrix_trans(pq::pack_f16(w0, w1)), pb1 = movmatrix_trans(pq::pack_f16(w2, w3));
         if (DYN) {
-          lacc[0] = fmaf(w0, rs[v][0], lacc[0]), lacc[1] = fmaf(w1, rs[v][0], lacc[1]);
-          lacc[0] = fmaf(w2, rs[v][1], lacc[0]), lacc[1] = fmaf(w3, rs[v][1], lacc[1]);
-        } else {  // the denominator sums the same rounded weights the output MMA multiplies with
-          mma_f16(lacc, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u, pb0, pb1);
+          den0 = fmaf(w0, rs[v][0], den0), den1 = fmaf(w1, rs[v][0], den1);
+          den0 = fmaf(w2, rs[v][1], den0), den1 = fmaf(w3, rs[v][1], den1);
         }
-        // ---- O^T += V^T P^T. A merged word pairs the same four dims of two neighbouring keys; nibbles 1 and 3 give 16 x code (rows g + 8 of the
-        // tile, rescaled at the end).
+        mma_f16(zero, codes_lo(0u), codes_hi(0u), codes_lo(0u), codes_hi(0u), pb0, pb1);
+        // ---- O^T += V^T P^T. A merged word pairs the same four dims of two neighbouring keys; nibbles 1 and 3 (16 x) are the rows g + 8 of the tile.
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4) {
           const uint32_t sel = (q4 & 1) ? 0x7632u : 0x5410u;
           const uint32_t ya = __byte_perm(q4 < 2 ? vc0.x : vc0.y, q4 < 2 ? vc1.x : vc1.y, sel);
           const uint32_t yb = __byte_perm(q4 < 2 ? vc2.x : vc2.y, q4 < 2 ? vc3.x : vc3.y, sel);
           const uint32_t ya8 = ya >> 8, yb8 = yb >> 8;
-          mma_f16(o[2 * q4], codes_lo(ya), codes_hi16(ya), codes_lo(yb), codes_hi16(yb), pb0, pb1);
-          mma_f16(o[2 * q4 + 1], codes_lo(ya8), codes_hi16(ya8), codes_lo(yb8), codes_hi16(yb8), pb0, pb1);
+          mma_f16(o[2 * q4], codes_lo(ya), codes_hi(ya), codes_lo(yb), codes_hi(yb), pb0, pb1);
+          mma_f16(o[2 * q4 + 1], codes_lo(ya8), codes_hi(ya8), codes_lo(yb8), codes_hi(yb8), pb0, pb1);
         }
       }
       ++n_done;
@@ -389,32 +446,44 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
       issue();
     }
 
-    // ---- merge the warps of this CTA and the prefix into one partial, in value units
-    __syncthreads();  // the partials of the piece before have been read
+    // ---- merge the warps of this CTA and the prefix into one partial, in value units. The next piece's first loads and the first prefix values are
+    // requested ahead of the barrier.
+    const Piece done = x;
+    const int done_row = row, next_u = u + (x.r1 - x.r0);
+    if (next_u < u1) {
+      advance(x, next_u);
+      request();
+    }
+    uint2 pv[4];
+    const uint2* const pv_row = reinterpret_cast<const uint2*>(p.prefix_v + static_cast<int64_t>(done.h) * p.n_prefix * 128) + lane;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) pv[j] = has_prefix && j < p.n_prefix ? pq::ld_dep(pv_row + j * 32) : make_uint2(0u, 0u);
 #pragma unroll
     for (int hh = 0; hh < 2; ++hh) {
       const int head = 2 * t + hh;
       if (head < G) {
 #pragma unroll
         for (int m = 0; m < 8; ++m)
-          *reinterpret_cast<float2*>(sm_o + (warp * DP_ROWS + head) * DP_SO_STRIDE + 16 * m + 2 * g) = make_float2(o[m][hh], o[m][2 + hh] * 0.0625f);
+          *reinterpret_cast<float2*>(sm_o + (warp * G + head) * DP_SO_STRIDE + 16 * m + 2 * g) = make_float2((o[m][hh] - zero[hh]) * 16777216.0f, (o[m][2 + hh] - zero[2 + hh]) * 1048576.0f);
       }
     }
     if (DYN) {
 #pragma unroll
       for (int d = 4; d < 32; d <<= 1) {
-        lacc[0] += __shfl_xor_sync(0xffffffffu, lacc[0], d);
-        lacc[1] += __shfl_xor_sync(0xffffffffu, lacc[1], d);
+        den0 += __shfl_xor_sync(0xffffffffu, den0, d);
+        den1 += __shfl_xor_sync(0xffffffffu, den1, d);
       }
+    } else {
+      den0 = zero[0] * 2097152.0f, den1 = zero[1] * 2097152.0f;  // 2^24 / 8
     }
     if (g == 0) {
-      if (2 * t < G) sm_ml[warp][2 * t][0] = m0, sm_ml[warp][2 * t][1] = lacc[0];
-      if (2 * t + 1 < G) sm_ml[warp][2 * t + 1][0] = m1, sm_ml[warp][2 * t + 1][1] = lacc[1];
+      if (2 * t < G) sm_ml[warp][2 * t][0] = m0, sm_ml[warp][2 * t][1] = den0;
+      if (2 * t + 1 < G) sm_ml[warp][2 * t + 1][0] = m1, sm_ml[warp][2 * t + 1][1] = den1;
     }
     __syncthreads();
     // partial of this worker: slot 2w when the pair began with an earlier worker, 2w + 1 when it begins here and goes on
-    const int64_t ws_slot = (2 * static_cast<int64_t>(worker) + (x.r0 == 0 ? 1 : 0)) * G;
-    __nv_bfloat16* dst = p.out + (static_cast<int64_t>(row) * p.Hq + static_cast<int64_t>(x.h) * G) * 128;
+    const int64_t ws_slot = (2 * static_cast<int64_t>(worker) + (done.r0 == 0 ? 1 : 0)) * G;
+    __nv_bfloat16* dst = p.out + (static_cast<int64_t>(done_row) * p.Hq + static_cast<int64_t>(done.h) * G) * 128;
     {
       // warp w takes the heads w, w + 4; a lane the head dims 4 lane .. 4 lane + 3
       const int n_pre = has_prefix ? p.n_prefix : 0;
@@ -423,28 +492,32 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
         float m = -INFINITY;
 #pragma unroll
         for (int w = 0; w < DP_WARPS; ++w) m = fmaxf(m, sm_ml[w][r][0]);
-        for (int j = 0; j < n_pre; ++j) m = fmaxf(m, sm_pre[r][j]);
+        for (int j = 0; j < n_pre; ++j) m = fmaxf(m, sm_pre[r * p.n_prefix + j]);
         float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         float l = 0.0f;
 #pragma unroll
         for (int w = 0; w < DP_WARPS; ++w) {
           const float mw = sm_ml[w][r][0];
           const float e = mw == -INFINITY ? 0.0f : pq::ex2_approx(mw - m);
-          const float* src = sm_o + (w * DP_ROWS + r) * DP_SO_STRIDE + qpos;
+          const float* src = sm_o + (w * G + r) * DP_SO_STRIDE + qpos;
           const float2 lo = *reinterpret_cast<const float2*>(src), hi = *reinterpret_cast<const float2*>(src + 16);
           acc.x = fmaf(lo.x, e, acc.x), acc.y = fmaf(lo.y, e, acc.y), acc.z = fmaf(hi.x, e, acc.z), acc.w = fmaf(hi.y, e, acc.w);
           l = fmaf(sm_ml[w][r][1], e, l);
         }
-        acc.x *= s_v_h, acc.y *= s_v_h, acc.z *= s_v_h, acc.w *= s_v_h;
-        for (int j = 0; j < n_pre; ++j) {
-          const float e = pq::ex2_approx(sm_pre[r][j] - m);
-          const uint2 pv = pq::ld_dep(reinterpret_cast<const uint2*>(p.prefix_v + (static_cast<int64_t>(x.h) * p.n_prefix + j) * 128) + lane);
-          const float2 v01 = __half22float2(*reinterpret_cast<const __half2*>(&pv.x)), v23 = __half22float2(*reinterpret_cast<const __half2*>(&pv.y));
+        acc.x *= value_unit, acc.y *= value_unit, acc.z *= value_unit, acc.w *= value_unit;
+        auto add_prefix = [&](int j, const uint2& v) {
+          const float e = pq::ex2_approx(sm_pre[r * p.n_prefix + j] - m);
+          const float2 v01 = __half22float2(*reinterpret_cast<const __half2*>(&v.x)), v23 = __half22float2(*reinterpret_cast<const __half2*>(&v.y));
           acc.x = fmaf(e, v01.x, acc.x), acc.y = fmaf(e, v01.y, acc.y), acc.z = fmaf(e, v23.x, acc.z), acc.w = fmaf(e, v23.y, acc.w);
           l += e;
-        }
+        };
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (j < n_pre) add_prefix(j, pv[j]);
+        for (int j = 4; j < n_pre; ++j) add_prefix(j, pq::ld_dep(pv_row + j * 32));
         if (csize > 1) {
-          *reinterpret_cast<float4*>(cl_o + r * 128 + 4 * lane) = acc;
+          __syncwarp();  // the rows of this head are this warp's alone: all lanes have read them
+          *reinterpret_cast<float4*>(cl_o + r * DP_SO_STRIDE + 4 * lane) = acc;
           if (lane == 0) cl_ml[r] = make_float2(m, l);
         } else if (whole) {
           store_out(dst + r * 128 + 4 * lane, acc, l > 0.0f ? 1.0f / l : 0.0f);
@@ -459,7 +532,7 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
       pq::cluster_sync();
       for (int item = rank * DP_THREADS + threadIdx.x; item < G * 32; item += csize * DP_THREADS) {
         const int r = item >> 5, c4 = item & 31;
-        const uint32_t o_addr = pq::smem_u32(cl_o + r * 128 + 4 * c4), ml_addr = pq::smem_u32(cl_ml + r);
+        const uint32_t o_addr = pq::smem_u32(cl_o + r * DP_SO_STRIDE + 4 * c4), ml_addr = pq::smem_u32(cl_ml + r);
         float4 v[DP_MAX_CLUSTER];
         float2 ml[DP_MAX_CLUSTER];
 #pragma unroll
@@ -488,49 +561,67 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
       }
       pq::cluster_sync();  // the partials in shared memory have been read, those in the workspace written
     }
-    if (!whole && rank == 0) {
-      // the pair's units are shared by the workers w0 .. w1; the last of them to come here merges their partials in that order
-      const int pair0 = u - x.r0, pair1 = pair0 + x.rounds - 1;
+    if (!whole) {  // the pair's units are shared by several workers
+      const int pair0 = u - done.r0;
       auto worker_of = [&](int unit) { return static_cast<int>(((static_cast<int64_t>(unit) + 1) * n_workers - 1) / U); };
-      const int w0 = worker_of(pair0), w1 = worker_of(pair1);
-      __threadfence();
-      __syncthreads();
-      if (threadIdx.x == 0) sm_last = atomicAdd(p.tickets + PQ_PAGED_TICKET0 + w0, 1u) == static_cast<uint32_t>(w1 - w0);
-      __syncthreads();
-      if (sm_last) {
-        __threadfence();
-        for (int r = warp; r < G; r += DP_WARPS) {
-          float m = -INFINITY, l = 0.0f;
-          float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-          for (int base = w0; base <= w1; base += 32) {  // a lane per partial for the weights, then the partials in turn
-            const int n = min(32, w1 - base + 1);
-            const int64_t mine = 2 * static_cast<int64_t>(base + lane) + (base + lane == w0 ? 1 : 0);
-            const float2 ml = lane < n ? __ldcg(reinterpret_cast<const float2*>(p.ws_ml) + mine * G + r) : make_float2(-INFINITY, 0.0f);
-            float mc = ml.x;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) mc = fmaxf(mc, __shfl_xor_sync(0xffffffffu, mc, d));
-            const float mn = fmaxf(m, mc), keep = m == -INFINITY ? 0.0f : pq::ex2_approx(m - mn);
-            const float w = ml.x == -INFINITY ? 0.0f : pq::ex2_approx(ml.x - mn);
-            float lw = ml.y * w;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) lw += __shfl_xor_sync(0xffffffffu, lw, d);
-            l = l * keep + lw;
-            m = mn;
-            acc.x *= keep, acc.y *= keep, acc.z *= keep, acc.w *= keep;
-#pragma unroll 8
-            for (int i = 0; i < n; ++i) {
-              const int64_t slot = 2 * static_cast<int64_t>(base + i) + (base + i == w0 ? 1 : 0);
-              const float4 v = __ldcg(reinterpret_cast<const float4*>(p.ws_o) + (slot * G + r) * 32 + lane);
-              const float wi = __shfl_sync(0xffffffffu, w, i);
-              acc.x = fmaf(v.x, wi, acc.x), acc.y = fmaf(v.y, wi, acc.y), acc.z = fmaf(v.z, wi, acc.z), acc.w = fmaf(v.w, wi, acc.w);
-            }
-          }
-          store_out(dst + r * 128 + 4 * lane, acc, l > 0.0f ? 1.0f / l : 0.0f);
-        }
-        if (threadIdx.x == 0) p.tickets[PQ_PAGED_TICKET0 + w0] = 0;
-      }
+      if (threadIdx.x == 0) sm_shared[n_shared & 1] = make_int4(done_row, done.h, worker_of(pair0), worker_of(pair0 + done.rounds - 1));
+      ++n_shared;
     }
-    u += x.r1 - x.r0;
+    u = next_u;
+  }
+  // ---- the last of the workers w0 .. w1 of a shared pair to come here merges their partials, in that order. The tickets of both pairs are
+  // drawn together at the end: one trip, and the fence in front of it has little left to wait for.
+  if (n_shared > 0 && rank == 0) {
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x < n_shared) {
+      const int w0 = sm_shared[threadIdx.x].z, w1 = sm_shared[threadIdx.x].w;
+      sm_last[threadIdx.x] = atomicAdd(p.tickets + PQ_PAGED_TICKET0 + w0, 1u) == static_cast<uint32_t>(w1 - w0);
+    }
+    __syncthreads();
+    __threadfence();
+    for (int i = 0; i < n_shared; ++i) {
+      if (!sm_last[i]) continue;
+      const int w0 = sm_shared[i].z, w1 = sm_shared[i].w;
+      __nv_bfloat16* dst = p.out + (static_cast<int64_t>(sm_shared[i].x) * p.Hq + static_cast<int64_t>(sm_shared[i].y) * G) * 128;
+      for (int r = warp; r < G; r += DP_WARPS) {
+        float m = -INFINITY, l = 0.0f;
+        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int base = w0; base <= w1; base += 32) {  // a lane per partial for the weights, then the partials in turn
+          const int n = min(32, w1 - base + 1);
+          const int64_t mine = 2 * static_cast<int64_t>(base + lane) + (base + lane == w0 ? 1 : 0);
+          const float2 ml = lane < n ? __ldcg(reinterpret_cast<const float2*>(p.ws_ml) + mine * G + r) : make_float2(-INFINITY, 0.0f);
+          float4 ahead[8];  // the first partials are on their way while the weights are formed
+          auto load = [&](int k) {
+            const int64_t slot = 2 * static_cast<int64_t>(base + k) + (base + k == w0 ? 1 : 0);
+            return __ldcg(reinterpret_cast<const float4*>(p.ws_o) + (slot * G + r) * 32 + lane);
+          };
+#pragma unroll
+          for (int k = 0; k < 8; ++k) ahead[k] = k < n ? load(k) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          float mc = ml.x;
+#pragma unroll
+          for (int d = 1; d < 32; d <<= 1) mc = fmaxf(mc, __shfl_xor_sync(0xffffffffu, mc, d));
+          const float mn = fmaxf(m, mc), keep = m == -INFINITY ? 0.0f : pq::ex2_approx(m - mn);
+          const float w = ml.x == -INFINITY ? 0.0f : pq::ex2_approx(ml.x - mn);
+          float lw = ml.y * w;
+#pragma unroll
+          for (int d = 1; d < 32; d <<= 1) lw += __shfl_xor_sync(0xffffffffu, lw, d);
+          l = l * keep + lw;
+          m = mn;
+          acc.x *= keep, acc.y *= keep, acc.z *= keep, acc.w *= keep;
+          auto add = [&](const float4& v, int k) {
+            const float wk = __shfl_sync(0xffffffffu, w, k);
+            acc.x = fmaf(v.x, wk, acc.x), acc.y = fmaf(v.y, wk, acc.y), acc.z = fmaf(v.z, wk, acc.z), acc.w = fmaf(v.w, wk, acc.w);
+          };
+#pragma unroll
+          for (int k = 0; k < 8; ++k) add(ahead[k], k);  // (those past n are zeros)
+#pragma unroll 4
+          for (int k = 8; k < n; ++k) add(load(k), k);
+        }
+        store_out(dst + r * 128 + 4 * lane, acc, l > 0.0f ? 1.0f / l : 0.0f);
+      }
+      if (threadIdx.x == 0) p.tickets[PQ_PAGED_TICKET0 + w0] = 0;
+    }
   }
   // every copy that was started has landed before the shared memory is given back (after a wait that ran out some are still on their way)
   if (lane == 0) {
@@ -540,42 +631,81 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
   __syncwarp();
 }
 
-int resident_ctas(const pq_ctx* ctx) { return 4 * ctx->sm_count; }
+constexpr int DP_CTAS_PER_SM = 4;
+
+int most_ctas(const pq_ctx* ctx) { return DP_CTAS_PER_SM * ctx->sm_count; }
+
+// Clusters of csize CTAs that are resident at once: fewer than the CTAs alone would be, since a cluster stays inside a group of SMs. Asked once per
+// device, kernel, cluster size and size class of the shared memory.
+int resident_workers(const pq_ctx* ctx, void (*kern)(const PagedAttnParams), bool dyn, int csize, size_t smem) {
+  static std::atomic<int> known[64][2][4][32] = {};
+  const int size_class = static_cast<int>((smem + 8191) / 8192), ci = csize == 8 ? 3 : csize == 4 ? 2 : csize == 2 ? 1 : 0;
+  std::atomic<int>& slot = known[ctx->device][dyn][ci][size_class < 32 ? size_class : 31];
+  int n = slot.load(std::memory_order_relaxed);
+  if (n > 0) return n;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(most_ctas(ctx) / csize * csize);
+  cfg.blockDim = dim3(DP_THREADS);
+  cfg.dynamicSmemBytes = smem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = csize, attr[0].val.clusterDim.y = 1, attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n < 1) {
+    cudaGetLastError();
+    n = ctx->sm_count / csize;
+  }
+  if (n > most_ctas(ctx) / csize) n = most_ctas(ctx) / csize;
+  slot.store(n, std::memory_order_relaxed);
+  return n;
+}
 
 }  // namespace
 
 size_t pq_paged_decode_ws_bytes(const pq_ctx* ctx, const pq_kv4_paged* c) {
-  return static_cast<size_t>(2) * resident_ctas(ctx) * (c->Hq / c->Hkv) * (128 + 2) * sizeof(float);
+  return static_cast<size_t>(2) * most_ctas(ctx) * (c->Hq / c->Hkv) * (128 + 2) * sizeof(float);
 }
 
 pq_status pq_paged_decode_launch(pq_ctx* ctx, const pq_kv4_paged* c, PagedAttnParams p, int64_t max_len, void* ws, cudaStream_t st) {
-  const int64_t pairs = static_cast<int64_t>(p.B) * p.Hkv, resident = resident_ctas(ctx);
-  const int64_t rounds = (max_len + DP_ROUND - 1) / DP_ROUND;
-  // Few pairs share the chip: a cluster of CTAs to a pair or stretch keeps the partials that meet in the workspace few.
-  int64_t csize = pairs > 0 ? resident / pairs : 1;
-  csize = csize >= 8 ? 8 : csize >= 4 ? 4 : csize >= 2 ? 2 : 1;
-  const bool direct = pairs * csize <= resident && rounds <= 32;
-  if (direct)
-    while (csize > 1 && csize > rounds) csize >>= 1;
-  p.csize = static_cast<int32_t>(csize);
-  p.workers = direct ? 0 : static_cast<int32_t>(resident / csize);
-  if (p.workers > PQ_PAGED_MAX_WORKERS) p.workers = PQ_PAGED_MAX_WORKERS;
-  p.ws_o = static_cast<float*>(ws);
-  p.ws_ml = p.ws_o + static_cast<size_t>(2) * p.workers * p.G * 128;
   const bool dyn = p.steps != nullptr;
-  const size_t smem = fixed_smem(dyn) + (direct ? 0 : (2 * static_cast<size_t>(p.B) + 1) * sizeof(int32_t));
   void (*const kern)(const PagedAttnParams) = dyn ? paged_decode_kernel<true> : paged_decode_kernel<false>;
-  // the largest there is (8192 sequences), once per device and kernel
-  static bool attr_set[64][2] = {};
+  // the largest there is, once per device and kernel
+  static std::atomic<bool> attr_set[64][2] = {};
   if (ctx->device < 0 || ctx->device >= 64) return PQ_ERR_UNSUPPORTED;
-  if (!attr_set[ctx->device][dyn]) {
-    const int most = fixed_smem(dyn) + (2 * PQ_PAGED_MAX_SEQS + 1) * 4;
+  if (!attr_set[ctx->device][dyn].load(std::memory_order_relaxed)) {
+    const int most = static_cast<int>(dynamic_smem(dyn, DP_ROWS, PQ_PAGED_MAX_PREFIX, PQ_PAGED_MAX_SEQS));
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess) {
       cudaGetLastError();
       return PQ_ERR_CUDA;
     }
-    attr_set[ctx->device][dyn] = true;
+    attr_set[ctx->device][dyn].store(true, std::memory_order_relaxed);
   }
+  const int64_t pairs = static_cast<int64_t>(p.B) * p.Hkv, most = most_ctas(ctx);
+  const int64_t rounds = (max_len + DP_ROUND - 1) / DP_ROUND;
+  // Few pairs share the chip: a cluster of CTAs to a pair or stretch keeps the partials that meet in the workspace few.
+  int64_t csize = most / pairs;
+  csize = csize >= 8 ? 8 : csize >= 4 ? 4 : csize >= 2 ? 2 : 1;
+  // One worker per pair or equal stretches, by an estimate for sequences of max_len tokens: a round of a CTA takes 0.6 us and 0.45 us for every CTA on its
+  // SM; equal stretches fill the SMs (1.95 us a round) but cost 10 us more (prefix sums, a second piece, the merge through the workspace). us, one
+  // worker per pair / equal stretches: 1 sequence x 6000 tokens x 8 KV heads 12 / 18, 5 x 5000 14.7 / 26, 5 x 10000 22.9 / 32.5, 5 x 20000 38.8 / 43.1,
+  // 5 ragged to 50000 69 / 58, 48 ragged to 6000 70 / 56.
+  int64_t one = csize;
+  while (one > 1 && one > rounds) one >>= 1;
+  bool direct = pairs <= resident_workers(ctx, kern, dyn, static_cast<int>(one), dynamic_smem(dyn, p.G, p.n_prefix, 0));
+  if (direct) {
+    const double sms = ctx->sm_count, per_sm = pairs * one > ctx->sm_count ? pairs * one / sms : 1.0;
+    const double t_one = static_cast<double>((rounds + one - 1) / one) * (0.6 + 0.45 * per_sm);
+    const double t_equal = 10.0 + 1.95 * static_cast<double>(pairs * rounds) / (DP_CTAS_PER_SM * sms);
+    direct = t_one <= t_equal;
+  }
+  if (direct) csize = one;
+  const size_t smem = dynamic_smem(dyn, p.G, p.n_prefix, direct ? 0 : p.B);
+  p.csize = static_cast<int32_t>(csize);
+  p.workers = direct ? 0 : resident_workers(ctx, kern, dyn, p.csize, smem);
+  if (p.workers > PQ_PAGED_MAX_WORKERS) p.workers = PQ_PAGED_MAX_WORKERS;
+  p.ws_o = static_cast<float*>(ws);
+  p.ws_ml = p.ws_o + static_cast<size_t>(2) * p.workers * p.G * 128;
   const int64_t grid = (direct ? pairs : p.workers) * csize;
   return pq_launch_cluster_pdl(kern, dim3(static_cast<unsigned>(grid)), DP_THREADS, smem, p.csize, st, p);
 }
