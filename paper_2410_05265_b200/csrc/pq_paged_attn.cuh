@@ -35,6 +35,8 @@ struct PagedAttnParams {
 #define PQ_PAGED_MAX_WORKERS 4096
 
 size_t pq_paged_decode_ws_bytes(const pq_ctx* ctx, const pq_kv4_paged* c);
+size_t pq_paged_prefill_ws_bytes(const pq_ctx* ctx);
+pq_status pq_paged_prefill_launch(pq_ctx* ctx, PagedAttnParams p, void* ws, cudaStream_t st);
 pq_status pq_paged_decode_launch(pq_ctx* ctx, const pq_kv4_paged* c, PagedAttnParams p, int64_t max_len, void* ws, cudaStream_t st);
 
 namespace pq {

@@ -1,0 +1,840 @@
+// Causal attention of sequences with several rows (prompts, chunks of prompts) over [full-precision prefix || paged 4-bit cache].
+//
+// Both products run on tcgen05.mma kind::f16 with fp32 accumulators in tensor memory. An item is (sequence, KV head, 2 x floor(128/G) consecutive tokens):
+// the G query heads of the KV head fill two 128-row tiles, so that a key tile is expanded once for all of them. An item walks its key tiles (the
+// prefix, up to 64 full-precision keys, is a first tile of its own; then 128 cached keys each).
+// Work is counted in key tiles. One CTA per SM takes an equal stretch of the tiles of all items laid end to end (prefix sums over the sequences; inside a
+// sequence the number of tiles before an item is a sum of floors with a closed form), whatever the lengths are: a chunk of a long prompt and
+// short prompts fill the chip alike. An item inside one stretch is final; an item that several stretches share leaves partials in the
+// workspace, and the last CTA to finish merges them in the order of the CTAs.
+//   loader warp      bulk copies of the packed K and V rows (and steps) of a key tile, page by page, into a landing ring
+//   expansion warps  codes -> K as bf16 integers, V as fp16 integers, both exact, written as [key][dim] tiles in the 128-byte-swizzled layout that serves as
+//                    the K-major B operand of S = Q K^T and as the MN-major B operand of O = P V. With own steps they also prepare, per
+//                    key, (step of the key x scale, log2 and reciprocal of the step of the value).
+//   MMA warp         S_i = Q_i K^T (bf16: every query is exact, whatever its magnitude; prefix keys, fp16, as two bf16 terms), O_i += P_i V with P as the
+//                    tensor-memory A operand (fp16)
+//   softmax warps    one thread per query row. The exponent of a weight takes log2 of the value's step with it, w = 2^(s + log2 step - m): O is in value
+//                    units, fp16 holds the largest of what enters the sum whatever the steps are, the denominator is the sum of w / step
+//                    in fp32. The reference m moves only when an exponent exceeds it by more than 8.
+// Inside every group of eight head dims the expansion leaves the order 0,4,1,5,2,6,3,7; Q and the prefix rows are stored in the same order and the output
+// columns are put back when they are written. Every wait is bounded.
+#include <atomic>
+
+#include "pq_paged_attn.cuh"
+
+namespace {
+
+constexpr int PP_ROWS = 128;          // query rows per tile (MMA M)
+constexpr int PP_KEYS = 128;          // keys per tile
+constexpr int PP_PREFIX = 64;         // key rows of the prefix tile
+constexpr int PP_HALF = 128 * 128;    // bytes of one half tile: 128 rows x 64 two-byte values (128 bytes, swizzled)
+constexpr int PP_TILE = 2 * PP_HALF;  // a [128][128] tile: dims 0..63, then dims 64..127
+constexpr int PP_LAND = PP_KEYS * 64 + 2 * PP_KEYS * 4;  // packed rows of K or V, behind those of V the steps of both
+constexpr int PP_LANDS = 3;           // landing slots: K and V rows of a tile take one each
+constexpr int PP_STAGES = 2;
+constexpr int PP_SOFTMAX_WARPS = 8, PP_EXPAND_WARPS = 4;
+constexpr int PP_WARP_EXPAND0 = PP_SOFTMAX_WARPS, PP_WARP_MMA = PP_WARP_EXPAND0 + PP_EXPAND_WARPS, PP_WARP_LOAD = PP_WARP_MMA + 1;
+constexpr int PP_THREADS = (PP_WARP_LOAD + 1) * 32;  // 448
+constexpr int PP_TMEM_COLS = 512;     // S0 | S1 | O0 | O1, 128 columns each; P_i lies over the first 64 columns of S_i
+constexpr float PP_LAZY = 8.0f;       // log2 units an exponent may exceed the reference before it is moved
+constexpr int PP_TICKET0 = PQ_PAGED_TICKET0 + PQ_PAGED_MAX_WORKERS;
+constexpr int PP_PARTIAL = 256 * 128;  // floats of an item's partial output: [dims / 4][row][4]
+
+struct PpStart {  // where a worker's stretch begins
+  int b, h, rt, j0, u0, u1, U, workers;
+};
+struct PpShared {  // an item that several workers share
+  int w0, w1, b, h, rt, row0, n;
+};
+struct PpBarriers {
+  uint64_t land_full[PP_LANDS], land_empty[PP_LANDS];
+  uint64_t k_full[PP_STAGES], k_empty[PP_STAGES], v_full[PP_STAGES], v_empty[PP_STAGES];
+  uint64_t s_full[2], p_full[2], o_final[2];
+  uint64_t q_ready, drain;
+  int64_t part[PP_THREADS / 32];
+  uint32_t tmem_base;
+  volatile int abort_flag;
+  int merge[2];
+  PpStart start;
+  PpShared shared[2];
+};
+struct PpSteps {  // of pairs of keys: (key step x scale, of both, log2 of the value step, of both) and (1 / value step, of both)
+  float4 key[PP_KEYS / 2];
+  float2 inv[PP_KEYS / 2];
+};
+constexpr size_t PP_SMEM_BYTES = 1024 /*alignment slack*/ + 2 * PP_TILE /*Q*/ + PP_STAGES * 2 * PP_TILE /*K, V*/ + PP_LANDS * PP_LAND +
+                                 PP_STAGES * sizeof(PpSteps) + sizeof(PpBarriers);
+static_assert(PP_SMEM_BYTES <= 227 * 1024, "shared memory budget");
+static_assert((PQ_PAGED_MAX_SEQS + 1) * 4 <= PP_STAGES * 2 * PP_TILE, "the prefix sums lie in the K and V buffers before the pipeline starts");
+
+__device__ __forceinline__ float max3f(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ uint32_t hfma2_u32(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t d;
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+  return d;
+}
+__device__ __forceinline__ uint32_t bsub2_u32(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+// Eight codes of one packed word (nibble i = head dim i of the group) as exact fp16 integers in the order (0,4) (1,5) (2,6) (3,7): nibbles 0 and 4 under the
+// exponent of 1024 read 1032 + code, nibbles 1 and 5 stay four bits up and read 1152 + 16 * code; one fused multiply-add each removes the offset
+// (and the factor 16).
+__device__ __forceinline__ uint4 expand8_f16(uint32_t w) {
+  const uint32_t w8 = w >> 8;
+  const uint32_t ONE = 0x3C003C00u, SIXTEENTH = 0x2C002C00u;  // half2(1, 1), half2(1/16, 1/16)
+  const uint32_t M1032 = 0xE408E408u, M72 = 0xD480D480u;      // half2(-1032, -1032), half2(-72, -72)
+  uint4 o;
+  o.x = hfma2_u32(pq::and_xor<0x000F000Fu, 0x64086408u>(w), ONE, M1032);
+  o.y = hfma2_u32(pq::and_xor<0x00F000F0u, 0x64806480u>(w), SIXTEENTH, M72);
+  o.z = hfma2_u32(pq::and_xor<0x000F000Fu, 0x64086408u>(w8), ONE, M1032);
+  o.w = hfma2_u32(pq::and_xor<0x00F000F0u, 0x64806480u>(w8), SIXTEENTH, M72);
+  return o;
+}
+// The same as exact bf16 integers: under the exponent of 128 (bf16 has seven fraction bits) a nibble reads 136 + code.
+__device__ __forceinline__ uint4 expand8_bf16(uint32_t w) {
+  const uint32_t OFF = 0x43084308u;  // bf16x2(136, 136)
+  return make_uint4(bsub2_u32(pq::and_xor<0x000F000Fu, 0x43084308u>(w), OFF), bsub2_u32(pq::and_xor<0x000F000Fu, 0x43084308u>(w >> 4), OFF),
+                    bsub2_u32(pq::and_xor<0x000F000Fu, 0x43084308u>(w >> 8), OFF), bsub2_u32(pq::and_xor<0x000F000Fu, 0x43084308u>(w >> 12), OFF));
+}
+// Eight two-byte values (d0 .. d7 in four words) in the same order (0,4) (1,5) (2,6) (3,7).
+__device__ __forceinline__ uint4 permute8(const uint4& v) {
+  return make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
+}
+// Two fp16 values as two bf16 terms whose sum they are (8 + 8 of at most 11 significand bits): the first or the second.
+__device__ __forceinline__ uint32_t bf16_term(uint32_t h2, bool second) {
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h2));
+  __nv_bfloat162 b = __floats2bfloat162_rn(f.x, f.y);
+  if (second) {
+    const float2 hi = __bfloat1622float2(b);
+    b = __floats2bfloat162_rn(f.x - hi.x, f.y - hi.y);
+  }
+  return *reinterpret_cast<const uint32_t*>(&b);
+}
+// Byte offset of 16-byte chunk c16 (eight dims; 0..15) of row r inside a [rows][128] tile of two-byte values.
+__device__ __forceinline__ uint32_t tile_off(int r, int c16) {
+  return static_cast<uint32_t>((c16 >> 3) * PP_HALF + r * 128 + (((c16 & 7) ^ (r & 7)) << 4));
+}
+__device__ __forceinline__ void sts128(uint32_t a, const uint4& v) {
+  asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
+// ---- tcgen05 forms used here (cta_group::1, kind::f16) ----------------------------------------------------
+// Instruction descriptor: A and B both fp16 or both bf16 -> fp32, A K-major (or in tensor memory), B K-major or MN-major.
+__host__ __device__ constexpr uint32_t idesc_16(int M, int N, bool bf16, bool b_mn_major) {
+  return (1u << 4) /*D = f32*/ | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (b_mn_major ? (1u << 16) : 0u) | (static_cast<uint32_t>(N >> 3) << 17) |
+         (static_cast<uint32_t>(M >> 4) << 24);
+}
+// Shared-memory descriptor of a 128-byte-swizzled operand whose rows are 128 bytes and whose 8-row groups are 1024 bytes apart. K-major use: rows =
+// M/N index, the row's bytes = 64 K elements (lbo unused). MN-major use: rows = K index, the row's bytes = 64 M/N elements, lbo = distance
+// to the next 64 M/N elements.
+__device__ __forceinline__ uint64_t desc_sw128(uint32_t smem_addr, uint32_t lbo_bytes) {
+  uint64_t d = 0;
+  d |= static_cast<uint64_t>((smem_addr >> 4) & 0x3FFF);
+  d |= static_cast<uint64_t>((lbo_bytes >> 4) & 0x3FFF) << 16;
+  d |= static_cast<uint64_t>(1024 >> 4) << 32;
+  d |= static_cast<uint64_t>(1) << 46;
+  d |= static_cast<uint64_t>(2) << 61;
+  return d;
+}
+__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      "setp.ne.b32 p, %4, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
+      "}\n" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      "setp.ne.b32 p, %4, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
+      "}\n" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+
+// sum_{i=0}^{n-1} floor((a i + b) / m) for a, b >= 0, m > 0, by the Euclidean reduction of the lattice points under a line.
+__device__ int64_t floor_sum(int64_t n, int64_t m, int64_t a, int64_t b) {
+  int64_t s = 0;
+  for (;;) {
+    s += (a / m) * (n * (n - 1) / 2) + (b / m) * n;
+    a %= m, b %= m;
+    const int64_t top = a * n + b;
+    if (top < m) return s;
+    n = top / m, b = top % m;
+    const int64_t t = m;
+    m = a, a = t;
+  }
+}
+
+// The stretch of a worker as the roles walk it, item by item.
+struct PpItem {
+  int b, h, rt;         // sequence, KV head, row tile pair
+  int n, len, row0;     // of the sequence: new rows, cached keys, first row
+  int base;             // cached keys before the new rows: len - n
+  int tiles, j0, j1;    // key tiles of the item (the prefix first), and this worker's
+  int u;                // unit of j0
+};
+
+template <bool DYN>
+__global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const PagedAttnParams p) {
+  extern __shared__ uint8_t pp_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(pp_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* q_buf = smem;                               // two Q tiles
+  uint8_t* kv_buf = q_buf + 2 * PP_TILE;               // stage s: K tile, then V tile
+  uint8_t* land = kv_buf + PP_STAGES * 2 * PP_TILE;    // packed rows of K or V
+  PpSteps* steps_buf = reinterpret_cast<PpSteps*>(land + PP_LANDS * PP_LAND);
+  PpBarriers* bars = reinterpret_cast<PpBarriers*>(steps_buf + PP_STAGES);
+
+  const int warp = pq::warp_index(), lane = threadIdx.x & 31;
+  const int G = p.G, RT = PP_ROWS / G, R = 2 * RT;     // tokens of a row tile and of an item
+  const int has_prefix = p.n_prefix > 0 ? 1 : 0;
+  volatile int* abort_flag = &bars->abort_flag;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < PP_LANDS; ++i) {
+      pq::mbar_init(&bars->land_full[i], 1);
+      pq::mbar_init(&bars->land_empty[i], PP_EXPAND_WARPS);
+    }
+    for (int i = 0; i < PP_STAGES; ++i) {
+      pq::mbar_init(&bars->k_full[i], PP_EXPAND_WARPS);
+      pq::mbar_init(&bars->k_empty[i], 1);
+      pq::mbar_init(&bars->v_full[i], PP_EXPAND_WARPS);
+      pq::mbar_init(&bars->v_empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      pq::mbar_init(&bars->s_full[i], 1);
+      pq::mbar_init(&bars->p_full[i], 4);
+      pq::mbar_init(&bars->o_final[i], 1);
+    }
+    pq::mbar_init(&bars->q_ready, PP_SOFTMAX_WARPS);
+    pq::mbar_init(&bars->drain, 1);
+    bars->abort_flag = 0;
+    pq::mbar_fence_init();
+  }
+  if (warp == PP_WARP_MMA) {
+    pq::tmem_alloc(&bars->tmem_base, PP_TMEM_COLS);
+    pq::tmem_relinquish();
+  }
+  pq::pdl_wait();
+  pq::pdl_trigger();
+
+  // ---- the sequences: number of key tiles of all row tiles of one KV head, prefix sums, and where this worker's stretch begins
+  const int64_t capacity = static_cast<int64_t>(p.max_pages) << p.page_log2;
+  auto load_seq = [&](PpItem& x, bool& odd) {  // n = 0 for a sequence that is not this kernel's
+    const int r0 = pq::ld_dep(p.q_begin + x.b), r1 = pq::ld_dep(p.q_begin + x.b + 1), l = pq::ld_dep(p.len + x.b);
+    const int64_t n = static_cast<int64_t>(r1) - r0;
+    x.row0 = r0;
+    x.len = l < 0 ? 0 : l > capacity ? static_cast<int>(capacity) : l;
+    odd = n > p.max_new || n < 0 || (n > 0 && (r0 < 0 || r1 > p.n_rows || l != x.len));
+    x.n = n >= 2 && n <= p.max_new && r0 >= 0 && r1 <= p.n_rows ? static_cast<int>(n) : 0;
+    x.base = x.len - x.n;
+  };
+  // key tiles of row tile rt; an item with fewer cached keys than rows counts the tiles as if the keys began at zero
+  auto tiles_of = [&](const PpItem& x, int rt) { return has_prefix + (max(x.base, 0) + min(x.n, (rt + 1) * R) + PP_KEYS - 1) / PP_KEYS; };
+  auto tiles_before = [&](const PpItem& x, int rt) {  // of the row tiles 0 .. rt - 1, all of them full
+    return static_cast<int64_t>(rt) * has_prefix + (rt > 0 ? floor_sum(rt, PP_KEYS, R, static_cast<int64_t>(max(x.base, 0)) + R + PP_KEYS - 1) : 0);
+  };
+  auto row_tiles = [&](const PpItem& x) { return (x.n + R - 1) / R; };
+  int32_t* scan = reinterpret_cast<int32_t*>(kv_buf);
+  __syncthreads();
+  for (int b = threadIdx.x; b < p.B; b += PP_THREADS) {
+    PpItem x;
+    x.b = b;
+    bool odd;
+    load_seq(x, odd);
+    int64_t t = 0;
+    if (x.n > 0) {
+      const int nt = row_tiles(x);
+      t = tiles_before(x, nt - 1) + tiles_of(x, nt - 1);
+    }
+    if (odd || t * p.Hkv > 0x7fffffffll) {
+      pq::report(p.status, PQ_ERR_SHAPE);
+      t = t * p.Hkv > 0x7fffffffll ? 0 : t;  // (more work than any chip's memory holds keys for)
+    }
+    scan[b] = static_cast<int32_t>(t);
+  }
+  __syncthreads();
+  const int64_t total = pq::block_scan<PP_THREADS>(scan, p.B, bars->part) * p.Hkv;
+  if (threadIdx.x == 0) {
+    PpStart st{};
+    const bool too_many = total > 0x7fffffffll;
+    if (too_many) pq::report(p.status, PQ_ERR_SHAPE);
+    st.U = too_many ? 0 : static_cast<int>(total);
+    st.workers = min(static_cast<int>(gridDim.x), max(1, st.U / 2));  // two tiles at least
+    if (st.U > 0 && static_cast<int>(blockIdx.x) < st.workers) {
+      st.u0 = static_cast<int>(static_cast<int64_t>(st.U) * blockIdx.x / st.workers);
+      st.u1 = static_cast<int>(static_cast<int64_t>(st.U) * (blockIdx.x + 1) / st.workers);
+      PpItem x;
+      x.b = pq::find_segment(scan, p.B, st.u0 / p.Hkv);
+      bool odd;
+      load_seq(x, odd);
+      const int per_head = scan[x.b + 1] - scan[x.b], rel = st.u0 - scan[x.b] * p.Hkv;
+      st.b = x.b, st.h = rel / per_head;
+      const int v = rel - st.h * per_head;
+      int lo = 0, hi = row_tiles(x) - 1;  // last row tile with tiles_before <= v
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (tiles_before(x, mid) <= v)
+          lo = mid;
+        else
+          hi = mid - 1;
+      }
+      st.rt = lo, st.j0 = v - static_cast<int>(tiles_before(x, lo));
+    }
+    bars->start = st;
+  }
+  pq::tc_fence_before();
+  __syncthreads();
+  pq::tc_fence_after();
+  const PpStart start = bars->start;
+  const uint32_t tmem_base = __shfl_sync(0xffffffffu, bars->tmem_base, 0);
+
+  auto first_item = [&]() {
+    PpItem x;
+    x.b = start.b, x.h = start.h, x.rt = start.rt;
+    bool odd;
+    load_seq(x, odd);
+    x.tiles = tiles_of(x, x.rt), x.j0 = start.j0, x.u = start.u0;
+    x.j1 = min(x.tiles, x.j0 + (start.u1 - start.u0));
+    return x;
+  };
+  auto next_item = [&](PpItem& x) {  // false at the end of the stretch
+    x.u += x.j1 - x.j0;
+    if (x.u >= start.u1) return false;
+    if (++x.rt == row_tiles(x)) {
+      x.rt = 0;
+      if (++x.h == p.Hkv) {
+        x.h = 0;
+        bool odd;
+        do {
+          ++x.b;
+          load_seq(x, odd);
+        } while (x.n == 0);
+      }
+    }
+    x.tiles = tiles_of(x, x.rt), x.j0 = 0;
+    x.j1 = min(x.tiles, start.u1 - x.u);
+    return true;
+  };
+  auto n_ctx_of = [&](const PpItem& x) { return min(x.len, max(x.base, 0) + min(x.n, (x.rt + 1) * R)); };  // cached keys a row of the item may see
+  auto second_tile = [&](const PpItem& x) { return x.n > x.rt * R + RT; };  // does the second row tile have rows
+
+  // Bounded wait; also gives up when another role of the CTA has raised the abort flag.
+  auto wait = [&](uint64_t* bar, uint32_t parity) -> bool {
+    if (pq::mbar_try_wait(bar, parity)) return true;
+    const long long c0 = clock64();
+    for (;;) {
+      if (pq::mbar_try_wait(bar, parity)) return true;
+      if (*abort_flag) return false;
+      if (clock64() - c0 > p.wait_clocks) return false;
+    }
+  };
+  auto wait_warp = [&](uint64_t* bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, wait(bar, parity)); };
+  auto give_up = [&]() {
+    bars->abort_flag = 1;
+    pq::report(p.status, PQ_ERR_TIMEOUT);
+  };
+
+  const bool any = start.u1 > start.u0;
+  int lands_issued = 0;  // loader only
+
+  if (warp < PP_SOFTMAX_WARPS) {
+    // ================================================================== softmax warps: one thread per query row
+    const int i = warp >> 2, row = (warp & 3) * 32 + lane;  // row tile and row inside it
+    const int tok_in = i * RT + row / G, g_in = row % G;    // token of the item and query head of the group (rows past RT * G have none)
+    const bool row_used = row < RT * G;
+    const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t s_addr = tmem_base + lane_base + i * 128, o_addr = tmem_base + lane_base + 256 + i * 128;
+    bool ok = true;
+    int n_tiles_done = 0, n_items_done = 0, n_all_items = 0, c = 0, n_shared = 0;  // of this group: tiles, items; of the CTA: items, tiles
+    PpItem x;
+    if (any) x = first_item();
+    for (bool more = any; more && ok; more = next_item(x)) {
+      const bool active = i == 0 || second_tile(x);
+      const int t0 = x.rt * R, tok = min(t0 + tok_in, x.n - 1), head = x.h * G + g_in;
+      if (active) {
+        // Q staging: the warp brings its 32 rows in, two rows (512 contiguous bytes) per load instruction
+        const uint32_t dst = pq::smem_u32(q_buf + i * PP_TILE);
+        const int c16 = lane & 15, rw0 = (warp & 3) * 32;
+        uint4 qv[16];
+#pragma unroll
+        for (int it = 0; it < 16; ++it) {
+          const int rq = min(rw0 + it * 2 + (lane >> 4), RT * G - 1);
+          const int tq = min(t0 + i * RT + rq / G, x.n - 1), hq = x.h * G + rq % G;
+          const uint4* src = reinterpret_cast<const uint4*>(p.q + static_cast<int64_t>(x.row0 + tq) * p.ldq + hq * 128) + c16;
+          qv[it] = pq::ld_dep(src);
+        }
+#pragma unroll
+        for (int it = 0; it < 16; ++it) sts128(dst + tile_off(rw0 + it * 2 + (lane >> 4), c16), permute8(qv[it]));
+        pq::fence_proxy_async_smem();
+      }
+      __syncwarp();
+      if (lane == 0) pq::mbar_arrive(&bars->q_ready);
+      // a group without rows waits for the others' arrivals: two of its own must not meet in one phase
+      if (!active && __any_sync(0xffffffffu, !wait(&bars->q_ready, n_all_items & 1))) {
+        ok = false;
+        break;
+      }
+      ++n_all_items;
+      const float s_k = DYN ? 1.0f : pq::ld_dep(p.s_k + x.h), s_v = DYN ? 1.0f : fmaxf(pq::ld_dep(p.s_v + x.h), 0x1p-60f);
+      const float scale_ctx = s_k * p.scale2, log2_sv = DYN ? 0.0f : pq::lg2_approx(s_v), inv_sv = DYN ? 1.0f : 1.0f / s_v;
+      const int n_ctx = n_ctx_of(x), tile_min_tok = t0 + i * RT;
+      float m_ref = -INFINITY, l = 0.0f;
+      for (int jt = x.j0; jt < x.j1; ++jt, ++c) {
+        if (!active) continue;
+        const bool is_pre = has_prefix && jt == 0;
+        const int key0 = (jt - has_prefix) * PP_KEYS;
+        if (__any_sync(0xffffffffu, !wait(&bars->s_full[i], n_tiles_done & 1) || (DYN && !wait(&bars->v_full[c % PP_STAGES], (c / PP_STAGES) & 1)))) {
+          ok = false;
+          break;
+        }
+        pq::tc_fence_after();
+        const int n_chunks = is_pre ? PP_PREFIX / 32 : PP_KEYS / 32;
+        const float scale = is_pre ? p.scale2 : scale_ctx, add = is_pre ? 0.0f : log2_sv;
+        const int limit = is_pre ? p.n_prefix : min(n_ctx - key0, x.base + tok - key0 + 1);  // columns below it are visible
+        const bool need_mask = is_pre ? p.n_prefix < PP_PREFIX : (key0 + PP_KEYS > x.base + tile_min_tok + 1 || key0 + PP_KEYS > n_ctx);
+        const PpSteps* st = steps_buf + c % PP_STAGES;
+        auto exponents = [&](const uint32_t(&r)[32], int c0, int e) {  // DYN: of columns e, e + 1 of the chunk
+          const float4 k = st->key[(c0 * 32 + e) >> 1];
+          return __ffma2_rn(make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), make_float2(k.x, k.y), make_float2(k.z, k.w));
+        };
+        // ---- pass 1: the row's largest exponent over the visible keys of this tile. The next 32 columns are requested before the current ones are
+        // worked on (the last request is pass 2's first).
+        uint32_t rr[2][32];
+        float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        pq::tmem_ld_32x32(s_addr, rr[0]);
+#pragma unroll
+        for (int cc = 0; cc < PP_KEYS / 32; ++cc) {
+          if (cc < n_chunks) {
+            pq::tmem_ld_wait_for(rr[cc & 1]);
+            pq::tmem_ld_32x32(s_addr + (cc + 1 < n_chunks ? (cc + 1) * 32 : 0), rr[(cc + 1) & 1]);
+            const uint32_t(&r)[32] = rr[cc & 1];
+            if (need_mask) {
+#pragma unroll
+              for (int e = 0; e < 32; e += 2) {
+                const float2 v = DYN ? exponents(r, cc, e) : make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1]));
+                mx4[(e >> 1) & 3] = max3f(mx4[(e >> 1) & 3], cc * 32 + e < limit ? v.x : -INFINITY, cc * 32 + e + 1 < limit ? v.y : -INFINITY);
+              }
+            } else {
+#pragma unroll
+              for (int e = 0; e < 32; e += 2) {
+                const float2 v = DYN ? exponents(r, cc, e) : make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1]));
+                mx4[(e >> 1) & 3] = max3f(mx4[(e >> 1) & 3], v.x, v.y);
+              }
+            }
+          }
+        }
+        const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
+        const float mx_s = DYN ? mx : fmaf(mx, scale, add);
+        const bool grow = mx_s > m_ref + PP_LAZY;  // also the first visible key of a row (m_ref = -inf)
+        if (__any_sync(0xffffffffu, grow)) {
+          const float m_new = grow ? mx_s : m_ref;
+          const float alpha = grow ? pq::ex2_approx(m_ref - m_new) : 1.0f;  // 2^(-inf) = 0 for a row that had seen nothing
+          l *= alpha;
+          if (jt > x.j0) {  // S_i of this tile is complete, so O_i += P V of the tile before is, too
+            for (int cc = 0; cc < 4; ++cc) {
+              uint32_t r[32];
+              pq::tmem_ld_32x32(o_addr + cc * 32, r);
+              pq::tmem_ld_wait();
+#pragma unroll
+              for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * alpha);
+              pq::tmem_st_32x32(o_addr + cc * 32, r);
+            }
+          }
+          m_ref = m_new;
+        }
+        // ---- pass 2: w = 2^(exponent - m), fp16, written over the first columns of S_i
+        const float m_use = m_ref == -INFINITY ? 0.0f : m_ref;  // such a row has every column masked
+        const float2 scale2 = make_float2(scale, scale), moff2 = DYN ? make_float2(-m_use, -m_use) : make_float2(add - m_use, add - m_use);
+        float2 l4[4] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+#pragma unroll
+        for (int cc = 0; cc < PP_KEYS / 32; ++cc) {  // n_chunks is even: pass 1 left the request for columns 0..31 in rr[0]
+          if (cc < n_chunks) {
+            pq::tmem_ld_wait_for(rr[cc & 1]);
+            if (cc + 1 < n_chunks) pq::tmem_ld_32x32(s_addr + (cc + 1) * 32, rr[(cc + 1) & 1]);
+            const uint32_t(&r)[32] = rr[cc & 1];
+            uint32_t pk[16];
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) {
+              const float2 ex = DYN ? __fadd2_rn(exponents(r, cc, e), moff2)
+                                    : __ffma2_rn(make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), scale2, moff2);
+              float2 w = make_float2(pq::ex2_approx(ex.x), pq::ex2_approx(ex.y));
+              if (need_mask) {
+                w.x = cc * 32 + e < limit ? w.x : 0.0f;
+                w.y = cc * 32 + e + 1 < limit ? w.y : 0.0f;
+              }
+              if (DYN)
+                l4[(e >> 1) & 3] = __ffma2_rn(w, st->inv[(cc * 32 + e) >> 1], l4[(e >> 1) & 3]);
+              else
+                l4[(e >> 1) & 3] = __fadd2_rn(l4[(e >> 1) & 3], w);
+              pk[e >> 1] = pq::pack_f16(w.x, w.y);
+            }
+            tmem_st_32x16(s_addr + cc * 16, pk);
+          }
+        }
+        {
+          const float lt = ((l4[0].x + l4[0].y) + (l4[1].x + l4[1].y)) + ((l4[2].x + l4[2].y) + (l4[3].x + l4[3].y));
+          l += DYN || is_pre ? lt : lt * inv_sv;
+        }
+        pq::tmem_st_wait();
+        pq::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) pq::mbar_arrive(&bars->p_full[i]);
+        ++n_tiles_done;
+      }
+      if (ok && active) {
+        if (__any_sync(0xffffffffu, !wait(&bars->o_final[i], n_items_done & 1))) {
+          ok = false;
+        } else {
+          ++n_items_done;
+          pq::tc_fence_after();
+          const bool whole = x.j0 == 0 && x.j1 == x.tiles, live = row_used && t0 + tok_in < x.n;
+          const float norm = l > 0.0f ? 1.0f / l : 0.0f;
+          __nv_bfloat16* dst = p.out + (static_cast<int64_t>(x.row0 + tok) * p.Hq + head) * 128;
+          const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (x.j0 == 0 ? 1 : 0);
+          float4* part = reinterpret_cast<float4*>(p.ws_o + slot * PP_PARTIAL) + i * PP_ROWS + row;  // [dims / 4][256 rows]
+          for (int cc = 0; cc < 4; ++cc) {
+            uint32_t r[32];
+            pq::tmem_ld_32x32(o_addr + cc * 32, r);
+            pq::tmem_ld_wait();
+            if (!live) continue;
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {  // columns 8a .. 8a+7 hold dims 0,4,1,5,2,6,3,7 of the group
+              float v[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(r[8 * a + e]);
+              if (whole) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] *= norm;
+                const __nv_bfloat162 d01 = __floats2bfloat162_rn(v[0], v[2]), d23 = __floats2bfloat162_rn(v[4], v[6]);
+                const __nv_bfloat162 d45 = __floats2bfloat162_rn(v[1], v[3]), d67 = __floats2bfloat162_rn(v[5], v[7]);
+                *reinterpret_cast<uint4*>(dst + cc * 32 + a * 8) =
+                    make_uint4(*reinterpret_cast<const uint32_t*>(&d01), *reinterpret_cast<const uint32_t*>(&d23),
+                               *reinterpret_cast<const uint32_t*>(&d45), *reinterpret_cast<const uint32_t*>(&d67));
+              } else {
+                part[(cc * 8 + a * 2) * 256] = make_float4(v[0], v[2], v[4], v[6]);
+                part[(cc * 8 + a * 2 + 1) * 256] = make_float4(v[1], v[3], v[5], v[7]);
+              }
+            }
+          }
+          if (!whole && live) *reinterpret_cast<float2*>(p.ws_ml + (slot * 256 + i * PP_ROWS + row) * 2) = make_float2(m_ref, l);
+          pq::tc_fence_before();
+        }
+      }
+      if (x.j0 != 0 || x.j1 != x.tiles) {
+        if (threadIdx.x == 0) {
+          const int u = x.u - x.j0;
+          auto worker_of = [&](int unit) { return static_cast<int>(((static_cast<int64_t>(unit) + 1) * start.workers - 1) / start.U); };
+          bars->shared[n_shared & 1] = PpShared{worker_of(u), worker_of(u + x.tiles - 1), x.b, x.h, x.rt, x.row0, x.n};
+        }
+        ++n_shared;
+      }
+    }
+    // ---- the last of the workers w0 .. w1 of a shared item to come here merges their partials, in that order
+    if (!ok && lane == 0) give_up();
+    __threadfence();
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    if (threadIdx.x < 2) {
+      const bool go = !bars->abort_flag && static_cast<int>(threadIdx.x) < n_shared;
+      const PpShared sh = bars->shared[threadIdx.x];
+      bars->merge[threadIdx.x] = go && atomicAdd(p.tickets + PP_TICKET0 + sh.w0, 1u) == static_cast<uint32_t>(sh.w1 - sh.w0) ? 1 : 0;
+    }
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    __threadfence();
+    for (int k = 0; k < 2; ++k) {
+      if (!bars->merge[k]) continue;
+      const PpShared sh = bars->shared[k];
+      const int tok = sh.rt * R + tok_in;
+      if (row_used && tok < sh.n) {
+        auto slot_of = [&](int w) { return 2 * static_cast<int64_t>(w) + (w == sh.w0 ? 1 : 0); };
+        const int my = i * PP_ROWS + row;
+        float m = -INFINITY, l = 0.0f;
+        for (int w = sh.w0; w <= sh.w1; ++w) m = fmaxf(m, __ldcg(p.ws_ml + (slot_of(w) * 256 + my) * 2));
+        const float m_use = m == -INFINITY ? 0.0f : m;
+        __nv_bfloat16* dst = p.out + (static_cast<int64_t>(sh.row0 + tok) * p.Hq + sh.h * G + g_in) * 128;
+        for (int w = sh.w0; w <= sh.w1; ++w) {
+          const float2 ml = __ldcg(reinterpret_cast<const float2*>(p.ws_ml) + slot_of(w) * 256 + my);
+          l = fmaf(ml.y, pq::ex2_approx(ml.x - m_use), l);
+        }
+        const float norm = l > 0.0f ? 1.0f / l : 0.0f;
+        for (int cc = 0; cc < 4; ++cc) {  // 32 dims at a time
+          float4 acc[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) acc[e] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          for (int w = sh.w0; w <= sh.w1; ++w) {
+            const int64_t slot = slot_of(w);
+            const float wt = pq::ex2_approx(__ldcg(p.ws_ml + (slot * 256 + my) * 2) - m_use) * norm;
+            const float4* part = reinterpret_cast<const float4*>(p.ws_o + slot * PP_PARTIAL) + cc * 8 * 256 + my;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float4 v = __ldcg(part + e * 256);
+              acc[e].x = fmaf(v.x, wt, acc[e].x), acc[e].y = fmaf(v.y, wt, acc[e].y), acc[e].z = fmaf(v.z, wt, acc[e].z), acc[e].w = fmaf(v.w, wt, acc[e].w);
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) {
+            const __nv_bfloat162 a = __floats2bfloat162_rn(acc[e].x, acc[e].y), b = __floats2bfloat162_rn(acc[e].z, acc[e].w);
+            const __nv_bfloat162 c2 = __floats2bfloat162_rn(acc[e + 1].x, acc[e + 1].y), d = __floats2bfloat162_rn(acc[e + 1].z, acc[e + 1].w);
+            *reinterpret_cast<uint4*>(dst + cc * 32 + e * 4) = make_uint4(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b),
+                                                                        *reinterpret_cast<const uint32_t*>(&c2), *reinterpret_cast<const uint32_t*>(&d));
+          }
+        }
+      }
+      if (threadIdx.x == 0) p.tickets[PP_TICKET0 + sh.w0] = 0;
+    }
+  } else if (warp < PP_WARP_MMA) {
+    // ================================================================== expansion warps
+    const int tid_e = (warp - PP_WARP_EXPAND0) * 32 + lane;
+    bool ok = true;
+    int c = 0, lc = 0;  // tiles and landing slots so far
+    PpItem x;
+    if (any) x = first_item();
+    for (bool more = any; more && ok; more = next_item(x)) {
+      const int n_ctx = n_ctx_of(x);
+      for (int jt = x.j0; jt < x.j1 && ok; ++jt, ++c) {
+        const int stage = c % PP_STAGES;
+        const uint32_t ph = (c / PP_STAGES) & 1;
+        const bool is_pre = has_prefix && jt == 0;
+        const uint32_t k_tile = pq::smem_u32(kv_buf + stage * 2 * PP_TILE), v_tile = k_tile + PP_TILE;
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+          const int slot = lc % PP_LANDS;
+          if (!is_pre && __any_sync(0xffffffffu, !wait(&bars->land_full[slot], (lc / PP_LANDS) & 1))) ok = false;
+          if (!ok || __any_sync(0xffffffffu, !wait(kv ? &bars->v_empty[stage] : &bars->k_empty[stage], ph ^ 1))) {
+            ok = false;
+            break;
+          }
+          const uint32_t tile = kv ? v_tile : k_tile;
+          if (is_pre) {
+            // full-precision rows (reordered inside groups of eight dims); rows past n_prefix are zero
+            for (int unit = tid_e; unit < PP_PREFIX * 16; unit += PP_EXPAND_WARPS * 32) {
+              const int r = unit >> 4, c16 = unit & 15;
+              uint4 v = make_uint4(0, 0, 0, 0);
+              if (r < p.n_prefix)
+                v = permute8(pq::ld_dep(reinterpret_cast<const uint4*>((kv ? p.prefix_v : p.prefix_k) + (static_cast<int64_t>(x.h) * p.n_prefix + r) * 128 + c16 * 8)));
+              if (kv) {
+                sts128(tile + tile_off(r, c16), v);
+              } else {  // two bf16 terms: rows 0 .. 63 and 64 .. 127
+                sts128(tile + tile_off(r, c16), make_uint4(bf16_term(v.x, false), bf16_term(v.y, false), bf16_term(v.z, false), bf16_term(v.w, false)));
+                sts128(tile + tile_off(PP_PREFIX + r, c16), make_uint4(bf16_term(v.x, true), bf16_term(v.y, true), bf16_term(v.z, true), bf16_term(v.w, true)));
+              }
+            }
+          } else {
+            const uint32_t src = pq::smem_u32(land + slot * PP_LAND);
+#pragma unroll 2
+            for (int it = 0; it < PP_KEYS * 4 / (PP_EXPAND_WARPS * 32); ++it) {  // 128 keys x 4 chunks of 16 packed bytes
+              const int unit = it * (PP_EXPAND_WARPS * 32) + tid_e, r = unit >> 2, part = unit & 3;  // 32 dims: chunks 4 part .. +3
+              const uint4 w4 = pq::lds128(src + unit * 16);
+              const uint32_t ww[4] = {w4.x, w4.y, w4.z, w4.w};
+#pragma unroll
+              for (int w = 0; w < 4; ++w) sts128(tile + tile_off(r, 4 * part + w), kv ? expand8_f16(ww[w]) : expand8_bf16(ww[w]));
+            }
+          }
+          if (DYN && kv) {  // thread j: key j of the tile. A key that no row sees adds nothing.
+            const float* st = reinterpret_cast<const float*>(land + slot * PP_LAND + PP_KEYS * 64);
+            const int key = (jt - has_prefix) * PP_KEYS + tid_e;
+            const bool in = !is_pre && key < n_ctx;
+            const float k_step = in ? st[tid_e] : 1.0f, v_step = in ? st[PP_KEYS + tid_e] : 1.0f;
+            float* key_out = reinterpret_cast<float*>(&steps_buf[stage].key[tid_e >> 1]) + (tid_e & 1);
+            key_out[0] = k_step * p.scale2, key_out[2] = pq::lg2_approx(v_step);
+            reinterpret_cast<float*>(steps_buf[stage].inv)[tid_e] = pq::rcp_approx(v_step);
+          }
+          pq::fence_proxy_async_smem();  // generic-proxy writes -> visible to the tensor core's async proxy
+          __syncwarp();
+          if (lane == 0) {
+            pq::mbar_arrive(kv ? &bars->v_full[stage] : &bars->k_full[stage]);
+            if (!is_pre) pq::mbar_arrive(&bars->land_empty[slot]);
+          }
+          if (!is_pre) ++lc;
+        }
+      }
+    }
+    if (!ok && lane == 0) give_up();
+  } else if (warp == PP_WARP_LOAD) {
+    // ================================================================== loader
+    // A lane to a copy: lanes 0 .. 7 the pages of the tile (fewer for larger pages); with own steps lanes 8 .. 15 and 16 .. 23 the steps of their keys and
+    // values, which go with the rows of V.
+    const int pages = PP_KEYS >> p.page_log2, pg = lane & 7, kind = lane >> 3, page = 1 << p.page_log2;
+    bool ok = true;
+    PpItem x;
+    if (any) x = first_item();
+    for (bool more = any; more && ok; more = next_item(x)) {
+      const int n_ctx = n_ctx_of(x);
+      const int32_t* row = p.table + static_cast<int64_t>(x.b) * p.max_pages;
+      for (int jt = max(x.j0, has_prefix); jt < x.j1 && ok; ++jt) {
+        const int key0 = (jt - has_prefix) * PP_KEYS, n_here = min(pages, (n_ctx - key0 + page - 1) >> p.page_log2);  // pages with keys in them
+        const bool mine = pg < n_here && kind < (DYN ? 3 : 1);
+        int id = 0;
+        if (mine) {
+          id = pq::ld_dep(row + (key0 >> p.page_log2) + pg);
+          if (static_cast<uint32_t>(id) >= static_cast<uint32_t>(p.n_pages)) {  // an id that is none is reported and page 0 read in its place
+            pq::report(p.status, PQ_ERR_SHAPE);
+            id = 0;
+          }
+        }
+        const int64_t vec = ((static_cast<int64_t>(id) * p.Hkv + x.h) * 2) << p.page_log2;
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+          const int slot = lands_issued % PP_LANDS;
+          if (!wait_warp(&bars->land_empty[slot], ((lands_issued / PP_LANDS) & 1) ^ 1)) {
+            ok = false;
+            break;
+          }
+          const uint32_t dst = pq::smem_u32(land + slot * PP_LAND);
+          const uint32_t n_pages = static_cast<uint32_t>(max(n_here, 0));
+          if (lane == 0) pq::mbar_arrive_expect_tx(&bars->land_full[slot], n_pages * page * (64 + (DYN && kv ? 8 : 0)));
+          __syncwarp();
+          if (mine && kind == 0)
+            pq::bulk_load(dst + pg * page * 64, p.codes + (vec + kv * page) * 64, page * 64, &bars->land_full[slot]);
+          else if (mine && kv)
+            pq::bulk_load(dst + PP_KEYS * 64 + (kind - 1) * (PP_KEYS * 4) + pg * page * 4, p.steps + vec + (kind - 1) * page, page * 4, &bars->land_full[slot]);
+          ++lands_issued;
+        }
+      }
+    }
+    if (!ok && lane == 0) give_up();
+  } else {
+    // ================================================================== MMA issuer: the whole warp runs the loop, the elected lane issues
+    constexpr uint32_t IDESC_S = idesc_16(PP_ROWS, PP_KEYS, true, false), IDESC_S_PRE = idesc_16(PP_ROWS, PP_PREFIX, true, false);
+    constexpr uint32_t IDESC_O = idesc_16(PP_ROWS, 128, false, true);
+    const bool leader = pq::elect_one();
+    const uint64_t q_desc0 = desc_sw128(pq::smem_u32(q_buf), 16), k_desc0 = desc_sw128(pq::smem_u32(kv_buf), 16);
+    const uint64_t v_desc0 = desc_sw128(pq::smem_u32(kv_buf + PP_TILE), PP_HALF);
+    auto issue_s = [&](int i, int c, bool is_pre) {  // by the elected lane
+      const uint64_t q_desc = q_desc0 + i * (PP_TILE >> 4), k_desc = k_desc0 + (c % PP_STAGES) * (2 * PP_TILE >> 4);
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk) {  // 16 head dims per instruction
+        const uint32_t off = ((kk >> 2) * PP_HALF + (kk & 3) * 32) >> 4;
+        mma_ss(tmem_base + i * 128, q_desc + off, k_desc + off, is_pre ? IDESC_S_PRE : IDESC_S, kk ? 1u : 0u);
+      }
+      if (is_pre)  // the second terms of the prefix keys, 64 rows on
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk) {
+          const uint32_t off = ((kk >> 2) * PP_HALF + (kk & 3) * 32) >> 4;
+          mma_ss(tmem_base + i * 128, q_desc + off, k_desc + off + (PP_PREFIX * 128 >> 4), IDESC_S_PRE, 1u);
+        }
+      pq::mma_commit(&bars->s_full[i]);
+    };
+    auto issue_pv = [&](int i, int c, bool is_pre, bool first) {
+      const uint32_t o_tm = tmem_base + 256 + i * 128, p_tm = tmem_base + i * 128;
+      const uint64_t v_desc = v_desc0 + (c % PP_STAGES) * (2 * PP_TILE >> 4);
+#pragma unroll
+      for (int kk = 0; kk < PP_PREFIX / 16; ++kk)  // 16 keys per instruction
+        mma_ts(o_tm, p_tm + kk * 8, v_desc + kk * (2048 >> 4), IDESC_O, (!first || kk > 0) ? 1u : 0u);
+      if (!is_pre)
+#pragma unroll
+        for (int kk = PP_PREFIX / 16; kk < PP_KEYS / 16; ++kk) mma_ts(o_tm, p_tm + kk * 8, v_desc + kk * (2048 >> 4), IDESC_O, 1u);
+    };
+    bool ok = true;
+    int c = 0, n_items = 0, n_p[2] = {0, 0};
+    PpItem x;
+    if (any) x = first_item();
+    for (bool more = any; more && ok; more = next_item(x), ++n_items) {
+      const int groups = second_tile(x) ? 2 : 1;
+      if (!wait_warp(&bars->q_ready, n_items & 1) || !wait_warp(&bars->k_full[c % PP_STAGES], (c / PP_STAGES) & 1)) {
+        ok = false;
+        break;
+      }
+      pq::tc_fence_after();
+      if (leader) {
+        const bool is_pre = has_prefix && x.j0 == 0;
+        for (int i = 0; i < groups; ++i) issue_s(i, c, is_pre);
+        pq::mma_commit(&bars->k_empty[c % PP_STAGES]);
+      }
+      __syncwarp();
+      for (int jt = x.j0; jt < x.j1 && ok; ++jt, ++c) {
+        const bool is_pre = has_prefix && jt == 0, last = jt + 1 == x.j1;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if (i >= groups) break;
+          if (!wait_warp(&bars->p_full[i], n_p[i] & 1) || (i == 0 && !wait_warp(&bars->v_full[c % PP_STAGES], (c / PP_STAGES) & 1))) {
+            ok = false;
+            break;
+          }
+          ++n_p[i];
+          pq::tc_fence_after();
+          if (leader) {
+            issue_pv(i, c, is_pre, jt == x.j0);
+            if (i == groups - 1) pq::mma_commit(&bars->v_empty[c % PP_STAGES]);
+          }
+          __syncwarp();
+          if (!last) {
+            if (i == 0 && !wait_warp(&bars->k_full[(c + 1) % PP_STAGES], ((c + 1) / PP_STAGES) & 1)) {
+              ok = false;
+              break;
+            }
+            pq::tc_fence_after();
+            if (leader) {
+              issue_s(i, c + 1, false);
+              if (i == groups - 1) pq::mma_commit(&bars->k_empty[(c + 1) % PP_STAGES]);
+            }
+          } else if (leader) {
+            pq::mma_commit(&bars->o_final[i]);
+          }
+          __syncwarp();
+        }
+      }
+    }
+    if (leader) {
+      if (!ok) give_up();
+      // whatever was issued has finished before tensor memory is released or shared memory given back
+      pq::mma_commit(&bars->drain);
+    }
+    __syncwarp();
+    pq::mbar_wait(&bars->drain, 0);
+  }
+
+  pq::tc_fence_before();
+  __syncthreads();
+  if (warp == PP_WARP_LOAD && lane == 0 && bars->abort_flag) {
+    // copies that nobody consumed must have landed before the CTA may exit
+    for (int k = max(0, lands_issued - PP_LANDS); k < lands_issued; ++k) pq::mbar_wait(&bars->land_full[k % PP_LANDS], (k / PP_LANDS) & 1);
+  }
+  __syncthreads();
+  if (warp == PP_WARP_MMA) {
+    pq::tc_fence_after();
+    pq::tmem_dealloc(tmem_base, PP_TMEM_COLS);
+  }
+}
+
+}  // namespace
+
+size_t pq_paged_prefill_ws_bytes(const pq_ctx* ctx) {
+  return static_cast<size_t>(2) * ctx->sm_count * (PP_PARTIAL + 256 * 2) * sizeof(float);
+}
+
+pq_status pq_paged_prefill_launch(pq_ctx* ctx, PagedAttnParams p, void* ws, cudaStream_t st) {
+  const bool dyn = p.steps != nullptr;
+  void (*const kern)(const PagedAttnParams) = dyn ? paged_prefill_kernel<true> : paged_prefill_kernel<false>;
+  static std::atomic<bool> attr_set[64][2] = {};
+  if (ctx->device < 0 || ctx->device >= 64 || ctx->sm_count > PQ_PAGED_MAX_WORKERS) return PQ_ERR_UNSUPPORTED;
+  if (!attr_set[ctx->device][dyn].load(std::memory_order_relaxed)) {
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(PP_SMEM_BYTES)) != cudaSuccess) {
+      cudaGetLastError();
+      return PQ_ERR_CUDA;
+    }
+    attr_set[ctx->device][dyn].store(true, std::memory_order_relaxed);
+  }
+  p.ws_o = static_cast<float*>(ws);
+  p.ws_ml = p.ws_o + static_cast<size_t>(2) * ctx->sm_count * PP_PARTIAL;
+  return pq_launch_pdl(kern, dim3(ctx->sm_count), PP_THREADS, PP_SMEM_BYTES, st, p);
+}

@@ -456,3 +456,93 @@ def test_results_do_not_depend_on_timing(ctx):
         first = attend(ctx, cache, lengths, [1] * 4)[2]
         for _ in range(20):
             assert torch.equal(first, attend(ctx, cache, lengths, [1] * 4)[2])
+
+
+@pytest.mark.parametrize("steps", ["head", "vector"])
+@pytest.mark.parametrize("Hq,Hkv", [(8, 1), (4, 4), (6, 2), (5, 1), (7, 1), (4, 2), (12, 4)])
+@pytest.mark.parametrize("page,n_prefix", [(16, 4), (32, 0), (64, 64), (128, 1)])
+def test_prompts_of_many_lengths(ctx, steps, Hq, Hkv, page, n_prefix):
+    """Whole prompts, chunks behind cached keys and single tokens in one batch; row tiles and key tiles that are full, nearly empty and one more."""
+    new = [2, 3, 17, 33, 64, 65, 1, 127, 128, 129, 0, 200, 1]
+    lengths = [2, 3, 17, 40, 64, 65, 500, 256, 128, 400, 30, 201, 1]
+    cache = ref.make_cache(lengths, Hq, Hkv, page, steps, seed=page + Hq, n_prefix=n_prefix)
+    check_attention(ctx, cache, lengths, new, pad=2)
+
+
+@pytest.mark.parametrize("steps", ["head", "vector"])
+@pytest.mark.parametrize("lengths,new,Hq,Hkv", [
+    ([700], [700], 8, 2), ([5000], [2], 8, 1), ([20000], [5], 16, 2), ([3000], [300], 4, 4), ([9000, 100, 4000], [40, 100, 2], 8, 1), ([2], [2], 1, 1),
+    ([257 + 3 * i for i in range(40)], [2 + (11 * i) % 90 for i in range(40)], 4, 1), ([4 + i % 3 for i in range(300)], [2 + i % 3 for i in range(300)], 2, 2)])
+def test_chunks_that_several_workers_share(ctx, steps, lengths, new, Hq, Hkv):
+    cache = ref.make_cache(lengths, Hq, Hkv, 32, steps, seed=len(lengths))
+    check_attention(ctx, cache, lengths, new)
+
+
+@pytest.mark.parametrize("steps", ["head", "vector"])
+def test_rows_without_keys(ctx, steps):
+    """More rows than cached keys: the first rows see the prefix alone, or nothing."""
+    for n_prefix in (0, 3):
+        lengths, new = [3, 0, 150], [9, 4, 200]
+        cache = ref.make_cache(lengths, 8, 2, 16, steps, n_prefix=n_prefix, seed=2)
+        out = check_attention(ctx, cache, lengths, new)
+        if n_prefix == 0:
+            assert (out[:6] == 0).all() and (out[9:13] == 0).all()
+
+
+@pytest.mark.parametrize("steps", ["head", "vector"])
+@pytest.mark.parametrize("scale", [1e-30, 1e-3, 30.0, 1e25])
+def test_prompt_queries_of_any_magnitude(ctx, steps, scale):
+    lengths = [150, 90]
+    cache = ref.make_cache(lengths, 8, 2, 16, steps, seed=3)
+    check_attention(ctx, cache, lengths, [150, 20], scale=scale, sm_scale=min(1 / math.sqrt(D), 20 / scale / D) if scale > 1 else 1 / math.sqrt(D) / scale)
+
+
+@pytest.mark.parametrize("lo,hi", [(-50.0, -40.0), (40.0, 50.0), (-20.0, 20.0)])
+def test_prompt_own_steps_of_any_magnitude(ctx, lo, hi):
+    lengths = [70, 600]
+    cache = ref.make_cache(lengths, 4, 2, 16, "vector", n_prefix=0, seed=5, step_range=(lo, hi))
+    cache.steps[:, :, 0] = 0.4
+    check_attention(ctx, cache, lengths, [70, 40])
+
+
+def test_prompt_scores_that_climb(ctx):
+    lengths = [800]
+    cache = ref.make_cache(lengths, 8, 1, 16, "vector", seed=6)
+    order = cache.pages.table[0, :50].long()
+    cache.steps[order, :, 0] = torch.linspace(0.01, 6.0, 800, device=DEV).view(50, 1, 16)
+    check_attention(ctx, cache, lengths, [300])
+
+
+def test_prompt_ids_that_are_none_do_not_fault(ctx):
+    cache = ref.make_cache([300, 40], 4, 2, 16, seed=8)
+    cache.pages.table[0, 3] = 10**6
+    cache.pages.table[0, 18] = -1
+    q, ws = ref.queries(14, 4), ctx.attn_kv4_paged_workspace(cache, 14, 10)
+    out = ctx.attn_kv4_paged(cache, q, i32([0, 10, 14]), 10, 0.1, ws)
+    assert ctx.check_status() == 2
+    cache.pages.table[0] = 0
+    want, tol = ref.attention(cache, q[10:], [0, 0, 4], [0, 40], 0.1)
+    assert ((out[10:].double() - want).abs() <= tol).all()
+
+
+def test_prompt_rows_out_of_range_are_reported(ctx):
+    cache = ref.make_cache([100, 40], 4, 2, 16, seed=8, width=8)
+    for begin, length, rows, max_new in (([0, 5, 9], None, 9, 4), ([0, 5, 9], [-4, 40], 9, 5), ([0, 5, 9], [100, 129], 9, 5), ([0, 5, 12], None, 9, 7), ([-3, 5, 9], None, 9, 8),
+                                         ([4, 2, 9], None, 9, 9)):
+        if length:
+            cache.pages.length.copy_(i32(length))
+        out = torch.full((rows, 4, D), 9.0, dtype=torch.bfloat16, device=DEV)
+        ctx.attn_kv4_paged(cache, ref.queries(rows, 4), i32(begin), max_new, 0.1, ctx.attn_kv4_paged_workspace(cache, rows, max_new), out=out)
+        assert ctx.check_status() == 2
+        cache.pages.length.copy_(i32([100, 40]))
+        if begin == [0, 5, 9] and max_new == 4:
+            assert (out[:5] == 9.0).all() and (out[5:] != 9.0).any()  # the sequence that is too long is left out, the other is not
+
+
+def test_prompt_results_do_not_depend_on_timing(ctx):
+    lengths, new = [9000, 700, 300, 4500], [30, 700, 3, 150]
+    for steps in ("head", "vector"):
+        cache = ref.make_cache(lengths, 16, 2, 16, steps, seed=9)
+        first = attend(ctx, cache, lengths, new)[2]
+        for _ in range(20):
+            assert torch.equal(first, attend(ctx, cache, lengths, new)[2])
