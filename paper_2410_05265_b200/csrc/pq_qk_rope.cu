@@ -1,16 +1,15 @@
 // Norm of every query and key head and rotary embedding with positions of one to three axes in one pass (pq_qk_norm_rope), the same with the
 // quantize-on-write into the paged KV4 cache (pq_qk_norm_rope_kv4_paged_append), and the read-back of cached vectors (pq_kv4_paged_read).
 //
-// Bound by HBM: a head is read once and written once (256 bytes each way, 64 bytes as codes). Sixteen lanes take a head, a warp two heads of a
-// kind; a lane holds dims 4l .. 4l+3 and 64+4l .. 64+4l+3, so both halves of a rotary pair and the index bits 0, 1 and 6 of the
-// Hadamard transform are inside the lane, its bits 2 to 5 four shuffles away. Angles are reduced in 64 bits as fractions of a turn (a position
-// of 10^5 leaves an fp32 angle three digits).
+// Bound by HBM: a head is read once and written once (256 bytes each way, 64 bytes as codes). L lanes take a head, a warp 32 / L heads of a block of tokens; a
+// lane holds C = 64 / L dims of each half, t C .. t C + C - 1 and 64 + t C ..: both halves of a rotary pair and the lower stages of the Hadamard
+// transform are inside the lane, log2 L stages are shuffles, and the fp32 arithmetic runs on packed pairs. L = 4 for many tokens (with L = 16 the
+// kernel is bound by instruction issue: 4099 x 72 heads with R3 48.5 us), L = 16 for few, where the chain of one head is the time. Angles are reduced in 64 bits as fractions of a turn (a
+// position of 10^5 leaves an fp32 angle three digits).
 // The key heads of the append are computed in 64 bits up to the quotient that is rounded to a code: with fp32 about one code in a million depends
 // on the order of a sum, so that a prompt cached in chunks would differ from the same prompt cached at once. They are a small share of
 // the heads.
 #include <math.h>
-
-#include <type_traits>
 
 #include "pq_paged.cuh"
 
@@ -18,7 +17,8 @@ namespace {
 
 constexpr int QR_THREADS = 128;
 constexpr int QR_WARPS = QR_THREADS / 32;
-constexpr int QR_AHEAD = 4;  // units (two heads each) a warp requests together
+constexpr int QR_TOKENS = 4;  // most tokens of a CTA
+constexpr int QR_ROW = 80;    // 64 angles, every sixteen followed by four words: four lanes that read sixteen each meet in no bank
 
 struct QkParams {
   const __nv_bfloat16* x;
@@ -42,6 +42,7 @@ struct QkParams {
   int32_t* status;
   int64_t n_slots;
   int32_t page_log2;
+  int32_t tokens;    // of a CTA
   double turns[64];  // theta^(-2i/128) / (2 pi)
 };
 
@@ -51,201 +52,286 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
-__device__ __forceinline__ void unpack8(const uint2& a, const uint2& b, float (&f)[8]) {
-  f[0] = bf16_lo(a.x), f[1] = bf16_hi(a.x), f[2] = bf16_lo(a.y), f[3] = bf16_hi(a.y);
-  f[4] = bf16_lo(b.x), f[5] = bf16_hi(b.x), f[6] = bf16_lo(b.y), f[7] = bf16_hi(b.y);
+__device__ __forceinline__ int angle_at(int i) { return i + ((i >> 4) << 2); }
+__device__ __forceinline__ float2 unpack_bf16(uint32_t w) { return make_float2(bf16_lo(w), bf16_hi(w)); }
+
+// The elements of a lane: C dims of the lower half as pairs in a, of the upper half in b.
+template <int C>
+struct Lane {
+  float2 a[C / 2], b[C / 2];
+};
+
+__device__ __forceinline__ void butterfly(float2& x, float2& y) {
+  const float2 u = x;
+  x = __fadd2_rn(u, y), y = __ffma2_rn(y, make_float2(-1.0f, -1.0f), u);
 }
 
-template <typename T>
-__device__ __forceinline__ T half_warp_sum(T v) {
-#pragma unroll
-  for (int m = 1; m < 16; m <<= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
-  return v;
-}
-template <typename T>
-__device__ __forceinline__ T half_warp_max(T v) {
-#pragma unroll
-  for (int m = 1; m < 16; m <<= 1) {
-    const T o = __shfl_xor_sync(0xffffffffu, v, m);
-    v = o > v ? o : v;
-  }
-  return v;
-}
-
-__device__ __forceinline__ float inv_sqrt(float x) { return 1.0f / sqrtf(x); }
-__device__ __forceinline__ double inv_sqrt(double x) { return 1.0 / sqrt(x); }
-
-// norm, gain, rotary position and, on demand, the Hadamard transform of one head, in T
-template <typename T>
-__device__ __forceinline__ void transform(T (&f)[8], bool norm, T eps, const float (&g)[8], const T* cs, const T* sn, int l, bool rotate) {
+// norm, gain, rotary position and, on demand, the Hadamard transform of one head. gains, cs, sn: this lane's stretches (C + C, C, C floats)
+template <int C>
+__device__ __forceinline__ void transform(Lane<C>& f, bool norm, float eps, const float* gain_a, const float* gain_b, const float* cs, const float* sn, int t,
+                                          bool rotate) {
+  constexpr int P = C / 2, L = 64 / C;
+  const float turn = rotate ? 0.08838834764831845f : 1.0f;  // 1 / sqrt(128) of the transform
+  float r = turn;
   if (norm) {
-    T ss = T(0);
+    float2 s0 = make_float2(0.0f, 0.0f), s1 = s0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) ss = fma(f[e], f[e], ss);
-    const T r = inv_sqrt(half_warp_sum(ss) * T(0.0078125) + eps);
+    for (int j = 0; j < P; ++j) s0 = __ffma2_rn(f.a[j], f.a[j], s0), s1 = __ffma2_rn(f.b[j], f.b[j], s1);
+    float ss = (s0.x + s0.y) + (s1.x + s1.y);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = f[e] * r * T(g[e]);
+    for (int m = 1; m < L; m <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
+    r = turn / sqrtf(ss * 0.0078125f + eps);
   }
+  const float2 r2 = make_float2(r, r);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const T c = cs[4 * l + e], s = sn[4 * l + e], a = f[e], b = f[4 + e];
-    f[e] = fma(a, c, -(b * s));
-    f[4 + e] = fma(b, c, a * s);
+  for (int j = 0; j < P; j += 2) {
+    const float4 c4 = *reinterpret_cast<const float4*>(cs + 2 * j), s4 = *reinterpret_cast<const float4*>(sn + 2 * j);
+    float4 ga = make_float4(1.0f, 1.0f, 1.0f, 1.0f), gb = ga;
+    if (norm) ga = *reinterpret_cast<const float4*>(gain_a + 2 * j), gb = *reinterpret_cast<const float4*>(gain_b + 2 * j);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const float2 c = k ? make_float2(c4.z, c4.w) : make_float2(c4.x, c4.y), s = k ? make_float2(s4.z, s4.w) : make_float2(s4.x, s4.y);
+      float2 a = __fmul2_rn(f.a[j + k], r2), b = __fmul2_rn(f.b[j + k], r2);
+      if (norm) {
+        a = __fmul2_rn(a, k ? make_float2(ga.z, ga.w) : make_float2(ga.x, ga.y));
+        b = __fmul2_rn(b, k ? make_float2(gb.z, gb.w) : make_float2(gb.x, gb.y));
+      }
+      f.a[j + k] = __ffma2_rn(b, make_float2(-s.x, -s.y), __fmul2_rn(a, c));
+      f.b[j + k] = __ffma2_rn(b, c, __fmul2_rn(a, s));
+    }
   }
   if (rotate) {
 #pragma unroll
-    for (int m = 1; m < 8; m <<= 1) {  // index bits 0, 1 and 6
+    for (int j = 0; j < P; ++j) {  // index bit 6, then bit 0
+      butterfly(f.a[j], f.b[j]);
+      f.a[j] = make_float2(f.a[j].x + f.a[j].y, f.a[j].x - f.a[j].y);
+      f.b[j] = make_float2(f.b[j].x + f.b[j].y, f.b[j].x - f.b[j].y);
+    }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (e & m) continue;
-        const T a = f[e], b = f[e | m];
-        f[e] = a + b, f[e | m] = a - b;
+    for (int m = 1; m < P; m <<= 1)  // the other bits inside the lane
+#pragma unroll
+      for (int j = 0; j < P; ++j)
+        if (!(j & m)) butterfly(f.a[j], f.a[j | m]), butterfly(f.b[j], f.b[j | m]);
+#pragma unroll
+    for (int m = 1; m < L; m <<= 1) {  // across lanes: the upper partner holds the difference
+      const float2 sg = t & m ? make_float2(-1.0f, -1.0f) : make_float2(1.0f, 1.0f);
+#pragma unroll
+      for (int j = 0; j < P; ++j) {
+        const float2 oa = make_float2(__shfl_xor_sync(0xffffffffu, f.a[j].x, m), __shfl_xor_sync(0xffffffffu, f.a[j].y, m));
+        const float2 ob = make_float2(__shfl_xor_sync(0xffffffffu, f.b[j].x, m), __shfl_xor_sync(0xffffffffu, f.b[j].y, m));
+        f.a[j] = __ffma2_rn(f.a[j], sg, oa), f.b[j] = __ffma2_rn(f.b[j], sg, ob);
       }
     }
+  }
+}
+
+// The same in 64 bits: y[0 .. C-1] of the lower half, y[C .. 2C-1] of the upper.
+template <int C>
+__device__ __forceinline__ void transform64(double (&y)[2 * C], bool norm, double eps, const float* gain_a, const float* gain_b, const double* cs,
+                                            const double* sn, int t, bool rotate) {
+  constexpr int L = 64 / C;
+  const double turn = rotate ? 0.08838834764831844055 : 1.0;
+  double r = turn;
+  if (norm) {
+    double s0 = 0.0, s1 = 0.0;
 #pragma unroll
-    for (int m = 1; m < 16; m <<= 1) {  // index bits 2 to 5: the upper partner holds the difference
-      const T sg = l & m ? T(-1) : T(1);
+    for (int e = 0; e < C; ++e) s0 = fma(y[e], y[e], s0), s1 = fma(y[C + e], y[C + e], s1);
+    double ss = s0 + s1;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] = fma(f[e], sg, __shfl_xor_sync(0xffffffffu, f[e], m));
+    for (int m = 1; m < L; m <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
+    r = turn / sqrt(ss * 0.0078125 + eps);
+  }
+#pragma unroll
+  for (int e = 0; e < C; ++e) {
+    double a = y[e] * r, b = y[C + e] * r;
+    if (norm) a *= static_cast<double>(gain_a[e]), b *= static_cast<double>(gain_b[e]);
+    const double c = cs[e], s = sn[e];
+    y[e] = fma(a, c, -(b * s));
+    y[C + e] = fma(b, c, a * s);
+  }
+  if (rotate) {
+#pragma unroll
+    for (int m = 1; m < 2 * C; m <<= 1)  // the bits inside the lane
+#pragma unroll
+      for (int e = 0; e < 2 * C; ++e)
+        if (!(e & m)) {
+          const double u = y[e], v = y[e | m];
+          y[e] = u + v, y[e | m] = u - v;
+        }
+#pragma unroll
+    for (int m = 1; m < L; m <<= 1) {
+      const double sg = t & m ? -1.0 : 1.0;
+#pragma unroll
+      for (int e = 0; e < 2 * C; ++e) y[e] = fma(y[e], sg, __shfl_xor_sync(0xffffffffu, y[e], m));
     }
-    const T norm128 = T(0.08838834764831844055);  // 1 / sqrt(128)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] *= norm128;
   }
 }
 
 __device__ __forceinline__ uint32_t clamp_code(float q) { return static_cast<uint32_t>(max(-8, min(7, __float2int_rn(q)))) & 0xFu; }
 
-template <bool APPEND>
-__global__ void __launch_bounds__(QR_THREADS) qk_norm_rope_kernel(const QkParams p) {
-  __shared__ float cs[64], sn[64];
-  __shared__ double csk[APPEND ? 64 : 1], snk[APPEND ? 64 : 1];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, l = lane & 15, half = lane >> 4;
-  const int uq = (p.Hq + 1) >> 1, uk = (p.Hk + 1) >> 1;
-  const int n_units = uq + (APPEND ? 2 : 1) * uk;  // keys, then (append) values, then queries: the longest first
+template <bool APPEND, int L>
+__global__ void __launch_bounds__(QR_THREADS, 4) qk_norm_rope_kernel(const QkParams p) {
+  constexpr int C = 64 / L, P = C / 2, W = C / 4, PER_WARP = 32 / L;  // dims of a half, pairs, 8-byte words, heads of a unit
+  __shared__ __align__(16) float cs[QR_TOKENS][QR_ROW], sn[QR_TOKENS][QR_ROW];
+  __shared__ __align__(16) double csk[APPEND ? QR_TOKENS : 1][APPEND ? QR_ROW : 1], snk[APPEND ? QR_TOKENS : 1][APPEND ? QR_ROW : 1];
+  __shared__ __align__(16) float gains[2][2 * QR_ROW];  // queries, keys; dims 0 .. 63 and 64 .. 127 padded as the angles are
+  __shared__ int64_t slots[QR_TOKENS];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t = lane & (L - 1), group = lane / L;
+  const int64_t t0 = static_cast<int64_t>(blockIdx.x) * p.tokens;
+  const int n_tok = static_cast<int>(min(static_cast<int64_t>(p.tokens), p.N - t0));
+  // Heads of the block, token by token, PER_WARP to a unit: the append's keys (the longest), its values, and what goes out as bf16.
+  const int n_k = APPEND ? n_tok * p.Hk : 0, n_out = n_tok * (APPEND ? p.Hq : p.Hq + p.Hk);
+  const int uk = (n_k + PER_WARP - 1) / PER_WARP, n_units = 2 * uk + (n_out + PER_WARP - 1) / PER_WARP;
+  struct Unit {
+    int kind, tok, h;  // kind 0 keys, 1 values, 2 out as bf16: the same for the warp
+    bool live;
+    uint2 w[2 * W];
+  };
   pq::pdl_wait();
   if (!APPEND) pq::pdl_trigger();  // a writer of cache rows does not (see pq_launch_pdl)
-  const bool norm = p.gq != nullptr;
-  float gq[8], gk[8];
-  {
-    uint2 a = make_uint2(0u, 0u), b = a, c = a, d = a;
-    if (norm) {
-      a = pq::ld_dep(reinterpret_cast<const uint2*>(p.gq) + l), b = pq::ld_dep(reinterpret_cast<const uint2*>(p.gq) + 16 + l);
-      c = pq::ld_dep(reinterpret_cast<const uint2*>(p.gk) + l), d = pq::ld_dep(reinterpret_cast<const uint2*>(p.gk) + 16 + l);
+  if (APPEND && threadIdx.x < n_tok) {
+    int64_t s = pq::ld_dep(p.slot + t0 + threadIdx.x);
+    if (s >= p.n_slots) {
+      pq::report(p.status, PQ_ERR_SHAPE);
+      s = -1;
     }
-    unpack8(a, b, gq);
-    unpack8(c, d, gk);
+    slots[threadIdx.x] = s;
   }
-  for (int64_t t = blockIdx.x; t < p.N; t += gridDim.x) {
-    int64_t slot = 0;
-    if (APPEND) {
-      slot = pq::ld_dep(p.slot + t);
-      if (slot < 0) continue;
-      if (slot >= p.n_slots) {
-        if (threadIdx.x == 0) pq::report(p.status, PQ_ERR_SHAPE);
-        continue;
-      }
-    }
-    __syncthreads();  // the angles of the token before have been used
-    if (threadIdx.x < 64) {
-      const int i = threadIdx.x;
-      const int axis = i < p.end0 ? 0 : i < p.end1 ? 1 : 2;
-      const double turn = static_cast<double>(pq::ld_dep(p.pos + axis * p.ld_pos + t)) * p.turns[i];
-      const double frac = turn - rint(turn);  // in [-1/2, 1/2], exact
-      if (APPEND) {
-        double s, c;
-        sincospi(2.0 * frac, &s, &c);
-        csk[APPEND ? i : 0] = c, snk[APPEND ? i : 0] = s;
-        cs[i] = static_cast<float>(c), sn[i] = static_cast<float>(s);
+  if (APPEND) __syncthreads();
+  auto request = [&](int u, Unit& x) {
+    x.kind = u < uk ? 0 : u < 2 * uk ? 1 : 2;
+    const int per = x.kind == 2 ? (APPEND ? p.Hq : p.Hq + p.Hk) : p.Hk;
+    const int v = PER_WARP * (x.kind == 0 ? u : x.kind == 1 ? u - uk : u - 2 * uk) + group;
+    const bool in = v < (x.kind == 2 ? n_out : n_k);
+    x.tok = in ? v / per : 0, x.h = in ? v - x.tok * per : 0;
+    x.live = in && (!APPEND || slots[x.tok] >= 0);
+    const int head = x.kind == 0 ? p.Hq + x.h : x.kind == 1 ? p.Hq + p.Hk + x.h : x.h;
+    const __nv_bfloat16* src = p.x + (t0 + x.tok) * p.ld + static_cast<int64_t>(head) * 128 + t * C;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (W >= 2) {
+#pragma unroll
+        for (int j = 0; j < W; j += 2) {
+          const uint4 v4 = x.live ? pq::ld_dep(reinterpret_cast<const uint4*>(src + 64 * i) + j / 2) : make_uint4(0, 0, 0, 0);
+          x.w[i * W + j] = make_uint2(v4.x, v4.y), x.w[i * W + (W > 1 ? j + 1 : j)] = make_uint2(v4.z, v4.w);
+        }
       } else {
-        float s, c;
-        sincospif(static_cast<float>(2.0 * frac), &s, &c);
-        cs[i] = c, sn[i] = s;
+        x.w[i] = x.live ? pq::ld_dep(reinterpret_cast<const uint2*>(src + 64 * i)) : make_uint2(0, 0);
       }
     }
-    __syncthreads();
-    const uint8_t* xr = reinterpret_cast<const uint8_t*>(p.x + t * p.ld);
-    for (int first = warp; first < n_units; first += QR_AHEAD * QR_WARPS) {
-      uint2 wa[QR_AHEAD], wb[QR_AHEAD];
-      int head[QR_AHEAD];
+  };
+  Unit next;
+  if (warp < n_units) request(warp, next);  // on its way while the angles are formed
+  const bool norm = p.gq != nullptr;
+  if (norm) {  // a pair of gains to a thread
+    const int which = threadIdx.x >> 6, i = threadIdx.x & 63;
+    const uint32_t w = pq::ld_dep(reinterpret_cast<const uint32_t*>(which ? p.gk : p.gq) + i);
+    float* dst = gains[which] + (i >= 32 ? QR_ROW : 0) + angle_at((2 * i) & 63);
+    dst[0] = bf16_lo(w), dst[1] = bf16_hi(w);
+  }
+  for (int k = threadIdx.x; k < n_tok * 64; k += QR_THREADS) {
+    const int i = k & 63, tok = k >> 6;
+    const int axis = i < p.end0 ? 0 : i < p.end1 ? 1 : 2;
+    const double turn = static_cast<double>(pq::ld_dep(p.pos + axis * p.ld_pos + t0 + tok)) * p.turns[i];
+    const double frac = turn - rint(turn);  // in [-1/2, 1/2], exact
+    if (APPEND) {
+      double s, c;
+      sincospi(2.0 * frac, &s, &c);
+      csk[APPEND ? tok : 0][APPEND ? angle_at(i) : 0] = c, snk[APPEND ? tok : 0][APPEND ? angle_at(i) : 0] = s;
+      cs[tok][angle_at(i)] = static_cast<float>(c), sn[tok][angle_at(i)] = static_cast<float>(s);
+    } else {
+      float s, c;
+      sincospif(static_cast<float>(2.0 * frac), &s, &c);
+      cs[tok][angle_at(i)] = c, sn[tok][angle_at(i)] = s;
+    }
+  }
+  __syncthreads();
+  const int col = angle_at(t * C);  // of this lane's stretch in a padded row
+
+  for (int u = warp; u < n_units; u += QR_WARPS) {
+    const Unit x = next;
+    if (u + QR_WARPS < n_units) request(u + QR_WARPS, next);
+    const int64_t row = t0 + x.tok;
+    Lane<C> f;
 #pragma unroll
-      for (int a = 0; a < QR_AHEAD; ++a) {
-        const int u = first + a * QR_WARPS;
-        if (u >= n_units) break;
-        // kind 0: keys, 1: values, 2: queries; the second half of an odd last pair repeats its head and stores nothing
-        const int kind = u < uk ? 0 : (APPEND && u < 2 * uk) ? 1 : 2;
-        const int in_kind = 2 * (kind == 0 ? u : kind == 1 ? u - uk : u - (APPEND ? 2 : 1) * uk) + half;
-        const int count = kind == 2 ? p.Hq : p.Hk;
-        const int h = min(in_kind, count - 1);
-        head[a] = in_kind < count ? h : -1 - h;
-        const int col = kind == 2 ? h : kind == 0 ? p.Hq + h : p.Hq + p.Hk + h;
-        const uint2* src = reinterpret_cast<const uint2*>(xr + static_cast<int64_t>(col) * 256);
-        wa[a] = pq::ld_dep(src + l), wb[a] = pq::ld_dep(src + 16 + l);
-      }
+    for (int i = 0; i < W; ++i) {
+      f.a[2 * i] = unpack_bf16(x.w[i].x), f.a[2 * i + 1] = unpack_bf16(x.w[i].y);
+      f.b[2 * i] = unpack_bf16(x.w[W + i].x), f.b[2 * i + 1] = unpack_bf16(x.w[W + i].y);
+    }
+    if (!APPEND || x.kind == 2) {
+      const float* g = gains[!APPEND && x.h >= p.Hq ? 1 : 0] + col;
+      transform<C>(f, norm, p.eps, g, g + QR_ROW, cs[x.tok] + col, sn[x.tok] + col, t, p.rotate != 0);
+      if (x.live) {
+        __nv_bfloat16* dst = p.y + row * p.ldy + static_cast<int64_t>(x.h) * 128 + t * C;
 #pragma unroll
-      for (int a = 0; a < QR_AHEAD; ++a) {
-        const int u = first + a * QR_WARPS;
-        if (u >= n_units) break;
-        const int kind = u < uk ? 0 : (APPEND && u < 2 * uk) ? 1 : 2;
-        const bool mine = head[a] >= 0;
-        const int h = mine ? head[a] : -1 - head[a];
-        float f[8];
-        unpack8(wa[a], wb[a], f);
-        if (!APPEND || kind == 2) {
-          const bool is_q = kind == 2;
-          float g[8];
+        for (int i = 0; i < 2; ++i) {
+          const float2* o = i ? f.b : f.a;
+          if (W >= 2) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) g[e] = is_q ? gq[e] : gk[e];
-          transform<float>(f, norm, p.eps, g, cs, sn, l, p.rotate != 0);
-          if (mine) {
-            uint2* dst = reinterpret_cast<uint2*>(p.y + t * p.ldy + static_cast<int64_t>(is_q ? h : p.Hq + h) * 128);
-            dst[l] = make_uint2(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]));
-            dst[16 + l] = make_uint2(pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
-          }
-          continue;
-        }
-        uint32_t code[8];
-        float s;
-        if (kind == 0) {
-          double y[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = static_cast<double>(f[e]);
-          transform<double>(y, norm, static_cast<double>(p.eps), gk, csk, snk, l, p.rotate != 0);
-          if (p.steps) {
-            double mx = 0.0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) mx = fmax(mx, fabs(y[e]));
-            mx = half_warp_max(mx);
-            s = mx < 0x1p-57 ? 1.0f : __double2float_rn(mx / 7.0);
+            for (int j = 0; j < P; j += 4)
+              reinterpret_cast<uint4*>(dst + 64 * i)[j / 4] = make_uint4(pack_bf16(o[j].x, o[j].y), pack_bf16(o[j + 1].x, o[j + 1].y),
+                                                                         pack_bf16(o[(j + 2) % P].x, o[(j + 2) % P].y), pack_bf16(o[(j + 3) % P].x, o[(j + 3) % P].y));
           } else {
-            s = pq::ld_dep(p.s_k + h);
+            *reinterpret_cast<uint2*>(dst + 64 * i) = make_uint2(pack_bf16(o[0].x, o[0].y), pack_bf16(o[1].x, o[1].y));
           }
-          // (1 / s in 64 bits leaves the quotient exact to 2^-52: rounded to fp32 it is the exact quotient's fp32 value, ties of representable ones included)
-          const double inv = 1.0 / static_cast<double>(s);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) code[e] = clamp_code(__double2float_rn(y[e] * inv));
-        } else {
-          if (p.steps) {
-            float mx = 0.0f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) mx = fmaxf(mx, fabsf(f[e]));
-            mx = half_warp_max(mx);
-            s = mx < 0x1p-57f ? 1.0f : __fdiv_rn(mx, 7.0f);
-          } else {
-            s = pq::ld_dep(p.s_v + h);
-          }
-#pragma unroll
-          for (int e = 0; e < 8; ++e) code[e] = clamp_code(__fdiv_rn(f[e], s));
-        }
-        if (mine) {
-          const int64_t row = ((slot >> p.page_log2) * p.Hk + h) * 2 + kind;  // (page, head, keys or values)
-          const int64_t vec = (row << p.page_log2) + (slot & ((1 << p.page_log2) - 1));
-          uint16_t* dst = reinterpret_cast<uint16_t*>(p.codes + vec * 64);
-          dst[l] = static_cast<uint16_t>(code[0] | code[1] << 4 | code[2] << 8 | code[3] << 12);
-          dst[16 + l] = static_cast<uint16_t>(code[4] | code[5] << 4 | code[6] << 8 | code[7] << 12);
-          if (p.steps && l == 0) p.steps[vec] = s;
         }
       }
+      continue;
+    }
+    uint32_t codes[2][(C + 7) / 8] = {};  // eight to a word
+    float s;
+    if (x.kind == 0) {
+      double y[2 * C];
+#pragma unroll
+      for (int j = 0; j < P; ++j) {
+        y[2 * j] = static_cast<double>(f.a[j].x), y[2 * j + 1] = static_cast<double>(f.a[j].y);
+        y[C + 2 * j] = static_cast<double>(f.b[j].x), y[C + 2 * j + 1] = static_cast<double>(f.b[j].y);
+      }
+      transform64<C>(y, norm, static_cast<double>(p.eps), gains[1] + col, gains[1] + QR_ROW + col, csk[APPEND ? x.tok : 0] + (APPEND ? col : 0),
+                     snk[APPEND ? x.tok : 0] + (APPEND ? col : 0), t, p.rotate != 0);
+      if (p.steps) {
+        double mx = 0.0;
+#pragma unroll
+        for (int e = 0; e < 2 * C; ++e) mx = fmax(mx, fabs(y[e]));
+#pragma unroll
+        for (int m = 1; m < L; m <<= 1) mx = fmax(mx, __shfl_xor_sync(0xffffffffu, mx, m));
+        s = mx < 0x1p-57 ? 1.0f : __double2float_rn(mx / 7.0);
+      } else {
+        s = pq::ld_dep(p.s_k + x.h);
+      }
+      // (1 / s in 64 bits leaves the quotient exact to 2^-52: rounded to fp32 it is the exact quotient's fp32 value, ties of representable ones included)
+      const double inv = 1.0 / static_cast<double>(s);
+#pragma unroll
+      for (int e = 0; e < 2 * C; ++e) codes[e / C][(e % C) >> 3] |= clamp_code(__double2float_rn(y[e] * inv)) << (4 * (e & 7 & (C - 1)));
+    } else {
+      if (p.steps) {
+        float mx = 0.0f;
+#pragma unroll
+        for (int j = 0; j < P; ++j) mx = fmaxf(fmaxf(mx, fmaxf(fabsf(f.a[j].x), fabsf(f.a[j].y))), fmaxf(fabsf(f.b[j].x), fabsf(f.b[j].y)));
+#pragma unroll
+        for (int m = 1; m < L; m <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, m));
+        s = mx < 0x1p-57f ? 1.0f : __fdiv_rn(mx, 7.0f);
+      } else {
+        s = pq::ld_dep(p.s_v + x.h);
+      }
+#pragma unroll
+      for (int e = 0; e < 2 * C; ++e) {
+        const float2 pair = e < C ? f.a[(e % C) >> 1] : f.b[(e % C) >> 1];
+        codes[e / C][(e % C) >> 3] |= clamp_code(__fdiv_rn(e & 1 ? pair.y : pair.x, s)) << (4 * (e & 7 & (C - 1)));
+      }
+    }
+    if (x.live) {
+      const int64_t slot = slots[x.tok];
+      const int64_t vec = ((((slot >> p.page_log2) * p.Hk + x.h) * 2 + x.kind) << p.page_log2) + (slot & ((1 << p.page_log2) - 1));  // (page, head, keys or values)
+      uint8_t* dst = p.codes + vec * 64 + t * P;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (C >= 16)
+          *reinterpret_cast<uint2*>(dst + 32 * i) = make_uint2(codes[i][0], codes[i][(C + 7) / 8 - 1]);
+        else
+          *reinterpret_cast<uint16_t*>(dst + 32 * i) = static_cast<uint16_t>(codes[i][0]);
+      }
+      if (p.steps && t == 0) p.steps[vec] = s;
     }
   }
 }
@@ -307,8 +393,23 @@ pq_status rope_params(QkParams& p, const void* x, int64_t N, int32_t Hq, int32_t
   p.y = static_cast<__nv_bfloat16*>(y), p.ldy = ldy;
   p.N = N, p.eps = eps, p.Hq = Hq, p.Hk = Hk, p.rotate = rotate;
   p.end0 = sec[0], p.end1 = sec[0] + sec[1];
-  for (int i = 0; i < 64; ++i) p.turns[i] = pow(theta, -2.0 * i / 128.0) / 6.283185307179586476925286766559;
+  // the frequencies of the last theta of this thread: 64 powers cost as much as the launch
+  static thread_local double of_theta = 0.0, turns[64];
+  if (theta != of_theta) {
+    for (int i = 0; i < 64; ++i) turns[i] = pow(theta, -2.0 * i / 128.0) / 6.283185307179586476925286766559;
+    of_theta = theta;
+  }
+  for (int i = 0; i < 64; ++i) p.turns[i] = turns[i];
   return PQ_OK;
+}
+
+// A CTA takes one token while the tokens do not fill the SMs four times over, then more, up to QR_TOKENS.
+pq_status launch(void (*many)(const QkParams), void (*few)(const QkParams), pq_ctx* ctx, QkParams& p, cudaStream_t st) {
+  const int64_t per = p.N / (4LL * ctx->sm_count);
+  p.tokens = static_cast<int32_t>(per < 1 ? 1 : per > QR_TOKENS ? QR_TOKENS : per);
+  const int64_t grid = (p.N + p.tokens - 1) / p.tokens;
+  if (grid > 0x7fffffffll) return PQ_ERR_SHAPE;
+  return pq_launch_pdl(p.N <= 2LL * ctx->sm_count ? few : many, dim3(static_cast<unsigned>(grid)), QR_THREADS, 0, st, p);
 }
 
 }  // namespace
@@ -323,8 +424,7 @@ extern "C" pq_status pq_qk_norm_rope(pq_ctx* ctx, const void* x, int64_t N, int3
   const int64_t cols = (static_cast<int64_t>(Hq) + Hk) * 128;
   const pq_status st = rope_params(p, x, N, Hq, Hk, cols, ld, gq, gk, eps, pos, n_axes, ld_pos, sections, theta, rotate, y, ldy, cols);
   if (st != PQ_OK) return st;
-  const int64_t grid = N < 16LL * ctx->sm_count ? N : 16LL * ctx->sm_count;
-  return pq_launch_pdl(qk_norm_rope_kernel<false>, dim3(static_cast<unsigned>(grid)), QR_THREADS, 0, static_cast<cudaStream_t>(stream), p);
+  return launch(qk_norm_rope_kernel<false, 4>, qk_norm_rope_kernel<false, 16>, ctx, p, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" pq_status pq_qk_norm_rope_kv4_paged_append(pq_ctx* ctx, const pq_kv4_paged* c, const void* qkv, int64_t N, int64_t ld, const void* gq,
@@ -343,8 +443,7 @@ extern "C" pq_status pq_qk_norm_rope_kv4_paged_append(pq_ctx* ctx, const pq_kv4_
   p.slot = slot, p.codes = c->codes, p.steps = c->steps, p.s_k = c->s_k, p.s_v = c->s_v, p.status = ctx->d_status;
   p.page_log2 = pq_page_log2(c->pages.page);
   p.n_slots = static_cast<int64_t>(c->pages.n_pages) << p.page_log2;
-  const int64_t grid = N < 16LL * ctx->sm_count ? N : 16LL * ctx->sm_count;
-  return pq_launch_pdl(qk_norm_rope_kernel<true>, dim3(static_cast<unsigned>(grid)), QR_THREADS, 0, static_cast<cudaStream_t>(stream), p);
+  return launch(qk_norm_rope_kernel<true, 4>, qk_norm_rope_kernel<true, 16>, ctx, p, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" pq_status pq_kv4_paged_read(pq_ctx* ctx, const pq_kv4_paged* c, const int64_t* slot, int64_t N, void* out, void* stream) {
