@@ -18,6 +18,7 @@ namespace {
 constexpr int QR_THREADS = 128;
 constexpr int QR_WARPS = QR_THREADS / 32;
 constexpr int QR_TOKENS = 4;  // most tokens of a CTA
+static_assert(QR_TOKENS == 4, "the search for a head's token");
 constexpr int QR_ROW = 80;    // 64 angles, every sixteen followed by four words: four lanes that read sixteen each meet in no bank
 
 struct QkParams {
@@ -66,13 +67,13 @@ __device__ __forceinline__ void butterfly(float2& x, float2& y) {
   x = __fadd2_rn(u, y), y = __ffma2_rn(y, make_float2(-1.0f, -1.0f), u);
 }
 
-// norm, gain, rotary position and, on demand, the Hadamard transform of one head. gains, cs, sn: this lane's stretches (C + C, C, C floats)
+// norm, gain, rotary position and, on demand, the Hadamard transform of one head. `f4`: this lane's stretch of the token's factors, four rows of QR_ROW: with the
+// gains ga, gb of the two halves, cos ga, -sin gb, cos gb, sin ga. The factor of the norm is common to the head: it is returned and applied to
+// what leaves.
 template <int C>
-__device__ __forceinline__ void transform(Lane<C>& f, bool norm, float eps, const float* gain_a, const float* gain_b, const float* cs, const float* sn, int t,
-                                          bool rotate) {
+__device__ __forceinline__ float transform(Lane<C>& f, bool norm, float eps, const float* f4, int t, bool rotate) {
   constexpr int P = C / 2, L = 64 / C;
-  const float turn = rotate ? 0.08838834764831845f : 1.0f;  // 1 / sqrt(128) of the transform
-  float r = turn;
+  float r = rotate ? 0.08838834764831845f : 1.0f;  // 1 / sqrt(128) of the transform
   if (norm) {
     float2 s0 = make_float2(0.0f, 0.0f), s1 = s0;
 #pragma unroll
@@ -80,25 +81,17 @@ __device__ __forceinline__ void transform(Lane<C>& f, bool norm, float eps, cons
     float ss = (s0.x + s0.y) + (s1.x + s1.y);
 #pragma unroll
     for (int m = 1; m < L; m <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
-    r = turn / sqrtf(ss * 0.0078125f + eps);
+    r = r / sqrtf(ss * 0.0078125f + eps);
   }
-  const float2 r2 = make_float2(r, r);
 #pragma unroll
   for (int j = 0; j < P; j += 2) {
-    const float4 c4 = *reinterpret_cast<const float4*>(cs + 2 * j), s4 = *reinterpret_cast<const float4*>(sn + 2 * j);
-    float4 ga = make_float4(1.0f, 1.0f, 1.0f, 1.0f), gb = ga;
-    if (norm) ga = *reinterpret_cast<const float4*>(gain_a + 2 * j), gb = *reinterpret_cast<const float4*>(gain_b + 2 * j);
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const float2 c = k ? make_float2(c4.z, c4.w) : make_float2(c4.x, c4.y), s = k ? make_float2(s4.z, s4.w) : make_float2(s4.x, s4.y);
-      float2 a = __fmul2_rn(f.a[j + k], r2), b = __fmul2_rn(f.b[j + k], r2);
-      if (norm) {
-        a = __fmul2_rn(a, k ? make_float2(ga.z, ga.w) : make_float2(ga.x, ga.y));
-        b = __fmul2_rn(b, k ? make_float2(gb.z, gb.w) : make_float2(gb.x, gb.y));
-      }
-      f.a[j + k] = __ffma2_rn(b, make_float2(-s.x, -s.y), __fmul2_rn(a, c));
-      f.b[j + k] = __ffma2_rn(b, c, __fmul2_rn(a, s));
-    }
+    const float4 ca = *reinterpret_cast<const float4*>(f4 + 2 * j), sb = *reinterpret_cast<const float4*>(f4 + QR_ROW + 2 * j);
+    const float4 cb = *reinterpret_cast<const float4*>(f4 + 2 * QR_ROW + 2 * j), sa = *reinterpret_cast<const float4*>(f4 + 3 * QR_ROW + 2 * j);
+    const float2 a0 = f.a[j], b0 = f.b[j], a1 = f.a[j + 1], b1 = f.b[j + 1];
+    f.a[j] = __ffma2_rn(b0, make_float2(sb.x, sb.y), __fmul2_rn(a0, make_float2(ca.x, ca.y)));
+    f.b[j] = __ffma2_rn(b0, make_float2(cb.x, cb.y), __fmul2_rn(a0, make_float2(sa.x, sa.y)));
+    f.a[j + 1] = __ffma2_rn(b1, make_float2(sb.z, sb.w), __fmul2_rn(a1, make_float2(ca.z, ca.w)));
+    f.b[j + 1] = __ffma2_rn(b1, make_float2(cb.z, cb.w), __fmul2_rn(a1, make_float2(sa.z, sa.w)));
   }
   if (rotate) {
 #pragma unroll
@@ -123,6 +116,7 @@ __device__ __forceinline__ void transform(Lane<C>& f, bool norm, float eps, cons
       }
     }
   }
+  return r;
 }
 
 // The same in 64 bits: y[0 .. C-1] of the lower half, y[C .. 2C-1] of the upper.
@@ -170,9 +164,9 @@ __device__ __forceinline__ void transform64(double (&y)[2 * C], bool norm, doubl
 __device__ __forceinline__ uint32_t clamp_code(float q) { return static_cast<uint32_t>(max(-8, min(7, __float2int_rn(q)))) & 0xFu; }
 
 template <bool APPEND, int L>
-__global__ void __launch_bounds__(QR_THREADS, 4) qk_norm_rope_kernel(const QkParams p) {
+__global__ void __launch_bounds__(QR_THREADS, APPEND ? 4 : 5) qk_norm_rope_kernel(const QkParams p) {
   constexpr int C = 64 / L, P = C / 2, W = C / 4, PER_WARP = 32 / L;  // dims of a half, pairs, 8-byte words, heads of a unit
-  __shared__ __align__(16) float cs[QR_TOKENS][QR_ROW], sn[QR_TOKENS][QR_ROW];
+  __shared__ __align__(16) float factors[QR_TOKENS][APPEND ? 1 : 2][4][QR_ROW];  // of the queries and (what is not appended) of the keys
   __shared__ __align__(16) double csk[APPEND ? QR_TOKENS : 1][APPEND ? QR_ROW : 1], snk[APPEND ? QR_TOKENS : 1][APPEND ? QR_ROW : 1];
   __shared__ __align__(16) float gains[2][2 * QR_ROW];  // queries, keys; dims 0 .. 63 and 64 .. 127 padded as the angles are
   __shared__ int64_t slots[QR_TOKENS];
@@ -203,7 +197,8 @@ __global__ void __launch_bounds__(QR_THREADS, 4) qk_norm_rope_kernel(const QkPar
     const int per = x.kind == 2 ? (APPEND ? p.Hq : p.Hq + p.Hk) : p.Hk;
     const int v = PER_WARP * (x.kind == 0 ? u : x.kind == 1 ? u - uk : u - 2 * uk) + group;
     const bool in = v < (x.kind == 2 ? n_out : n_k);
-    x.tok = in ? v / per : 0, x.h = in ? v - x.tok * per : 0;
+    x.tok = in ? (v >= per) + (v >= 2 * per) + (v >= 3 * per) : 0;  // of at most QR_TOKENS
+    x.h = in ? v - x.tok * per : 0;
     x.live = in && (!APPEND || slots[x.tok] >= 0);
     const int head = x.kind == 0 ? p.Hq + x.h : x.kind == 1 ? p.Hq + p.Hk + x.h : x.h;
     const __nv_bfloat16* src = p.x + (t0 + x.tok) * p.ld + static_cast<int64_t>(head) * 128 + t * C;
@@ -229,6 +224,16 @@ __global__ void __launch_bounds__(QR_THREADS, 4) qk_norm_rope_kernel(const QkPar
     float* dst = gains[which] + (i >= 32 ? QR_ROW : 0) + angle_at((2 * i) & 63);
     dst[0] = bf16_lo(w), dst[1] = bf16_hi(w);
   }
+  __syncthreads();
+  auto put = [&](int tok, int i, float c, float s) {
+    const int at = angle_at(i);
+#pragma unroll
+    for (int which = 0; which < (APPEND ? 1 : 2); ++which) {
+      const float ga = norm ? gains[which][at] : 1.0f, gb = norm ? gains[which][QR_ROW + at] : 1.0f;
+      float(*f)[QR_ROW] = factors[tok][which];
+      f[0][at] = c * ga, f[1][at] = -s * gb, f[2][at] = c * gb, f[3][at] = s * ga;
+    }
+  };
   for (int k = threadIdx.x; k < n_tok * 64; k += QR_THREADS) {
     const int i = k & 63, tok = k >> 6;
     const int axis = i < p.end0 ? 0 : i < p.end1 ? 1 : 2;
@@ -238,11 +243,11 @@ __global__ void __launch_bounds__(QR_THREADS, 4) qk_norm_rope_kernel(const QkPar
       double s, c;
       sincospi(2.0 * frac, &s, &c);
       csk[APPEND ? tok : 0][APPEND ? angle_at(i) : 0] = c, snk[APPEND ? tok : 0][APPEND ? angle_at(i) : 0] = s;
-      cs[tok][angle_at(i)] = static_cast<float>(c), sn[tok][angle_at(i)] = static_cast<float>(s);
+      put(tok, i, static_cast<float>(c), static_cast<float>(s));
     } else {
       float s, c;
       sincospif(static_cast<float>(2.0 * frac), &s, &c);
-      cs[tok][angle_at(i)] = c, sn[tok][angle_at(i)] = s;
+      put(tok, i, c, s);
     }
   }
   __syncthreads();
@@ -259,8 +264,10 @@ __global__ void __launch_bounds__(QR_THREADS, 4) qk_norm_rope_kernel(const QkPar
       f.b[2 * i] = unpack_bf16(x.w[W + i].x), f.b[2 * i + 1] = unpack_bf16(x.w[W + i].y);
     }
     if (!APPEND || x.kind == 2) {
-      const float* g = gains[!APPEND && x.h >= p.Hq ? 1 : 0] + col;
-      transform<C>(f, norm, p.eps, g, g + QR_ROW, cs[x.tok] + col, sn[x.tok] + col, t, p.rotate != 0);
+      const float r = transform<C>(f, norm, p.eps, factors[x.tok][!APPEND && x.h >= p.Hq ? 1 : 0][0] + col, t, p.rotate != 0);
+      const float2 r2 = make_float2(r, r);
+#pragma unroll
+      for (int j = 0; j < P; ++j) f.a[j] = __fmul2_rn(f.a[j], r2), f.b[j] = __fmul2_rn(f.b[j], r2);
       if (x.live) {
         __nv_bfloat16* dst = p.y + row * p.ldy + static_cast<int64_t>(x.h) * 128 + t * C;
 #pragma unroll
