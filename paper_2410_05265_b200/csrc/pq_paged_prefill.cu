@@ -34,9 +34,12 @@ constexpr int PP_LANDS = 3;           // landing slots: K and V rows of a tile t
 constexpr int PP_STAGES = 2;
 constexpr int PP_SOFTMAX_WARPS = 8, PP_EXPAND_WARPS = 4;
 constexpr int PP_WARP_EXPAND0 = PP_SOFTMAX_WARPS, PP_WARP_MMA = PP_WARP_EXPAND0 + PP_EXPAND_WARPS, PP_WARP_LOAD = PP_WARP_MMA + 1;
-constexpr int PP_THREADS = (PP_WARP_LOAD + 1) * 32;  // 448
+constexpr int PP_THREADS = 512;  // the warps behind the loader only give their registers
 constexpr int PP_TMEM_COLS = 512;     // S0 | S1 | O0 | O1, 128 columns each; P_i lies over the first 64 columns of S_i
-constexpr float PP_LAZY = 8.0f;       // log2 units an exponent may exceed the reference before it is moved
+constexpr int PP_SHORT = 8;         // an item of so many key tiles or fewer is not shared between workers
+constexpr float PP_LAZY = 15.0f;      // log2 units an exponent may exceed the reference before it is moved: weights stay inside fp16
+// Registers: 512 threads at 128; the softmax warpgroups take 168, the others leave 88 (256 x 168 + 256 x 88 = 512 x 128).
+constexpr int PP_REGS_SOFTMAX = 168, PP_REGS_OTHERS = 88;
 constexpr int PP_TICKET0 = PQ_PAGED_TICKET0 + PQ_PAGED_MAX_WORKERS;
 constexpr int PP_PARTIAL = 256 * 128;  // floats of an item's partial output: [dims / 4][row][4]
 
@@ -162,6 +165,37 @@ __device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_
       "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
+constexpr int PP_CHUNK = 16;  // score columns a softmax thread requests at a time
+__device__ __forceinline__ void tmem_ld_chunk(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+        "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+}
+// The wait with the loaded registers as operands: every use of r stays behind it.
+__device__ __forceinline__ void tmem_ld_wait_chunk(uint32_t (&r)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
+                 "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+               :
+               : "memory");
+}
+__device__ __forceinline__ void tmem_ld_32x16(uint32_t taddr, uint32_t (&r)[16]) {
+  tmem_ld_chunk(taddr, r);
+  tmem_ld_wait_chunk(r);
+}
+// Exchanges between lanes l and l ^ m: the lane with the bit clear keeps a and receives the other's a as b, the other keeps b and receives b as a.
+__device__ __forceinline__ void swap_halves(uint4& a, uint4& b, bool bit, int m) {
+  uint4 t = bit ? a : b;
+  t.x = __shfl_xor_sync(0xffffffffu, t.x, m), t.y = __shfl_xor_sync(0xffffffffu, t.y, m);
+  t.z = __shfl_xor_sync(0xffffffffu, t.z, m), t.w = __shfl_xor_sync(0xffffffffu, t.w, m);
+  if (bit)
+    a = t;
+  else
+    b = t;
+}
 __device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
@@ -281,24 +315,35 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     st.U = too_many ? 0 : static_cast<int>(total);
     st.workers = min(static_cast<int>(gridDim.x), max(1, st.U / 2));  // two tiles at least
     if (st.U > 0 && static_cast<int>(blockIdx.x) < st.workers) {
-      st.u0 = static_cast<int>(static_cast<int64_t>(st.U) * blockIdx.x / st.workers);
-      st.u1 = static_cast<int>(static_cast<int64_t>(st.U) * (blockIdx.x + 1) / st.workers);
-      PpItem x;
-      x.b = pq::find_segment(scan, p.B, st.u0 / p.Hkv);
-      bool odd;
-      load_seq(x, odd);
-      const int per_head = scan[x.b + 1] - scan[x.b], rel = st.u0 - scan[x.b] * p.Hkv;
-      st.b = x.b, st.h = rel / per_head;
-      const int v = rel - st.h * per_head;
-      int lo = 0, hi = row_tiles(x) - 1;  // last row tile with tiles_before <= v
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (tiles_before(x, mid) <= v)
-          lo = mid;
-        else
-          hi = mid - 1;
-      }
-      st.rt = lo, st.j0 = v - static_cast<int>(tiles_before(x, lo));
+      int tiles = 0;
+      auto locate = [&](int u) {  // unit u into (b, h, rt, j0) and the tiles of its item
+        PpItem x;
+        x.b = pq::find_segment(scan, p.B, u / p.Hkv);
+        bool odd;
+        load_seq(x, odd);
+        const int per_head = scan[x.b + 1] - scan[x.b], rel = u - scan[x.b] * p.Hkv;
+        st.b = x.b, st.h = rel / per_head;
+        const int v = rel - st.h * per_head;
+        int lo = 0, hi = row_tiles(x) - 1;  // last row tile with tiles_before <= v
+        while (lo < hi) {
+          const int mid = (lo + hi + 1) >> 1;
+          if (tiles_before(x, mid) <= v)
+            lo = mid;
+          else
+            hi = mid - 1;
+        }
+        st.rt = lo, st.j0 = v - static_cast<int>(tiles_before(x, lo)), tiles = tiles_of(x, lo);
+      };
+      // where stretch w begins: inside a short item the nearer of its ends is taken, so that no partials are left for a few tiles
+      auto border = [&](int w) {
+        const int u = static_cast<int>(static_cast<int64_t>(st.U) * w / st.workers);
+        if (w == 0 || w == st.workers) return u;
+        locate(u);
+        return st.j0 == 0 || tiles > PP_SHORT ? u : 2 * st.j0 < tiles ? u - st.j0 : u + tiles - st.j0;
+      };
+      st.u1 = border(blockIdx.x + 1);
+      st.u0 = border(blockIdx.x);
+      if (st.u0 < st.u1) locate(st.u0);
     }
     bars->start = st;
   }
@@ -354,10 +399,11 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     pq::report(p.status, PQ_ERR_TIMEOUT);
   };
 
-  const bool any = start.u1 > start.u0;
+  const bool any = start.u0 < start.u1;
   int lands_issued = 0;  // loader only
 
   if (warp < PP_SOFTMAX_WARPS) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(PP_REGS_SOFTMAX));
     // ================================================================== softmax warps: one thread per query row
     const int i = warp >> 2, row = (warp & 3) * 32 + lane;  // row tile and row inside it
     const int tok_in = i * RT + row / G, g_in = row % G;    // token of the item and query head of the group (rows past RT * G have none)
@@ -366,22 +412,21 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     const uint32_t s_addr = tmem_base + lane_base + i * 128, o_addr = tmem_base + lane_base + 256 + i * 128;
     bool ok = true;
     int n_tiles_done = 0, n_items_done = 0, n_all_items = 0, c = 0, n_shared = 0;  // of this group: tiles, items; of the CTA: items, tiles
-    PpItem x;
-    if (any) x = first_item();
-    for (bool more = any; more && ok; more = next_item(x)) {
-      const bool active = i == 0 || second_tile(x);
-      const int t0 = x.rt * R, tok = min(t0 + tok_in, x.n - 1), head = x.h * G + g_in;
-      if (active) {
-        // Q staging: the warp brings its 32 rows in, two rows (512 contiguous bytes) per load instruction
+    PpItem x, ahead;
+    // Q staging of this group's row tile: the warp brings its 32 rows in, two rows (512 contiguous bytes) per load instruction
+    auto stage_q = [&](const PpItem& y) {
+      if (i == 0 || second_tile(y)) {
         const uint32_t dst = pq::smem_u32(q_buf + i * PP_TILE);
         const int c16 = lane & 15, rw0 = (warp & 3) * 32;
+        const __nv_bfloat16* base = p.q + static_cast<int64_t>(y.row0) * p.ldq + static_cast<int64_t>(y.h) * G * 128 + c16 * 8;
+        int rq = rw0 + (lane >> 4), tq = rq / G, gq = rq % G;
+        const int tq0 = y.rt * R + i * RT, tq_last = min(RT, y.n - tq0) - 1;  // rows that do not exist repeat the last token
         uint4 qv[16];
 #pragma unroll
         for (int it = 0; it < 16; ++it) {
-          const int rq = min(rw0 + it * 2 + (lane >> 4), RT * G - 1);
-          const int tq = min(t0 + i * RT + rq / G, x.n - 1), hq = x.h * G + rq % G;
-          const uint4* src = reinterpret_cast<const uint4*>(p.q + static_cast<int64_t>(x.row0 + tq) * p.ldq + hq * 128) + c16;
-          qv[it] = pq::ld_dep(src);
+          qv[it] = pq::ld_dep(reinterpret_cast<const uint4*>(base + static_cast<int64_t>(tq0 + min(tq, tq_last)) * p.ldq + gq * 128));
+          gq += 2;
+          while (gq >= G) gq -= G, ++tq;
         }
 #pragma unroll
         for (int it = 0; it < 16; ++it) sts128(dst + tile_off(rw0 + it * 2 + (lane >> 4), c16), permute8(qv[it]));
@@ -389,13 +434,21 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
       }
       __syncwarp();
       if (lane == 0) pq::mbar_arrive(&bars->q_ready);
+    };
+    if (any) {
+      x = first_item();
+      stage_q(x);
+    }
+    for (bool more = any; more && ok; x = ahead) {
+      const bool active = i == 0 || second_tile(x);
+      const int t0 = x.rt * R, tok = min(t0 + tok_in, x.n - 1), head = x.h * G + g_in;
       // a group without rows waits for the others' arrivals: two of its own must not meet in one phase
       if (!active && __any_sync(0xffffffffu, !wait(&bars->q_ready, n_all_items & 1))) {
         ok = false;
         break;
       }
       ++n_all_items;
-      const float s_k = DYN ? 1.0f : pq::ld_dep(p.s_k + x.h), s_v = DYN ? 1.0f : fmaxf(pq::ld_dep(p.s_v + x.h), 0x1p-60f);
+      const float s_k = DYN ? 1.0f : fmaxf(pq::ld_dep(p.s_k + x.h), 0x1p-60f), s_v = DYN ? 1.0f : fmaxf(pq::ld_dep(p.s_v + x.h), 0x1p-60f);
       const float scale_ctx = s_k * p.scale2, log2_sv = DYN ? 0.0f : pq::lg2_approx(s_v), inv_sv = DYN ? 1.0f : 1.0f / s_v;
       const int n_ctx = n_ctx_of(x), tile_min_tok = t0 + i * RT;
       float m_ref = -INFINITY, l = 0.0f;
@@ -408,100 +461,101 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
           break;
         }
         pq::tc_fence_after();
-        const int n_chunks = is_pre ? PP_PREFIX / 32 : PP_KEYS / 32;
+        const int n_chunks = (is_pre ? PP_PREFIX : PP_KEYS) / PP_CHUNK;
         const float scale = is_pre ? p.scale2 : scale_ctx, add = is_pre ? 0.0f : log2_sv;
         const int limit = is_pre ? p.n_prefix : min(n_ctx - key0, x.base + tok - key0 + 1);  // columns below it are visible
         const bool need_mask = is_pre ? p.n_prefix < PP_PREFIX : (key0 + PP_KEYS > x.base + tile_min_tok + 1 || key0 + PP_KEYS > n_ctx);
         const PpSteps* st = steps_buf + c % PP_STAGES;
-        auto exponents = [&](const uint32_t(&r)[32], int c0, int e) {  // DYN: of columns e, e + 1 of the chunk
-          const float4 k = st->key[(c0 * 32 + e) >> 1];
-          return __ffma2_rn(make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), make_float2(k.x, k.y), make_float2(k.z, k.w));
-        };
-        // ---- pass 1: the row's largest exponent over the visible keys of this tile. The next 32 columns are requested before the current ones are
-        // worked on (the last request is pass 2's first).
-        uint32_t rr[2][32];
-        float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        pq::tmem_ld_32x32(s_addr, rr[0]);
+        // w = 2^(exponent - m) against the reference so far, fp16, kept in registers until the whole tile has been looked at. Where an exponent is more than
+        // PP_LAZY above the reference (or there is none yet), the reference is moved to a whole number, the sums and O_i are multiplied by the power
+        // of two that makes, and the tile's weights are formed again. The scores stay where they are meanwhile: the weights overwrite them
+        // at the end only. The next columns are requested before the current ones are worked on.
+        const float2 scale2 = make_float2(scale, scale);
+        uint32_t pk[PP_KEYS / 2];
+        float2 l4[4];
+        for (bool again = false;; again = true) {
+          const float m_use = m_ref == -INFINITY ? 0.0f : m_ref;
+          const float off = DYN ? -m_use : add - m_use;
+          const float2 off2 = make_float2(off, off);
+          float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int cc = 0; cc < PP_KEYS / 32; ++cc) {
-          if (cc < n_chunks) {
-            pq::tmem_ld_wait_for(rr[cc & 1]);
-            pq::tmem_ld_32x32(s_addr + (cc + 1 < n_chunks ? (cc + 1) * 32 : 0), rr[(cc + 1) & 1]);
-            const uint32_t(&r)[32] = rr[cc & 1];
-            if (need_mask) {
+          for (int k = 0; k < 4; ++k) l4[k] = make_float2(0.0f, 0.0f);
+          uint32_t rr[2][PP_CHUNK];
+          tmem_ld_chunk(s_addr, rr[0]);
 #pragma unroll
-              for (int e = 0; e < 32; e += 2) {
-                const float2 v = DYN ? exponents(r, cc, e) : make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1]));
-                mx4[(e >> 1) & 3] = max3f(mx4[(e >> 1) & 3], cc * 32 + e < limit ? v.x : -INFINITY, cc * 32 + e + 1 < limit ? v.y : -INFINITY);
+          for (int cc = 0; cc < PP_KEYS / PP_CHUNK; ++cc) {
+            if (cc < n_chunks) {
+              tmem_ld_wait_chunk(rr[cc & 1]);
+              if (cc + 1 < n_chunks) tmem_ld_chunk(s_addr + (cc + 1) * PP_CHUNK, rr[(cc + 1) & 1]);
+              uint32_t(&r)[PP_CHUNK] = rr[cc & 1];
+              float2 ex[PP_CHUNK / 2];
+#pragma unroll
+              for (int e = 0; e < PP_CHUNK; e += 2) {
+                const float2 v = make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1]));
+                if (DYN) {
+                  const float4 k = st->key[(cc * PP_CHUNK + e) >> 1];
+                  ex[e >> 1] = __fadd2_rn(__ffma2_rn(v, make_float2(k.x, k.y), make_float2(k.z, k.w)), off2);
+                } else {
+                  ex[e >> 1] = __ffma2_rn(v, scale2, off2);
+                }
               }
-            } else {
+              if (need_mask) {
 #pragma unroll
-              for (int e = 0; e < 32; e += 2) {
-                const float2 v = DYN ? exponents(r, cc, e) : make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1]));
-                mx4[(e >> 1) & 3] = max3f(mx4[(e >> 1) & 3], v.x, v.y);
+                for (int e = 0; e < PP_CHUNK; e += 2) {
+                  ex[e >> 1].x = cc * PP_CHUNK + e < limit ? ex[e >> 1].x : -INFINITY;
+                  ex[e >> 1].y = cc * PP_CHUNK + e + 1 < limit ? ex[e >> 1].y : -INFINITY;
+                }
+              }
+#pragma unroll
+              for (int e = 0; e < PP_CHUNK; e += 2) {
+                const float2 x2 = ex[e >> 1];
+                top[(e >> 1) & 3] = max3f(top[(e >> 1) & 3], x2.x, x2.y);
+                const float2 w = make_float2(pq::ex2_approx(x2.x), pq::ex2_approx(x2.y));
+                if (DYN)
+                  l4[(e >> 1) & 3] = __ffma2_rn(w, st->inv[(cc * PP_CHUNK + e) >> 1], l4[(e >> 1) & 3]);
+                else
+                  l4[(e >> 1) & 3] = __fadd2_rn(l4[(e >> 1) & 3], w);
+                pk[(cc * PP_CHUNK + e) >> 1] = pq::pack_f16(w.x, w.y);
               }
             }
           }
-        }
-        const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
-        const float mx_s = DYN ? mx : fmaf(mx, scale, add);
-        const bool grow = mx_s > m_ref + PP_LAZY;  // also the first visible key of a row (m_ref = -inf)
-        if (__any_sync(0xffffffffu, grow)) {
-          const float m_new = grow ? mx_s : m_ref;
+          if (again) break;
+          const float most = fmaxf(max3f(top[0], top[1], top[2]), top[3]);
+          const bool grow = most > (m_ref == -INFINITY ? -INFINITY : PP_LAZY);
+          if (!__any_sync(0xffffffffu, grow)) break;
+          const float m_new = grow ? ceilf(m_use + most) : m_ref;
           const float alpha = grow ? pq::ex2_approx(m_ref - m_new) : 1.0f;  // 2^(-inf) = 0 for a row that had seen nothing
           l *= alpha;
           if (jt > x.j0) {  // S_i of this tile is complete, so O_i += P V of the tile before is, too
-            for (int cc = 0; cc < 4; ++cc) {
-              uint32_t r[32];
-              pq::tmem_ld_32x32(o_addr + cc * 32, r);
-              pq::tmem_ld_wait();
+            for (int k = 0; k < 8; ++k) {
+              uint32_t q[16];
+              tmem_ld_32x16(o_addr + k * 16, q);
 #pragma unroll
-              for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * alpha);
-              pq::tmem_st_32x32(o_addr + cc * 32, r);
+              for (int e = 0; e < 16; ++e) q[e] = __float_as_uint(__uint_as_float(q[e]) * alpha);
+              tmem_st_32x16(o_addr + k * 16, q);
             }
           }
           m_ref = m_new;
-        }
-        // ---- pass 2: w = 2^(exponent - m), fp16, written over the first columns of S_i
-        const float m_use = m_ref == -INFINITY ? 0.0f : m_ref;  // such a row has every column masked
-        const float2 scale2 = make_float2(scale, scale), moff2 = DYN ? make_float2(-m_use, -m_use) : make_float2(add - m_use, add - m_use);
-        float2 l4[4] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-#pragma unroll
-        for (int cc = 0; cc < PP_KEYS / 32; ++cc) {  // n_chunks is even: pass 1 left the request for columns 0..31 in rr[0]
-          if (cc < n_chunks) {
-            pq::tmem_ld_wait_for(rr[cc & 1]);
-            if (cc + 1 < n_chunks) pq::tmem_ld_32x32(s_addr + (cc + 1) * 32, rr[(cc + 1) & 1]);
-            const uint32_t(&r)[32] = rr[cc & 1];
-            uint32_t pk[16];
-#pragma unroll
-            for (int e = 0; e < 32; e += 2) {
-              const float2 ex = DYN ? __fadd2_rn(exponents(r, cc, e), moff2)
-                                    : __ffma2_rn(make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), scale2, moff2);
-              float2 w = make_float2(pq::ex2_approx(ex.x), pq::ex2_approx(ex.y));
-              if (need_mask) {
-                w.x = cc * 32 + e < limit ? w.x : 0.0f;
-                w.y = cc * 32 + e + 1 < limit ? w.y : 0.0f;
-              }
-              if (DYN)
-                l4[(e >> 1) & 3] = __ffma2_rn(w, st->inv[(cc * 32 + e) >> 1], l4[(e >> 1) & 3]);
-              else
-                l4[(e >> 1) & 3] = __fadd2_rn(l4[(e >> 1) & 3], w);
-              pk[e >> 1] = pq::pack_f16(w.x, w.y);
-            }
-            tmem_st_32x16(s_addr + cc * 16, pk);
-          }
         }
         {
           const float lt = ((l4[0].x + l4[0].y) + (l4[1].x + l4[1].y)) + ((l4[2].x + l4[2].y) + (l4[3].x + l4[3].y));
           l += DYN || is_pre ? lt : lt * inv_sv;
         }
+#pragma unroll
+        for (int k = 0; k < PP_KEYS / 64; ++k)
+          if (k * 64 < n_chunks * PP_CHUNK) pq::tmem_st_32x32(s_addr + k * 32, reinterpret_cast<const uint32_t(&)[32]>(pk[k * 32]));
         pq::tmem_st_wait();
         pq::tc_fence_before();
         __syncwarp();
         if (lane == 0) pq::mbar_arrive(&bars->p_full[i]);
         ++n_tiles_done;
       }
-      if (ok && active) {
+      if (!ok) break;
+      // the scores of the item are done, its Q tile is free: the next item's queries come in under the last product, its scores under the epilogue
+      ahead = x;
+      more = next_item(ahead);
+      if (more) stage_q(ahead);
+      if (active) {
         if (__any_sync(0xffffffffu, !wait(&bars->o_final[i], n_items_done & 1))) {
           ok = false;
         } else {
@@ -509,32 +563,42 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
           pq::tc_fence_after();
           const bool whole = x.j0 == 0 && x.j1 == x.tiles, live = row_used && t0 + tok_in < x.n;
           const float norm = l > 0.0f ? 1.0f / l : 0.0f;
-          __nv_bfloat16* dst = p.out + (static_cast<int64_t>(x.row0 + tok) * p.Hq + head) * 128;
+          // rows of the output as this lane stores them: piece `lane & 3` (16 bytes) of 64 bytes of the four rows of its quad
+          const int64_t my_row = live ? static_cast<int64_t>(x.row0 + tok) * p.Hq + head : -1;
+          int64_t out_row[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) out_row[k] = __shfl_sync(0xffffffffu, my_row, (lane & ~3) + k);
           const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (x.j0 == 0 ? 1 : 0);
           float4* part = reinterpret_cast<float4*>(p.ws_o + slot * PP_PARTIAL) + i * PP_ROWS + row;  // [dims / 4][256 rows]
           for (int cc = 0; cc < 4; ++cc) {
             uint32_t r[32];
             pq::tmem_ld_32x32(o_addr + cc * 32, r);
-            pq::tmem_ld_wait();
-            if (!live) continue;
+            pq::tmem_ld_wait_for(r);
+            if (whole) {
+              uint4 piece[4];
 #pragma unroll
-            for (int a = 0; a < 4; ++a) {  // columns 8a .. 8a+7 hold dims 0,4,1,5,2,6,3,7 of the group
-              float v[8];
+              for (int a = 0; a < 4; ++a) {  // columns 8a .. 8a+7 hold dims 0,4,1,5,2,6,3,7 of the group
+                float v[8];
 #pragma unroll
-              for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(r[8 * a + e]);
-              if (whole) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] *= norm;
+                for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(r[8 * a + e]) * norm;
                 const __nv_bfloat162 d01 = __floats2bfloat162_rn(v[0], v[2]), d23 = __floats2bfloat162_rn(v[4], v[6]);
                 const __nv_bfloat162 d45 = __floats2bfloat162_rn(v[1], v[3]), d67 = __floats2bfloat162_rn(v[5], v[7]);
-                *reinterpret_cast<uint4*>(dst + cc * 32 + a * 8) =
-                    make_uint4(*reinterpret_cast<const uint32_t*>(&d01), *reinterpret_cast<const uint32_t*>(&d23),
-                               *reinterpret_cast<const uint32_t*>(&d45), *reinterpret_cast<const uint32_t*>(&d67));
-              } else {
-                part[(cc * 8 + a * 2) * 256] = make_float4(v[0], v[2], v[4], v[6]);
-                part[(cc * 8 + a * 2 + 1) * 256] = make_float4(v[1], v[3], v[5], v[7]);
+                piece[a] = make_uint4(*reinterpret_cast<const uint32_t*>(&d01), *reinterpret_cast<const uint32_t*>(&d23), *reinterpret_cast<const uint32_t*>(&d45),
+                                      *reinterpret_cast<const uint32_t*>(&d67));
+              }
+              swap_halves(piece[0], piece[1], lane & 1, 1), swap_halves(piece[2], piece[3], lane & 1, 1);
+              swap_halves(piece[0], piece[2], lane & 2, 2), swap_halves(piece[1], piece[3], lane & 2, 2);
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                if (out_row[k] >= 0) *reinterpret_cast<uint4*>(p.out + out_row[k] * 128 + cc * 32 + (lane & 3) * 8) = piece[k];
+            } else if (live) {
+#pragma unroll
+              for (int a = 0; a < 4; ++a) {
+                part[(cc * 8 + a * 2) * 256] = make_float4(__uint_as_float(r[8 * a]), __uint_as_float(r[8 * a + 2]), __uint_as_float(r[8 * a + 4]), __uint_as_float(r[8 * a + 6]));
+                part[(cc * 8 + a * 2 + 1) * 256] = make_float4(__uint_as_float(r[8 * a + 1]), __uint_as_float(r[8 * a + 3]), __uint_as_float(r[8 * a + 5]), __uint_as_float(r[8 * a + 7]));
               }
             }
+            __syncwarp();
           }
           if (!whole && live) *reinterpret_cast<float2*>(p.ws_ml + (slot * 256 + i * PP_ROWS + row) * 2) = make_float2(m_ref, l);
           pq::tc_fence_before();
@@ -568,26 +632,37 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
         auto slot_of = [&](int w) { return 2 * static_cast<int64_t>(w) + (w == sh.w0 ? 1 : 0); };
         const int my = i * PP_ROWS + row;
         float m = -INFINITY, l = 0.0f;
-        for (int w = sh.w0; w <= sh.w1; ++w) m = fmaxf(m, __ldcg(p.ws_ml + (slot_of(w) * 256 + my) * 2));
-        const float m_use = m == -INFINITY ? 0.0f : m;
-        __nv_bfloat16* dst = p.out + (static_cast<int64_t>(sh.row0 + tok) * p.Hq + sh.h * G + g_in) * 128;
-        for (int w = sh.w0; w <= sh.w1; ++w) {
-          const float2 ml = __ldcg(reinterpret_cast<const float2*>(p.ws_ml) + slot_of(w) * 256 + my);
-          l = fmaf(ml.y, pq::ex2_approx(ml.x - m_use), l);
+        for (int w0 = sh.w0; w0 <= sh.w1; w0 += 4) {  // references and denominators, four requests at a time
+          float2 ml[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            ml[k] = w0 + k <= sh.w1 ? __ldcg(reinterpret_cast<const float2*>(p.ws_ml) + slot_of(w0 + k) * 256 + my) : make_float2(-INFINITY, 0.0f);
+          const float mn = fmaxf(m, fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)));
+          l = m == -INFINITY ? 0.0f : l * pq::ex2_approx(m - mn);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) l = ml[k].x == -INFINITY ? l : fmaf(ml[k].y, pq::ex2_approx(ml[k].x - mn), l);
+          m = mn;
         }
-        const float norm = l > 0.0f ? 1.0f / l : 0.0f;
-        for (int cc = 0; cc < 4; ++cc) {  // 32 dims at a time
+        const float m_use = m == -INFINITY ? 0.0f : m, norm = l > 0.0f ? 1.0f / l : 0.0f;
+        __nv_bfloat16* dst = p.out + (static_cast<int64_t>(sh.row0 + tok) * p.Hq + sh.h * G + g_in) * 128;
+        for (int cc = 0; cc < 4; ++cc) {  // 32 dims at a time, two partials requested together
           float4 acc[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) acc[e] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-          for (int w = sh.w0; w <= sh.w1; ++w) {
-            const int64_t slot = slot_of(w);
-            const float wt = pq::ex2_approx(__ldcg(p.ws_ml + (slot * 256 + my) * 2) - m_use) * norm;
-            const float4* part = reinterpret_cast<const float4*>(p.ws_o + slot * PP_PARTIAL) + cc * 8 * 256 + my;
+          for (int w = sh.w0; w <= sh.w1; w += 2) {
+            const bool two = w < sh.w1;
+            const int64_t sa = slot_of(w), sb = two ? slot_of(w + 1) : sa;
+            const float4 *pa = reinterpret_cast<const float4*>(p.ws_o + sa * PP_PARTIAL) + cc * 8 * 256 + my;
+            const float4 *pb = reinterpret_cast<const float4*>(p.ws_o + sb * PP_PARTIAL) + cc * 8 * 256 + my;
+            const float ma = __ldcg(p.ws_ml + (sa * 256 + my) * 2), mb = __ldcg(p.ws_ml + (sb * 256 + my) * 2);
+            float4 va[8], vb[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) va[e] = __ldcg(pa + e * 256), vb[e] = __ldcg(pb + e * 256);
+            const float fa = ma == -INFINITY ? 0.0f : pq::ex2_approx(ma - m_use) * norm, fb = !two || mb == -INFINITY ? 0.0f : pq::ex2_approx(mb - m_use) * norm;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-              const float4 v = __ldcg(part + e * 256);
-              acc[e].x = fmaf(v.x, wt, acc[e].x), acc[e].y = fmaf(v.y, wt, acc[e].y), acc[e].z = fmaf(v.z, wt, acc[e].z), acc[e].w = fmaf(v.w, wt, acc[e].w);
+              acc[e].x = fmaf(vb[e].x, fb, fmaf(va[e].x, fa, acc[e].x)), acc[e].y = fmaf(vb[e].y, fb, fmaf(va[e].y, fa, acc[e].y));
+              acc[e].z = fmaf(vb[e].z, fb, fmaf(va[e].z, fa, acc[e].z)), acc[e].w = fmaf(vb[e].w, fb, fmaf(va[e].w, fa, acc[e].w));
             }
           }
 #pragma unroll
@@ -602,6 +677,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
       if (threadIdx.x == 0) p.tickets[PP_TICKET0 + sh.w0] = 0;
     }
   } else if (warp < PP_WARP_MMA) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PP_REGS_OTHERS));
     // ================================================================== expansion warps
     const int tid_e = (warp - PP_WARP_EXPAND0) * 32 + lane;
     bool ok = true;
@@ -669,7 +745,9 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
       }
     }
     if (!ok && lane == 0) give_up();
-  } else if (warp == PP_WARP_LOAD) {
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PP_REGS_OTHERS));
+    if (warp == PP_WARP_LOAD) {
     // ================================================================== loader
     // A lane to a copy: lanes 0 .. 7 the pages of the tile (fewer for larger pages); with own steps lanes 8 .. 15 and 16 .. 23 the steps of their keys and
     // values, which go with the rows of V.
@@ -712,7 +790,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
       }
     }
     if (!ok && lane == 0) give_up();
-  } else {
+    } else if (warp == PP_WARP_MMA) {
     // ================================================================== MMA issuer: the whole warp runs the loop, the elected lane issues
     constexpr uint32_t IDESC_S = idesc_16(PP_ROWS, PP_KEYS, true, false), IDESC_S_PRE = idesc_16(PP_ROWS, PP_PREFIX, true, false);
     constexpr uint32_t IDESC_O = idesc_16(PP_ROWS, 128, false, true);
@@ -801,6 +879,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     }
     __syncwarp();
     pq::mbar_wait(&bars->drain, 0);
+    }
   }
 
   pq::tc_fence_before();
