@@ -32,14 +32,15 @@ constexpr int PP_TILE = 2 * PP_HALF;  // a [128][128] tile: dims 0..63, then dim
 constexpr int PP_LAND = PP_KEYS * 64 + 2 * PP_KEYS * 4;  // packed rows of K or V, behind those of V the steps of both
 constexpr int PP_LANDS = 3;           // landing slots: K and V rows of a tile take one each
 constexpr int PP_STAGES = 2;
-constexpr int PP_SOFTMAX_WARPS = 8, PP_EXPAND_WARPS = 4;
+constexpr int PP_SOFTMAX_WARPS = 16, PP_EXPAND_WARPS = 4;  // per row tile two sets of four warps, a set takes half of the key columns
 constexpr int PP_WARP_EXPAND0 = PP_SOFTMAX_WARPS, PP_WARP_MMA = PP_WARP_EXPAND0 + PP_EXPAND_WARPS, PP_WARP_LOAD = PP_WARP_MMA + 1;
-constexpr int PP_THREADS = 512;  // the warps behind the loader only give their registers
-constexpr int PP_TMEM_COLS = 512;     // S0 | S1 | O0 | O1, 128 columns each; P_i lies over the first 64 columns of S_i
+constexpr int PP_THREADS = 768;  // the warps behind the loader only give their registers
+constexpr int PP_TMEM_COLS = 512;     // S0 | S1 | O0 | O1, 128 columns each; each half of P_i lies over the first half of its columns of S_i
 constexpr int PP_SHORT = 8;         // an item of so many key tiles or fewer is not shared between workers
 constexpr float PP_LAZY = 15.0f;      // log2 units an exponent may exceed the reference before it is moved: weights stay inside fp16
-// Registers: 512 threads at 128; the softmax warpgroups take 168, the others leave 88 (256 x 168 + 256 x 88 = 512 x 128).
-constexpr int PP_REGS_SOFTMAX = 168, PP_REGS_OTHERS = 88;
+// Registers: 768 threads at 80; the softmax warpgroups take 96, the others leave 48 (512 x 96 + 256 x 48 = 768 x 80).
+constexpr int PP_REGS_SOFTMAX = 96, PP_REGS_OTHERS = 48;
+constexpr int PP_HALF_KEYS = PP_KEYS / 2;  // key columns of a softmax thread
 constexpr int PP_TICKET0 = PQ_PAGED_TICKET0 + PQ_PAGED_MAX_WORKERS;
 constexpr int PP_PARTIAL = 256 * 128;  // floats of an item's partial output: [dims / 4][row][4]
 
@@ -60,6 +61,7 @@ struct PpBarriers {
   int merge[2];
   PpStart start;
   PpShared shared[2];
+  float row[2][2][PP_ROWS];  // [row tile][set]: what the two threads of a row tell each other
 };
 struct PpSteps {  // of pairs of keys: (key step x scale, of both, log2 of the value step, of both) and (1 / value step, of both)
   float4 key[PP_KEYS / 2];
@@ -256,7 +258,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     }
     for (int i = 0; i < 2; ++i) {
       pq::mbar_init(&bars->s_full[i], 1);
-      pq::mbar_init(&bars->p_full[i], 4);
+      pq::mbar_init(&bars->p_full[i], PP_SOFTMAX_WARPS / 2);
       pq::mbar_init(&bars->o_final[i], 1);
     }
     pq::mbar_init(&bars->q_ready, PP_SOFTMAX_WARPS);
@@ -404,32 +406,45 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
 
   if (warp < PP_SOFTMAX_WARPS) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(PP_REGS_SOFTMAX));
-    // ================================================================== softmax warps: one thread per query row
-    const int i = warp >> 2, row = (warp & 3) * 32 + lane;  // row tile and row inside it
-    const int tok_in = i * RT + row / G, g_in = row % G;    // token of the item and query head of the group (rows past RT * G have none)
+    // ================================================================== softmax warps: two threads per query row, one for each half of the key columns
+    const int i = warp >> 3, set = (warp >> 2) & 1, row = (warp & 3) * 32 + lane;  // row tile, half of the columns, row of the tile
+    const int tok_in = i * RT + row / G, g_in = row % G;  // token of the item and query head of the group (rows past RT * G have none)
     const bool row_used = row < RT * G;
     const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t s_addr = tmem_base + lane_base + i * 128, o_addr = tmem_base + lane_base + 256 + i * 128;
+    const uint32_t s_addr = tmem_base + lane_base + i * 128 + set * PP_HALF_KEYS, o_addr = tmem_base + lane_base + 256 + i * 128 + set * 64;
+    const int pair_bar = 2 + i * 4 + (warp & 3);  // named barrier of the two warps of these rows
+    auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory"); };
+    auto pair_any = [&](bool v) {  // does any of the 64 threads say so
+      uint32_t r;
+      asm volatile(
+          "{\n.reg .pred p, q;\nsetp.ne.u32 p, %2, 0;\nbarrier.cta.red.or.pred q, %1, 64, p;\nselp.u32 %0, 1, 0, q;\n}\n"
+          : "=r"(r)
+          : "r"(pair_bar), "r"(static_cast<uint32_t>(v))
+          : "memory");
+      return r != 0;
+    };
+    float* const mine = &bars->row[i][set][row];
+    const volatile float* const other = &bars->row[i][set ^ 1][row];
     bool ok = true;
     int n_tiles_done = 0, n_items_done = 0, n_all_items = 0, c = 0, n_shared = 0;  // of this group: tiles, items; of the CTA: items, tiles
     PpItem x, ahead;
-    // Q staging of this group's row tile: the warp brings its 32 rows in, two rows (512 contiguous bytes) per load instruction
+    // Q staging of the row tile: the warp brings 16 rows in, two rows (512 contiguous bytes) per load instruction
     auto stage_q = [&](const PpItem& y) {
       if (i == 0 || second_tile(y)) {
         const uint32_t dst = pq::smem_u32(q_buf + i * PP_TILE);
-        const int c16 = lane & 15, rw0 = (warp & 3) * 32;
+        const int c16 = lane & 15, rw0 = (warp & 7) * 16;
         const __nv_bfloat16* base = p.q + static_cast<int64_t>(y.row0) * p.ldq + static_cast<int64_t>(y.h) * G * 128 + c16 * 8;
         int rq = rw0 + (lane >> 4), tq = rq / G, gq = rq % G;
         const int tq0 = y.rt * R + i * RT, tq_last = min(RT, y.n - tq0) - 1;  // rows that do not exist repeat the last token
-        uint4 qv[16];
+        uint4 qv[8];
 #pragma unroll
-        for (int it = 0; it < 16; ++it) {
+        for (int it = 0; it < 8; ++it) {
           qv[it] = pq::ld_dep(reinterpret_cast<const uint4*>(base + static_cast<int64_t>(tq0 + min(tq, tq_last)) * p.ldq + gq * 128));
           gq += 2;
           while (gq >= G) gq -= G, ++tq;
         }
 #pragma unroll
-        for (int it = 0; it < 16; ++it) sts128(dst + tile_off(rw0 + it * 2 + (lane >> 4), c16), permute8(qv[it]));
+        for (int it = 0; it < 8; ++it) sts128(dst + tile_off(rw0 + it * 2 + (lane >> 4), c16), permute8(qv[it]));
         pq::fence_proxy_async_smem();
       }
       __syncwarp();
@@ -461,9 +476,10 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
           break;
         }
         pq::tc_fence_after();
-        const int n_chunks = (is_pre ? PP_PREFIX : PP_KEYS) / PP_CHUNK;
+        const int c0 = set * PP_HALF_KEYS;  // this thread's first column; the prefix tile has columns for the first set only
+        const bool idle = is_pre && set == 1;
         const float scale = is_pre ? p.scale2 : scale_ctx, add = is_pre ? 0.0f : log2_sv;
-        const int limit = is_pre ? p.n_prefix : min(n_ctx - key0, x.base + tok - key0 + 1);  // columns below it are visible
+        const int limit = is_pre ? p.n_prefix : min(n_ctx - key0, x.base + tok - key0 + 1) - c0;  // columns below it are visible
         const bool need_mask = is_pre ? p.n_prefix < PP_PREFIX : (key0 + PP_KEYS > x.base + tile_min_tok + 1 || key0 + PP_KEYS > n_ctx);
         const PpSteps* st = steps_buf + c % PP_STAGES;
         // w = 2^(exponent - m) against the reference so far, fp16, kept in registers until the whole tile has been looked at. Where an exponent is more than
@@ -471,7 +487,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
         // of two that makes, and the tile's weights are formed again. The scores stay where they are meanwhile: the weights overwrite them
         // at the end only. The next columns are requested before the current ones are worked on.
         const float2 scale2 = make_float2(scale, scale);
-        uint32_t pk[PP_KEYS / 2];
+        uint32_t pk[PP_HALF_KEYS / 2];
         float2 l4[4];
         for (bool again = false;; again = true) {
           const float m_use = m_ref == -INFINITY ? 0.0f : m_ref;
@@ -481,19 +497,20 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
 #pragma unroll
           for (int k = 0; k < 4; ++k) l4[k] = make_float2(0.0f, 0.0f);
           uint32_t rr[2][PP_CHUNK];
+          if (!idle) {
           tmem_ld_chunk(s_addr, rr[0]);
 #pragma unroll
-          for (int cc = 0; cc < PP_KEYS / PP_CHUNK; ++cc) {
-            if (cc < n_chunks) {
+          for (int cc = 0; cc < PP_HALF_KEYS / PP_CHUNK; ++cc) {
+            {
               tmem_ld_wait_chunk(rr[cc & 1]);
-              if (cc + 1 < n_chunks) tmem_ld_chunk(s_addr + (cc + 1) * PP_CHUNK, rr[(cc + 1) & 1]);
+              if (cc + 1 < PP_HALF_KEYS / PP_CHUNK) tmem_ld_chunk(s_addr + (cc + 1) * PP_CHUNK, rr[(cc + 1) & 1]);
               uint32_t(&r)[PP_CHUNK] = rr[cc & 1];
               float2 ex[PP_CHUNK / 2];
 #pragma unroll
               for (int e = 0; e < PP_CHUNK; e += 2) {
                 const float2 v = make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1]));
                 if (DYN) {
-                  const float4 k = st->key[(cc * PP_CHUNK + e) >> 1];
+                  const float4 k = st->key[(c0 + cc * PP_CHUNK + e) >> 1];
                   ex[e >> 1] = __fadd2_rn(__ffma2_rn(v, make_float2(k.x, k.y), make_float2(k.z, k.w)), off2);
                 } else {
                   ex[e >> 1] = __ffma2_rn(v, scale2, off2);
@@ -512,22 +529,27 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
                 top[(e >> 1) & 3] = max3f(top[(e >> 1) & 3], x2.x, x2.y);
                 const float2 w = make_float2(pq::ex2_approx(x2.x), pq::ex2_approx(x2.y));
                 if (DYN)
-                  l4[(e >> 1) & 3] = __ffma2_rn(w, st->inv[(cc * PP_CHUNK + e) >> 1], l4[(e >> 1) & 3]);
+                  l4[(e >> 1) & 3] = __ffma2_rn(w, st->inv[(c0 + cc * PP_CHUNK + e) >> 1], l4[(e >> 1) & 3]);
                 else
                   l4[(e >> 1) & 3] = __fadd2_rn(l4[(e >> 1) & 3], w);
                 pk[(cc * PP_CHUNK + e) >> 1] = pq::pack_f16(w.x, w.y);
               }
             }
           }
+          }
           if (again) break;
-          const float most = fmaxf(max3f(top[0], top[1], top[2]), top[3]);
-          const bool grow = most > (m_ref == -INFINITY ? -INFINITY : PP_LAZY);
-          if (!__any_sync(0xffffffffu, grow)) break;
+          float most = fmaxf(max3f(top[0], top[1], top[2]), top[3]);
+          const float bar_at = m_ref == -INFINITY ? -INFINITY : PP_LAZY;
+          if (!pair_any(most > bar_at)) break;
+          *mine = most;  // (the last reader of the exchange before is behind this barrier)
+          pair_sync();
+          most = fmaxf(most, *other);
+          const bool grow = most > bar_at;
           const float m_new = grow ? ceilf(m_use + most) : m_ref;
           const float alpha = grow ? pq::ex2_approx(m_ref - m_new) : 1.0f;  // 2^(-inf) = 0 for a row that had seen nothing
           l *= alpha;
           if (jt > x.j0) {  // S_i of this tile is complete, so O_i += P V of the tile before is, too
-            for (int k = 0; k < 8; ++k) {
+            for (int k = 0; k < 4; ++k) {  // this set's half of the dims
               uint32_t q[16];
               tmem_ld_32x16(o_addr + k * 16, q);
 #pragma unroll
@@ -541,9 +563,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
           const float lt = ((l4[0].x + l4[0].y) + (l4[1].x + l4[1].y)) + ((l4[2].x + l4[2].y) + (l4[3].x + l4[3].y));
           l += DYN || is_pre ? lt : lt * inv_sv;
         }
-#pragma unroll
-        for (int k = 0; k < PP_KEYS / 64; ++k)
-          if (k * 64 < n_chunks * PP_CHUNK) pq::tmem_st_32x32(s_addr + k * 32, reinterpret_cast<const uint32_t(&)[32]>(pk[k * 32]));
+        if (!idle) pq::tmem_st_32x32(s_addr, pk);
         pq::tmem_st_wait();
         pq::tc_fence_before();
         __syncwarp();
@@ -562,6 +582,9 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
           ++n_items_done;
           pq::tc_fence_after();
           const bool whole = x.j0 == 0 && x.j1 == x.tiles, live = row_used && t0 + tok_in < x.n;
+          *mine = l;  // the sums of the two halves of the columns
+          pair_sync();
+          l += *other;
           const float norm = l > 0.0f ? 1.0f / l : 0.0f;
           // rows of the output as this lane stores them: piece `lane & 3` (16 bytes) of 64 bytes of the four rows of its quad
           const int64_t my_row = live ? static_cast<int64_t>(x.row0 + tok) * p.Hq + head : -1;
@@ -570,9 +593,10 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
           for (int k = 0; k < 4; ++k) out_row[k] = __shfl_sync(0xffffffffu, my_row, (lane & ~3) + k);
           const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (x.j0 == 0 ? 1 : 0);
           float4* part = reinterpret_cast<float4*>(p.ws_o + slot * PP_PARTIAL) + i * PP_ROWS + row;  // [dims / 4][256 rows]
-          for (int cc = 0; cc < 4; ++cc) {
+          pair_sync();  // both have read before either writes again
+          for (int cc = 2 * set; cc < 2 * set + 2; ++cc) {  // this set's half of the dims
             uint32_t r[32];
-            pq::tmem_ld_32x32(o_addr + cc * 32, r);
+            pq::tmem_ld_32x32(o_addr + (cc & 1) * 32, r);
             pq::tmem_ld_wait_for(r);
             if (whole) {
               uint4 piece[4];
@@ -600,7 +624,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
             }
             __syncwarp();
           }
-          if (!whole && live) *reinterpret_cast<float2*>(p.ws_ml + (slot * 256 + i * PP_ROWS + row) * 2) = make_float2(m_ref, l);
+          if (!whole && live && set == 0) *reinterpret_cast<float2*>(p.ws_ml + (slot * 256 + i * PP_ROWS + row) * 2) = make_float2(m_ref, l);
           pq::tc_fence_before();
         }
       }
@@ -616,13 +640,13 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     // ---- the last of the workers w0 .. w1 of a shared item to come here merges their partials, in that order
     if (!ok && lane == 0) give_up();
     __threadfence();
-    asm volatile("bar.sync 1, 256;" ::: "memory");
+    asm volatile("bar.sync 1, 512;" ::: "memory");
     if (threadIdx.x < 2) {
       const bool go = !bars->abort_flag && static_cast<int>(threadIdx.x) < n_shared;
       const PpShared sh = bars->shared[threadIdx.x];
       bars->merge[threadIdx.x] = go && atomicAdd(p.tickets + PP_TICKET0 + sh.w0, 1u) == static_cast<uint32_t>(sh.w1 - sh.w0) ? 1 : 0;
     }
-    asm volatile("bar.sync 1, 256;" ::: "memory");
+    asm volatile("bar.sync 1, 512;" ::: "memory");
     __threadfence();
     for (int k = 0; k < 2; ++k) {
       if (!bars->merge[k]) continue;
@@ -645,7 +669,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
         }
         const float m_use = m == -INFINITY ? 0.0f : m, norm = l > 0.0f ? 1.0f / l : 0.0f;
         __nv_bfloat16* dst = p.out + (static_cast<int64_t>(sh.row0 + tok) * p.Hq + sh.h * G + g_in) * 128;
-        for (int cc = 0; cc < 4; ++cc) {  // 32 dims at a time, two partials requested together
+        for (int cc = 2 * set; cc < 2 * set + 2; ++cc) {  // 32 dims at a time, two partials requested together
           float4 acc[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) acc[e] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -820,7 +844,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
         mma_ts(o_tm, p_tm + kk * 8, v_desc + kk * (2048 >> 4), IDESC_O, (!first || kk > 0) ? 1u : 0u);
       if (!is_pre)
 #pragma unroll
-        for (int kk = PP_PREFIX / 16; kk < PP_KEYS / 16; ++kk) mma_ts(o_tm, p_tm + kk * 8, v_desc + kk * (2048 >> 4), IDESC_O, 1u);
+        for (int kk = PP_PREFIX / 16; kk < PP_KEYS / 16; ++kk) mma_ts(o_tm, p_tm + PP_HALF_KEYS / 2 + kk * 8, v_desc + kk * (2048 >> 4), IDESC_O, 1u);
     };
     bool ok = true;
     int c = 0, n_items = 0, n_p[2] = {0, 0};
