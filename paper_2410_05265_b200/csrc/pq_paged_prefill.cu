@@ -19,6 +19,7 @@
 // Inside every group of eight head dims the expansion leaves the order 0,4,1,5,2,6,3,7; Q and the prefix rows are stored in the same order and the output
 // columns are put back when they are written. Every wait is bounded.
 #include <atomic>
+#include <type_traits>
 
 #include "pq_paged_attn.cuh"
 
@@ -26,7 +27,7 @@ namespace {
 
 constexpr int PP_ROWS = 128;          // query rows per tile (MMA M)
 constexpr int PP_KEYS = 128;          // keys per tile
-constexpr int PP_PREFIX = 64;         // key rows of the prefix tile
+constexpr int PP_PREFIX = 64;         // most key rows of the prefix tile
 constexpr int PP_HALF = 128 * 128;    // bytes of one half tile: 128 rows x 64 two-byte values (128 bytes, swizzled)
 constexpr int PP_TILE = 2 * PP_HALF;  // a [128][128] tile: dims 0..63, then dims 64..127
 constexpr int PP_LAND = PP_KEYS * 64 + 2 * PP_KEYS * 4;  // packed rows of K or V, behind those of V the steps of both
@@ -36,6 +37,7 @@ constexpr int PP_SOFTMAX_WARPS = 16, PP_EXPAND_WARPS = 4;  // per row tile two s
 constexpr int PP_WARP_EXPAND0 = PP_SOFTMAX_WARPS, PP_WARP_MMA = PP_WARP_EXPAND0 + PP_EXPAND_WARPS, PP_WARP_LOAD = PP_WARP_MMA + 1;
 constexpr int PP_THREADS = 768;  // the warps behind the loader only give their registers
 constexpr int PP_TMEM_COLS = 512;     // S0 | S1 | O0 | O1, 128 columns each; each half of P_i lies over the first half of its columns of S_i
+constexpr int PP_ITEM_UNITS = 4;    // units of work that an item costs besides its key tiles (queries, prefix, output: 9 us; a tile 2.4)
 constexpr int PP_SHORT = 8;         // an item of so many key tiles or fewer is not shared between workers
 constexpr float PP_LAZY = 15.0f;      // log2 units an exponent may exceed the reference before it is moved: weights stay inside fp16
 // Registers: 768 threads at 80; the softmax warpgroups take 96, the others leave 48 (512 x 96 + 256 x 48 = 768 x 80).
@@ -227,7 +229,7 @@ struct PpItem {
   int n, len, row0;     // of the sequence: new rows, cached keys, first row
   int base;             // cached keys before the new rows: len - n
   int tiles, j0, j1;    // key tiles of the item (the prefix first), and this worker's
-  int u;                // unit of j0
+  int u;                // unit where this worker's share begins (an item is PP_ITEM_UNITS units and its tiles)
 };
 
 template <bool DYN>
@@ -242,7 +244,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
 
   const int warp = pq::warp_index(), lane = threadIdx.x & 31;
   const int G = p.G, RT = PP_ROWS / G, R = 2 * RT;     // tokens of a row tile and of an item
-  const int has_prefix = p.n_prefix > 0 ? 1 : 0;
+  const int has_prefix = p.n_prefix > 0 ? 1 : 0, pre_cols = p.n_prefix <= 16 ? 16 : PP_PREFIX;  // key rows of the prefix tile
   volatile int* abort_flag = &bars->abort_flag;
 
   if (threadIdx.x == 0) {
@@ -286,8 +288,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
   };
   // key tiles of row tile rt; an item with fewer cached keys than rows counts the tiles as if the keys began at zero
   auto tiles_of = [&](const PpItem& x, int rt) { return has_prefix + (max(x.base, 0) + min(x.n, (rt + 1) * R) + PP_KEYS - 1) / PP_KEYS; };
-  auto tiles_before = [&](const PpItem& x, int rt) {  // of the row tiles 0 .. rt - 1, all of them full
-    return static_cast<int64_t>(rt) * has_prefix + (rt > 0 ? floor_sum(rt, PP_KEYS, R, static_cast<int64_t>(max(x.base, 0)) + R + PP_KEYS - 1) : 0);
+  auto units_before = [&](const PpItem& x, int rt) {  // of the row tiles 0 .. rt - 1, all of them full
+    return static_cast<int64_t>(rt) * (has_prefix + PP_ITEM_UNITS) + (rt > 0 ? floor_sum(rt, PP_KEYS, R, static_cast<int64_t>(max(x.base, 0)) + R + PP_KEYS - 1) : 0);
   };
   auto row_tiles = [&](const PpItem& x) { return (x.n + R - 1) / R; };
   int32_t* scan = reinterpret_cast<int32_t*>(kv_buf);
@@ -300,7 +302,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     int64_t t = 0;
     if (x.n > 0) {
       const int nt = row_tiles(x);
-      t = tiles_before(x, nt - 1) + tiles_of(x, nt - 1);
+      t = units_before(x, nt - 1) + PP_ITEM_UNITS + tiles_of(x, nt - 1);
     }
     if (odd || t * p.Hkv > 0x7fffffffll) {
       pq::report(p.status, PQ_ERR_SHAPE);
@@ -315,9 +317,9 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     const bool too_many = total > 0x7fffffffll;
     if (too_many) pq::report(p.status, PQ_ERR_SHAPE);
     st.U = too_many ? 0 : static_cast<int>(total);
-    st.workers = min(static_cast<int>(gridDim.x), max(1, st.U / 2));  // two tiles at least
+    st.workers = min(static_cast<int>(gridDim.x), max(1, st.U / (PP_ITEM_UNITS + 1)));  // as much as an item of one tile at least
     if (st.U > 0 && static_cast<int>(blockIdx.x) < st.workers) {
-      int tiles = 0;
+      int tiles = 0, at = 0;  // of the item: key tiles, and the unit's place in it (an item's own units come before its tiles)
       auto locate = [&](int u) {  // unit u into (b, h, rt, j0) and the tiles of its item
         PpItem x;
         x.b = pq::find_segment(scan, p.B, u / p.Hkv);
@@ -326,22 +328,24 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
         const int per_head = scan[x.b + 1] - scan[x.b], rel = u - scan[x.b] * p.Hkv;
         st.b = x.b, st.h = rel / per_head;
         const int v = rel - st.h * per_head;
-        int lo = 0, hi = row_tiles(x) - 1;  // last row tile with tiles_before <= v
+        int lo = 0, hi = row_tiles(x) - 1;  // last row tile with units_before <= v
         while (lo < hi) {
           const int mid = (lo + hi + 1) >> 1;
-          if (tiles_before(x, mid) <= v)
+          if (units_before(x, mid) <= v)
             lo = mid;
           else
             hi = mid - 1;
         }
-        st.rt = lo, st.j0 = v - static_cast<int>(tiles_before(x, lo)), tiles = tiles_of(x, lo);
+        at = v - static_cast<int>(units_before(x, lo)), tiles = tiles_of(x, lo);
+        st.rt = lo, st.j0 = max(0, at - PP_ITEM_UNITS);
       };
-      // where stretch w begins: inside a short item the nearer of its ends is taken, so that no partials are left for a few tiles
+      // where stretch w begins: inside a short item, or among an item's own units, an end of the item is taken, so that no partials are left for a few tiles
       auto border = [&](int w) {
         const int u = static_cast<int>(static_cast<int64_t>(st.U) * w / st.workers);
         if (w == 0 || w == st.workers) return u;
         locate(u);
-        return st.j0 == 0 || tiles > PP_SHORT ? u : 2 * st.j0 < tiles ? u - st.j0 : u + tiles - st.j0;
+        if (st.j0 == 0) return u - at;
+        return tiles > PP_SHORT ? u : 2 * st.j0 < tiles ? u - at : u + tiles - st.j0;
       };
       st.u1 = border(blockIdx.x + 1);
       st.u0 = border(blockIdx.x);
@@ -361,11 +365,11 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     bool odd;
     load_seq(x, odd);
     x.tiles = tiles_of(x, x.rt), x.j0 = start.j0, x.u = start.u0;
-    x.j1 = min(x.tiles, x.j0 + (start.u1 - start.u0));
+    x.j1 = min(x.tiles, x.j0 + (start.u1 - x.u) - (x.j0 == 0 ? PP_ITEM_UNITS : 0));
     return x;
   };
   auto next_item = [&](PpItem& x) {  // false at the end of the stretch
-    x.u += x.j1 - x.j0;
+    x.u += x.j1 - x.j0 + (x.j0 == 0 ? PP_ITEM_UNITS : 0);
     if (x.u >= start.u1) return false;
     if (++x.rt == row_tiles(x)) {
       x.rt = 0;
@@ -379,7 +383,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
       }
     }
     x.tiles = tiles_of(x, x.rt), x.j0 = 0;
-    x.j1 = min(x.tiles, start.u1 - x.u);
+    x.j1 = min(x.tiles, start.u1 - x.u - PP_ITEM_UNITS);
     return true;
   };
   auto n_ctx_of = [&](const PpItem& x) { return min(x.len, max(x.base, 0) + min(x.n, (x.rt + 1) * R)); };  // cached keys a row of the item may see
@@ -429,7 +433,9 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     int n_tiles_done = 0, n_items_done = 0, n_all_items = 0, c = 0, n_shared = 0;  // of this group: tiles, items; of the CTA: items, tiles
     PpItem x, ahead;
     // Q staging of the row tile: the warp brings 16 rows in, two rows (512 contiguous bytes) per load instruction
+    float next_s_k = 1.0f, next_s_v = 1.0f;
     auto stage_q = [&](const PpItem& y) {
+      if (!DYN) next_s_k = fmaxf(pq::ld_dep(p.s_k + y.h), 0x1p-60f), next_s_v = fmaxf(pq::ld_dep(p.s_v + y.h), 0x1p-60f);
       if (i == 0 || second_tile(y)) {
         const uint32_t dst = pq::smem_u32(q_buf + i * PP_TILE);
         const int c16 = lane & 15, rw0 = (warp & 7) * 16;
@@ -463,7 +469,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
         break;
       }
       ++n_all_items;
-      const float s_k = DYN ? 1.0f : fmaxf(pq::ld_dep(p.s_k + x.h), 0x1p-60f), s_v = DYN ? 1.0f : fmaxf(pq::ld_dep(p.s_v + x.h), 0x1p-60f);
+      const float s_k = next_s_k, s_v = next_s_v;
       const float scale_ctx = s_k * p.scale2, log2_sv = DYN ? 0.0f : pq::lg2_approx(s_v), inv_sv = DYN ? 1.0f : 1.0f / s_v;
       const int n_ctx = n_ctx_of(x), tile_min_tok = t0 + i * RT;
       float m_ref = -INFINITY, l = 0.0f;
@@ -480,7 +486,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
         const bool idle = is_pre && set == 1;
         const float scale = is_pre ? p.scale2 : scale_ctx, add = is_pre ? 0.0f : log2_sv;
         const int limit = is_pre ? p.n_prefix : min(n_ctx - key0, x.base + tok - key0 + 1) - c0;  // columns below it are visible
-        const bool need_mask = is_pre ? p.n_prefix < PP_PREFIX : (key0 + PP_KEYS > x.base + tile_min_tok + 1 || key0 + PP_KEYS > n_ctx);
+        const bool need_mask = is_pre ? p.n_prefix < pre_cols : (key0 + PP_KEYS > x.base + tile_min_tok + 1 || key0 + PP_KEYS > n_ctx);
         const PpSteps* st = steps_buf + c % PP_STAGES;
         // w = 2^(exponent - m) against the reference so far, fp16, kept in registers until the whole tile has been looked at. Where an exponent is more than
         // PP_LAZY above the reference (or there is none yet), the reference is moved to a whole number, the sums and O_i are multiplied by the power
@@ -496,14 +502,14 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
           float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
           for (int k = 0; k < 4; ++k) l4[k] = make_float2(0.0f, 0.0f);
+          auto form = [&](auto chunks) {  // the weights of so many times sixteen columns
           uint32_t rr[2][PP_CHUNK];
-          if (!idle) {
           tmem_ld_chunk(s_addr, rr[0]);
 #pragma unroll
-          for (int cc = 0; cc < PP_HALF_KEYS / PP_CHUNK; ++cc) {
+          for (int cc = 0; cc < chunks.value; ++cc) {
             {
               tmem_ld_wait_chunk(rr[cc & 1]);
-              if (cc + 1 < PP_HALF_KEYS / PP_CHUNK) tmem_ld_chunk(s_addr + (cc + 1) * PP_CHUNK, rr[(cc + 1) & 1]);
+              if (cc + 1 < chunks.value) tmem_ld_chunk(s_addr + (cc + 1) * PP_CHUNK, rr[(cc + 1) & 1]);
               uint32_t(&r)[PP_CHUNK] = rr[cc & 1];
               float2 ex[PP_CHUNK / 2];
 #pragma unroll
@@ -536,6 +542,11 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
               }
             }
           }
+          };
+          if (is_pre && pre_cols == PP_CHUNK) {
+            if (!idle) form(std::integral_constant<int, 1>());
+          } else if (!idle) {
+            form(std::integral_constant<int, PP_HALF_KEYS / PP_CHUNK>());
           }
           if (again) break;
           float most = fmaxf(max3f(top[0], top[1], top[2]), top[3]);
@@ -630,7 +641,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
       }
       if (x.j0 != 0 || x.j1 != x.tiles) {
         if (threadIdx.x == 0) {
-          const int u = x.u - x.j0;
+          const int u = x.j0 == 0 ? x.u + PP_ITEM_UNITS : x.u - x.j0;  // of the item's first tile
           auto worker_of = [&](int unit) { return static_cast<int>(((static_cast<int64_t>(unit) + 1) * start.workers - 1) / start.U); };
           bars->shared[n_shared & 1] = PpShared{worker_of(u), worker_of(u + x.tiles - 1), x.b, x.h, x.rt, x.row0, x.n};
         }
@@ -726,7 +737,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
           const uint32_t tile = kv ? v_tile : k_tile;
           if (is_pre) {
             // full-precision rows (reordered inside groups of eight dims); rows past n_prefix are zero
-            for (int unit = tid_e; unit < PP_PREFIX * 16; unit += PP_EXPAND_WARPS * 32) {
+            for (int unit = tid_e; unit < pre_cols * 16; unit += PP_EXPAND_WARPS * 32) {
               const int r = unit >> 4, c16 = unit & 15;
               uint4 v = make_uint4(0, 0, 0, 0);
               if (r < p.n_prefix)
@@ -816,7 +827,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     if (!ok && lane == 0) give_up();
     } else if (warp == PP_WARP_MMA) {
     // ================================================================== MMA issuer: the whole warp runs the loop, the elected lane issues
-    constexpr uint32_t IDESC_S = idesc_16(PP_ROWS, PP_KEYS, true, false), IDESC_S_PRE = idesc_16(PP_ROWS, PP_PREFIX, true, false);
+    constexpr uint32_t IDESC_S = idesc_16(PP_ROWS, PP_KEYS, true, false);
+    const uint32_t IDESC_S_PRE = idesc_16(PP_ROWS, pre_cols, true, false);
     constexpr uint32_t IDESC_O = idesc_16(PP_ROWS, 128, false, true);
     const bool leader = pq::elect_one();
     const uint64_t q_desc0 = desc_sw128(pq::smem_u32(q_buf), 16), k_desc0 = desc_sw128(pq::smem_u32(kv_buf), 16);
@@ -841,7 +853,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
       const uint64_t v_desc = v_desc0 + (c % PP_STAGES) * (2 * PP_TILE >> 4);
 #pragma unroll
       for (int kk = 0; kk < PP_PREFIX / 16; ++kk)  // 16 keys per instruction
-        mma_ts(o_tm, p_tm + kk * 8, v_desc + kk * (2048 >> 4), IDESC_O, (!first || kk > 0) ? 1u : 0u);
+        if (!is_pre || kk * 16 < pre_cols) mma_ts(o_tm, p_tm + kk * 8, v_desc + kk * (2048 >> 4), IDESC_O, (!first || kk > 0) ? 1u : 0u);
       if (!is_pre)
 #pragma unroll
         for (int kk = PP_PREFIX / 16; kk < PP_KEYS / 16; ++kk) mma_ts(o_tm, p_tm + PP_HALF_KEYS / 2 + kk * 8, v_desc + kk * (2048 >> 4), IDESC_O, 1u);
