@@ -56,7 +56,7 @@ struct PpBarriers {
   uint64_t land_full[PP_LANDS], land_empty[PP_LANDS];
   uint64_t k_full[PP_STAGES], k_empty[PP_STAGES], v_full[PP_STAGES], v_empty[PP_STAGES];
   uint64_t s_full[2], p_full[2], o_final[2];
-  uint64_t q_ready, drain;
+  uint64_t q_ready[2], drain;
   int64_t part[PP_THREADS / 32];
   uint32_t tmem_base;
   volatile int abort_flag;
@@ -262,8 +262,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
       pq::mbar_init(&bars->s_full[i], 1);
       pq::mbar_init(&bars->p_full[i], PP_SOFTMAX_WARPS / 2);
       pq::mbar_init(&bars->o_final[i], 1);
+      pq::mbar_init(&bars->q_ready[i], PP_SOFTMAX_WARPS / 2);
     }
-    pq::mbar_init(&bars->q_ready, PP_SOFTMAX_WARPS);
     pq::mbar_init(&bars->drain, 1);
     bars->abort_flag = 0;
     pq::mbar_fence_init();
@@ -430,13 +430,14 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     float* const mine = &bars->row[i][set][row];
     const volatile float* const other = &bars->row[i][set ^ 1][row];
     bool ok = true;
-    int n_tiles_done = 0, n_items_done = 0, n_all_items = 0, c = 0, n_shared = 0;  // of this group: tiles, items; of the CTA: items, tiles
+    int n_tiles_done = 0, n_items_done = 0, c = 0, n_shared = 0;  // of this group: tiles, items; of the CTA: tiles
     PpItem x, ahead;
     // Q staging of the row tile: the warp brings 16 rows in, two rows (512 contiguous bytes) per load instruction
     float next_s_k = 1.0f, next_s_v = 1.0f;
     auto stage_q = [&](const PpItem& y) {
       if (!DYN) next_s_k = fmaxf(pq::ld_dep(p.s_k + y.h), 0x1p-60f), next_s_v = fmaxf(pq::ld_dep(p.s_v + y.h), 0x1p-60f);
-      if (i == 0 || second_tile(y)) {
+      if (i == 1 && !second_tile(y)) return;
+      {
         const uint32_t dst = pq::smem_u32(q_buf + i * PP_TILE);
         const int c16 = lane & 15, rw0 = (warp & 7) * 16;
         const __nv_bfloat16* base = p.q + static_cast<int64_t>(y.row0) * p.ldq + static_cast<int64_t>(y.h) * G * 128 + c16 * 8;
@@ -454,7 +455,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
         pq::fence_proxy_async_smem();
       }
       __syncwarp();
-      if (lane == 0) pq::mbar_arrive(&bars->q_ready);
+      if (lane == 0) pq::mbar_arrive(&bars->q_ready[i]);
     };
     if (any) {
       x = first_item();
@@ -463,12 +464,6 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     for (bool more = any; more && ok; x = ahead) {
       const bool active = i == 0 || second_tile(x);
       const int t0 = x.rt * R, tok = min(t0 + tok_in, x.n - 1), head = x.h * G + g_in;
-      // a group without rows waits for the others' arrivals: two of its own must not meet in one phase
-      if (!active && __any_sync(0xffffffffu, !wait(&bars->q_ready, n_all_items & 1))) {
-        ok = false;
-        break;
-      }
-      ++n_all_items;
       const float s_k = next_s_k, s_v = next_s_v;
       const float scale_ctx = s_k * p.scale2, log2_sv = DYN ? 0.0f : pq::lg2_approx(s_v), inv_sv = DYN ? 1.0f : 1.0f / s_v;
       const int n_ctx = n_ctx_of(x), tile_min_tok = t0 + i * RT;
@@ -859,22 +854,25 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
         for (int kk = PP_PREFIX / 16; kk < PP_KEYS / 16; ++kk) mma_ts(o_tm, p_tm + PP_HALF_KEYS / 2 + kk * 8, v_desc + kk * (2048 >> 4), IDESC_O, 1u);
     };
     bool ok = true;
-    int c = 0, n_items = 0, n_p[2] = {0, 0};
+    int c = 0, n_q[2] = {0, 0}, n_p[2] = {0, 0};
     PpItem x;
     if (any) x = first_item();
-    for (bool more = any; more && ok; more = next_item(x), ++n_items) {
+    for (bool more = any; more && ok; more = next_item(x)) {
       const int groups = second_tile(x) ? 2 : 1;
-      if (!wait_warp(&bars->q_ready, n_items & 1) || !wait_warp(&bars->k_full[c % PP_STAGES], (c / PP_STAGES) & 1)) {
-        ok = false;
-        break;
+      ok = wait_warp(&bars->k_full[c % PP_STAGES], (c / PP_STAGES) & 1);
+      for (int i = 0; i < groups && ok; ++i) {
+        if (!wait_warp(&bars->q_ready[i], n_q[i] & 1)) {
+          ok = false;
+          break;
+        }
+        ++n_q[i];
+        pq::tc_fence_after();
+        if (leader) {
+          issue_s(i, c, has_prefix && x.j0 == 0);
+          if (i == groups - 1) pq::mma_commit(&bars->k_empty[c % PP_STAGES]);
+        }
+        __syncwarp();
       }
-      pq::tc_fence_after();
-      if (leader) {
-        const bool is_pre = has_prefix && x.j0 == 0;
-        for (int i = 0; i < groups; ++i) issue_s(i, c, is_pre);
-        pq::mma_commit(&bars->k_empty[c % PP_STAGES]);
-      }
-      __syncwarp();
       for (int jt = x.j0; jt < x.j1 && ok; ++jt, ++c) {
         const bool is_pre = has_prefix && jt == 0, last = jt + 1 == x.j1;
 #pragma unroll
