@@ -31,9 +31,10 @@ constexpr int PP_PREFIX = 64;         // most key rows of the prefix tile
 constexpr int PP_HALF = 128 * 128;    // bytes of one half tile: 128 rows x 64 two-byte values (128 bytes, swizzled)
 constexpr int PP_TILE = 2 * PP_HALF;  // a [128][128] tile: dims 0..63, then dims 64..127
 constexpr int PP_LAND = PP_KEYS * 64 + 2 * PP_KEYS * 4;  // packed rows of K or V, behind those of V the steps of both
-constexpr int PP_LANDS = 3;           // landing slots: K and V rows of a tile take one each
+constexpr int PP_LANDS = 3;           // landing slots: K and V rows of a tile take one each, in turn
 constexpr int PP_STAGES = 2;
-constexpr int PP_SOFTMAX_WARPS = 16, PP_EXPAND_WARPS = 4;  // per row tile two sets of four warps, a set takes half of the key columns
+constexpr int PP_SOFTMAX_WARPS = 16;  // per row tile two sets of four warps, a set takes half of the key columns
+constexpr int PP_EXPAND_WARPS = 4;
 constexpr int PP_WARP_EXPAND0 = PP_SOFTMAX_WARPS, PP_WARP_MMA = PP_WARP_EXPAND0 + PP_EXPAND_WARPS, PP_WARP_LOAD = PP_WARP_MMA + 1;
 constexpr int PP_THREADS = 768;  // the warps behind the loader only give their registers
 constexpr int PP_TMEM_COLS = 512;     // S0 | S1 | O0 | O1, 128 columns each; each half of P_i lies over the first half of its columns of S_i
@@ -709,69 +710,78 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
   } else if (warp < PP_WARP_MMA) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PP_REGS_OTHERS));
     // ================================================================== expansion warps
-    const int tid_e = (warp - PP_WARP_EXPAND0) * 32 + lane;
+    const int tid_e = threadIdx.x & (PP_EXPAND_WARPS * 32 - 1);
+    // A thread takes 16 packed bytes of a row at a time, 32 dims: four 16-byte chunks. Threads of the upper 64 dims begin with their third chunk, so that
+    // the lanes of a store meet in no bank.
+    const int part = tid_e & 3, turn = part & 2;
     bool ok = true;
-    int c = 0, lc = 0;  // tiles and landing slots so far
+    int c = 0, lc = 0;  // tile of the CTA, landing slot
     PpItem x;
     if (any) x = first_item();
     for (bool more = any; more && ok; more = next_item(x)) {
       const int n_ctx = n_ctx_of(x);
       for (int jt = x.j0; jt < x.j1 && ok; ++jt, ++c) {
         const int stage = c % PP_STAGES;
-        const uint32_t ph = (c / PP_STAGES) & 1;
         const bool is_pre = has_prefix && jt == 0;
-        const uint32_t k_tile = pq::smem_u32(kv_buf + stage * 2 * PP_TILE), v_tile = k_tile + PP_TILE;
 #pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-          const int slot = lc % PP_LANDS;
-          if (!is_pre && __any_sync(0xffffffffu, !wait(&bars->land_full[slot], (lc / PP_LANDS) & 1))) ok = false;
-          if (!ok || __any_sync(0xffffffffu, !wait(kv ? &bars->v_empty[stage] : &bars->k_empty[stage], ph ^ 1))) {
-            ok = false;
-            break;
-          }
-          const uint32_t tile = kv ? v_tile : k_tile;
-          if (is_pre) {
-            // full-precision rows (reordered inside groups of eight dims); rows past n_prefix are zero
-            for (int unit = tid_e; unit < pre_cols * 16; unit += PP_EXPAND_WARPS * 32) {
-              const int r = unit >> 4, c16 = unit & 15;
-              uint4 v = make_uint4(0, 0, 0, 0);
-              if (r < p.n_prefix)
-                v = permute8(pq::ld_dep(reinterpret_cast<const uint4*>((kv ? p.prefix_v : p.prefix_k) + (static_cast<int64_t>(x.h) * p.n_prefix + r) * 128 + c16 * 8)));
-              if (kv) {
-                sts128(tile + tile_off(r, c16), v);
-              } else {  // two bf16 terms: rows 0 .. 63 and 64 .. 127
-                sts128(tile + tile_off(r, c16), make_uint4(bf16_term(v.x, false), bf16_term(v.y, false), bf16_term(v.z, false), bf16_term(v.w, false)));
-                sts128(tile + tile_off(PP_PREFIX + r, c16), make_uint4(bf16_term(v.x, true), bf16_term(v.y, true), bf16_term(v.z, true), bf16_term(v.w, true)));
-              }
-            }
-          } else {
-            const uint32_t src = pq::smem_u32(land + slot * PP_LAND);
-#pragma unroll 2
-            for (int it = 0; it < PP_KEYS * 4 / (PP_EXPAND_WARPS * 32); ++it) {  // 128 keys x 4 chunks of 16 packed bytes
-              const int unit = it * (PP_EXPAND_WARPS * 32) + tid_e, r = unit >> 2, part = unit & 3;  // 32 dims: chunks 4 part .. +3
-              const uint4 w4 = pq::lds128(src + unit * 16);
-              const uint32_t ww[4] = {w4.x, w4.y, w4.z, w4.w};
-#pragma unroll
-              for (int w = 0; w < 4; ++w) sts128(tile + tile_off(r, 4 * part + w), kv ? expand8_f16(ww[w]) : expand8_bf16(ww[w]));
-            }
-          }
-          if (DYN && kv) {  // thread j: key j of the tile. A key that no row sees adds nothing.
-            const float* st = reinterpret_cast<const float*>(land + slot * PP_LAND + PP_KEYS * 64);
-            const int key = (jt - has_prefix) * PP_KEYS + tid_e;
-            const bool in = !is_pre && key < n_ctx;
-            const float k_step = in ? st[tid_e] : 1.0f, v_step = in ? st[PP_KEYS + tid_e] : 1.0f;
-            float* key_out = reinterpret_cast<float*>(&steps_buf[stage].key[tid_e >> 1]) + (tid_e & 1);
-            key_out[0] = k_step * p.scale2, key_out[2] = pq::lg2_approx(v_step);
-            reinterpret_cast<float*>(steps_buf[stage].inv)[tid_e] = pq::rcp_approx(v_step);
-          }
-          pq::fence_proxy_async_smem();  // generic-proxy writes -> visible to the tensor core's async proxy
-          __syncwarp();
-          if (lane == 0) {
-            pq::mbar_arrive(kv ? &bars->v_full[stage] : &bars->k_full[stage]);
-            if (!is_pre) pq::mbar_arrive(&bars->land_empty[slot]);
-          }
-          if (!is_pre) ++lc;
+       for (int kv = 0; kv < 2; ++kv) {  // keys, then values
+        const int slot = lc % PP_LANDS;
+        uint64_t *const full = kv ? bars->v_full : bars->k_full, *const empty = kv ? bars->v_empty : bars->k_empty;
+        const uint32_t tile = pq::smem_u32(kv_buf + stage * 2 * PP_TILE + kv * PP_TILE);
+        if ((!is_pre && __any_sync(0xffffffffu, !wait(&bars->land_full[slot], (lc / PP_LANDS) & 1))) ||
+            __any_sync(0xffffffffu, !wait(&empty[stage], ((c / PP_STAGES) & 1) ^ 1))) {
+          ok = false;
+          break;
         }
+        if (is_pre) {
+          // full-precision rows (reordered inside groups of eight dims); rows past n_prefix are zero
+          for (int unit = tid_e; unit < pre_cols * 16; unit += PP_EXPAND_WARPS * 32) {
+            const int r = unit >> 4, c16 = unit & 15;
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (r < p.n_prefix)
+              v = permute8(pq::ld_dep(reinterpret_cast<const uint4*>((kv ? p.prefix_v : p.prefix_k) + (static_cast<int64_t>(x.h) * p.n_prefix + r) * 128 + c16 * 8)));
+            if (kv) {
+              sts128(tile + tile_off(r, c16), v);
+            } else {  // two bf16 terms: rows 0 .. and rows 64 ..
+              sts128(tile + tile_off(r, c16), make_uint4(bf16_term(v.x, false), bf16_term(v.y, false), bf16_term(v.z, false), bf16_term(v.w, false)));
+              sts128(tile + tile_off(PP_PREFIX + r, c16), make_uint4(bf16_term(v.x, true), bf16_term(v.y, true), bf16_term(v.z, true), bf16_term(v.w, true)));
+            }
+          }
+        } else {
+          const uint32_t src = pq::smem_u32(land + slot * PP_LAND) + tid_e * 16;
+          uint4 w4[PP_KEYS * 4 / (PP_EXPAND_WARPS * 32)];
+#pragma unroll
+          for (int it = 0; it < PP_KEYS / PP_EXPAND_WARPS / 8; ++it) w4[it] = pq::lds128(src + it * (PP_EXPAND_WARPS * 32 * 16));
+#pragma unroll
+          for (int it = 0; it < PP_KEYS / PP_EXPAND_WARPS / 8; ++it) {
+            const int r = it * (PP_EXPAND_WARPS * 8) + (tid_e >> 2);
+            const uint32_t ww[4] = {turn ? w4[it].z : w4[it].x, turn ? w4[it].w : w4[it].y, turn ? w4[it].x : w4[it].z, turn ? w4[it].y : w4[it].w};
+            if (kv) {
+#pragma unroll
+              for (int w = 0; w < 4; ++w) sts128(tile + tile_off(r, 4 * part + (w ^ turn)), expand8_f16(ww[w]));
+            } else {
+#pragma unroll
+              for (int w = 0; w < 4; ++w) sts128(tile + tile_off(r, 4 * part + (w ^ turn)), expand8_bf16(ww[w]));
+            }
+          }
+        }
+        if (DYN && kv) {  // thread j: key j of the tile. A key that no row sees adds nothing.
+          const float* st = reinterpret_cast<const float*>(land + slot * PP_LAND + PP_KEYS * 64);
+          const int key = (jt - has_prefix) * PP_KEYS + tid_e;
+          const bool in = !is_pre && key < n_ctx;
+          const float k_step = in ? st[tid_e] : 1.0f, v_step = in ? st[PP_KEYS + tid_e] : 1.0f;
+          float* key_out = reinterpret_cast<float*>(&steps_buf[stage].key[tid_e >> 1]) + (tid_e & 1);
+          key_out[0] = k_step * p.scale2, key_out[2] = pq::lg2_approx(v_step);
+          reinterpret_cast<float*>(steps_buf[stage].inv)[tid_e] = pq::rcp_approx(v_step);
+        }
+        pq::fence_proxy_async_smem();  // generic-proxy writes -> visible to the tensor core's async proxy
+        __syncwarp();
+        if (lane == 0) {
+          pq::mbar_arrive(&full[stage]);
+          if (!is_pre) pq::mbar_arrive(&bars->land_empty[slot]);
+        }
+        if (!is_pre) ++lc;
+       }
       }
     }
     if (!ok && lane == 0) give_up();
