@@ -7,7 +7,7 @@
 extern "C" size_t pq_attn_kv4_paged_workspace_bytes(const pq_ctx* ctx, const pq_kv4_paged* cache, int64_t n_rows, int32_t max_new) {
   if (!ctx || pq_check_paged(cache) != PQ_OK || n_rows <= 0 || max_new <= 0) return 0;
   const size_t one = pq_paged_decode_ws_bytes(ctx, cache), more = max_new > 1 ? pq_paged_prefill_ws_bytes(ctx) : 0;
-  return one > more ? one : more;  // the launches follow each other
+  return one + more;  // the two kernels overlap
 }
 
 extern "C" pq_status pq_attn_kv4_paged(pq_ctx* ctx, const pq_kv4_paged* c, const void* q, int64_t ldq, const int32_t* q_begin, int64_t n_rows,
@@ -33,5 +33,5 @@ extern "C" pq_status pq_attn_kv4_paged(pq_ctx* ctx, const pq_kv4_paged* c, const
   const int64_t bound = max_len > 0 && max_len < capacity ? max_len : capacity;
   st = pq_paged_decode_launch(ctx, c, p, bound, ws, static_cast<cudaStream_t>(stream));
   if (st != PQ_OK || max_new == 1) return st;
-  return pq_paged_prefill_launch(ctx, p, ws, static_cast<cudaStream_t>(stream));
+  return pq_paged_prefill_launch(ctx, p, static_cast<uint8_t*>(ws) + pq_paged_decode_ws_bytes(ctx, c), static_cast<cudaStream_t>(stream));
 }

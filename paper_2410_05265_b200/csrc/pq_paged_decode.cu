@@ -108,7 +108,10 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int G = p.G, page_log2 = p.page_log2;
   pq::pdl_wait();
-  pq::pdl_trigger();
+  if (p.max_new > 1)  // the kernel for several rows follows, which only needs what this wait waited for
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  else
+    pq::pdl_trigger();
   if (lane == 0) {
     for (int s = 0; s < DP_SLOTS; ++s) pq::mbar_init(&full[warp][s], 1);
     pq::mbar_fence_init();

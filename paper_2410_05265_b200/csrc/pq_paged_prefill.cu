@@ -48,7 +48,7 @@ constexpr int PP_TICKET0 = PQ_PAGED_TICKET0 + PQ_PAGED_MAX_WORKERS;
 constexpr int PP_PARTIAL = 256 * 128;  // floats of an item's partial output: [dims / 4][row][4]
 
 struct PpStart {  // where a worker's stretch begins
-  int b, h, rt, j0, u0, u1, U, workers;
+  int b, h, rt, j0, u0, u1, U, workers;  // (u1 comes by itself)
 };
 struct PpShared {  // an item that several workers share
   int w0, w1, b, h, rt, row0, n;
@@ -210,24 +210,33 @@ __device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r
       : "memory");
 }
 
-// sum_{i=0}^{n-1} floor((a i + b) / m) for a, b >= 0, m > 0, by the Euclidean reduction of the lattice points under a line.
-__device__ int64_t floor_sum(int64_t n, int64_t m, int64_t a, int64_t b) {
-  int64_t s = 0;
+// sum_{i=0}^{n-1} floor((a i + b) / 128) for a, b >= 0, by the Euclidean reduction of the lattice points under a line (the first step is by shifts).
+__device__ int64_t floor_sum_128(int64_t n, int64_t a, int64_t b) {
+  int64_t s = (a >> 7) * (n * (n - 1) / 2) + (b >> 7) * n;
+  a &= 127, b &= 127;
+  int64_t top = a * n + b;
+  if (top < 128) return s;
+  n = top >> 7;
+  uint32_t m32 = static_cast<uint32_t>(a), a32 = 128, b32 = static_cast<uint32_t>(top & 127);  // all below 2^8 from here on
   for (;;) {
-    s += (a / m) * (n * (n - 1) / 2) + (b / m) * n;
-    a %= m, b %= m;
-    const int64_t top = a * n + b;
-    if (top < m) return s;
-    n = top / m, b = top % m;
-    const int64_t t = m;
-    m = a, a = t;
+    s += static_cast<int64_t>(a32 / m32) * (n * (n - 1) / 2) + static_cast<int64_t>(b32 / m32) * n;
+    a32 %= m32, b32 %= m32;
+    top = a32 * n + b32;
+    if (top < m32) return s;
+    if (top < (1ll << 32)) {
+      n = static_cast<uint32_t>(top) / m32, b32 = static_cast<uint32_t>(top) % m32;
+    } else {
+      n = top / m32, b32 = static_cast<uint32_t>(top % m32);
+    }
+    const uint32_t t = m32;
+    m32 = a32, a32 = t;
   }
 }
 
 // The stretch of a worker as the roles walk it, item by item.
 struct PpItem {
   int b, h, rt;         // sequence, KV head, row tile pair
-  int n, len, row0;     // of the sequence: new rows, cached keys, first row
+  int n, len, row0, nt; // of the sequence: new rows, cached keys, first row, row tile pairs
   int base;             // cached keys before the new rows: len - n
   int tiles, j0, j1;    // key tiles of the item (the prefix first), and this worker's
   int u;                // unit where this worker's share begins (an item is PP_ITEM_UNITS units and its tiles)
@@ -273,8 +282,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     pq::tmem_alloc(&bars->tmem_base, PP_TMEM_COLS);
     pq::tmem_relinquish();
   }
-  pq::pdl_wait();
-  pq::pdl_trigger();
+  // No wait here: this kernel always follows the one for single tokens, which lets it start behind its own wait for what came before, and the two have
+  // nothing in common but what both read. The wait is this kernel's last step, so that it ends no earlier than the other.
 
   // ---- the sequences: number of key tiles of all row tiles of one KV head, prefix sums, and where this worker's stretch begins
   const int64_t capacity = static_cast<int64_t>(p.max_pages) << p.page_log2;
@@ -286,13 +295,13 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     odd = n > p.max_new || n < 0 || (n > 0 && (r0 < 0 || r1 > p.n_rows || l != x.len));
     x.n = n >= 2 && n <= p.max_new && r0 >= 0 && r1 <= p.n_rows ? static_cast<int>(n) : 0;
     x.base = x.len - x.n;
+    x.nt = (x.n + R - 1) / R;
   };
   // key tiles of row tile rt; an item with fewer cached keys than rows counts the tiles as if the keys began at zero
   auto tiles_of = [&](const PpItem& x, int rt) { return has_prefix + (max(x.base, 0) + min(x.n, (rt + 1) * R) + PP_KEYS - 1) / PP_KEYS; };
   auto units_before = [&](const PpItem& x, int rt) {  // of the row tiles 0 .. rt - 1, all of them full
-    return static_cast<int64_t>(rt) * (has_prefix + PP_ITEM_UNITS) + (rt > 0 ? floor_sum(rt, PP_KEYS, R, static_cast<int64_t>(max(x.base, 0)) + R + PP_KEYS - 1) : 0);
+    return static_cast<int64_t>(rt) * (has_prefix + PP_ITEM_UNITS) + (rt > 0 ? floor_sum_128(rt, R, static_cast<int64_t>(max(x.base, 0)) + R + PP_KEYS - 1) : 0);
   };
-  auto row_tiles = [&](const PpItem& x) { return (x.n + R - 1) / R; };
   int32_t* scan = reinterpret_cast<int32_t*>(kv_buf);
   __syncthreads();
   for (int b = threadIdx.x; b < p.B; b += PP_THREADS) {
@@ -302,8 +311,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     load_seq(x, odd);
     int64_t t = 0;
     if (x.n > 0) {
-      const int nt = row_tiles(x);
-      t = units_before(x, nt - 1) + PP_ITEM_UNITS + tiles_of(x, nt - 1);
+      t = units_before(x, x.nt - 1) + PP_ITEM_UNITS + tiles_of(x, x.nt - 1);
     }
     if (odd || t * p.Hkv > 0x7fffffffll) {
       pq::report(p.status, PQ_ERR_SHAPE);
@@ -313,15 +321,15 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
   }
   __syncthreads();
   const int64_t total = pq::block_scan<PP_THREADS>(scan, p.B, bars->part) * p.Hkv;
-  if (threadIdx.x == 0) {
-    PpStart st{};
+  if (warp < 2) {  // the two borders of this CTA's stretch, a warp each
     const bool too_many = total > 0x7fffffffll;
-    if (too_many) pq::report(p.status, PQ_ERR_SHAPE);
+    if (too_many && threadIdx.x == 0) pq::report(p.status, PQ_ERR_SHAPE);
+    PpStart st{};
     st.U = too_many ? 0 : static_cast<int>(total);
     st.workers = min(static_cast<int>(gridDim.x), max(1, st.U / (PP_ITEM_UNITS + 1)));  // as much as an item of one tile at least
     if (st.U > 0 && static_cast<int>(blockIdx.x) < st.workers) {
       int tiles = 0, at = 0;  // of the item: key tiles, and the unit's place in it (an item's own units come before its tiles)
-      auto locate = [&](int u) {  // unit u into (b, h, rt, j0) and the tiles of its item
+      auto locate = [&](int u) {  // unit u into (b, h, rt, j0) and the tiles of its item; 32 row tiles are looked at at a time
         PpItem x;
         x.b = pq::find_segment(scan, p.B, u / p.Hkv);
         bool odd;
@@ -329,13 +337,12 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
         const int per_head = scan[x.b + 1] - scan[x.b], rel = u - scan[x.b] * p.Hkv;
         st.b = x.b, st.h = rel / per_head;
         const int v = rel - st.h * per_head;
-        int lo = 0, hi = row_tiles(x) - 1;  // last row tile with units_before <= v
-        while (lo < hi) {
-          const int mid = (lo + hi + 1) >> 1;
-          if (units_before(x, mid) <= v)
-            lo = mid;
-          else
-            hi = mid - 1;
+        int lo = 0, hi = x.nt;  // the item lies in [lo, hi)
+        while (hi - lo > 1) {
+          const int step = (hi - lo + 31) >> 5, mine = lo + lane * step;
+          const uint32_t below = __ballot_sync(0xffffffffu, mine < hi && units_before(x, mine) <= v);  // lanes 0 .. k: ascending, and lane 0 always
+          lo += (31 - __clz(below)) * step;
+          hi = min(hi, lo + step);
         }
         at = v - static_cast<int>(units_before(x, lo)), tiles = tiles_of(x, lo);
         st.rt = lo, st.j0 = max(0, at - PP_ITEM_UNITS);
@@ -343,21 +350,34 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
       // where stretch w begins: inside a short item, or among an item's own units, an end of the item is taken, so that no partials are left for a few tiles
       auto border = [&](int w) {
         const int u = static_cast<int>(static_cast<int64_t>(st.U) * w / st.workers);
-        if (w == 0 || w == st.workers) return u;
+        if (w == st.workers) return u;
         locate(u);
-        if (st.j0 == 0) return u - at;
-        return tiles > PP_SHORT ? u : 2 * st.j0 < tiles ? u - at : u + tiles - st.j0;
+        int to = u;
+        if (st.j0 == 0)
+          to = u - at;
+        else if (tiles <= PP_SHORT)
+          to = 2 * st.j0 < tiles ? u - at : u + tiles - st.j0;
+        if (to > u && to < st.U) locate(to);
+        if (to < u) st.j0 = 0;
+        return to;
       };
-      st.u1 = border(blockIdx.x + 1);
-      st.u0 = border(blockIdx.x);
-      if (st.u0 < st.u1) locate(st.u0);
+      const int u = border(blockIdx.x + warp);
+      if (lane == 0) {
+        if (warp == 0)
+          bars->start = st, bars->start.u0 = u;
+        else
+          bars->part[0] = u;
+      }
+    } else if (lane == 0) {
+      if (warp == 0) bars->start = st;
+      if (warp == 1) bars->part[0] = 0;
     }
-    bars->start = st;
   }
   pq::tc_fence_before();
   __syncthreads();
   pq::tc_fence_after();
-  const PpStart start = bars->start;
+  PpStart start = bars->start;
+  start.u1 = static_cast<int>(bars->part[0]);
   const uint32_t tmem_base = __shfl_sync(0xffffffffu, bars->tmem_base, 0);
 
   auto first_item = [&]() {
@@ -372,7 +392,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
   auto next_item = [&](PpItem& x) {  // false at the end of the stretch
     x.u += x.j1 - x.j0 + (x.j0 == 0 ? PP_ITEM_UNITS : 0);
     if (x.u >= start.u1) return false;
-    if (++x.rt == row_tiles(x)) {
+    if (++x.rt == x.nt) {
       x.rt = 0;
       if (++x.h == p.Hkv) {
         x.h = 0;
@@ -466,6 +486,11 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
       const bool active = i == 0 || second_tile(x);
       const int t0 = x.rt * R, tok = min(t0 + tok_in, x.n - 1), head = x.h * G + g_in;
       const float s_k = next_s_k, s_v = next_s_v;
+      if (x.rt + 1 < x.nt) {  // the queries of the sequence's next row tiles into L2: a thread 128 bytes of them
+        const int t_next = t0 + R + (threadIdx.x >> 1) / G, g_next = (threadIdx.x >> 1) % G;
+        if (threadIdx.x < 2 * R * G && t_next < x.n)
+          asm volatile("prefetch.global.L2 [%0];" ::"l"(p.q + static_cast<int64_t>(x.row0 + t_next) * p.ldq + (x.h * G + g_next) * 128 + (threadIdx.x & 1) * 64));
+      }
       const float scale_ctx = s_k * p.scale2, log2_sv = DYN ? 0.0f : pq::lg2_approx(s_v), inv_sv = DYN ? 1.0f : 1.0f / s_v;
       const int n_ctx = n_ctx_of(x), tile_min_tok = t0 + i * RT;
       float m_ref = -INFINITY, l = 0.0f;
@@ -937,6 +962,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     pq::tc_fence_after();
     pq::tmem_dealloc(tmem_base, PP_TMEM_COLS);
   }
+  pq::pdl_wait();
 }
 
 }  // namespace
