@@ -7,6 +7,7 @@ torch; there is no CPU fallback: without the compiled library every call fails.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 from ctypes import POINTER, Structure, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_void_p
@@ -177,6 +178,11 @@ def _ok(status: int, where: str):
 def _row_stride(t: torch.Tensor) -> int:
     """Elements between the rows of t; of a single row, whose stride says nothing, its own width."""
     return t.stride(0) if t.shape[0] > 1 else math.prod(t.shape[1:])
+
+
+@functools.lru_cache(maxsize=64)
+def _sections(sections: tuple):
+    return (c_int32 * len(sections))(*sections)  # the library reads it during the call
 
 
 def _dev(t: torch.Tensor, dtype, name: str):
@@ -674,10 +680,12 @@ class Context:
 
     def _here(self, *tensors):
         """The tensors of a call live on the context's device, which is the current one: its stream is the one that is used."""
-        current = torch._C._cuda_getDevice()
+        here = self.device
+        if torch._C._cuda_getDevice() != here:
+            raise ValueError(f"cuda:{torch._C._cuda_getDevice()} is current in a call to a context of cuda:{here}")
         for t in tensors:
-            if t is not None and (t.device.index != self.device or current != self.device):
-                raise ValueError(f"a tensor on {t.device} with cuda:{current} current in a context of cuda:{self.device}")
+            if t is not None and t.get_device() != here:  # (t.device.index takes five times as long)
+                raise ValueError(f"a tensor on {t.device} in a call to a context of cuda:{here}")
 
     @staticmethod
     def _rope_args(N, gq, gk, pos, sections):
@@ -692,7 +700,8 @@ class Context:
         assert pos.shape[-1] == N and (N <= 1 or pos.stride(-1) == 1)
         if sections is not None:
             assert len(sections) == axes
-        return axes, pos.stride(0) if pos.dim() == 2 else N, (c_int32 * axes)(*sections) if sections is not None else None
+            sections = _sections(tuple(sections))
+        return axes, N if axes == 1 else pos.stride(0), sections
 
     def qk_norm_rope(self, x: torch.Tensor, Hq: int, gq, gk, eps: float, pos: torch.Tensor, theta: float, sections=None, rotate: bool = False,
                      out: torch.Tensor | None = None):
