@@ -64,6 +64,7 @@ struct PpBarriers {
   int merge[2];
   PpStart start;
   PpShared shared[2];
+  uint32_t pair_out[2][4];   // [row tile][rows / 32]: a warp of these rows has given up
   float row[2][2][PP_ROWS];  // [row tile][set]: what the two threads of a row tell each other
 };
 struct PpSteps {  // of pairs of keys: (key step x scale, of both, log2 of the value step, of both) and (1 / value step, of both)
@@ -276,6 +277,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     }
     pq::mbar_init(&bars->drain, 1);
     bars->abort_flag = 0;
+    for (int k = 0; k < 8; ++k) bars->pair_out[k >> 2][k & 3] = 0;
     pq::mbar_fence_init();
   }
   if (warp == PP_WARP_MMA) {
@@ -451,6 +453,14 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     float* const mine = &bars->row[i][set][row];
     const volatile float* const other = &bars->row[i][set ^ 1][row];
     bool ok = true;
+    // A warp whose wait ran out still comes to the next barrier that the other warp of its rows may be at, and has left word before: named barriers have no
+    // bound of their own. Both have passed the same barriers, so that the next one is the same for both.
+    volatile uint32_t* const pair_out = &bars->pair_out[i][warp & 3];
+    auto leave = [&]() {
+      if (lane == 0) *pair_out = 1;
+      __syncwarp();
+      ok = false;
+    };
     int n_tiles_done = 0, n_items_done = 0, c = 0, n_shared = 0;  // of this group: tiles, items; of the CTA: tiles
     PpItem x, ahead;
     // Q staging of the row tile: the warp brings 16 rows in, two rows (512 contiguous bytes) per load instruction
@@ -499,7 +509,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
         const bool is_pre = has_prefix && jt == 0;
         const int key0 = (jt - has_prefix) * PP_KEYS;
         if (__any_sync(0xffffffffu, !wait(&bars->s_full[i], n_tiles_done & 1) || (DYN && !wait(&bars->v_full[c % PP_STAGES], (c / PP_STAGES) & 1)))) {
-          ok = false;
+          leave();
+          pair_any(true);  // the other warp of the rows comes to its vote and learns of it there
           break;
         }
         pq::tc_fence_after();
@@ -573,6 +584,10 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
           float most = fmaxf(max3f(top[0], top[1], top[2]), top[3]);
           const float bar_at = m_ref == -INFINITY ? -INFINITY : PP_LAZY;
           if (!pair_any(most > bar_at)) break;
+          if (*pair_out) {
+            ok = false;
+            break;
+          }
           *mine = most;  // (the last reader of the exchange before is behind this barrier)
           pair_sync();
           most = fmaxf(most, *other);
@@ -591,6 +606,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
           }
           m_ref = m_new;
         }
+        if (!ok) break;
         {
           const float lt = ((l4[0].x + l4[0].y) + (l4[1].x + l4[1].y)) + ((l4[2].x + l4[2].y) + (l4[3].x + l4[3].y));
           l += DYN || is_pre ? lt : lt * inv_sv;
@@ -609,13 +625,18 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
       if (more) stage_q(ahead);
       if (active) {
         if (__any_sync(0xffffffffu, !wait(&bars->o_final[i], n_items_done & 1))) {
-          ok = false;
+          leave();
+          pair_sync();
         } else {
           ++n_items_done;
           pq::tc_fence_after();
           const bool whole = x.j0 == 0 && x.j1 == x.tiles, live = row_used && t0 + tok_in < x.n;
           *mine = l;  // the sums of the two halves of the columns
           pair_sync();
+          if (*pair_out) {
+            ok = false;
+            break;
+          }
           l += *other;
           const float norm = l > 0.0f ? 1.0f / l : 0.0f;
           // rows of the output as this lane stores them: piece `lane & 3` (16 bytes) of 64 bytes of the four rows of its quad
