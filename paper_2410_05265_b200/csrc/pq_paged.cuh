@@ -12,8 +12,8 @@ static inline bool pq_misaligned16(const void* p) { return (reinterpret_cast<uin
 static inline int pq_page_log2(int page) { return page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : 7; }
 
 static inline pq_status pq_check_pages(const pq_pages* c) {
-  if (!c || !c->table || !c->len || !c->free_list || !c->n_free) return PQ_ERR_INVALID_ARG;
-  if (c->B < 0 || c->max_pages < 0 || c->n_pages < 0) return PQ_ERR_INVALID_ARG;
+  if (!c || !c->n_free || c->B < 0 || c->max_pages < 0 || c->n_pages < 0) return PQ_ERR_INVALID_ARG;
+  if ((c->B > 0 && (!c->len || (c->max_pages > 0 && !c->table))) || (c->n_pages > 0 && !c->free_list)) return PQ_ERR_INVALID_ARG;  // (an empty array has no address)
   if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return PQ_ERR_SHAPE;
   if (c->B > PQ_PAGED_MAX_SEQS || static_cast<int64_t>(c->max_pages) * c->page > 0x7fffffffll) return PQ_ERR_SHAPE;
   return PQ_OK;
@@ -23,7 +23,7 @@ static inline pq_status pq_check_paged(const pq_kv4_paged* c) {
   if (!c) return PQ_ERR_INVALID_ARG;
   const pq_status st = pq_check_pages(&c->pages);
   if (st != PQ_OK) return st;
-  if (!c->codes || (!c->steps && (!c->s_k || !c->s_v))) return PQ_ERR_INVALID_ARG;
+  if ((!c->codes && c->pages.n_pages > 0) || (!c->steps && (!c->s_k || !c->s_v))) return PQ_ERR_INVALID_ARG;
   if (c->Hq <= 0 || c->Hkv <= 0 || c->n_prefix < 0 || (c->n_prefix > 0 && (!c->prefix_k || !c->prefix_v))) return PQ_ERR_INVALID_ARG;
   if (c->D != 128 || c->Hq % c->Hkv != 0 || c->Hq / c->Hkv > PQ_PAGED_MAX_GROUP || c->n_prefix > PQ_PAGED_MAX_PREFIX || c->Hkv > 4096)
     return PQ_ERR_SHAPE;

@@ -178,9 +178,10 @@ PlanParams base_params(pq_ctx* ctx, const pq_pages* c) {
 
 extern "C" pq_status pq_page_plan(pq_ctx* ctx, const pq_pages* pages, const int32_t* n_new, int32_t pos0, int64_t n_rows, int32_t* q_begin,
                                   int64_t* slot, int32_t* pos, int32_t* len_out, int32_t* n_free_out, void* stream) {
-  if (!ctx || !n_new || !q_begin || !len_out || !n_free_out || n_rows < 0 || pos0 < 0 || (n_rows > 0 && (!slot || !pos))) return PQ_ERR_INVALID_ARG;
+  if (!ctx || !q_begin || !n_free_out || n_rows < 0 || pos0 < 0 || (n_rows > 0 && (!slot || !pos))) return PQ_ERR_INVALID_ARG;
   const pq_status st = pq_check_pages(pages);
   if (st != PQ_OK) return st;
+  if (pages->B > 0 && (!n_new || !len_out)) return PQ_ERR_INVALID_ARG;
   if (n_rows > 0x7fffffffll) return PQ_ERR_SHAPE;
   if (static_cast<int64_t>(pages->max_pages) * pages->page + pos0 > 0x7fffffffll) return PQ_ERR_SHAPE;  // a position would not fit
   if (pq_misaligned16(slot) || pq_misaligned16(pos)) return PQ_ERR_ALIGN;
@@ -190,9 +191,10 @@ extern "C" pq_status pq_page_plan(pq_ctx* ctx, const pq_pages* pages, const int3
 }
 
 extern "C" pq_status pq_page_release(pq_ctx* ctx, const pq_pages* pages, const int32_t* done, int32_t* len_out, int32_t* n_free_out, void* stream) {
-  if (!ctx || !done || !len_out || !n_free_out) return PQ_ERR_INVALID_ARG;
+  if (!ctx || !n_free_out) return PQ_ERR_INVALID_ARG;
   const pq_status st = pq_check_pages(pages);
   if (st != PQ_OK) return st;
+  if (pages->B > 0 && (!done || !len_out)) return PQ_ERR_INVALID_ARG;
   PlanParams p = base_params(ctx, pages);
   p.n_new = done, p.len_out = len_out, p.n_free_out = n_free_out;
   return launch(page_release_kernel, p, pages->n_pages, (2 * static_cast<size_t>(p.B) + 1) * sizeof(int32_t), static_cast<cudaStream_t>(stream));
