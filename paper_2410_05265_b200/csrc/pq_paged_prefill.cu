@@ -171,26 +171,38 @@ __device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_
       "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-constexpr int PP_CHUNK = 16;  // score columns a softmax thread requests at a time
-__device__ __forceinline__ void tmem_ld_chunk(uint32_t taddr, uint32_t (&r)[16]) {
+constexpr int PP_CHUNK = 16;  // score columns of a step of the softmax
+// 16 rows x 16 columns as a matrix fragment: lane 4g + t gets columns 8n + 2t, 8n + 2t + 1 of row g (r[4n], r[4n + 1]) and of row g + 8 (r[4n + 2], r[4n + 3]).
+__device__ __forceinline__ void tmem_ld_frag(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
+}
+// The wait with the loaded registers as operands: every use of r stays behind it.
+__device__ __forceinline__ void tmem_ld_wait_frag(uint32_t (&r)[8]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7])
+               :
+               : "memory");
+}
+// 16 rows x 32 words, the counterpart: lane 4g + t has word 4n + t of row g (r[2n]) and of row g + 8 (r[2n + 1]).
+__device__ __forceinline__ void tmem_st_frag(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      "tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_ld_32x16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
+      "tcgen05.wait::ld.sync.aligned;"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
         "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(taddr)
       : "memory");
-}
-// The wait with the loaded registers as operands: every use of r stays behind it.
-__device__ __forceinline__ void tmem_ld_wait_chunk(uint32_t (&r)[16]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
-                 "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
-               :
-               : "memory");
-}
-__device__ __forceinline__ void tmem_ld_32x16(uint32_t taddr, uint32_t (&r)[16]) {
-  tmem_ld_chunk(taddr, r);
-  tmem_ld_wait_chunk(r);
 }
 // Exchanges between lanes l and l ^ m: the lane with the bit clear keeps a and receives the other's a as b, the other keeps b and receives b as a.
 __device__ __forceinline__ void swap_halves(uint4& a, uint4& b, bool bit, int m) {
@@ -246,7 +258,7 @@ struct PpItem {
 template <bool DYN>
 __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const PagedAttnParams p) {
   extern __shared__ uint8_t pp_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(pp_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* smem = pp_raw + (-pq::smem_u32(pp_raw) & 1023u);  // (through an integer the compiler would lose sight of shared memory and use generic loads)
   uint8_t* q_buf = smem;                               // two Q tiles
   uint8_t* kv_buf = q_buf + 2 * PP_TILE;               // stage s: K tile, then V tile
   uint8_t* land = kv_buf + PP_STAGES * 2 * PP_TILE;    // packed rows of K or V
@@ -452,6 +464,20 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     };
     float* const mine = &bars->row[i][set][row];
     const volatile float* const other = &bars->row[i][set ^ 1][row];
+    // While weights are formed a thread has the columns 2t, 2t + 1 of every eight of its set, of four rows: fr + 8k. What it needs per key is then read for four
+    // rows at once.
+    const int fg = lane >> 2, ft = lane & 3, fr = (warp & 3) * 32 + fg;
+    uint32_t tok4 = 0;  // tokens of the four rows, a byte each
+    for (int k = 0; k < 4; ++k) tok4 |= static_cast<uint32_t>(i * RT + (fr + 8 * k) / G) << (8 * k);
+    auto of_lane = [&](const float (&v)[4]) {  // of the row of this lane, where the four lanes of a quad hold the same for their rows
+      float r = 0.0f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float x = __shfl_sync(0xffffffffu, v[k], (lane & 7) * 4);
+        if (lane >> 3 == k) r = x;
+      }
+      return r;
+    };
     bool ok = true;
     // A warp whose wait ran out still comes to the next barrier that the other warp of its rows may be at, and has left word before: named barriers have no
     // bound of their own. Both have passed the same barriers, so that the next one is the same for both.
@@ -503,7 +529,9 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
       }
       const float scale_ctx = s_k * p.scale2, log2_sv = DYN ? 0.0f : pq::lg2_approx(s_v), inv_sv = DYN ? 1.0f : 1.0f / s_v;
       const int n_ctx = n_ctx_of(x), tile_min_tok = t0 + i * RT;
-      float m_ref = -INFINITY, l = 0.0f;
+      float m_ref[4], l[4];  // l: of this thread's columns
+#pragma unroll
+      for (int k = 0; k < 4; ++k) m_ref[k] = -INFINITY, l[k] = 0.0f;
       for (int jt = x.j0; jt < x.j1; ++jt, ++c) {
         if (!active) continue;
         const bool is_pre = has_prefix && jt == 0;
@@ -517,7 +545,6 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
         const int c0 = set * PP_HALF_KEYS;  // this thread's first column; the prefix tile has columns for the first set only
         const bool idle = is_pre && set == 1;
         const float scale = is_pre ? p.scale2 : scale_ctx, add = is_pre ? 0.0f : log2_sv;
-        const int limit = is_pre ? p.n_prefix : min(n_ctx - key0, x.base + tok - key0 + 1) - c0;  // columns below it are visible
         const bool need_mask = is_pre ? p.n_prefix < pre_cols : (key0 + PP_KEYS > x.base + tile_min_tok + 1 || key0 + PP_KEYS > n_ctx);
         const PpSteps* st = steps_buf + c % PP_STAGES;
         // w = 2^(exponent - m) against the reference so far, fp16, kept in registers until the whole tile has been looked at. Where an exponent is more than
@@ -525,55 +552,77 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
         // of two that makes, and the tile's weights are formed again. The scores stay where they are meanwhile: the weights overwrite them
         // at the end only. The next columns are requested before the current ones are worked on.
         const float2 scale2 = make_float2(scale, scale);
-        uint32_t pk[PP_HALF_KEYS / 2];
-        float2 l4[4];
+        uint32_t pk[2][16];  // the weights as they are stored: rows fr, fr + 8, then rows fr + 16, fr + 24
+        float2 l2[4];
         for (bool again = false;; again = true) {
-          const float m_use = m_ref == -INFINITY ? 0.0f : m_ref;
-          const float off = DYN ? -m_use : add - m_use;
-          const float2 off2 = make_float2(off, off);
-          float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          float off[4], top[4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) l4[k] = make_float2(0.0f, 0.0f);
+          for (int k = 0; k < 4; ++k) {
+            const float m_use = m_ref[k] == -INFINITY ? 0.0f : m_ref[k];
+            off[k] = DYN ? -m_use : add - m_use, top[k] = -INFINITY, l2[k] = make_float2(0.0f, 0.0f);
+          }
           auto form = [&](auto chunks) {  // the weights of so many times sixteen columns
-          uint32_t rr[2][PP_CHUNK];
-          tmem_ld_chunk(s_addr, rr[0]);
+            uint32_t rr[2][8];
+            tmem_ld_frag(s_addr, rr[0]);
 #pragma unroll
-          for (int cc = 0; cc < chunks.value; ++cc) {
-            {
-              tmem_ld_wait_chunk(rr[cc & 1]);
-              if (cc + 1 < chunks.value) tmem_ld_chunk(s_addr + (cc + 1) * PP_CHUNK, rr[(cc + 1) & 1]);
-              uint32_t(&r)[PP_CHUNK] = rr[cc & 1];
-              float2 ex[PP_CHUNK / 2];
+            for (int cc = 0; cc < chunks.value; ++cc) {
+              float4 key[2];
+              float2 inv[2];
+              if (DYN) {
 #pragma unroll
-              for (int e = 0; e < PP_CHUNK; e += 2) {
-                const float2 v = make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1]));
-                if (DYN) {
-                  const float4 k = st->key[(c0 + cc * PP_CHUNK + e) >> 1];
-                  ex[e >> 1] = __fadd2_rn(__ffma2_rn(v, make_float2(k.x, k.y), make_float2(k.z, k.w)), off2);
-                } else {
-                  ex[e >> 1] = __ffma2_rn(v, scale2, off2);
-                }
-              }
-              if (need_mask) {
-#pragma unroll
-                for (int e = 0; e < PP_CHUNK; e += 2) {
-                  ex[e >> 1].x = cc * PP_CHUNK + e < limit ? ex[e >> 1].x : -INFINITY;
-                  ex[e >> 1].y = cc * PP_CHUNK + e + 1 < limit ? ex[e >> 1].y : -INFINITY;
+                for (int n = 0; n < 2; ++n) {
+                  const int pair = ((c0 + cc * PP_CHUNK + n * 8) >> 1) + ft;
+                  key[n] = st->key[pair], inv[n] = st->inv[pair];
                 }
               }
 #pragma unroll
-              for (int e = 0; e < PP_CHUNK; e += 2) {
-                const float2 x2 = ex[e >> 1];
-                top[(e >> 1) & 3] = max3f(top[(e >> 1) & 3], x2.x, x2.y);
-                const float2 w = make_float2(pq::ex2_approx(x2.x), pq::ex2_approx(x2.y));
-                if (DYN)
-                  l4[(e >> 1) & 3] = __ffma2_rn(w, st->inv[(c0 + cc * PP_CHUNK + e) >> 1], l4[(e >> 1) & 3]);
-                else
-                  l4[(e >> 1) & 3] = __fadd2_rn(l4[(e >> 1) & 3], w);
-                pk[(cc * PP_CHUNK + e) >> 1] = pq::pack_f16(w.x, w.y);
+              for (int hf = 0; hf < 2; ++hf) {  // rows fr, fr + 8; rows fr + 16, fr + 24
+                uint32_t(&r)[8] = rr[hf];
+                tmem_ld_wait_frag(r);
+                if (hf == 0)
+                  tmem_ld_frag(s_addr + (16u << 16) + cc * PP_CHUNK, rr[1]);
+                else if (cc + 1 < chunks.value)
+                  tmem_ld_frag(s_addr + (cc + 1) * PP_CHUNK, rr[0]);
+                float2 ex[4];
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                  for (int y = 0; y < 2; ++y) {
+                    const float2 v = make_float2(__uint_as_float(r[4 * n + 2 * y]), __uint_as_float(r[4 * n + 2 * y + 1]));
+                    const float2 off2 = make_float2(off[2 * hf + y], off[2 * hf + y]);
+                    if (DYN)
+                      ex[2 * n + y] = __fadd2_rn(__ffma2_rn(v, make_float2(key[n].x, key[n].y), make_float2(key[n].z, key[n].w)), off2);
+                    else
+                      ex[2 * n + y] = __ffma2_rn(v, scale2, off2);
+                  }
+                if (need_mask) {
+#pragma unroll
+                  for (int y = 0; y < 2; ++y) {
+                    const int tk = min(t0 + static_cast<int>((tok4 >> (16 * hf + 8 * y)) & 255u), x.n - 1);
+                    // visible columns of the row, counted from this thread's first
+                    const int limit = (is_pre ? p.n_prefix : min(n_ctx - key0, x.base + tk - key0 + 1)) - c0 - 2 * ft;
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) {
+                      ex[2 * n + y].x = cc * PP_CHUNK + 8 * n < limit ? ex[2 * n + y].x : -INFINITY;
+                      ex[2 * n + y].y = cc * PP_CHUNK + 8 * n + 1 < limit ? ex[2 * n + y].y : -INFINITY;
+                    }
+                  }
+                }
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                  for (int y = 0; y < 2; ++y) {
+                    const float2 x2 = ex[2 * n + y];
+                    top[2 * hf + y] = max3f(top[2 * hf + y], x2.x, x2.y);
+                    const float2 w = make_float2(pq::ex2_approx(x2.x), pq::ex2_approx(x2.y));
+                    if (DYN)
+                      l2[2 * hf + y] = __ffma2_rn(w, inv[n], l2[2 * hf + y]);
+                    else
+                      l2[2 * hf + y] = __fadd2_rn(l2[2 * hf + y], w);
+                    pk[hf][4 * cc + 2 * n + y] = pq::pack_f16(w.x, w.y);
+                  }
               }
             }
-          }
           };
           if (is_pre && pre_cols == PP_CHUNK) {
             if (!idle) form(std::integral_constant<int, 1>());
@@ -581,37 +630,50 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
             form(std::integral_constant<int, PP_HALF_KEYS / PP_CHUNK>());
           }
           if (again) break;
-          float most = fmaxf(max3f(top[0], top[1], top[2]), top[3]);
-          const float bar_at = m_ref == -INFINITY ? -INFINITY : PP_LAZY;
-          if (!pair_any(most > bar_at)) break;
+          bool over = false;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) over |= top[k] > (m_ref[k] == -INFINITY ? -INFINITY : PP_LAZY);
+          if (!pair_any(over)) break;
           if (*pair_out) {
             ok = false;
             break;
           }
-          *mine = most;  // (the last reader of the exchange before is behind this barrier)
+          // the rows' maxima: over the four lanes, then over the two halves of the columns (the last reader of the exchange before is behind the vote)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 1));
+            top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 2));
+            if (ft == k) bars->row[i][set][fr + 8 * k] = top[k];
+          }
           pair_sync();
-          most = fmaxf(most, *other);
-          const bool grow = most > bar_at;
-          const float m_new = grow ? ceilf(m_use + most) : m_ref;
-          const float alpha = grow ? pq::ex2_approx(m_ref - m_new) : 1.0f;  // 2^(-inf) = 0 for a row that had seen nothing
-          l *= alpha;
+          float alpha[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float most = fmaxf(top[k], *const_cast<const volatile float*>(&bars->row[i][set ^ 1][fr + 8 * k]));
+            const bool first = m_ref[k] == -INFINITY, grow = most > (first ? -INFINITY : PP_LAZY);
+            const float m_new = grow ? ceilf((first ? 0.0f : m_ref[k]) + most) : m_ref[k];
+            alpha[k] = grow ? pq::ex2_approx(m_ref[k] - m_new) : 1.0f;  // 2^(-inf) = 0 for a row that had seen nothing
+            l[k] *= alpha[k];
+            m_ref[k] = m_new;
+          }
           if (jt > x.j0) {  // S_i of this tile is complete, so O_i += P V of the tile before is, too
+            const float f = of_lane(alpha);
             for (int k = 0; k < 4; ++k) {  // this set's half of the dims
               uint32_t q[16];
               tmem_ld_32x16(o_addr + k * 16, q);
 #pragma unroll
-              for (int e = 0; e < 16; ++e) q[e] = __float_as_uint(__uint_as_float(q[e]) * alpha);
+              for (int e = 0; e < 16; ++e) q[e] = __float_as_uint(__uint_as_float(q[e]) * f);
               tmem_st_32x16(o_addr + k * 16, q);
             }
           }
-          m_ref = m_new;
         }
         if (!ok) break;
-        {
-          const float lt = ((l4[0].x + l4[0].y) + (l4[1].x + l4[1].y)) + ((l4[2].x + l4[2].y) + (l4[3].x + l4[3].y));
-          l += DYN || is_pre ? lt : lt * inv_sv;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float lt = l2[k].x + l2[k].y;
+          l[k] += DYN || is_pre ? lt : lt * inv_sv;
         }
-        if (!idle) pq::tmem_st_32x32(s_addr, pk);
+        if (!idle) tmem_st_frag(s_addr, pk[0]), tmem_st_frag(s_addr + (16u << 16), pk[1]);
         pq::tmem_st_wait();
         pq::tc_fence_before();
         __syncwarp();
@@ -631,14 +693,20 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
           ++n_items_done;
           pq::tc_fence_after();
           const bool whole = x.j0 == 0 && x.j1 == x.tiles, live = row_used && t0 + tok_in < x.n;
-          *mine = l;  // the sums of the two halves of the columns
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            l[k] += __shfl_xor_sync(0xffffffffu, l[k], 1);
+            l[k] += __shfl_xor_sync(0xffffffffu, l[k], 2);
+          }
+          float sum = of_lane(l);
+          *mine = sum;  // the sums of the two halves of the columns
           pair_sync();
           if (*pair_out) {
             ok = false;
             break;
           }
-          l += *other;
-          const float norm = l > 0.0f ? 1.0f / l : 0.0f;
+          sum += *other;
+          const float norm = sum > 0.0f ? 1.0f / sum : 0.0f;
           // rows of the output as this lane stores them: piece `lane & 3` (16 bytes) of 64 bytes of the four rows of its quad
           const int64_t my_row = live ? static_cast<int64_t>(x.row0 + tok) * p.Hq + head : -1;
           int64_t out_row[4];
@@ -677,7 +745,10 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
             }
             __syncwarp();
           }
-          if (!whole && live && set == 0) *reinterpret_cast<float2*>(p.ws_ml + (slot * 256 + i * PP_ROWS + row) * 2) = make_float2(m_ref, l);
+          if (!whole) {
+            const float m_row = of_lane(m_ref);
+            if (live && set == 0) *reinterpret_cast<float2*>(p.ws_ml + (slot * 256 + i * PP_ROWS + row) * 2) = make_float2(m_row, sum);
+          }
           pq::tc_fence_before();
         }
       }
