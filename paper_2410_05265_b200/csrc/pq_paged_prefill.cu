@@ -3,21 +3,33 @@
 // Both products run on tcgen05.mma kind::f16 with fp32 accumulators in tensor memory. An item is (sequence, KV head, 2 x floor(128/G) consecutive tokens):
 // the G query heads of the KV head fill two 128-row tiles, so that a key tile is expanded once for all of them. An item walks its key tiles (the
 // prefix, up to 64 full-precision keys, is a first tile of its own; then 128 cached keys each).
-// Work is counted in key tiles. One CTA per SM takes an equal stretch of the tiles of all items laid end to end (prefix sums over the sequences; inside a
-// sequence the number of tiles before an item is a sum of floors with a closed form), whatever the lengths are: a chunk of a long prompt and
-// short prompts fill the chip alike. An item inside one stretch is final; an item that several stretches share leaves partials in the
-// workspace, and the last CTA to finish merges them in the order of the CTAs.
+// Work is counted in key tiles and a few more for every item. One CTA per SM takes an equal stretch of the units of all items laid end to end (prefix sums over
+// the sequences; inside a sequence the number of tiles before an item is a sum of floors with a closed form), whatever the lengths are: a chunk of a
+// long prompt and short prompts fill the chip alike. An item inside one stretch is final; a long item that several stretches share leaves
+// partials in the workspace, and the last CTA to finish merges them in the order of the CTAs (short items are not cut).
 //   loader warp      bulk copies of the packed K and V rows (and steps) of a key tile, page by page, into a landing ring
 //   expansion warps  codes -> K as bf16 integers, V as fp16 integers, both exact, written as [key][dim] tiles in the 128-byte-swizzled layout that serves as
 //                    the K-major B operand of S = Q K^T and as the MN-major B operand of O = P V. With own steps they also prepare, per
 //                    key, (step of the key x scale, log2 and reciprocal of the step of the value).
 //   MMA warp         S_i = Q_i K^T (bf16: every query is exact, whatever its magnitude; prefix keys, fp16, as two bf16 terms), O_i += P_i V with P as the
 //                    tensor-memory A operand (fp16)
-//   softmax warps    one thread per query row. The exponent of a weight takes log2 of the value's step with it, w = 2^(s + log2 step - m): O is in value
-//                    units, fp16 holds the largest of what enters the sum whatever the steps are, the denominator is the sum of w / step
-//                    in fp32. The reference m moves only when an exponent exceeds it by more than 8.
+//   softmax warps    eight per row tile, four for each half of the key columns. A thread has two columns of every eight of four rows (the fragment layout of
+//                    tcgen05.ld 16x256b), so that what is read per key serves four rows. The exponent of a weight takes log2 of the value's
+//                    step with it, w = 2^(s + log2 step - m): O is in value units, fp16 holds the largest of what enters the sum whatever
+//                    the steps are, the denominator is the sum of w / step in fp32. Weights are formed in one pass against the
+//                    reference m so far; it moves, and the pass is repeated, only when an exponent exceeds it by more than 15.
+// Roundings to fewer bits: w to fp16 (2^-11; below 2^-14 in steps of 2^-25 of the largest weight's scale), the result to bf16.
 // Inside every group of eight head dims the expansion leaves the order 0,4,1,5,2,6,3,7; Q and the prefix rows are stored in the same order and the output
 // columns are put back when they are written. Every wait is bounded.
+//
+// Bound by the exponentials and the hand-overs between softmax and tensor core: a key tile of an item takes about 4300 clocks, of which the two products need
+// 2048 on the tensor core and the 32768 exponentials 2048 on the four special-function units; both row tiles' exponentials overlap (2100), then follow the
+// vote on the reference and the store of the weights (700) and the wait for the products (1500). An item costs 10000 clocks more (queries, first
+// scores, prefix, output). Measured: 2048 rows x 64 heads behind 21952 keys 1473 us, 0.65 of the measured bf16 rate on the products of visible pairs (own
+// steps 1752), 4096 rows x 64 heads 357, 2048 rows 133, 4 ragged prompts up to 2000 x 32 heads 165 (own steps 190), 515 rows 25.
+// Tried and slower: a thread per row (own steps 2011 us: the constants of 64 keys per thread), half tiles of 64 keys with the scores of two in flight,
+// row tiles that form their weights in turn (1631; 1573 with half of the pass shared), queries of later items brought in by the expansion warps (the same),
+// eight expansion warps (their 48 registers spill).
 #include <atomic>
 #include <type_traits>
 
@@ -841,205 +853,205 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
         const int stage = c % PP_STAGES;
         const bool is_pre = has_prefix && jt == 0;
 #pragma unroll
-       for (int kv = 0; kv < 2; ++kv) {  // keys, then values
-        const int slot = lc % PP_LANDS;
-        uint64_t *const full = kv ? bars->v_full : bars->k_full, *const empty = kv ? bars->v_empty : bars->k_empty;
-        const uint32_t tile = pq::smem_u32(kv_buf + stage * 2 * PP_TILE + kv * PP_TILE);
-        if ((!is_pre && __any_sync(0xffffffffu, !wait(&bars->land_full[slot], (lc / PP_LANDS) & 1))) ||
-            __any_sync(0xffffffffu, !wait(&empty[stage], ((c / PP_STAGES) & 1) ^ 1))) {
-          ok = false;
-          break;
-        }
-        if (is_pre) {
-          // full-precision rows (reordered inside groups of eight dims); rows past n_prefix are zero
-          for (int unit = tid_e; unit < pre_cols * 16; unit += PP_EXPAND_WARPS * 32) {
-            const int r = unit >> 4, c16 = unit & 15;
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (r < p.n_prefix)
-              v = permute8(pq::ld_dep(reinterpret_cast<const uint4*>((kv ? p.prefix_v : p.prefix_k) + (static_cast<int64_t>(x.h) * p.n_prefix + r) * 128 + c16 * 8)));
-            if (kv) {
-              sts128(tile + tile_off(r, c16), v);
-            } else {  // two bf16 terms: rows 0 .. and rows 64 ..
-              sts128(tile + tile_off(r, c16), make_uint4(bf16_term(v.x, false), bf16_term(v.y, false), bf16_term(v.z, false), bf16_term(v.w, false)));
-              sts128(tile + tile_off(PP_PREFIX + r, c16), make_uint4(bf16_term(v.x, true), bf16_term(v.y, true), bf16_term(v.z, true), bf16_term(v.w, true)));
+        for (int kv = 0; kv < 2; ++kv) {  // keys, then values
+          const int slot = lc % PP_LANDS;
+          uint64_t *const full = kv ? bars->v_full : bars->k_full, *const empty = kv ? bars->v_empty : bars->k_empty;
+          const uint32_t tile = pq::smem_u32(kv_buf + stage * 2 * PP_TILE + kv * PP_TILE);
+          if ((!is_pre && __any_sync(0xffffffffu, !wait(&bars->land_full[slot], (lc / PP_LANDS) & 1))) ||
+              __any_sync(0xffffffffu, !wait(&empty[stage], ((c / PP_STAGES) & 1) ^ 1))) {
+            ok = false;
+            break;
+          }
+          if (is_pre) {
+            // full-precision rows (reordered inside groups of eight dims); rows past n_prefix are zero
+            for (int unit = tid_e; unit < pre_cols * 16; unit += PP_EXPAND_WARPS * 32) {
+              const int r = unit >> 4, c16 = unit & 15;
+              uint4 v = make_uint4(0, 0, 0, 0);
+              if (r < p.n_prefix)
+                v = permute8(pq::ld_dep(reinterpret_cast<const uint4*>((kv ? p.prefix_v : p.prefix_k) + (static_cast<int64_t>(x.h) * p.n_prefix + r) * 128 + c16 * 8)));
+              if (kv) {
+                sts128(tile + tile_off(r, c16), v);
+              } else {  // two bf16 terms: rows 0 .. and rows 64 ..
+                sts128(tile + tile_off(r, c16), make_uint4(bf16_term(v.x, false), bf16_term(v.y, false), bf16_term(v.z, false), bf16_term(v.w, false)));
+                sts128(tile + tile_off(PP_PREFIX + r, c16), make_uint4(bf16_term(v.x, true), bf16_term(v.y, true), bf16_term(v.z, true), bf16_term(v.w, true)));
+              }
+            }
+          } else {
+            const uint32_t src = pq::smem_u32(land + slot * PP_LAND) + tid_e * 16;
+            uint4 w4[PP_KEYS * 4 / (PP_EXPAND_WARPS * 32)];
+#pragma unroll
+            for (int it = 0; it < PP_KEYS / PP_EXPAND_WARPS / 8; ++it) w4[it] = pq::lds128(src + it * (PP_EXPAND_WARPS * 32 * 16));
+#pragma unroll
+            for (int it = 0; it < PP_KEYS / PP_EXPAND_WARPS / 8; ++it) {
+              const int r = it * (PP_EXPAND_WARPS * 8) + (tid_e >> 2);
+              const uint32_t ww[4] = {turn ? w4[it].z : w4[it].x, turn ? w4[it].w : w4[it].y, turn ? w4[it].x : w4[it].z, turn ? w4[it].y : w4[it].w};
+              if (kv) {
+#pragma unroll
+                for (int w = 0; w < 4; ++w) sts128(tile + tile_off(r, 4 * part + (w ^ turn)), expand8_f16(ww[w]));
+              } else {
+#pragma unroll
+                for (int w = 0; w < 4; ++w) sts128(tile + tile_off(r, 4 * part + (w ^ turn)), expand8_bf16(ww[w]));
+              }
             }
           }
-        } else {
-          const uint32_t src = pq::smem_u32(land + slot * PP_LAND) + tid_e * 16;
-          uint4 w4[PP_KEYS * 4 / (PP_EXPAND_WARPS * 32)];
-#pragma unroll
-          for (int it = 0; it < PP_KEYS / PP_EXPAND_WARPS / 8; ++it) w4[it] = pq::lds128(src + it * (PP_EXPAND_WARPS * 32 * 16));
-#pragma unroll
-          for (int it = 0; it < PP_KEYS / PP_EXPAND_WARPS / 8; ++it) {
-            const int r = it * (PP_EXPAND_WARPS * 8) + (tid_e >> 2);
-            const uint32_t ww[4] = {turn ? w4[it].z : w4[it].x, turn ? w4[it].w : w4[it].y, turn ? w4[it].x : w4[it].z, turn ? w4[it].y : w4[it].w};
-            if (kv) {
-#pragma unroll
-              for (int w = 0; w < 4; ++w) sts128(tile + tile_off(r, 4 * part + (w ^ turn)), expand8_f16(ww[w]));
-            } else {
-#pragma unroll
-              for (int w = 0; w < 4; ++w) sts128(tile + tile_off(r, 4 * part + (w ^ turn)), expand8_bf16(ww[w]));
-            }
+          if (DYN && kv) {  // thread j: key j of the tile. A key that no row sees adds nothing.
+            const float* st = reinterpret_cast<const float*>(land + slot * PP_LAND + PP_KEYS * 64);
+            const int key = (jt - has_prefix) * PP_KEYS + tid_e;
+            const bool in = !is_pre && key < n_ctx;
+            const float k_step = in ? st[tid_e] : 1.0f, v_step = in ? st[PP_KEYS + tid_e] : 1.0f;
+            float* key_out = reinterpret_cast<float*>(&steps_buf[stage].key[tid_e >> 1]) + (tid_e & 1);
+            key_out[0] = k_step * p.scale2, key_out[2] = pq::lg2_approx(v_step);
+            reinterpret_cast<float*>(steps_buf[stage].inv)[tid_e] = pq::rcp_approx(v_step);
           }
+          pq::fence_proxy_async_smem();  // generic-proxy writes -> visible to the tensor core's async proxy
+          __syncwarp();
+          if (lane == 0) {
+            pq::mbar_arrive(&full[stage]);
+            if (!is_pre) pq::mbar_arrive(&bars->land_empty[slot]);
+          }
+          if (!is_pre) ++lc;
         }
-        if (DYN && kv) {  // thread j: key j of the tile. A key that no row sees adds nothing.
-          const float* st = reinterpret_cast<const float*>(land + slot * PP_LAND + PP_KEYS * 64);
-          const int key = (jt - has_prefix) * PP_KEYS + tid_e;
-          const bool in = !is_pre && key < n_ctx;
-          const float k_step = in ? st[tid_e] : 1.0f, v_step = in ? st[PP_KEYS + tid_e] : 1.0f;
-          float* key_out = reinterpret_cast<float*>(&steps_buf[stage].key[tid_e >> 1]) + (tid_e & 1);
-          key_out[0] = k_step * p.scale2, key_out[2] = pq::lg2_approx(v_step);
-          reinterpret_cast<float*>(steps_buf[stage].inv)[tid_e] = pq::rcp_approx(v_step);
-        }
-        pq::fence_proxy_async_smem();  // generic-proxy writes -> visible to the tensor core's async proxy
-        __syncwarp();
-        if (lane == 0) {
-          pq::mbar_arrive(&full[stage]);
-          if (!is_pre) pq::mbar_arrive(&bars->land_empty[slot]);
-        }
-        if (!is_pre) ++lc;
-       }
       }
     }
     if (!ok && lane == 0) give_up();
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PP_REGS_OTHERS));
     if (warp == PP_WARP_LOAD) {
-    // ================================================================== loader
-    // A lane to a copy: lanes 0 .. 7 the pages of the tile (fewer for larger pages); with own steps lanes 8 .. 15 and 16 .. 23 the steps of their keys and
-    // values, which go with the rows of V.
-    const int pages = PP_KEYS >> p.page_log2, pg = lane & 7, kind = lane >> 3, page = 1 << p.page_log2;
-    bool ok = true;
-    PpItem x;
-    if (any) x = first_item();
-    for (bool more = any; more && ok; more = next_item(x)) {
-      const int n_ctx = n_ctx_of(x);
-      const int32_t* row = p.table + static_cast<int64_t>(x.b) * p.max_pages;
-      for (int jt = max(x.j0, has_prefix); jt < x.j1 && ok; ++jt) {
-        const int key0 = (jt - has_prefix) * PP_KEYS, n_here = min(pages, (n_ctx - key0 + page - 1) >> p.page_log2);  // pages with keys in them
-        const bool mine = pg < n_here && kind < (DYN ? 3 : 1);
-        int id = 0;
-        if (mine) {
-          id = pq::ld_dep(row + (key0 >> p.page_log2) + pg);
-          if (static_cast<uint32_t>(id) >= static_cast<uint32_t>(p.n_pages)) {  // an id that is none is reported and page 0 read in its place
-            pq::report(p.status, PQ_ERR_SHAPE);
-            id = 0;
+      // ================================================================== loader
+      // A lane to a copy: lanes 0 .. 7 the pages of the tile (fewer for larger pages); with own steps lanes 8 .. 15 and 16 .. 23 the steps of their keys and
+      // values, which go with the rows of V.
+      const int pages = PP_KEYS >> p.page_log2, pg = lane & 7, kind = lane >> 3, page = 1 << p.page_log2;
+      bool ok = true;
+      PpItem x;
+      if (any) x = first_item();
+      for (bool more = any; more && ok; more = next_item(x)) {
+        const int n_ctx = n_ctx_of(x);
+        const int32_t* row = p.table + static_cast<int64_t>(x.b) * p.max_pages;
+        for (int jt = max(x.j0, has_prefix); jt < x.j1 && ok; ++jt) {
+          const int key0 = (jt - has_prefix) * PP_KEYS, n_here = min(pages, (n_ctx - key0 + page - 1) >> p.page_log2);  // pages with keys in them
+          const bool mine = pg < n_here && kind < (DYN ? 3 : 1);
+          int id = 0;
+          if (mine) {
+            id = pq::ld_dep(row + (key0 >> p.page_log2) + pg);
+            if (static_cast<uint32_t>(id) >= static_cast<uint32_t>(p.n_pages)) {  // an id that is none is reported and page 0 read in its place
+              pq::report(p.status, PQ_ERR_SHAPE);
+              id = 0;
+            }
           }
-        }
-        const int64_t vec = ((static_cast<int64_t>(id) * p.Hkv + x.h) * 2) << p.page_log2;
+          const int64_t vec = ((static_cast<int64_t>(id) * p.Hkv + x.h) * 2) << p.page_log2;
 #pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-          const int slot = lands_issued % PP_LANDS;
-          if (!wait_warp(&bars->land_empty[slot], ((lands_issued / PP_LANDS) & 1) ^ 1)) {
-            ok = false;
-            break;
-          }
-          const uint32_t dst = pq::smem_u32(land + slot * PP_LAND);
-          const uint32_t n_pages = static_cast<uint32_t>(max(n_here, 0));
-          if (lane == 0) pq::mbar_arrive_expect_tx(&bars->land_full[slot], n_pages * page * (64 + (DYN && kv ? 8 : 0)));
-          __syncwarp();
-          if (mine && kind == 0)
-            pq::bulk_load(dst + pg * page * 64, p.codes + (vec + kv * page) * 64, page * 64, &bars->land_full[slot]);
-          else if (mine && kv)
-            pq::bulk_load(dst + PP_KEYS * 64 + (kind - 1) * (PP_KEYS * 4) + pg * page * 4, p.steps + vec + (kind - 1) * page, page * 4, &bars->land_full[slot]);
-          ++lands_issued;
-        }
-      }
-    }
-    if (!ok && lane == 0) give_up();
-    } else if (warp == PP_WARP_MMA) {
-    // ================================================================== MMA issuer: the whole warp runs the loop, the elected lane issues
-    constexpr uint32_t IDESC_S = idesc_16(PP_ROWS, PP_KEYS, true, false);
-    const uint32_t IDESC_S_PRE = idesc_16(PP_ROWS, pre_cols, true, false);
-    constexpr uint32_t IDESC_O = idesc_16(PP_ROWS, 128, false, true);
-    const bool leader = pq::elect_one();
-    const uint64_t q_desc0 = desc_sw128(pq::smem_u32(q_buf), 16), k_desc0 = desc_sw128(pq::smem_u32(kv_buf), 16);
-    const uint64_t v_desc0 = desc_sw128(pq::smem_u32(kv_buf + PP_TILE), PP_HALF);
-    auto issue_s = [&](int i, int c, bool is_pre) {  // by the elected lane
-      const uint64_t q_desc = q_desc0 + i * (PP_TILE >> 4), k_desc = k_desc0 + (c % PP_STAGES) * (2 * PP_TILE >> 4);
-#pragma unroll
-      for (int kk = 0; kk < 8; ++kk) {  // 16 head dims per instruction
-        const uint32_t off = ((kk >> 2) * PP_HALF + (kk & 3) * 32) >> 4;
-        mma_ss(tmem_base + i * 128, q_desc + off, k_desc + off, is_pre ? IDESC_S_PRE : IDESC_S, kk ? 1u : 0u);
-      }
-      if (is_pre)  // the second terms of the prefix keys, 64 rows on
-#pragma unroll
-        for (int kk = 0; kk < 8; ++kk) {
-          const uint32_t off = ((kk >> 2) * PP_HALF + (kk & 3) * 32) >> 4;
-          mma_ss(tmem_base + i * 128, q_desc + off, k_desc + off + (PP_PREFIX * 128 >> 4), IDESC_S_PRE, 1u);
-        }
-      pq::mma_commit(&bars->s_full[i]);
-    };
-    auto issue_pv = [&](int i, int c, bool is_pre, bool first) {
-      const uint32_t o_tm = tmem_base + 256 + i * 128, p_tm = tmem_base + i * 128;
-      const uint64_t v_desc = v_desc0 + (c % PP_STAGES) * (2 * PP_TILE >> 4);
-#pragma unroll
-      for (int kk = 0; kk < PP_PREFIX / 16; ++kk)  // 16 keys per instruction
-        if (!is_pre || kk * 16 < pre_cols) mma_ts(o_tm, p_tm + kk * 8, v_desc + kk * (2048 >> 4), IDESC_O, (!first || kk > 0) ? 1u : 0u);
-      if (!is_pre)
-#pragma unroll
-        for (int kk = PP_PREFIX / 16; kk < PP_KEYS / 16; ++kk) mma_ts(o_tm, p_tm + PP_HALF_KEYS / 2 + kk * 8, v_desc + kk * (2048 >> 4), IDESC_O, 1u);
-    };
-    bool ok = true;
-    int c = 0, n_q[2] = {0, 0}, n_p[2] = {0, 0};
-    PpItem x;
-    if (any) x = first_item();
-    for (bool more = any; more && ok; more = next_item(x)) {
-      const int groups = second_tile(x) ? 2 : 1;
-      ok = wait_warp(&bars->k_full[c % PP_STAGES], (c / PP_STAGES) & 1);
-      for (int i = 0; i < groups && ok; ++i) {
-        if (!wait_warp(&bars->q_ready[i], n_q[i] & 1)) {
-          ok = false;
-          break;
-        }
-        ++n_q[i];
-        pq::tc_fence_after();
-        if (leader) {
-          issue_s(i, c, has_prefix && x.j0 == 0);
-          if (i == groups - 1) pq::mma_commit(&bars->k_empty[c % PP_STAGES]);
-        }
-        __syncwarp();
-      }
-      for (int jt = x.j0; jt < x.j1 && ok; ++jt, ++c) {
-        const bool is_pre = has_prefix && jt == 0, last = jt + 1 == x.j1;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          if (i >= groups) break;
-          if (!wait_warp(&bars->p_full[i], n_p[i] & 1) || (i == 0 && !wait_warp(&bars->v_full[c % PP_STAGES], (c / PP_STAGES) & 1))) {
-            ok = false;
-            break;
-          }
-          ++n_p[i];
-          pq::tc_fence_after();
-          if (leader) {
-            issue_pv(i, c, is_pre, jt == x.j0);
-            if (i == groups - 1) pq::mma_commit(&bars->v_empty[c % PP_STAGES]);
-          }
-          __syncwarp();
-          if (!last) {
-            if (i == 0 && !wait_warp(&bars->k_full[(c + 1) % PP_STAGES], ((c + 1) / PP_STAGES) & 1)) {
+          for (int kv = 0; kv < 2; ++kv) {
+            const int slot = lands_issued % PP_LANDS;
+            if (!wait_warp(&bars->land_empty[slot], ((lands_issued / PP_LANDS) & 1) ^ 1)) {
               ok = false;
               break;
             }
-            pq::tc_fence_after();
-            if (leader) {
-              issue_s(i, c + 1, false);
-              if (i == groups - 1) pq::mma_commit(&bars->k_empty[(c + 1) % PP_STAGES]);
-            }
-          } else if (leader) {
-            pq::mma_commit(&bars->o_final[i]);
+            const uint32_t dst = pq::smem_u32(land + slot * PP_LAND);
+            const uint32_t n_pages = static_cast<uint32_t>(max(n_here, 0));
+            if (lane == 0) pq::mbar_arrive_expect_tx(&bars->land_full[slot], n_pages * page * (64 + (DYN && kv ? 8 : 0)));
+            __syncwarp();
+            if (mine && kind == 0)
+              pq::bulk_load(dst + pg * page * 64, p.codes + (vec + kv * page) * 64, page * 64, &bars->land_full[slot]);
+            else if (mine && kv)
+              pq::bulk_load(dst + PP_KEYS * 64 + (kind - 1) * (PP_KEYS * 4) + pg * page * 4, p.steps + vec + (kind - 1) * page, page * 4, &bars->land_full[slot]);
+            ++lands_issued;
+          }
+        }
+      }
+      if (!ok && lane == 0) give_up();
+    } else if (warp == PP_WARP_MMA) {
+      // ================================================================== MMA issuer: the whole warp runs the loop, the elected lane issues
+      constexpr uint32_t IDESC_S = idesc_16(PP_ROWS, PP_KEYS, true, false);
+      const uint32_t IDESC_S_PRE = idesc_16(PP_ROWS, pre_cols, true, false);
+      constexpr uint32_t IDESC_O = idesc_16(PP_ROWS, 128, false, true);
+      const bool leader = pq::elect_one();
+      const uint64_t q_desc0 = desc_sw128(pq::smem_u32(q_buf), 16), k_desc0 = desc_sw128(pq::smem_u32(kv_buf), 16);
+      const uint64_t v_desc0 = desc_sw128(pq::smem_u32(kv_buf + PP_TILE), PP_HALF);
+      auto issue_s = [&](int i, int c, bool is_pre) {  // by the elected lane
+        const uint64_t q_desc = q_desc0 + i * (PP_TILE >> 4), k_desc = k_desc0 + (c % PP_STAGES) * (2 * PP_TILE >> 4);
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk) {  // 16 head dims per instruction
+          const uint32_t off = ((kk >> 2) * PP_HALF + (kk & 3) * 32) >> 4;
+          mma_ss(tmem_base + i * 128, q_desc + off, k_desc + off, is_pre ? IDESC_S_PRE : IDESC_S, kk ? 1u : 0u);
+        }
+        if (is_pre)  // the second terms of the prefix keys, 64 rows on
+#pragma unroll
+          for (int kk = 0; kk < 8; ++kk) {
+            const uint32_t off = ((kk >> 2) * PP_HALF + (kk & 3) * 32) >> 4;
+            mma_ss(tmem_base + i * 128, q_desc + off, k_desc + off + (PP_PREFIX * 128 >> 4), IDESC_S_PRE, 1u);
+          }
+        pq::mma_commit(&bars->s_full[i]);
+      };
+      auto issue_pv = [&](int i, int c, bool is_pre, bool first) {
+        const uint32_t o_tm = tmem_base + 256 + i * 128, p_tm = tmem_base + i * 128;
+        const uint64_t v_desc = v_desc0 + (c % PP_STAGES) * (2 * PP_TILE >> 4);
+#pragma unroll
+        for (int kk = 0; kk < PP_PREFIX / 16; ++kk)  // 16 keys per instruction
+          if (!is_pre || kk * 16 < pre_cols) mma_ts(o_tm, p_tm + kk * 8, v_desc + kk * (2048 >> 4), IDESC_O, (!first || kk > 0) ? 1u : 0u);
+        if (!is_pre)
+#pragma unroll
+          for (int kk = PP_PREFIX / 16; kk < PP_KEYS / 16; ++kk) mma_ts(o_tm, p_tm + PP_HALF_KEYS / 2 + kk * 8, v_desc + kk * (2048 >> 4), IDESC_O, 1u);
+      };
+      bool ok = true;
+      int c = 0, n_q[2] = {0, 0}, n_p[2] = {0, 0};
+      PpItem x;
+      if (any) x = first_item();
+      for (bool more = any; more && ok; more = next_item(x)) {
+        const int groups = second_tile(x) ? 2 : 1;
+        ok = wait_warp(&bars->k_full[c % PP_STAGES], (c / PP_STAGES) & 1);
+        for (int i = 0; i < groups && ok; ++i) {
+          if (!wait_warp(&bars->q_ready[i], n_q[i] & 1)) {
+            ok = false;
+            break;
+          }
+          ++n_q[i];
+          pq::tc_fence_after();
+          if (leader) {
+            issue_s(i, c, has_prefix && x.j0 == 0);
+            if (i == groups - 1) pq::mma_commit(&bars->k_empty[c % PP_STAGES]);
           }
           __syncwarp();
         }
+        for (int jt = x.j0; jt < x.j1 && ok; ++jt, ++c) {
+          const bool is_pre = has_prefix && jt == 0, last = jt + 1 == x.j1;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            if (i >= groups) break;
+            if (!wait_warp(&bars->p_full[i], n_p[i] & 1) || (i == 0 && !wait_warp(&bars->v_full[c % PP_STAGES], (c / PP_STAGES) & 1))) {
+              ok = false;
+              break;
+            }
+            ++n_p[i];
+            pq::tc_fence_after();
+            if (leader) {
+              issue_pv(i, c, is_pre, jt == x.j0);
+              if (i == groups - 1) pq::mma_commit(&bars->v_empty[c % PP_STAGES]);
+            }
+            __syncwarp();
+            if (!last) {
+              if (i == 0 && !wait_warp(&bars->k_full[(c + 1) % PP_STAGES], ((c + 1) / PP_STAGES) & 1)) {
+                ok = false;
+                break;
+              }
+              pq::tc_fence_after();
+              if (leader) {
+                issue_s(i, c + 1, false);
+                if (i == groups - 1) pq::mma_commit(&bars->k_empty[(c + 1) % PP_STAGES]);
+              }
+            } else if (leader) {
+              pq::mma_commit(&bars->o_final[i]);
+            }
+            __syncwarp();
+          }
+        }
       }
-    }
-    if (leader) {
-      if (!ok) give_up();
-      // whatever was issued has finished before tensor memory is released or shared memory given back
-      pq::mma_commit(&bars->drain);
-    }
-    __syncwarp();
-    pq::mbar_wait(&bars->drain, 0);
+      if (leader) {
+        if (!ok) give_up();
+        // whatever was issued has finished before tensor memory is released or shared memory given back
+        pq::mma_commit(&bars->drain);
+      }
+      __syncwarp();
+      pq::mbar_wait(&bars->drain, 0);
     }
   }
 
