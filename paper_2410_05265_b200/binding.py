@@ -8,7 +8,6 @@ from __future__ import annotations
 
 import ctypes
 import functools
-import math
 import os
 from ctypes import POINTER, Structure, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_void_p
 
@@ -175,9 +174,13 @@ def _ok(status: int, where: str):
         raise PQError(status, where)
 
 
-def _row_stride(t: torch.Tensor) -> int:
-    """Elements between the rows of t; of a single row, whose stride says nothing, its own width."""
-    return t.stride(0) if t.shape[0] > 1 else math.prod(t.shape[1:])
+def _head_rows(t: torch.Tensor, dtype, N: int, H: int, D: int, name: str) -> int:
+    """Checks t [N, H, D] with dense heads and returns the elements between its rows; of a single row, whose stride says nothing, its width."""
+    if not t.is_cuda or t.dtype != dtype:
+        raise TypeError(f"{name} must be a CUDA tensor of dtype {dtype}")
+    row, head, one = t.stride()
+    assert t.shape == (N, H, D) and one == 1 and (H == 1 or head == D), name
+    return row if N > 1 else H * D
 
 
 @functools.lru_cache(maxsize=64)
@@ -691,33 +694,31 @@ class Context:
     def _rope_args(N, gq, gk, pos, sections):
         """(axes, distance of the axes, sections) as the C calls take them; pos int32 [N] or [axes, N]."""
         _dev(pos, torch.int32, "pos")
-        for g, name in ((gq, "gq"), (gk, "gk")):
-            if g is not None:
-                _dev(g, torch.bfloat16, name)
-                assert g.shape == (128,) and g.is_contiguous(), name
         assert (gq is None) == (gk is None)
-        axes = 1 if pos.dim() == 1 else pos.shape[0]
-        assert pos.shape[-1] == N and (N <= 1 or pos.stride(-1) == 1)
+        if gq is not None:
+            _dev(gq, torch.bfloat16, "gq"), _dev(gk, torch.bfloat16, "gk")
+            assert gq.shape == gk.shape == (128,) and gq.is_contiguous() and gk.is_contiguous()
+        shape, stride = pos.shape, pos.stride()
+        axes = 1 if len(shape) == 1 else shape[0]
+        assert shape[-1] == N and (N <= 1 or stride[-1] == 1) and len(shape) <= 2
         if sections is not None:
             assert len(sections) == axes
             sections = _sections(tuple(sections))
-        return axes, N if axes == 1 else pos.stride(0), sections
+        return axes, N if axes == 1 else stride[0], sections
 
     def qk_norm_rope(self, x: torch.Tensor, Hq: int, gq, gk, eps: float, pos: torch.Tensor, theta: float, sections=None, rotate: bool = False,
                      out: torch.Tensor | None = None):
         """RMSNorm of every head (gains gq for the first Hq heads of x [N, H, 128], gk for the others; both None: no norm), rotary embedding with the
         positions pos int32 [N] or [axes, N] (frequencies dealt to the axes by `sections`), with rotate=True followed by R3. out may be x."""
-        _dev(x, torch.bfloat16, "x")
         N, H, D = x.shape
-        assert x.stride(2) == 1 and (H == 1 or x.stride(1) == D)
+        ld = _head_rows(x, torch.bfloat16, N, H, D, "x")
         axes, ld_pos, sec = self._rope_args(N, gq, gk, pos, sections)
         if out is None:
             out = torch.empty((N, H, D), dtype=x.dtype, device=x.device)
-        _dev(out, torch.bfloat16, "out")
-        assert out.shape == x.shape and out.stride(2) == 1 and (H == 1 or out.stride(1) == D)
+        ld_out = _head_rows(out, torch.bfloat16, N, H, D, "out")
         self._here(x, gq, gk, pos, out)
-        _ok(self.lib.pq_qk_norm_rope(self.h, _ptr(x), N, int(Hq), H - int(Hq), D, _row_stride(x), _ptr(gq), _ptr(gk), float(eps), _ptr(pos), axes, ld_pos,
-                                     sec, float(theta), 1 if rotate else 0, _ptr(out), _row_stride(out), _stream()), "pq_qk_norm_rope")
+        _ok(self.lib.pq_qk_norm_rope(self.h, _ptr(x), N, int(Hq), H - int(Hq), D, ld, _ptr(gq), _ptr(gk), float(eps), _ptr(pos), axes, ld_pos,
+                                     sec, float(theta), 1 if rotate else 0, _ptr(out), ld_out, _stream()), "pq_qk_norm_rope")
         return out
 
     def qk_norm_rope_kv4_paged_append(self, cache: KV4PagedCache, qkv: torch.Tensor, gq, gk, eps: float, pos: torch.Tensor, slot: torch.Tensor,
@@ -725,18 +726,18 @@ class Context:
         """qk_norm_rope of a projection output qkv [N, (Hq + 2 Hkv) * 128]: the query heads to q_out [N, Hq, 128] (returned), the key and value
         heads, quantized, to the slots of the paged cache. Rows with slot -1 are neither read nor written."""
         _dev(qkv, torch.bfloat16, "qkv"), _dev(slot, torch.int64, "slot")
-        N = qkv.shape[0]
-        assert qkv.dim() == 2 and qkv.stride(1) == 1 and qkv.shape[1] == (cache.Hq + 2 * cache.Hkv) * cache.D
+        N, cols = qkv.shape
+        ld, one = qkv.stride()
+        assert one == 1 and cols == (cache.Hq + 2 * cache.Hkv) * cache.D
         assert slot.shape == (N,) and slot.is_contiguous()
         axes, ld_pos, sec = self._rope_args(N, gq, gk, pos, sections)
         if q_out is None:
             q_out = torch.empty((N, cache.Hq, cache.D), dtype=qkv.dtype, device=qkv.device)
-        _dev(q_out, torch.bfloat16, "q_out")
-        assert q_out.shape == (N, cache.Hq, cache.D) and q_out.stride(2) == 1 and (cache.Hq == 1 or q_out.stride(1) == cache.D)
+        ld_out = _head_rows(q_out, torch.bfloat16, N, cache.Hq, cache.D, "q_out")
         self._here(cache.codes, qkv, gq, gk, pos, slot, q_out)
-        _ok(self.lib.pq_qk_norm_rope_kv4_paged_append(self.h, ctypes.byref(cache.struct), _ptr(qkv), N, _row_stride(qkv), _ptr(gq), _ptr(gk), float(eps),
+        _ok(self.lib.pq_qk_norm_rope_kv4_paged_append(self.h, ctypes.byref(cache.struct), _ptr(qkv), N, ld if N > 1 else cols, _ptr(gq), _ptr(gk), float(eps),
                                                       _ptr(pos), axes, ld_pos, sec, float(theta), 1 if rotate else 0, _ptr(slot), _ptr(q_out),
-                                                      _row_stride(q_out), _stream()), "pq_qk_norm_rope_kv4_paged_append")
+                                                      ld_out, _stream()), "pq_qk_norm_rope_kv4_paged_append")
         return q_out
 
     def kv4_paged_read(self, cache: KV4PagedCache, slot: torch.Tensor, out: torch.Tensor | None = None):
@@ -759,16 +760,16 @@ class Context:
                        max_len: int = 0, out: torch.Tensor | None = None):
         """Causal attention of the rows q [N, Hq, 128] of a ragged batch (sequence b: rows q_begin[b] .. q_begin[b + 1] - 1, its last tokens) over
         [prefix || paged cache]. max_new bounds the rows of a sequence, max_len (0: the capacity) the lengths; rows behind the last stay as they are."""
-        _dev(q, torch.bfloat16, "q"), _dev(q_begin, torch.int32, "q_begin"), _dev(ws, torch.uint8, "ws")
+        _dev(q_begin, torch.int32, "q_begin"), _dev(ws, torch.uint8, "ws")
         N = q.shape[0]
-        assert q.shape == (N, cache.Hq, cache.D) and q.stride(2) == 1 and (cache.Hq == 1 or q.stride(1) == cache.D)
+        ldq = _head_rows(q, torch.bfloat16, N, cache.Hq, cache.D, "q")
         assert q_begin.shape == (cache.pages.B + 1,) and q_begin.is_contiguous()
         if out is None:
             out = torch.zeros((N, cache.Hq, cache.D), dtype=q.dtype, device=q.device)
         _dev(out, torch.bfloat16, "out")
         assert out.shape == q.shape and out.is_contiguous()
         self._here(cache.codes, q, q_begin, ws, out)
-        _ok(self.lib.pq_attn_kv4_paged(self.h, ctypes.byref(cache.struct), _ptr(q), _row_stride(q), _ptr(q_begin), N, int(max_new), int(max_len), _ptr(out),
+        _ok(self.lib.pq_attn_kv4_paged(self.h, ctypes.byref(cache.struct), _ptr(q), ldq, _ptr(q_begin), N, int(max_new), int(max_len), _ptr(out),
                                        float(sm_scale), _ptr(ws), ws.numel(), _stream()), "pq_attn_kv4_paged")
         return out
 
