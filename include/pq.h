@@ -314,7 +314,7 @@ pq_status pq_rope_kv4_append(pq_ctx* ctx, const pq_kv4_cache* cache, int32_t seq
  *   len        int32 [B]             cached tokens of each sequence
  *   free_list  int32 [n_pages]       entries 0 .. *n_free - 1 are the ids of the free pages (a stack, taken from its end)
  *   n_free     int32 [1]
- *   page in {16, 32, 64, 128}; B <= 8192; max_pages * page < 2^31.
+ *   page in {16, 32, 64, 128}; B <= 8192; max_pages * page <= 2^30. A page belongs to one sequence at a time.
  * All on the device; a page id outside [0, n_pages) is never followed (PQ_ERR_SHAPE in the status word). */
 typedef struct pq_pages {
   int32_t* table;
@@ -396,7 +396,8 @@ pq_status pq_kv4_paged_read(pq_ctx* ctx, const pq_kv4_paged* cache, const int64_
  * q_begin[b] .. q_begin[b + 1] - 1 of q are the last n = q_begin[b + 1] - q_begin[b] tokens of the len[b] cached ones of sequence b
  * (pq_page_plan has advanced len, the append has written them). Row t of them sees every prefixed key and the cached keys 0 .. len[b] - n + t:
  *     out[row, g, :] = softmax_j(q[row, g, :] . K_j * sm_scale) . V      (zeros where nothing is visible)
- *   q        bf16 [n_rows, Hq, 128] with ldq elements between rows (a multiple of 8), out bf16 [n_rows, Hq, 128] dense, both 16-byte aligned
+ *   q        bf16 [n_rows, Hq, 128] with ldq elements between rows (a multiple of 8), out bf16 [n_rows, Hq, 128] dense, both 16-byte aligned; out
+ *            may be q (ldq = Hq * 128), else they must not overlap
  *   q_begin  int32 [B + 1], ascending, on the device; rows from q_begin[B] on (padding) are neither read nor written
  *   max_new  at least the largest n (a host bound); sequences with more rows are left out and PQ_ERR_SHAPE is reported
  *   max_len  at least the largest len (a host bound that only chooses how the work is split; 0: the capacity max_pages * page)

@@ -15,7 +15,7 @@ static inline pq_status pq_check_pages(const pq_pages* c) {
   if (!c || !c->n_free || c->B < 0 || c->max_pages < 0 || c->n_pages < 0) return PQ_ERR_INVALID_ARG;
   if ((c->B > 0 && (!c->len || (c->max_pages > 0 && !c->table))) || (c->n_pages > 0 && !c->free_list)) return PQ_ERR_INVALID_ARG;  // (an empty array has no address)
   if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return PQ_ERR_SHAPE;
-  if (c->B > PQ_PAGED_MAX_SEQS || static_cast<int64_t>(c->max_pages) * c->page > 0x7fffffffll) return PQ_ERR_SHAPE;
+  if (c->B > PQ_PAGED_MAX_SEQS || static_cast<int64_t>(c->max_pages) * c->page > (1ll << 30)) return PQ_ERR_SHAPE;  // (a key's number and a step beyond it fit 32 bits)
   return PQ_OK;
 }
 

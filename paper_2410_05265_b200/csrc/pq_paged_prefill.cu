@@ -309,7 +309,9 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     pq::tmem_relinquish();
   }
   // No wait here: this kernel always follows the one for single tokens, which lets it start behind its own wait for what came before, and the two have
-  // nothing in common but what both read. The wait is this kernel's last step, so that it ends no earlier than the other.
+  // nothing in common but what both read. The wait is this kernel's last step, so that it ends no earlier than the other. What a wait would do for the
+  // SM's L1 the fence does: loads behind it see what was written before the launch.
+  __threadfence();
 
   // ---- the sequences: number of key tiles of all row tiles of one KV head, prefix sums, and where this worker's stretch begins
   const int64_t capacity = static_cast<int64_t>(p.max_pages) << p.page_log2;

@@ -286,6 +286,46 @@ def test_nothing_to_do(ctx, steps):
 
 
 @pytest.mark.parametrize("steps", ["head", "vector"])
+@pytest.mark.parametrize("lengths,new,Hq,Hkv", [([700, 3, 9000, 40], [1, 1, 1, 1], 8, 2), ([40], [1], 8, 8), ([700, 300, 20, 9000], [700, 1, 20, 33], 16, 4),
+                                                ([6000], [300], 6, 2)])
+def test_the_output_may_be_the_queries(ctx, steps, lengths, new, Hq, Hkv):
+    cache = ref.make_cache(lengths, Hq, Hkv, 16, steps, seed=3)
+    begin = [0]
+    for n in new:
+        begin.append(begin[-1] + n)
+    q = ref.queries(begin[-1], Hq)
+    ws = ctx.attn_kv4_paged_workspace(cache, begin[-1], max(new))
+    want = ctx.attn_kv4_paged(cache, q, i32(begin), max(new), SCALE, ws)
+    assert torch.equal(ctx.attn_kv4_paged(cache, q, i32(begin), max(new), SCALE, ws, out=q), want)
+    ctx.check()
+
+
+@pytest.mark.parametrize("steps", ["head", "vector"])
+@pytest.mark.parametrize("ragged", [False, True])
+def test_the_largest_batch(ctx, steps, ragged):
+    """8192 sequences of a few tokens, single rows or several; a sample of them against the definition."""
+    r = random.Random(5)
+    B = 8192
+    new = [r.choice([0, 1, 2, 5]) if ragged else r.choice([0, 1, 1, 1]) for _ in range(B)]
+    lengths = [n + r.choice([0, 0, 3, 17, 60]) for n in new]
+    cache = ref.make_cache(lengths, 3, 1, 16, steps, n_prefix=1, seed=7)
+    begin = [0]
+    for n in new:
+        begin.append(begin[-1] + n)
+    q = ref.queries(begin[-1], 3)
+    out = ctx.attn_kv4_paged(cache, q, i32(begin), 5 if ragged else 1, SCALE, ctx.attn_kv4_paged_workspace(cache, begin[-1], 5 if ragged else 1))
+    ctx.check()
+    for lo in (0, 1000, 4095, B - 40):
+        some = range(lo, lo + 40)
+        part = binding.KV4PagedCache(binding.Pages(cache.pages.table[lo: lo + 40].contiguous(), cache.pages.length[lo: lo + 40].contiguous(), cache.pages.free_list,
+                                                   cache.pages.n_free, 16), cache.prefix_k, cache.prefix_v, cache.codes, 3, s_k=cache.s_k, s_v=cache.s_v,
+                                     steps=cache.steps)
+        r0, r1 = begin[lo], begin[lo + 40]
+        want, tol = ref.attention(part, q[r0:r1], [begin[b] - r0 for b in some] + [r1 - r0], [lengths[b] for b in some], SCALE)
+        assert ((out[r0:r1].double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("steps", ["head", "vector"])
 def test_offsets_past_32_bits(ctx, steps):
     """A cache of more than 2^32 bytes whose pages in use lie at its end, query rows that are 2^30 elements apart."""
     Hq, Hkv, page, n_pages = 8, 4, 128, 70000

@@ -39,6 +39,8 @@ def test_the_kernel_for_several_rows_waits_last_and_never_triggers():
     body = kernel_body("pq_paged_prefill.cu", "paged_prefill_kernel")
     assert not TRIGGER.search(body) and body.count("pdl_wait") == 1
     assert re.search(r"pq::pdl_wait\(\);\s*}$", body) and "__ldg(" not in body and "ld.global.nc" not in body
+    # in the wait's place a fence ahead of the first read
+    assert body.index("__threadfence()") < body.index("ld_dep(")
     # no thread returns ahead of it: what returns are lambdas
     assert len(re.findall(r"^  (?:if \(.*\) )?return;", body, re.M)) == 0
 
