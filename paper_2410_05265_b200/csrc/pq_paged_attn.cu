@@ -31,7 +31,10 @@ extern "C" pq_status pq_attn_kv4_paged(pq_ctx* ctx, const pq_kv4_paged* c, const
   p.Hq = c->Hq, p.Hkv = c->Hkv, p.G = c->Hq / c->Hkv, p.n_prefix = c->n_prefix, p.max_new = max_new;
   const int64_t capacity = static_cast<int64_t>(p.max_pages) << p.page_log2;
   const int64_t bound = max_len > 0 && max_len < capacity ? max_len : capacity;
-  st = pq_paged_decode_launch(ctx, c, p, bound, ws, static_cast<cudaStream_t>(stream));
-  if (st != PQ_OK || max_new == 1) return st;
-  return pq_paged_prefill_launch(ctx, p, static_cast<uint8_t*>(ws) + pq_paged_decode_ws_bytes(ctx, c), static_cast<cudaStream_t>(stream));
+  // The kernel for several rows takes whole SMs and goes first; the one for single tokens, whose CTAs are small, starts beside it on the SMs that it leaves.
+  if (max_new > 1) {
+    st = pq_paged_prefill_launch(ctx, p, static_cast<uint8_t*>(ws) + pq_paged_decode_ws_bytes(ctx, c), static_cast<cudaStream_t>(stream));
+    if (st != PQ_OK) return st;
+  }
+  return pq_paged_decode_launch(ctx, c, p, bound, ws, static_cast<cudaStream_t>(stream));
 }

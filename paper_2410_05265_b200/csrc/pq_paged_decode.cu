@@ -1,7 +1,12 @@
 // Attention of single tokens (decode) over [full-precision prefix || paged 4-bit cache]: the sequences of a ragged batch that have one row.
 //
-// Bound by HBM in principle (128 bytes, with own steps 136, per key and KV head; the query heads of a group share them), by issue slots close behind:
-// a 16-key block costs about 220 instructions, so a chip that streams at full rate issues on two cycles of three.
+// Bound by HBM in principle (128 bytes, with own steps 136, per key and KV head; the query heads of a group share them), in practice by the ALU close behind: a
+// block of 32 keys costs about 580 warp instructions, a logic instruction for every two codes among them (45 - 54 % of that pipe, 43 - 51 % of the issue
+// slots). A long cache streams at 0.72 of the measured copy rate and a call costs 20 - 26 us besides (prefix sums 2, first blocks 3.5, a stretch's
+// pieces merged 2 - 6 each, the joined pairs 2, CTAs of an SM that end one after another). 48 ragged sequences to 6000 tokens, 32 heads on 8: 64 us
+// (own steps), 56 (static); 5 ragged to 50000, 64 heads: 60; one of 1021: 6.7.
+// Tried: rings of three and four blocks, five CTAs to an SM (no difference), multiplications for the shifts (slower), clusters of 1, 2 and 4 where 8 are
+// taken (2 % either way), longer stretches for the CTAs that an SM favours (2 - 5 % faster with eight heads to a group of four, 3 % slower with more).
 //
 // A worker is one CTA or a cluster of CTAs, four warps each. Work is counted in rounds of 128 keys of a (sequence, KV head) pair.
 //   one worker per pair (workers == 0): short caches, one wave of CTAs; the cluster merges on chip, the result is final.
@@ -107,11 +112,19 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
   const int csize = p.csize, worker = blockIdx.x / csize, rank = blockIdx.x % csize;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int G = p.G, page_log2 = p.page_log2;
-  pq::pdl_wait();
-  if (p.max_new > 1)  // the kernel for several rows follows, which only needs what this wait waited for
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  else
+  // Behind the kernel for several rows (max_new > 1) there is no wait here: that kernel lets this one start behind its own wait for what came before, and the
+  // two have nothing in common but what both read. So that it ends no earlier than the other, its last CTA waits when it is done (one is enough, and
+  // the others give their SMs free). What a wait would do for the SM's L1 the fence does: loads behind it see what was written before the launch.
+  const bool beside = p.max_new > 1;
+  if (beside) {
+    __threadfence();
+  } else {
+    pq::pdl_wait();
     pq::pdl_trigger();
+  }
+  auto leave = [&]() {
+    if (beside && blockIdx.x == gridDim.x - 1) pq::pdl_wait();
+  };
   if (lane == 0) {
     for (int s = 0; s < DP_SLOTS; ++s) pq::mbar_init(&full[warp][s], 1);
     pq::mbar_fence_init();
@@ -128,7 +141,7 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
     len_direct = clip_len(l);
     const int r0 = pq::ld_dep(p.q_begin + b_direct), r1 = pq::ld_dep(p.q_begin + b_direct + 1);
     if (threadIdx.x == 0 && (r1 - r0 > p.max_new || (l != len_direct && r1 > r0))) pq::report(p.status, PQ_ERR_SHAPE);
-    if (r1 - r0 != 1 || r0 < 0 || r0 >= p.n_rows) return;  // the whole cluster alike
+    if (r1 - r0 != 1 || r0 < 0 || r0 >= p.n_rows) return leave();  // the whole cluster alike
     row_direct = r0;
     u1 = max(1, (len_direct + DP_ROUND - 1) / DP_ROUND);
     __syncwarp();
@@ -146,10 +159,10 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
     const int64_t total = pq::block_scan<DP_THREADS>(scan, p.B, part) * p.Hkv;
     if (total > 0x7fffffffll) odd = true;  // (more keys than the chip's memory holds)
     if (odd && blockIdx.x == 0) pq::report(p.status, PQ_ERR_SHAPE);
-    if (total > 0x7fffffffll || total == 0) return;
+    if (total > 0x7fffffffll || total == 0) return leave();
     U = static_cast<int>(total);
     n_workers = min(p.workers, max(1, U / csize));  // at least a round to a CTA
-    if (worker >= n_workers) return;
+    if (worker >= n_workers) return leave();
     u0 = static_cast<int>(static_cast<int64_t>(U) * worker / n_workers);
     u1 = static_cast<int>(static_cast<int64_t>(U) * (worker + 1) / n_workers);
   }
@@ -632,6 +645,7 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
     if (timed_out) pq::report(p.status, PQ_ERR_TIMEOUT);
   }
   __syncwarp();
+  leave();
 }
 
 constexpr int DP_CTAS_PER_SM = 4;

@@ -26,7 +26,7 @@
 // 2048 on the tensor core and the 32768 exponentials 2048 on the four special-function units; both row tiles' exponentials overlap (2100), then follow the
 // vote on the reference and the store of the weights (700) and the wait for the products (1500). An item costs 10000 clocks more (queries, first
 // scores, prefix, output). Measured: 2048 rows x 64 heads behind 21952 keys 1473 us, 0.65 of the measured bf16 rate on the products of visible pairs (own
-// steps 1752), 4096 rows x 64 heads 357, 2048 rows 133, 4 ragged prompts up to 2000 x 32 heads 165 (own steps 190), 515 rows 25.
+// steps 1752), 4096 rows x 64 heads 354, 2048 rows 132, 4 ragged prompts up to 2000 x 32 heads 160 (own steps 185), 515 rows 25.
 // Tried and slower: a thread per row (own steps 2011 us: the constants of 64 keys per thread), half tiles of 64 keys with the scores of two in flight,
 // row tiles that form their weights in turn (1631; 1573 with half of the pass shared), queries of later items brought in by the expansion warps (the same),
 // eight expansion warps (their 48 registers spill).
@@ -308,10 +308,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     pq::tmem_alloc(&bars->tmem_base, PP_TMEM_COLS);
     pq::tmem_relinquish();
   }
-  // No wait here: this kernel always follows the one for single tokens, which lets it start behind its own wait for what came before, and the two have
-  // nothing in common but what both read. The wait is this kernel's last step, so that it ends no earlier than the other. What a wait would do for the
-  // SM's L1 the fence does: loads behind it see what was written before the launch.
-  __threadfence();
+  pq::pdl_wait();
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the kernel for single tokens follows, which only needs what this wait waited for
 
   // ---- the sequences: number of key tiles of all row tiles of one KV head, prefix sums, and where this worker's stretch begins
   const int64_t capacity = static_cast<int64_t>(p.max_pages) << p.page_log2;
@@ -1068,7 +1066,6 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     pq::tc_fence_after();
     pq::tmem_dealloc(tmem_base, PP_TMEM_COLS);
   }
-  pq::pdl_wait();
 }
 
 }  // namespace

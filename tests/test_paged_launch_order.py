@@ -1,4 +1,5 @@
 """The paged KV4 kernels under programmatic dependent launch, read from the sources, and the device check of their binding."""
+import os
 import re
 
 import pytest
@@ -6,7 +7,11 @@ import torch
 
 from paper_2410_05265_b200 import binding
 
-from test_launch_order import TRIGGER, kernel_body
+from test_launch_order import CSRC, TRIGGER, kernel_body
+
+
+def source(name):
+    return os.path.join(CSRC, name)
 
 
 @pytest.mark.parametrize("name", ["page_plan_kernel", "page_release_kernel"])
@@ -22,7 +27,7 @@ def test_the_append_never_triggers():
 
 @pytest.mark.parametrize("source,name", [
     ("pq_pages.cu", "page_plan_kernel"), ("pq_pages.cu", "page_release_kernel"), ("pq_qk_rope.cu", "qk_norm_rope_kernel"),
-    ("pq_qk_rope.cu", "kv4_paged_read_kernel"), ("pq_paged_decode.cu", "paged_decode_kernel"),
+    ("pq_qk_rope.cu", "kv4_paged_read_kernel"), ("pq_paged_prefill.cu", "paged_prefill_kernel"),
 ])
 def test_the_wait_comes_before_every_read_and_before_the_trigger(source, name):
     body = kernel_body(source, name)
@@ -34,15 +39,21 @@ def test_the_wait_comes_before_every_read_and_before_the_trigger(source, name):
     assert "__ldg(" not in body and "ld.global.nc" not in body
 
 
-def test_the_kernel_for_several_rows_waits_last_and_never_triggers():
-    """It starts behind the wait of the kernel for single tokens, which always precedes it, and must not end before that one."""
-    body = kernel_body("pq_paged_prefill.cu", "paged_prefill_kernel")
-    assert not TRIGGER.search(body) and body.count("pdl_wait") == 1
-    assert re.search(r"pq::pdl_wait\(\);\s*}$", body) and "__ldg(" not in body and "ld.global.nc" not in body
-    # in the wait's place a fence ahead of the first read
-    assert body.index("__threadfence()") < body.index("ld_dep(")
-    # no thread returns ahead of it: what returns are lambdas
-    assert len(re.findall(r"^  (?:if \(.*\) )?return;", body, re.M)) == 0
+def test_the_kernel_for_single_tokens_ends_behind_the_one_for_several_rows():
+    """Alone it waits before it reads anything. Behind the kernel for several rows, which always precedes it then, it reads without a wait of its own (a fence
+    in its place), never triggers, and its last CTA waits on every way out."""
+    body = kernel_body("pq_paged_decode.cu", "paged_decode_kernel")
+    start = re.search(r"if \(beside\) \{\s*__threadfence\(\);\s*\} else \{\s*pq::pdl_wait\(\);\s*pq::pdl_trigger\(\);\s*\}", body)
+    assert start and "const bool beside = p.max_new > 1;" in body[: start.start()]
+    first = re.search(r"ld_dep|__ldcg|\bbulk_load|atomicAdd|report\(", body)
+    assert start.end() < first.start() and "__ldg(" not in body and "ld.global.nc" not in body
+    assert len(TRIGGER.findall(body)) == 1
+    assert re.search(r"auto leave = \[&\]\(\) \{\s*if \(beside && blockIdx.x == gridDim.x - 1\) pq::pdl_wait\(\);\s*\};", body)
+    assert re.search(r"leave\(\);\s*}$", body)
+    assert body.count("return leave();") == 3 and re.findall(r"^ {2,4}(?:if \(.*\) )?return;", body, re.M) == ["    if (!is_ok) return;"]  # (a lambda's)
+    with open(source("pq_paged_attn.cu")) as f:
+        text = f.read()
+    assert text.index("pq_paged_prefill_launch(") < text.index("return pq_paged_decode_launch(")
 
 
 class _Elsewhere:
