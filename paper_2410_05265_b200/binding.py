@@ -174,13 +174,28 @@ def _ok(status: int, where: str):
         raise PQError(status, where)
 
 
-def _head_rows(t: torch.Tensor, dtype, N: int, H: int, D: int, name: str) -> int:
-    """Checks t [N, H, D] with dense heads and returns the elements between its rows; of a single row, whose stride says nothing, its width."""
-    if not t.is_cuda or t.dtype != dtype:
-        raise TypeError(f"{name} must be a CUDA tensor of dtype {dtype}")
+def _refuse(t: torch.Tensor, dtype, here: int, name: str, want):
+    _dev(t, dtype, name)
+    if t.get_device() != here:
+        raise ValueError(f"{name} is on {t.device} in a call to a context of cuda:{here}")
+    raise AssertionError(f"{name}: shape {tuple(t.shape)} with strides {t.stride()}, not {want}")
+
+
+# The two checks of the paged calls, whose host time is most of a small call: a device number in place of `is_cuda` and `device` (a tenth of
+# their time), the address returned.
+def _arr(t: torch.Tensor, dtype, shape: tuple, here: int, name: str) -> int:
+    """The address of t, a contiguous tensor of that shape on device `here`."""
+    if t.dtype != dtype or t.get_device() != here or t.shape != shape or not t.is_contiguous():
+        _refuse(t, dtype, here, name, f"{shape} and contiguous")
+    return t.data_ptr()
+
+
+def _heads(t: torch.Tensor, N: int, H: int, D: int, here: int, name: str):
+    """The address of t bf16 [N, H, D] with dense heads and the elements between its rows; of a single row, whose stride says nothing, its width."""
     row, head, one = t.stride()
-    assert t.shape == (N, H, D) and one == 1 and (H == 1 or head == D), name
-    return row if N > 1 else H * D
+    if t.dtype != torch.bfloat16 or t.get_device() != here or t.shape != (N, H, D) or one != 1 or (H > 1 and head != D):
+        _refuse(t, torch.bfloat16, here, name, f"{(N, H, D)} with dense heads")
+    return t.data_ptr(), row if N > 1 else H * D
 
 
 @functools.lru_cache(maxsize=64)
@@ -653,103 +668,95 @@ class Context:
                                         1 if rotate else 0, _stream()), "pq_rope_kv4_append")
 
     # ---- paged KV4 cache ------------------------------------------------------------------------
+    def _here(self) -> int:
+        """The context's device, which is the current one: its current stream is the one that is used."""
+        if torch._C._cuda_getDevice() != self.device:
+            raise ValueError(f"cuda:{torch._C._cuda_getDevice()} is current in a call to a context of cuda:{self.device}")
+        return self.device
+
     def page_plan(self, pages: Pages, n_new: torch.Tensor, n_rows: int | None = None, pos0: int = 0, out=None, len_out=None, n_free_out=None):
         """Pages, slots and positions of a step in which sequence b gets n_new[b] tokens; n_rows is the number of rows of the (padded) step.
         Returns (q_begin int32 [B + 1], slot int64 [n_rows], pos int32 [n_rows]), which may be given as `out`. The lengths and the count
         of free pages advance in place unless len_out, n_free_out are given."""
-        _dev(n_new, torch.int32, "n_new")
-        assert n_new.shape == (pages.B,) and n_new.is_contiguous()
+        here, B, s = self._here(), pages.B, pages.struct
         if out is None:
-            out = (torch.empty((pages.B + 1,), dtype=torch.int32, device=n_new.device), torch.empty((n_rows,), dtype=torch.int64, device=n_new.device),
+            out = (torch.empty((B + 1,), dtype=torch.int32, device=n_new.device), torch.empty((n_rows,), dtype=torch.int64, device=n_new.device),
                    torch.empty((n_rows,), dtype=torch.int32, device=n_new.device))
         q_begin, slot, pos = out
-        len_out, n_free_out = pages.length if len_out is None else len_out, pages.n_free if n_free_out is None else n_free_out
-        _dev(q_begin, torch.int32, "q_begin"), _dev(slot, torch.int64, "slot"), _dev(pos, torch.int32, "pos")
-        _dev(len_out, torch.int32, "len_out"), _dev(n_free_out, torch.int32, "n_free_out")
-        assert q_begin.shape == (pages.B + 1,) and slot.dim() == 1 and slot.shape == pos.shape and (n_rows is None or slot.shape[0] == n_rows)
-        assert len_out.shape == (pages.B,) and n_free_out.numel() == 1 and all(t.is_contiguous() for t in (q_begin, slot, pos, len_out))
-        self._here(pages.table, n_new, q_begin, slot, pos, len_out, n_free_out)
-        _ok(self.lib.pq_page_plan(self.h, ctypes.byref(pages.struct), _ptr(n_new), int(pos0), slot.shape[0], _ptr(q_begin), _ptr(slot), _ptr(pos),
-                                  _ptr(len_out), _ptr(n_free_out), _stream()), "pq_page_plan")
+        rows = slot.numel()
+        assert n_rows is None or rows == n_rows, "n_rows"
+        _ok(self.lib.pq_page_plan(self.h, ctypes.byref(s), _arr(n_new, torch.int32, (B,), here, "n_new"), int(pos0), rows,
+                                  _arr(q_begin, torch.int32, (B + 1,), here, "q_begin"), _arr(slot, torch.int64, (rows,), here, "slot"),
+                                  _arr(pos, torch.int32, (rows,), here, "pos"),
+                                  s.len if len_out is None else _arr(len_out, torch.int32, (B,), here, "len_out"),
+                                  s.n_free if n_free_out is None else _arr(n_free_out, torch.int32, (1,), here, "n_free_out"),
+                                  torch._C._cuda_getCurrentRawStream(here)), "pq_page_plan")
         return out
 
     def page_release(self, pages: Pages, done: torch.Tensor, len_out=None, n_free_out=None) -> None:
         """The pages of the sequences with done[b] != 0 (int32 [B]) go back to the free list; lengths and count change in place by default."""
-        len_out, n_free_out = pages.length if len_out is None else len_out, pages.n_free if n_free_out is None else n_free_out
-        _dev(done, torch.int32, "done"), _dev(len_out, torch.int32, "len_out"), _dev(n_free_out, torch.int32, "n_free_out")
-        assert done.shape == (pages.B,) == len_out.shape and done.is_contiguous() and len_out.is_contiguous() and n_free_out.numel() == 1
-        self._here(pages.table, done, len_out, n_free_out)
-        _ok(self.lib.pq_page_release(self.h, ctypes.byref(pages.struct), _ptr(done), _ptr(len_out), _ptr(n_free_out), _stream()), "pq_page_release")
-
-    def _here(self, *tensors):
-        """The tensors of a call live on the context's device, which is the current one: its stream is the one that is used."""
-        here = self.device
-        if torch._C._cuda_getDevice() != here:
-            raise ValueError(f"cuda:{torch._C._cuda_getDevice()} is current in a call to a context of cuda:{here}")
-        for t in tensors:
-            if t is not None and t.get_device() != here:  # (t.device.index takes five times as long)
-                raise ValueError(f"a tensor on {t.device} in a call to a context of cuda:{here}")
+        here, B, s = self._here(), pages.B, pages.struct
+        _ok(self.lib.pq_page_release(self.h, ctypes.byref(s), _arr(done, torch.int32, (B,), here, "done"),
+                                     s.len if len_out is None else _arr(len_out, torch.int32, (B,), here, "len_out"),
+                                     s.n_free if n_free_out is None else _arr(n_free_out, torch.int32, (1,), here, "n_free_out"),
+                                     torch._C._cuda_getCurrentRawStream(here)), "pq_page_release")
 
     @staticmethod
-    def _rope_args(N, gq, gk, pos, sections):
-        """(axes, distance of the axes, sections) as the C calls take them; pos int32 [N] or [axes, N]."""
-        _dev(pos, torch.int32, "pos")
-        assert (gq is None) == (gk is None)
+    def _rope_args(N, gq, gk, pos, sections, here):
+        """(gq, gk, pos, axes, distance of the axes, sections) as the C calls take them; pos int32 [N] or [axes, N]."""
+        assert (gq is None) == (gk is None), "gq without gk"
         if gq is not None:
-            _dev(gq, torch.bfloat16, "gq"), _dev(gk, torch.bfloat16, "gk")
-            assert gq.shape == gk.shape == (128,) and gq.is_contiguous() and gk.is_contiguous()
+            gq, gk = _arr(gq, torch.bfloat16, (128,), here, "gq"), _arr(gk, torch.bfloat16, (128,), here, "gk")
         shape, stride = pos.shape, pos.stride()
         axes = 1 if len(shape) == 1 else shape[0]
-        assert shape[-1] == N and (N <= 1 or stride[-1] == 1) and len(shape) <= 2
+        if pos.dtype != torch.int32 or pos.get_device() != here or len(shape) > 2 or shape[-1] != N or (N > 1 and stride[-1] != 1):
+            _refuse(pos, torch.int32, here, "pos", f"[{N}] or [axes, {N}], dense")
         if sections is not None:
-            assert len(sections) == axes
+            assert len(sections) == axes, "sections"
             sections = _sections(tuple(sections))
-        return axes, N if axes == 1 else stride[0], sections
+        return gq, gk, pos.data_ptr(), axes, N if axes == 1 else stride[0], sections
 
     def qk_norm_rope(self, x: torch.Tensor, Hq: int, gq, gk, eps: float, pos: torch.Tensor, theta: float, sections=None, rotate: bool = False,
                      out: torch.Tensor | None = None):
         """RMSNorm of every head (gains gq for the first Hq heads of x [N, H, 128], gk for the others; both None: no norm), rotary embedding with the
         positions pos int32 [N] or [axes, N] (frequencies dealt to the axes by `sections`), with rotate=True followed by R3. out may be x."""
+        here = self._here()
         N, H, D = x.shape
-        ld = _head_rows(x, torch.bfloat16, N, H, D, "x")
-        axes, ld_pos, sec = self._rope_args(N, gq, gk, pos, sections)
+        x_at, ld = _heads(x, N, H, D, here, "x")
         if out is None:
             out = torch.empty((N, H, D), dtype=x.dtype, device=x.device)
-        ld_out = _head_rows(out, torch.bfloat16, N, H, D, "out")
-        self._here(x, gq, gk, pos, out)
-        _ok(self.lib.pq_qk_norm_rope(self.h, _ptr(x), N, int(Hq), H - int(Hq), D, ld, _ptr(gq), _ptr(gk), float(eps), _ptr(pos), axes, ld_pos,
-                                     sec, float(theta), 1 if rotate else 0, _ptr(out), ld_out, _stream()), "pq_qk_norm_rope")
+        out_at, ld_out = _heads(out, N, H, D, here, "out")
+        gq, gk, pos, axes, ld_pos, sec = self._rope_args(N, gq, gk, pos, sections, here)
+        _ok(self.lib.pq_qk_norm_rope(self.h, x_at, N, int(Hq), H - int(Hq), D, ld, gq, gk, float(eps), pos, axes, ld_pos, sec, float(theta),
+                                     1 if rotate else 0, out_at, ld_out, torch._C._cuda_getCurrentRawStream(here)), "pq_qk_norm_rope")
         return out
 
     def qk_norm_rope_kv4_paged_append(self, cache: KV4PagedCache, qkv: torch.Tensor, gq, gk, eps: float, pos: torch.Tensor, slot: torch.Tensor,
                                       theta: float, sections=None, rotate: bool = False, q_out: torch.Tensor | None = None):
         """qk_norm_rope of a projection output qkv [N, (Hq + 2 Hkv) * 128]: the query heads to q_out [N, Hq, 128] (returned), the key and value
         heads, quantized, to the slots of the paged cache. Rows with slot -1 are neither read nor written."""
-        _dev(qkv, torch.bfloat16, "qkv"), _dev(slot, torch.int64, "slot")
+        here = self._here()
         N, cols = qkv.shape
         ld, one = qkv.stride()
-        assert one == 1 and cols == (cache.Hq + 2 * cache.Hkv) * cache.D
-        assert slot.shape == (N,) and slot.is_contiguous()
-        axes, ld_pos, sec = self._rope_args(N, gq, gk, pos, sections)
+        if qkv.dtype != torch.bfloat16 or qkv.get_device() != here or one != 1 or cols != (cache.Hq + 2 * cache.Hkv) * cache.D:
+            _refuse(qkv, torch.bfloat16, here, "qkv", f"[N, {(cache.Hq + 2 * cache.Hkv) * cache.D}], dense rows")
         if q_out is None:
             q_out = torch.empty((N, cache.Hq, cache.D), dtype=qkv.dtype, device=qkv.device)
-        ld_out = _head_rows(q_out, torch.bfloat16, N, cache.Hq, cache.D, "q_out")
-        self._here(cache.codes, qkv, gq, gk, pos, slot, q_out)
-        _ok(self.lib.pq_qk_norm_rope_kv4_paged_append(self.h, ctypes.byref(cache.struct), _ptr(qkv), N, ld if N > 1 else cols, _ptr(gq), _ptr(gk), float(eps),
-                                                      _ptr(pos), axes, ld_pos, sec, float(theta), 1 if rotate else 0, _ptr(slot), _ptr(q_out),
-                                                      ld_out, _stream()), "pq_qk_norm_rope_kv4_paged_append")
+        out_at, ld_out = _heads(q_out, N, cache.Hq, cache.D, here, "q_out")
+        gq, gk, pos, axes, ld_pos, sec = self._rope_args(N, gq, gk, pos, sections, here)
+        _ok(self.lib.pq_qk_norm_rope_kv4_paged_append(self.h, ctypes.byref(cache.struct), qkv.data_ptr(), N, ld if N > 1 else cols, gq, gk, float(eps), pos,
+                                                      axes, ld_pos, sec, float(theta), 1 if rotate else 0, _arr(slot, torch.int64, (N,), here, "slot"),
+                                                      out_at, ld_out, torch._C._cuda_getCurrentRawStream(here)), "pq_qk_norm_rope_kv4_paged_append")
         return q_out
 
     def kv4_paged_read(self, cache: KV4PagedCache, slot: torch.Tensor, out: torch.Tensor | None = None):
         """Keys and values at the given slots as a reader of the cache finds them, bf16 [N, 2, Hkv, 128]; rows with slot -1 keep what out holds."""
-        _dev(slot, torch.int64, "slot")
-        N = slot.shape[0]
+        here, N = self._here(), slot.numel()
         if out is None:
             out = torch.zeros((N, 2, cache.Hkv, cache.D), dtype=torch.bfloat16, device=slot.device)
-        _dev(out, torch.bfloat16, "out")
-        assert slot.dim() == 1 and slot.is_contiguous() and out.shape == (N, 2, cache.Hkv, cache.D) and out.is_contiguous()
-        self._here(cache.codes, slot, out)
-        _ok(self.lib.pq_kv4_paged_read(self.h, ctypes.byref(cache.struct), _ptr(slot), N, _ptr(out), _stream()), "pq_kv4_paged_read")
+        _ok(self.lib.pq_kv4_paged_read(self.h, ctypes.byref(cache.struct), _arr(slot, torch.int64, (N,), here, "slot"), N,
+                                       _arr(out, torch.bfloat16, (N, 2, cache.Hkv, cache.D), here, "out"), torch._C._cuda_getCurrentRawStream(here)),
+            "pq_kv4_paged_read")
         return out
 
     def attn_kv4_paged_workspace(self, cache: KV4PagedCache, n_rows: int, max_new: int) -> torch.Tensor:
@@ -759,18 +766,16 @@ class Context:
     def attn_kv4_paged(self, cache: KV4PagedCache, q: torch.Tensor, q_begin: torch.Tensor, max_new: int, sm_scale: float, ws: torch.Tensor,
                        max_len: int = 0, out: torch.Tensor | None = None):
         """Causal attention of the rows q [N, Hq, 128] of a ragged batch (sequence b: rows q_begin[b] .. q_begin[b + 1] - 1, its last tokens) over
-        [prefix || paged cache]. max_new bounds the rows of a sequence, max_len (0: the capacity) the lengths; rows behind the last stay as they are."""
-        _dev(q_begin, torch.int32, "q_begin"), _dev(ws, torch.uint8, "ws")
-        N = q.shape[0]
-        ldq = _head_rows(q, torch.bfloat16, N, cache.Hq, cache.D, "q")
-        assert q_begin.shape == (cache.pages.B + 1,) and q_begin.is_contiguous()
+        [prefix || paged cache]. max_new bounds the rows of a sequence, max_len (0: the capacity) the lengths; rows behind the last stay as they are.
+        out may be q."""
+        here, N = self._here(), q.shape[0]
+        q_at, ldq = _heads(q, N, cache.Hq, cache.D, here, "q")
         if out is None:
             out = torch.zeros((N, cache.Hq, cache.D), dtype=q.dtype, device=q.device)
-        _dev(out, torch.bfloat16, "out")
-        assert out.shape == q.shape and out.is_contiguous()
-        self._here(cache.codes, q, q_begin, ws, out)
-        _ok(self.lib.pq_attn_kv4_paged(self.h, ctypes.byref(cache.struct), _ptr(q), ldq, _ptr(q_begin), N, int(max_new), int(max_len), _ptr(out),
-                                       float(sm_scale), _ptr(ws), ws.numel(), _stream()), "pq_attn_kv4_paged")
+        n_ws = ws.numel()
+        _ok(self.lib.pq_attn_kv4_paged(self.h, ctypes.byref(cache.struct), q_at, ldq, _arr(q_begin, torch.int32, (cache.pages.B + 1,), here, "q_begin"), N,
+                                       int(max_new), int(max_len), _arr(out, torch.bfloat16, (N, cache.Hq, cache.D), here, "out"), float(sm_scale),
+                                       _arr(ws, torch.uint8, (n_ws,), here, "ws"), n_ws, torch._C._cuda_getCurrentRawStream(here)), "pq_attn_kv4_paged")
         return out
 
     # ---- transformer-block glue -----------------------------------------------------------------

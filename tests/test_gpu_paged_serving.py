@@ -124,6 +124,37 @@ def test_steps_of_a_server(ctx, steps, page, Hq, Hkv, n_prefix, rotate):
     ctx.check()
 
 
+def test_the_binding_refuses(ctx):
+    """Shapes, types, strides and places that the calls do not take are refused before anything is launched."""
+    cache = ref.make_cache([20, 5], 4, 2, 16, seed=4)
+    pg, q, begin = cache.pages, ref.queries(3, 4), i32([0, 2, 3])
+    ws = ctx.attn_kv4_paged_workspace(cache, 3, 2)
+    qkv, slot, pos, (gq, gk) = projection(3, 4, 2, 1), torch.arange(3, device=DEV), i32([0, 1, 2]), gains(2)
+    out = (i32([0] * 3), torch.zeros(3, dtype=torch.int64, device=DEV), i32([0] * 3))
+    attn = lambda **k: ctx.attn_kv4_paged(**{**dict(cache=cache, q=q, q_begin=begin, max_new=2, sm_scale=SCALE, ws=ws), **k})
+    rope = lambda **k: ctx.qk_norm_rope(**{**dict(x=q, Hq=4, gq=gq, gk=gk, eps=1e-5, pos=pos, theta=1e4), **k})
+    append = lambda **k: ctx.qk_norm_rope_kv4_paged_append(**{**dict(cache=cache, qkv=qkv, gq=gq, gk=gk, eps=1e-5, pos=pos, slot=slot, theta=1e4), **k})
+    plan = lambda **k: ctx.page_plan(**{**dict(pages=pg, n_new=i32([1, 2]), out=out), **k})
+    state = [t.clone() for t in (cache.codes, pg.table, pg.length, pg.n_free, q)]
+    for call in (lambda: attn(q=q.half()), lambda: attn(q=q.cpu()), lambda: attn(q_begin=begin.long()), lambda: attn(ws=ws.int()), lambda: attn(out=q.float()),
+                 lambda: rope(x=q.float()), lambda: rope(pos=pos.long()), lambda: rope(gq=gq.float()), lambda: rope(out=q.cpu()), lambda: append(qkv=qkv.half()),
+                 lambda: append(slot=pos), lambda: append(q_out=q.float()), lambda: plan(n_new=slot[:2]), lambda: plan(out=(out[0], pos, out[2])),
+                 lambda: ctx.page_release(pg, slot[:2]), lambda: ctx.kv4_paged_read(cache, pos), lambda: plan(n_new=i32([1, 2]).cpu())):
+        with pytest.raises(TypeError):
+            call()
+    wide = torch.zeros((3, 8, D), dtype=torch.bfloat16, device=DEV)
+    for call in (lambda: attn(q=wide), lambda: attn(q=wide[:, ::2]), lambda: attn(q_begin=begin[:2]), lambda: attn(out=wide[:, :4]), lambda: attn(out=q[:2]),
+                 lambda: rope(pos=pos[:2]), lambda: rope(gq=gq[:64]), lambda: rope(gk=None), lambda: rope(gq=None), lambda: rope(pos=i32([0] * 6)[::2]),
+                 lambda: rope(pos=i32([[0] * 3] * 2), sections=[64]), lambda: rope(out=q[:2]), lambda: append(qkv=qkv[:, :-128]), lambda: append(slot=slot[:2]),
+                 lambda: append(slot=torch.arange(6, device=DEV)[::2]), lambda: append(q_out=wide), lambda: plan(n_new=i32([1])), lambda: plan(n_rows=4),
+                 lambda: plan(len_out=i32([0])), lambda: plan(n_free_out=i32([0, 0])), lambda: ctx.page_release(pg, i32([1])),
+                 lambda: ctx.kv4_paged_read(cache, slot, out=wide)):
+        with pytest.raises(AssertionError):
+            call()
+    ctx.check()
+    assert all(torch.equal(a, b) for a, b in zip(state, (cache.codes, pg.table, pg.length, pg.n_free, q)))
+
+
 class Loop:
     """One step of token-by-token serving on fixed buffers."""
 

@@ -56,24 +56,33 @@ def test_the_kernel_for_single_tokens_ends_behind_the_one_for_several_rows():
     assert text.index("pq_paged_prefill_launch(") < text.index("return pq_paged_decode_launch(")
 
 
-class _Elsewhere:
-    device = torch.device("cuda:1")
-
-    def get_device(self):
-        return 1
-
-
 def test_tensors_of_another_device_and_another_current_device_are_refused(monkeypatch):
     ctx = binding.Context.__new__(binding.Context)
     ctx.device = 0
     current = [0]
     monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: current[0], raising=False)
-    here = type("Here", (_Elsewhere,), {"get_device": lambda self: 0})()
-    ctx._here(here, None)
+    assert ctx._here() == 0
+
+    class Fake:
+        """An int32 vector that says it is on cuda:`at`."""
+        dtype, is_cuda, shape, device = torch.int32, True, torch.Size([4]), "cuda"
+        at = 0
+        get_device = lambda self: self.at
+        is_contiguous = lambda self: True
+        stride = lambda self: (1,)
+        data_ptr = lambda self: 64
+
+    here, there = Fake(), Fake()
+    there.at = 1
+    assert binding._arr(here, torch.int32, (4,), 0, "t") == 64
     with pytest.raises(ValueError):
-        ctx._here(here, _Elsewhere())
-    with pytest.raises(ValueError):
-        ctx._here(torch.zeros(1))
+        binding._arr(there, torch.int32, (4,), 0, "t")
+    with pytest.raises(TypeError):
+        binding._arr(torch.zeros(4, dtype=torch.int32), torch.int32, (4,), 0, "t")
+    with pytest.raises(TypeError):
+        binding._arr(here, torch.int64, (4,), 0, "t")
+    with pytest.raises(AssertionError):
+        binding._arr(here, torch.int32, (5,), 0, "t")
     current[0] = 1
     with pytest.raises(ValueError):
-        ctx._here(here)
+        ctx._here()
