@@ -227,15 +227,17 @@ def test_two_graphs_share_a_workspace(ctx, steps):
         assert all(torch.equal(x, y) for x, y in zip(a.state(), s.state()))
 
 
-def test_two_contexts_on_two_streams(ctx):
+@pytest.mark.parametrize("which", [(0, 1), (2, 2), (1, 2)])
+def test_two_contexts_on_two_streams(ctx, which):
     other = binding.Context()
-    ref_loops, loops = [Loop(ctx, "vector", *s) for s in SERVED[:2]], [Loop(c, "vector", *s) for c, s in zip((ctx, other), SERVED[:2])]
+    served = [SERVED[w] for w in which]
+    ref_loops, loops = [Loop(ctx, "vector", *s) for s in served], [Loop(c, "vector", *s) for c, s in zip((ctx, other), served)]
     for l in ref_loops:
-        for _ in range(6):
+        for _ in range(5):
             l.step()
     torch.cuda.synchronize()
     streams = [torch.cuda.Stream() for _ in loops]
-    for _ in range(6):
+    for _ in range(5):
         for l, s in zip(loops, streams):
             with torch.cuda.stream(s):
                 l.step()
