@@ -255,9 +255,6 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
     else
       next_piece();
   };
-  next_piece();
-  for (int s = 0; s < DP_SLOTS; ++s) issue();
-
   // What a piece needs first, requested while the piece before it is merged: 8 dims of a query head (sixteen threads to a head) and the steps.
   Piece x = first_piece();
   int row = 0;
@@ -271,6 +268,8 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
     s_k_h = DYN ? 1.0f : pq::ld_dep(p.s_k + x.h), s_v_h = DYN ? 1.0f : pq::ld_dep(p.s_v + x.h);
   };
   request();
+  next_piece();
+  for (int s = 0; s < DP_SLOTS; ++s) issue();
   int n_shared = 0;  // pairs this worker shares with others: its first and its last
   for (int u = u0; u < u1;) {
     const int kend = min(x.len, x.r1 * DP_ROUND);
@@ -703,17 +702,18 @@ pq_status pq_paged_decode_launch(pq_ctx* ctx, const pq_kv4_paged* c, PagedAttnPa
   // Few pairs share the chip: a cluster of CTAs to a pair or stretch keeps the partials that meet in the workspace few.
   int64_t csize = most / pairs;
   csize = csize >= 8 ? 8 : csize >= 4 ? 4 : csize >= 2 ? 2 : 1;
-  // One worker per pair or equal stretches, by an estimate for sequences of max_len tokens: a round of a CTA takes 0.6 us and 0.45 us for every CTA on its
-  // SM; equal stretches fill the SMs (1.95 us a round) but cost 10 us more (prefix sums, a second piece, the merge through the workspace). us, one
-  // worker per pair / equal stretches: 1 sequence x 6000 tokens x 8 KV heads 12 / 18, 5 x 5000 14.7 / 26, 5 x 10000 22.9 / 32.5, 5 x 20000 38.8 / 43.1,
-  // 5 ragged to 50000 69 / 58, 48 ragged to 6000 70 / 56.
+  // One worker per pair or equal stretches, by an estimate for sequences of max_len tokens: a round of a CTA takes 0.75 us and 0.45 us for every CTA on its
+  // SM, the call 6 us besides; equal stretches fill the SMs (2.1 us a round) but cost 20 us (prefix sums, a second piece, the merge through the
+  // workspace). us, one worker per pair / equal stretches, 8 KV heads: 1 sequence x 6000 tokens 12.3 / 21.2, x 12000 19.0 / 25.2, x 20000 27.6 / 27.5,
+  // x 60000 75 / 37; 4 x 12000 23.7 / 34.1, x 20000 34.6 / 40.8, x 35000 53.6 / 53.0, x 60000 86 / 75; 16 x 8000 44.8 / 54.0; 30 x 3000 35.6 / 44.6;
+  // 60 x 3000 61.5 / 64.8; 5 ragged to 50000 69 / 58, 48 ragged to 6000 70 / 56.
   int64_t one = csize;
   while (one > 1 && one > rounds) one >>= 1;
   bool direct = pairs <= resident_workers(ctx, kern, dyn, static_cast<int>(one), dynamic_smem(dyn, p.G, p.n_prefix, 0));
   if (direct) {
     const double sms = ctx->sm_count, per_sm = pairs * one > ctx->sm_count ? pairs * one / sms : 1.0;
-    const double t_one = static_cast<double>((rounds + one - 1) / one) * (0.6 + 0.45 * per_sm);
-    const double t_equal = 10.0 + 1.95 * static_cast<double>(pairs * rounds) / (DP_CTAS_PER_SM * sms);
+    const double t_one = static_cast<double>((rounds + one - 1) / one) * (0.75 + 0.45 * per_sm) + 6.0;
+    const double t_equal = 20.0 + 2.1 * static_cast<double>(pairs * rounds) / (DP_CTAS_PER_SM * sms);
     direct = t_one <= t_equal;
   }
   if (direct) csize = one;
