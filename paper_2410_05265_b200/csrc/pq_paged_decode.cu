@@ -39,7 +39,6 @@ constexpr int DP_ROWS = 8;     // query heads per KV head the MMA tile carries
 constexpr int DP_SO_STRIDE = 136;
 constexpr float DP_HEADROOM = 15.0f;  // log2 units: weights stay below 2^16, inside fp16
 constexpr int DP_SLOTS = 2;           // staged blocks per warp
-constexpr int DP_MAX_CLUSTER = 8;
 
 // Bytes of a staging slot: 32 rows of keys, 32 rows of values, with own steps 32 + 32 floats.
 __host__ __device__ constexpr int slot_bytes(bool dyn) { return DP_BLOCK * 128 + (dyn ? DP_BLOCK * 8 : 0); }
@@ -89,7 +88,8 @@ __device__ __forceinline__ void store_out(__nv_bfloat16* dst, const float4& a, f
   *reinterpret_cast<uint2*>(dst) = v;
 }
 
-template <bool DYN>
+// WIDE: clusters of sixteen, for a few long sequences (their merge in the other kernel would cost it registers).
+template <bool DYN, bool WIDE>
 __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const PagedAttnParams p) {
   constexpr int SLOT = slot_bytes(DYN);
   extern __shared__ __align__(128) uint8_t dp_smem[];
@@ -548,24 +548,30 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
       for (int item = rank * DP_THREADS + threadIdx.x; item < G * 32; item += csize * DP_THREADS) {
         const int r = item >> 5, c4 = item & 31;
         const uint32_t o_addr = pq::smem_u32(cl_o + r * DP_SO_STRIDE + 4 * c4), ml_addr = pq::smem_u32(cl_ml + r);
-        float4 v[DP_MAX_CLUSTER];
-        float2 ml[DP_MAX_CLUSTER];
-#pragma unroll
-        for (int sp = 0; sp < DP_MAX_CLUSTER; ++sp) {
-          v[sp] = make_float4(0.0f, 0.0f, 0.0f, 0.0f), ml[sp] = make_float2(-INFINITY, 0.0f);
-          if (sp < csize) v[sp] = ld_cluster_f4(map_cta(o_addr, sp)), ml[sp] = ld_cluster_f2(map_cta(ml_addr, sp));
-        }
-        float m = -INFINITY;
-#pragma unroll
-        for (int sp = 0; sp < DP_MAX_CLUSTER; ++sp) m = fmaxf(m, ml[sp].x);
+        float m = -INFINITY, l = 0.0f;
         float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        float l = 0.0f;
+        auto eight = [&](int sp0) {
+          float4 v[8];
+          float2 ml[8];
 #pragma unroll
-        for (int sp = 0; sp < DP_MAX_CLUSTER; ++sp) {
-          const float w = ml[sp].x == -INFINITY ? 0.0f : pq::ex2_approx(ml[sp].x - m);
-          acc.x = fmaf(v[sp].x, w, acc.x), acc.y = fmaf(v[sp].y, w, acc.y), acc.z = fmaf(v[sp].z, w, acc.z), acc.w = fmaf(v[sp].w, w, acc.w);
-          l = fmaf(ml[sp].y, w, l);
-        }
+          for (int k = 0; k < 8; ++k) {
+            v[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f), ml[k] = make_float2(-INFINITY, 0.0f);
+            if (sp0 + k < csize) v[k] = ld_cluster_f4(map_cta(o_addr, sp0 + k)), ml[k] = ld_cluster_f2(map_cta(ml_addr, sp0 + k));
+          }
+          float mn = m;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) mn = fmaxf(mn, ml[k].x);
+          const float keep = m == -INFINITY ? 0.0f : pq::ex2_approx(m - mn);
+          acc.x *= keep, acc.y *= keep, acc.z *= keep, acc.w *= keep, l *= keep, m = mn;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float w = ml[k].x == -INFINITY ? 0.0f : pq::ex2_approx(ml[k].x - m);
+            acc.x = fmaf(v[k].x, w, acc.x), acc.y = fmaf(v[k].y, w, acc.y), acc.z = fmaf(v[k].z, w, acc.z), acc.w = fmaf(v[k].w, w, acc.w);
+            l = fmaf(ml[k].y, w, l);
+          }
+        };
+        eight(0);
+        if (WIDE) eight(8);
         if (whole) {
           store_out(dst + r * 128 + 4 * c4, acc, l > 0.0f ? 1.0f / l : 0.0f);
         } else {
@@ -649,13 +655,18 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
 
 constexpr int DP_CTAS_PER_SM = 4;
 
+void (*kernel_of(bool dyn, int csize))(const PagedAttnParams) {
+  if (csize > 8) return dyn ? paged_decode_kernel<true, true> : paged_decode_kernel<false, true>;
+  return dyn ? paged_decode_kernel<true, false> : paged_decode_kernel<false, false>;
+}
+
 int most_ctas(const pq_ctx* ctx) { return DP_CTAS_PER_SM * ctx->sm_count; }
 
 // Clusters of csize CTAs that are resident at once: fewer than the CTAs alone would be, since a cluster stays inside a group of SMs. Asked once per
 // device, kernel, cluster size and size class of the shared memory.
-int resident_workers(const pq_ctx* ctx, void (*kern)(const PagedAttnParams), bool dyn, int csize, size_t smem) {
-  static std::atomic<int> known[64][2][4][32] = {};
-  const int size_class = static_cast<int>((smem + 8191) / 8192), ci = csize == 8 ? 3 : csize == 4 ? 2 : csize == 2 ? 1 : 0;
+int resident_workers(const pq_ctx* ctx, bool dyn, int csize, size_t smem) {
+  static std::atomic<int> known[64][2][5][32] = {};
+  const int size_class = static_cast<int>((smem + 8191) / 8192), ci = csize == 16 ? 4 : csize == 8 ? 3 : csize == 4 ? 2 : csize == 2 ? 1 : 0;
   std::atomic<int>& slot = known[ctx->device][dyn][ci][size_class < 32 ? size_class : 31];
   int n = slot.load(std::memory_order_relaxed);
   if (n > 0) return n;
@@ -668,9 +679,9 @@ int resident_workers(const pq_ctx* ctx, void (*kern)(const PagedAttnParams), boo
   attr[0].val.clusterDim.x = csize, attr[0].val.clusterDim.y = 1, attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n < 1) {
+  if (cudaOccupancyMaxActiveClusters(&n, kernel_of(dyn, csize), &cfg) != cudaSuccess || n < 1) {
     cudaGetLastError();
-    n = ctx->sm_count / csize;
+    n = csize > 8 ? 0 : ctx->sm_count / csize;  // (clusters of more than eight need not fit at all)
   }
   if (n > most_ctas(ctx) / csize) n = most_ctas(ctx) / csize;
   slot.store(n, std::memory_order_relaxed);
@@ -685,13 +696,14 @@ size_t pq_paged_decode_ws_bytes(const pq_ctx* ctx, const pq_kv4_paged* c) {
 
 pq_status pq_paged_decode_launch(pq_ctx* ctx, const pq_kv4_paged* c, PagedAttnParams p, int64_t max_len, void* ws, cudaStream_t st) {
   const bool dyn = p.steps != nullptr;
-  void (*const kern)(const PagedAttnParams) = dyn ? paged_decode_kernel<true> : paged_decode_kernel<false>;
   // the largest there is, once per device and kernel
   static std::atomic<bool> attr_set[64][2] = {};
   if (ctx->device < 0 || ctx->device >= 64) return PQ_ERR_UNSUPPORTED;
   if (!attr_set[ctx->device][dyn].load(std::memory_order_relaxed)) {
     const int most = static_cast<int>(dynamic_smem(dyn, DP_ROWS, PQ_PAGED_MAX_PREFIX, PQ_PAGED_MAX_SEQS));
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess) {
+    if (cudaFuncSetAttribute(kernel_of(dyn, 1), cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess ||
+        cudaFuncSetAttribute(kernel_of(dyn, 16), cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess ||
+        cudaFuncSetAttribute(kernel_of(dyn, 16), cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
       cudaGetLastError();
       return PQ_ERR_CUDA;
     }
@@ -707,9 +719,12 @@ pq_status pq_paged_decode_launch(pq_ctx* ctx, const pq_kv4_paged* c, PagedAttnPa
   // workspace). us, one worker per pair / equal stretches, 8 KV heads: 1 sequence x 6000 tokens 12.3 / 21.2, x 12000 19.0 / 25.2, x 20000 27.6 / 27.5,
   // x 60000 75 / 37; 4 x 12000 23.7 / 34.1, x 20000 34.6 / 40.8, x 35000 53.6 / 53.0, x 60000 86 / 75; 16 x 8000 44.8 / 54.0; 30 x 3000 35.6 / 44.6;
   // 60 x 3000 61.5 / 64.8; 5 ragged to 50000 69 / 58, 48 ragged to 6000 70 / 56.
+  const size_t smem_one = dynamic_smem(dyn, p.G, p.n_prefix, 0);
   int64_t one = csize;
   while (one > 1 && one > rounds) one >>= 1;
-  bool direct = pairs <= resident_workers(ctx, kern, dyn, static_cast<int>(one), dynamic_smem(dyn, p.G, p.n_prefix, 0));
+  // us with clusters of 8 / 16, 1 sequence of 2100 tokens (17 rounds) 8.3 / 8.9, 4000 10.7 / 9.7, 6000 12.3 / 11.1, 12000 18.9 / 15.0, 20000 27.1 / 20.0.
+  if (one == 8 && rounds >= 24 && pairs * 16 <= ctx->sm_count && pairs <= resident_workers(ctx, dyn, 16, smem_one)) one = 16;
+  bool direct = pairs <= resident_workers(ctx, dyn, static_cast<int>(one), smem_one);
   if (direct) {
     const double sms = ctx->sm_count, per_sm = pairs * one > ctx->sm_count ? pairs * one / sms : 1.0;
     const double t_one = static_cast<double>((rounds + one - 1) / one) * (0.75 + 0.45 * per_sm) + 6.0;
@@ -719,10 +734,10 @@ pq_status pq_paged_decode_launch(pq_ctx* ctx, const pq_kv4_paged* c, PagedAttnPa
   if (direct) csize = one;
   const size_t smem = dynamic_smem(dyn, p.G, p.n_prefix, direct ? 0 : p.B);
   p.csize = static_cast<int32_t>(csize);
-  p.workers = direct ? 0 : resident_workers(ctx, kern, dyn, p.csize, smem);
+  p.workers = direct ? 0 : resident_workers(ctx, dyn, p.csize, smem);
   if (p.workers > PQ_PAGED_MAX_WORKERS) p.workers = PQ_PAGED_MAX_WORKERS;
   p.ws_o = static_cast<float*>(ws);
   p.ws_ml = p.ws_o + static_cast<size_t>(2) * p.workers * p.G * 128;
   const int64_t grid = (direct ? pairs : p.workers) * csize;
-  return pq_launch_cluster_pdl(kern, dim3(static_cast<unsigned>(grid)), DP_THREADS, smem, p.csize, st, p);
+  return pq_launch_cluster_pdl(kernel_of(dyn, p.csize), dim3(static_cast<unsigned>(grid)), DP_THREADS, smem, p.csize, st, p);
 }

@@ -334,6 +334,21 @@ def test_the_output_may_be_the_queries(ctx, steps, lengths, new, Hq, Hkv):
 
 
 @pytest.mark.parametrize("steps", ["head", "vector"])
+@pytest.mark.parametrize("lengths,bound,Hq,Hkv,n_prefix", [([5000], 0, 8, 8, 4), ([12000], 12000, 32, 8, 1), ([3200, 5000], 0, 16, 4, 0), ([0], 6000, 8, 1, 64), ([1], 6000, 8, 1, 0),
+                                                           ([130, 4097], 9000, 14, 2, 5), ([9, 700, 33], 4000, 3, 3, 2)])
+def test_few_long_sequences(ctx, steps, lengths, bound, Hq, Hkv, n_prefix):
+    """Wide clusters to a (sequence, KV head), most of whose CTAs may have nothing to do."""
+    cache = ref.make_cache(lengths, Hq, Hkv, 16, steps, n_prefix, seed=11, width=max(ref.up(max(lengths + [bound]), 16), 1))
+    B = len(lengths)
+    q, begin = ref.queries(B, Hq), list(range(B + 1))
+    out = ctx.attn_kv4_paged(cache, q, i32(begin), 1, SCALE, ctx.attn_kv4_paged_workspace(cache, B, 1), max_len=bound)
+    again = ctx.attn_kv4_paged(cache, q, i32(begin), 1, SCALE, ctx.attn_kv4_paged_workspace(cache, B, 1), max_len=bound)
+    ctx.check()
+    want, tol = ref.attention(cache, q, begin, lengths, SCALE)
+    assert ((out.double() - want).abs() <= tol).all() and torch.equal(out, again)
+
+
+@pytest.mark.parametrize("steps", ["head", "vector"])
 @pytest.mark.parametrize("ragged", [False, True])
 def test_the_largest_batch(ctx, steps, ragged):
     """8192 sequences of a few tokens, single rows or several; a sample of them against the definition."""
