@@ -46,6 +46,15 @@ __device__ __forceinline__ float lg2_approx(float x) {
   asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// Own steps: the exponent of a weight carries log2 of the value's step, w = 2^(s + log2 step - m), and the denominator is the sum of w / step. Steps may lie 2^120
+// apart, and a key whose weight is 2^-120 of the largest still belongs in the denominator. So w is formed PQ_UP octaves up (2^(15 + 60) at most), where fp32
+// reaches down to 2^-186 of the reference, 1 / step is kept PQ_UP octaves down (no product leaves fp32), and what goes to the products is
+// w 2^-PQ_UP. What is lost of the denominator lies 2^-50 below the rest of it.
+constexpr float PQ_UP = 60.0f, PQ_DOWN = 0x1p-60f;
+// x 2^d for d <= 0, the denominator moved to another reference: in two factors, since references may then lie further apart than fp32 reaches.
+__device__ __forceinline__ float at_reference(float x, float d) {
+  return x * ex2_approx(fmaxf(d, -120.0f)) * ex2_approx(fminf(d + 120.0f, 0.0f));
+}
 // (a & M) ^ C in one LOP3; the constants are immediates
 template <uint32_t M, uint32_t C>
 __device__ __forceinline__ uint32_t and_xor(uint32_t a) {

@@ -24,7 +24,7 @@
 //   softmax  in log2 units against a reference exponent per head that moves only when a score exceeds it by more than DP_HEADROOM
 //   output   O^T = V^T P^T with the fp16 MMA, head dims on the 16-row side, codes + 8 as above; one more MMA over codes of zero gives what the offset adds
 //            and, for static steps, the denominator, both from the same rounded P. Own steps: the exponent of a weight takes log2 of the value's step with it, w = 2^(s + log2 step - m), so
-//            that fp16 holds the largest of what enters the sum whatever the steps are; the denominator is the sum of w / step in fp32.
+//            that fp16 holds the largest of what enters the sum whatever the steps are; the denominator is the sum of w / step in fp32 (PQ_UP).
 #include <atomic>
 
 #include "pq_paged_attn.cuh"
@@ -374,7 +374,7 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
         break;
       }
       const uint8_t* const slot = stage + s * SLOT;
-      float rs[2][2];  // DYN: 1 / step of the values of keys g, g + 8
+      float rs[2][2];  // DYN: 2^-PQ_UP / step of the values of keys g, g + 8
       float c[2][4];  // scores: [0], [1] = key g x heads 2t, 2t+1; [2], [3] = key g + 8 x the same heads
       if (DYN) {
         // lane j turns the steps of key j into what all lanes need, once: (step of the key, log2 and reciprocal of the step of the value); a key past the
@@ -382,7 +382,7 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
         const float* st = reinterpret_cast<const float*>(slot + DP_BLOCK * 128) + lane;
         const float k_step = st[0], v_step = st[DP_BLOCK];
         const bool dead = key0 + lane >= kend;
-        sm_step[warp][lane] = dead ? make_float4(0.0f, -INFINITY, 0.0f, 0.0f) : make_float4(k_step, pq::lg2_approx(v_step), pq::rcp_approx(v_step), 0.0f);
+        sm_step[warp][lane] = dead ? make_float4(0.0f, -INFINITY, 0.0f, 0.0f) : make_float4(k_step, pq::lg2_approx(v_step), pq::rcp_approx(v_step) * pq::PQ_DOWN, 0.0f);
         __syncwarp();
       }
 #pragma unroll
@@ -423,10 +423,11 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
           x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, d));
         }
         const float n0 = fmaxf(m0, x0), n1 = fmaxf(m1, x1);
-        const float a_lo = n0 == -INFINITY ? 1.0f : pq::ex2_approx(m0 - n0), a_hi = n1 == -INFINITY ? 1.0f : pq::ex2_approx(m1 - n1);
+        const float d_lo = n0 == -INFINITY ? 0.0f : m0 - n0, d_hi = n1 == -INFINITY ? 0.0f : m1 - n1;
+        const float a_lo = pq::ex2_approx(d_lo), a_hi = pq::ex2_approx(d_hi);
         m0 = n0, m1 = n1;
         zero[0] *= a_lo, zero[1] *= a_hi, zero[2] *= a_lo, zero[3] *= a_hi;
-        den0 *= a_lo, den1 *= a_hi;
+        if (DYN) den0 = pq::at_reference(den0, d_lo), den1 = pq::at_reference(den1, d_hi);
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[i][0] *= a_lo, o[i][1] *= a_hi, o[i][2] *= a_lo, o[i][3] *= a_hi;
         z0 = m0 == -INFINITY ? 0.0f : m0, z1 = m1 == -INFINITY ? 0.0f : m1;
@@ -436,10 +437,11 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
         const uint8_t* vb = slot + DP_BLOCK * 64 + v * 1024 + v_off;
         const uint2 vc0 = *reinterpret_cast<const uint2*>(vb), vc1 = *reinterpret_cast<const uint2*>(vb + 64);
         const uint2 vc2 = *reinterpret_cast<const uint2*>(vb + 8 * 64), vc3 = *reinterpret_cast<const uint2*>(vb + 9 * 64);
-        const float w0 = pq::ex2_approx(c[v][0] - z0), w1 = pq::ex2_approx(c[v][1] - z1);
-        const float w2 = pq::ex2_approx(c[v][2] - z0), w3 = pq::ex2_approx(c[v][3] - z1);
+        const float zu0 = DYN ? z0 - pq::PQ_UP : z0, zu1 = DYN ? z1 - pq::PQ_UP : z1, down = DYN ? pq::PQ_DOWN : 1.0f;
+        const float w0 = pq::ex2_approx(c[v][0] - zu0), w1 = pq::ex2_approx(c[v][1] - zu1);
+        const float w2 = pq::ex2_approx(c[v][2] - zu0), w3 = pq::ex2_approx(c[v][3] - zu1);
         // weights in fp16, transposed from (key, head pair) to the (key pair, head) layout of an MMA B operand
-        const uint32_t pb0 = movmatrix_trans(pq::pack_f16(w0, w1)), pb1 = movmatrix_trans(pq::pack_f16(w2, w3));
+        const uint32_t pb0 = movmatrix_trans(pq::pack_f16(w0 * down, w1 * down)), pb1 = movmatrix_trans(pq::pack_f16(w2 * down, w3 * down));
         if (DYN) {
           den0 = fmaf(w0, rs[v][0], den0), den1 = fmaf(w1, rs[v][0], den1);
           den0 = fmaf(w2, rs[v][1], den0), den1 = fmaf(w3, rs[v][1], den1);
@@ -517,7 +519,7 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
           const float* src = sm_o + (w * G + r) * DP_SO_STRIDE + qpos;
           const float2 lo = *reinterpret_cast<const float2*>(src), hi = *reinterpret_cast<const float2*>(src + 16);
           acc.x = fmaf(lo.x, e, acc.x), acc.y = fmaf(lo.y, e, acc.y), acc.z = fmaf(hi.x, e, acc.z), acc.w = fmaf(hi.y, e, acc.w);
-          l = fmaf(sm_ml[w][r][1], e, l);
+          l = DYN ? l + pq::at_reference(sm_ml[w][r][1], mw == -INFINITY ? mw : mw - m) : fmaf(sm_ml[w][r][1], e, l);
         }
         acc.x *= value_unit, acc.y *= value_unit, acc.z *= value_unit, acc.w *= value_unit;
         auto add_prefix = [&](int j, const uint2& v) {
@@ -562,12 +564,13 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
 #pragma unroll
           for (int k = 0; k < 8; ++k) mn = fmaxf(mn, ml[k].x);
           const float keep = m == -INFINITY ? 0.0f : pq::ex2_approx(m - mn);
-          acc.x *= keep, acc.y *= keep, acc.z *= keep, acc.w *= keep, l *= keep, m = mn;
+          l = DYN ? pq::at_reference(l, m == -INFINITY ? m : m - mn) : l * keep;
+          acc.x *= keep, acc.y *= keep, acc.z *= keep, acc.w *= keep, m = mn;
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
             const float w = ml[k].x == -INFINITY ? 0.0f : pq::ex2_approx(ml[k].x - m);
             acc.x = fmaf(v[k].x, w, acc.x), acc.y = fmaf(v[k].y, w, acc.y), acc.z = fmaf(v[k].z, w, acc.z), acc.w = fmaf(v[k].w, w, acc.w);
-            l = fmaf(ml[k].y, w, l);
+            l = DYN ? l + pq::at_reference(ml[k].y, ml[k].x == -INFINITY ? ml[k].x : ml[k].x - m) : fmaf(ml[k].y, w, l);
           }
         };
         eight(0);
@@ -624,10 +627,10 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
           for (int d = 1; d < 32; d <<= 1) mc = fmaxf(mc, __shfl_xor_sync(0xffffffffu, mc, d));
           const float mn = fmaxf(m, mc), keep = m == -INFINITY ? 0.0f : pq::ex2_approx(m - mn);
           const float w = ml.x == -INFINITY ? 0.0f : pq::ex2_approx(ml.x - mn);
-          float lw = ml.y * w;
+          float lw = DYN ? pq::at_reference(ml.y, ml.x == -INFINITY ? ml.x : ml.x - mn) : ml.y * w;
 #pragma unroll
           for (int d = 1; d < 32; d <<= 1) lw += __shfl_xor_sync(0xffffffffu, lw, d);
-          l = l * keep + lw;
+          l = (DYN ? pq::at_reference(l, m == -INFINITY ? m : m - mn) : l * keep) + lw;
           m = mn;
           acc.x *= keep, acc.y *= keep, acc.z *= keep, acc.w *= keep;
           auto add = [&](const float4& v, int k) {

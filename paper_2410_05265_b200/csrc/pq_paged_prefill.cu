@@ -16,7 +16,7 @@
 //   softmax warps    eight per row tile, four for each half of the key columns. A thread has two columns of every eight of four rows (the fragment layout of
 //                    tcgen05.ld 16x256b), so that what is read per key serves four rows. The exponent of a weight takes log2 of the value's
 //                    step with it, w = 2^(s + log2 step - m): O is in value units, fp16 holds the largest of what enters the sum whatever
-//                    the steps are, the denominator is the sum of w / step in fp32. Weights are formed in one pass against the
+//                    the steps are, the denominator is the sum of w / step in fp32 (PQ_UP). Weights are formed in one pass against the
 //                    reference m so far; it moves, and the pass is repeated, only when an exponent exceeds it by more than 15.
 // Roundings to fewer bits: w to fp16 (2^-11; below 2^-14 in steps of 2^-25 of the largest weight's scale), the result to bf16.
 // Inside every group of eight head dims the expansion leaves the order 0,4,1,5,2,6,3,7; Q and the prefix rows are stored in the same order and the output
@@ -79,7 +79,7 @@ struct PpBarriers {
   uint32_t pair_out[2][4];   // [row tile][rows / 32]: a warp of these rows has given up
   float row[2][2][PP_ROWS];  // [row tile][set]: what the two threads of a row tell each other
 };
-struct PpSteps {  // of pairs of keys: (key step x scale, of both, log2 of the value step, of both) and (1 / value step, of both)
+struct PpSteps {  // of pairs of keys: (key step x scale, of both, log2 of the value step, of both) and (2^-PQ_UP / value step, of both)
   float4 key[PP_KEYS / 2];
   float2 inv[PP_KEYS / 2];
 };
@@ -571,7 +571,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             const float m_use = m_ref[k] == -INFINITY ? 0.0f : m_ref[k];
-            off[k] = DYN ? -m_use : add - m_use, top[k] = -INFINITY, l2[k] = make_float2(0.0f, 0.0f);
+            off[k] = DYN ? pq::PQ_UP - m_use : add - m_use, top[k] = -INFINITY, l2[k] = make_float2(0.0f, 0.0f);
           }
           auto form = [&](auto chunks) {  // the weights of so many times sixteen columns
             uint32_t rr[2][8];
@@ -626,9 +626,9 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
                   for (int y = 0; y < 2; ++y) {
                     const float2 x2 = ex[2 * n + y];
                     top[2 * hf + y] = max3f(top[2 * hf + y], x2.x, x2.y);
-                    const float2 w = make_float2(pq::ex2_approx(x2.x), pq::ex2_approx(x2.y));
+                    float2 w = make_float2(pq::ex2_approx(x2.x), pq::ex2_approx(x2.y));
                     if (DYN)
-                      l2[2 * hf + y] = __ffma2_rn(w, inv[n], l2[2 * hf + y]);
+                      l2[2 * hf + y] = __ffma2_rn(w, inv[n], l2[2 * hf + y]), w = __fmul2_rn(w, make_float2(pq::PQ_DOWN, pq::PQ_DOWN));
                     else
                       l2[2 * hf + y] = __fadd2_rn(l2[2 * hf + y], w);
                     pk[hf][4 * cc + 2 * n + y] = pq::pack_f16(w.x, w.y);
@@ -644,7 +644,10 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
           if (again) break;
           bool over = false;
 #pragma unroll
-          for (int k = 0; k < 4; ++k) over |= top[k] > (m_ref[k] == -INFINITY ? -INFINITY : PP_LAZY);
+          for (int k = 0; k < 4; ++k) {
+            if (DYN) top[k] -= pq::PQ_UP;
+            over |= top[k] > (m_ref[k] == -INFINITY ? -INFINITY : PP_LAZY);
+          }
           if (!pair_any(over)) break;
           if (*pair_out) {
             ok = false;
@@ -665,7 +668,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
             const bool first = m_ref[k] == -INFINITY, grow = most > (first ? -INFINITY : PP_LAZY);
             const float m_new = grow ? ceilf((first ? 0.0f : m_ref[k]) + most) : m_ref[k];
             alpha[k] = grow ? pq::ex2_approx(m_ref[k] - m_new) : 1.0f;  // 2^(-inf) = 0 for a row that had seen nothing
-            l[k] *= alpha[k];
+            l[k] = DYN && grow ? pq::at_reference(l[k], m_ref[k] - m_new) : l[k] * alpha[k];
             m_ref[k] = m_new;
           }
           if (jt > x.j0) {  // S_i of this tile is complete, so O_i += P V of the tile before is, too
@@ -798,9 +801,9 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
           for (int k = 0; k < 4; ++k)
             ml[k] = w0 + k <= sh.w1 ? __ldcg(reinterpret_cast<const float2*>(p.ws_ml) + slot_of(w0 + k) * 256 + my) : make_float2(-INFINITY, 0.0f);
           const float mn = fmaxf(m, fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)));
-          l = m == -INFINITY ? 0.0f : l * pq::ex2_approx(m - mn);
+          l = m == -INFINITY ? 0.0f : DYN ? pq::at_reference(l, m - mn) : l * pq::ex2_approx(m - mn);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) l = ml[k].x == -INFINITY ? l : fmaf(ml[k].y, pq::ex2_approx(ml[k].x - mn), l);
+          for (int k = 0; k < 4; ++k) l = ml[k].x == -INFINITY ? l : DYN ? l + pq::at_reference(ml[k].y, ml[k].x - mn) : fmaf(ml[k].y, pq::ex2_approx(ml[k].x - mn), l);
           m = mn;
         }
         const float m_use = m == -INFINITY ? 0.0f : m, norm = l > 0.0f ? 1.0f / l : 0.0f;
@@ -901,7 +904,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
             const float k_step = in ? st[tid_e] : 1.0f, v_step = in ? st[PP_KEYS + tid_e] : 1.0f;
             float* key_out = reinterpret_cast<float*>(&steps_buf[stage].key[tid_e >> 1]) + (tid_e & 1);
             key_out[0] = k_step * p.scale2, key_out[2] = pq::lg2_approx(v_step);
-            reinterpret_cast<float*>(steps_buf[stage].inv)[tid_e] = pq::rcp_approx(v_step);
+            reinterpret_cast<float*>(steps_buf[stage].inv)[tid_e] = pq::rcp_approx(v_step) * pq::PQ_DOWN;
           }
           pq::fence_proxy_async_smem();  // generic-proxy writes -> visible to the tensor core's async proxy
           __syncwarp();
