@@ -17,8 +17,10 @@
 //                    tcgen05.ld 16x256b), so that what is read per key serves four rows. The exponent of a weight takes log2 of the value's
 //                    step with it, w = 2^(s + log2 step - m): O is in value units, fp16 holds the largest of what enters the sum whatever
 //                    the steps are, the denominator is the sum of w / step in fp32 (PQ_UP). Weights are formed in one pass against the
-//                    reference m so far; it moves, and the pass is repeated, only when an exponent exceeds it by more than 15.
-// Roundings to fewer bits: w to fp16 (2^-11; below 2^-14 in steps of 2^-25 of the largest weight's scale), the result to bf16.
+//                    reference m so far; it moves, and the pass is repeated, only when an exponent exceeds it by more than 15 (and at an item's second
+//                    tile where that lies far below, PP_LOW).
+// Roundings to fewer bits: w to fp16 (2^-11; below 2^-14 in steps of 2^-24 of the reference's weight), the result to bf16. The denominator is the sum of the weights before
+// their rounding.
 // Inside every group of eight head dims the expansion leaves the order 0,4,1,5,2,6,3,7; Q and the prefix rows are stored in the same order and the output
 // columns are put back when they are written. Every wait is bounded.
 //
@@ -53,6 +55,10 @@ constexpr int PP_TMEM_COLS = 512;     // S0 | S1 | O0 | O1, 128 columns each; ea
 constexpr int PP_ITEM_UNITS = 4;    // units of work that an item costs besides its key tiles (queries, prefix, output: 9 us; a tile 2.4)
 constexpr int PP_SHORT = 8;         // an item of so many key tiles or fewer is not shared between workers
 constexpr float PP_LAZY = 15.0f;      // log2 units an exponent may exceed the reference before it is moved: weights stay inside fp16
+// A prefixed key may draw nearly all of the weight while its value is small: what the other weights keep of their bits is then what the output keeps. So where the
+// largest exponent of an item's second tile lies more than PP_LOW below the reference, the reference goes down to it, by PP_FAR at most (the sums, in fp32, grow by
+// that). Tried instead: the reference 8 or 10 below the largest exponent always, which moves again and again (4 ragged prompts 191 -> 226 and 242 us).
+constexpr float PP_LOW = 10.0f, PP_FAR = 40.0f;
 // Registers: 768 threads at 80; the softmax warpgroups take 96, the others leave 48 (512 x 96 + 256 x 48 = 768 x 80).
 constexpr int PP_REGS_SOFTMAX = 96, PP_REGS_OTHERS = 48;
 constexpr int PP_HALF_KEYS = PP_KEYS / 2;  // key columns of a softmax thread
@@ -648,6 +654,13 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
             if (DYN) top[k] -= pq::PQ_UP;
             over |= top[k] > (m_ref[k] == -INFINITY ? -INFINITY : PP_LAZY);
           }
+          if (x.j0 == 0 && jt == 1)  // (of the row's columns of this set)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              float t = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 1));
+              t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
+              over |= t < -PP_LOW && t != -INFINITY;
+            }
           if (!pair_any(over)) break;
           if (*pair_out) {
             ok = false;
@@ -665,10 +678,10 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             const float most = fmaxf(top[k], *const_cast<const volatile float*>(&bars->row[i][set ^ 1][fr + 8 * k]));
-            const bool first = m_ref[k] == -INFINITY, grow = most > (first ? -INFINITY : PP_LAZY);
-            const float m_new = grow ? ceilf((first ? 0.0f : m_ref[k]) + most) : m_ref[k];
-            alpha[k] = grow ? pq::ex2_approx(m_ref[k] - m_new) : 1.0f;  // 2^(-inf) = 0 for a row that had seen nothing
-            l[k] = DYN && grow ? pq::at_reference(l[k], m_ref[k] - m_new) : l[k] * alpha[k];
+            const bool first = m_ref[k] == -INFINITY, move = most > (first ? -INFINITY : PP_LAZY) || (most < -PP_LOW && most != -INFINITY && jt == 1 && x.j0 == 0);
+            const float m_new = move ? ceilf(first ? most : m_ref[k] + fmaxf(most, -PP_FAR)) : m_ref[k];
+            alpha[k] = move ? pq::ex2_approx(m_ref[k] - m_new) : 1.0f;  // 2^(-inf) = 0 for a row that had seen nothing
+            l[k] = DYN && move ? pq::at_reference(l[k], m_ref[k] - m_new) : l[k] * alpha[k];
             m_ref[k] = m_new;
           }
           if (jt > x.j0) {  // S_i of this tile is complete, so O_i += P V of the tile before is, too

@@ -1,5 +1,6 @@
-"""Attention over the paged cache where one key outweighs the others: value steps at the two ends of their range in one sequence. Scores are set exactly: queries
-and keys have their first dim only, a key's score in log2 units is minus its step."""
+"""Attention over the paged cache where one key outweighs the others: value steps at the two ends of their range in one sequence, and a key that draws
+nearly all of the weight and whose value is small (what the prefixed tokens are). Scores are set exactly: queries and keys have their first dim only, a
+key's score in log2 units is minus its step."""
 import math
 
 import pytest
@@ -77,3 +78,43 @@ def test_value_steps_at_both_ends_of_their_range(ctx, lengths, new, Hq, Hkv, whe
     want, tol = ref.attention(cache, q, begin, lengths, LN2)
     bad = ~((out.double() - want).abs() <= tol)
     assert not bad.any(), f"{int(bad.sum())} of {bad.numel()}"
+
+
+@pytest.mark.parametrize("steps", ["head", "vector"])
+@pytest.mark.parametrize("above", [3.0, 12.3, 18.4, 21.7, 23.4, 30.0])
+@pytest.mark.parametrize("lengths,new,Hq,Hkv", [([1000], [1], 8, 2), ([9000, 700], [1, 1], 16, 2), ([700], [300], 8, 2), ([9000, 200, 40], [40, 200, 1], 8, 1),
+                                                ([130, 2, 129], [130, 2, 129], 4, 4)])
+@pytest.mark.parametrize("n_prefix", [1, 20])
+def test_a_prefixed_key_that_draws_nearly_all_of_the_weight(ctx, lengths, new, Hq, Hkv, n_prefix, above, steps):
+    """Its value is zero and its score `above` log2 units over all others, which are equal: what comes out is theirs, times 2^-above.
+
+    With p the softmax in 64 bits, a relative error e of the weights moves the quotient by at most e (sum p |v| + |out|): e is 2^-11 for the rounding to fp16, where the
+    cached keys' weights are normal numbers, and 2^-20 for the exponent. The other prefixed keys share the large one's reference, of whose weight theirs are rounded to
+    multiples of 2^-24 (it is 1 at most): each is off by 2^-25 of its p at most. The single-token kernel multiplies with code + 8 and takes 8 sum(p) off, in fp32 sums
+    of equal terms: each of the 16 products of a step and the sum so far is off by 2^-23 of 8 p per key, 17 x 8 x 2^-23 sum(p) of the largest step in all.
+    The store rounds by 2^-8."""
+    cache = cache_of(lengths, Hq, Hkv, steps, n_prefix)
+    if steps == "vector":
+        cache.steps[:, :, 0] = 2.0**-60
+    else:
+        cache.codes[:, :, 0] = 0
+    cache.prefix_k.zero_(), cache.prefix_v[:, 0].zero_()
+    cache.prefix_k[:, 0, 0] = above
+    q, begin, out = attend(ctx, cache, new)
+    want, _ = ref.attention(cache, q, begin, lengths, LN2)
+    tol = torch.zeros_like(want)
+    for b, n_keys in enumerate(lengths):
+        ids = cache.pages.table[b, : ref.up(n_keys, 16)].long()
+        step = cache.steps[ids].double()[..., None] if steps == "vector" else torch.stack((cache.s_k, cache.s_v), 1).double()[None, :, :, None, None]
+        v = (ref.unpack(cache.codes[ids]).double() * step)[:, :, 1].permute(1, 0, 2, 3).reshape(Hkv, -1, D)[:, :n_keys]
+        v = torch.cat((cache.prefix_v.double(), v), 1).abs()
+        unit = cache.steps[:, :, 1].max().double() if steps == "vector" else cache.s_v.max().double()
+        for t in range(new[b]):
+            seen = n_keys - new[b] + t + 1
+            p = 1.0 / (2.0 ** float(cache.prefix_k[0, 0, 0]) + n_prefix - 1 + seen)  # of each key but the one
+            r = begin[b] + t
+            a = (p * v[:, : n_prefix + seen].sum(1))[:, None].expand(-1, Hq // Hkv, -1).reshape(Hq, D)
+            near = 2.0**-25 * 2.0 ** float(cache.prefix_k[0, 0, 0]) * p * cache.prefix_v.double().abs().sum(1)
+            tol[r] = near[:, None].expand(-1, Hq // Hkv, -1).reshape(Hq, D) + (2.0**-11 + 2.0**-20) * (a + want[r].abs()) + 17 * 8 * 2.0**-23 * seen * p * unit + want[r].abs() * 2.0**-8 + 2.0**-125
+    bad = ~((out.double() - want).abs() <= tol)
+    assert not bad.any(), f"{int(bad.sum())} of {bad.numel()}; worst {float(((out.double() - want).abs() / tol).max())} of the tolerance"
