@@ -43,10 +43,12 @@ constexpr int DP_SLOTS = 2;           // staged blocks per warp
 // Bytes of a staging slot: 32 rows of keys, 32 rows of values, with own steps 32 + 32 floats.
 __host__ __device__ constexpr int slot_bytes(bool dyn) { return DP_BLOCK * 128 + (dyn ? DP_BLOCK * 8 : 0); }
 // Dynamic shared memory: staging, the warps' partial outputs, prefix scores, and (equal stretches) rounds and lengths of the sequences.
-size_t dynamic_smem(bool dyn, int G, int n_prefix, int seqs) {
+constexpr size_t dynamic_smem(bool dyn, int G, int n_prefix, int seqs) {
   return DP_WARPS * DP_SLOTS * slot_bytes(dyn) + static_cast<size_t>(DP_WARPS) * G * DP_SO_STRIDE * 4 + static_cast<size_t>(G) * n_prefix * 4 +
          (seqs > 0 ? (3 * static_cast<size_t>(seqs) + 1) * 4 : 0);
 }
+constexpr size_t smem_kb(size_t bytes) { return (bytes + 1023) / 1024; }
+constexpr size_t DP_MAX_KB = smem_kb(dynamic_smem(true, DP_ROWS, PQ_PAGED_MAX_PREFIX, PQ_PAGED_MAX_SEQS));
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -666,17 +668,17 @@ void (*kernel_of(bool dyn, int csize))(const PagedAttnParams) {
 int most_ctas(const pq_ctx* ctx) { return DP_CTAS_PER_SM * ctx->sm_count; }
 
 // Clusters of csize CTAs that are resident at once: fewer than the CTAs alone would be, since a cluster stays inside a group of SMs. Asked once per
-// device, kernel, cluster size and size class of the shared memory.
+// device, kernel, cluster size and size of the shared memory in whole KB: the answer, and with it how the work is split, follows from the call alone.
 int resident_workers(const pq_ctx* ctx, bool dyn, int csize, size_t smem) {
-  static std::atomic<int> known[64][2][5][32] = {};
-  const int size_class = static_cast<int>((smem + 8191) / 8192), ci = csize == 16 ? 4 : csize == 8 ? 3 : csize == 4 ? 2 : csize == 2 ? 1 : 0;
-  std::atomic<int>& slot = known[ctx->device][dyn][ci][size_class < 32 ? size_class : 31];
+  static std::atomic<uint16_t> known[64][2][5][DP_MAX_KB + 1] = {};  // one more than the answer
+  const int ci = csize == 16 ? 4 : csize == 8 ? 3 : csize == 4 ? 2 : csize == 2 ? 1 : 0;
+  std::atomic<uint16_t>& slot = known[ctx->device][dyn][ci][smem_kb(smem)];
   int n = slot.load(std::memory_order_relaxed);
-  if (n > 0) return n;
+  if (n > 0) return n - 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(most_ctas(ctx) / csize * csize);
   cfg.blockDim = dim3(DP_THREADS);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = smem_kb(smem) * 1024;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = csize, attr[0].val.clusterDim.y = 1, attr[0].val.clusterDim.z = 1;
@@ -687,7 +689,7 @@ int resident_workers(const pq_ctx* ctx, bool dyn, int csize, size_t smem) {
     n = csize > 8 ? 0 : ctx->sm_count / csize;  // (clusters of more than eight need not fit at all)
   }
   if (n > most_ctas(ctx) / csize) n = most_ctas(ctx) / csize;
-  slot.store(n, std::memory_order_relaxed);
+  slot.store(static_cast<uint16_t>(n + 1), std::memory_order_relaxed);
   return n;
 }
 
@@ -703,7 +705,7 @@ pq_status pq_paged_decode_launch(pq_ctx* ctx, const pq_kv4_paged* c, PagedAttnPa
   static std::atomic<bool> attr_set[64][2] = {};
   if (ctx->device < 0 || ctx->device >= 64) return PQ_ERR_UNSUPPORTED;
   if (!attr_set[ctx->device][dyn].load(std::memory_order_relaxed)) {
-    const int most = static_cast<int>(dynamic_smem(dyn, DP_ROWS, PQ_PAGED_MAX_PREFIX, PQ_PAGED_MAX_SEQS));
+    const int most = static_cast<int>(DP_MAX_KB * 1024);
     if (cudaFuncSetAttribute(kernel_of(dyn, 1), cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess ||
         cudaFuncSetAttribute(kernel_of(dyn, 16), cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess ||
         cudaFuncSetAttribute(kernel_of(dyn, 16), cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
