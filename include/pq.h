@@ -398,7 +398,8 @@ pq_status pq_kv4_paged_read(pq_ctx* ctx, const pq_kv4_paged* cache, const int64_
  *     out[row, g, :] = softmax_j(q[row, g, :] . K_j * sm_scale) . V      (zeros where nothing is visible)
  *   q        bf16 [n_rows, Hq, 128] with ldq elements between rows (a multiple of 8), out bf16 [n_rows, Hq, 128] dense, both 16-byte aligned; out
  *            may be q (ldq = Hq * 128), else they must not overlap
- *   q_begin  int32 [B + 1], ascending, on the device; rows from q_begin[B] on (padding) are neither read nor written
+ *   q_begin  int32 [B + 1], ascending, on the device; rows from q_begin[B] on (padding) are neither read nor written. Sequences with rows outside
+ *            [0, n_rows), or that end before they begin, are left out and PQ_ERR_SHAPE is reported
  *   max_new  at least the largest n (a host bound); sequences with more rows are left out and PQ_ERR_SHAPE is reported
  *   max_len  at least the largest len (a host bound that only chooses how the work is split; 0: the capacity max_pages * page)
  *   ws       scratch of pq_attn_kv4_paged_workspace_bytes(ctx, cache, n_rows, max_new) bytes, 16-byte aligned

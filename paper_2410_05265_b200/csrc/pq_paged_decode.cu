@@ -90,6 +90,13 @@ __device__ __forceinline__ void store_out(__nv_bfloat16* dst, const float4& a, f
   *reinterpret_cast<uint2*>(dst) = v;
 }
 
+// The rows r0 .. r1 - 1 of a sequence: is it this kernel's, and is it one that has to be reported (the rule of the kernel for several rows).
+__device__ __forceinline__ bool one_row(const PagedAttnParams& p, int r0, int r1) { return r0 >= 0 && r0 < p.n_rows && r1 == r0 + 1; }
+__device__ __forceinline__ bool odd_rows(const PagedAttnParams& p, int r0, int r1, bool bad_len) {
+  const int64_t n = static_cast<int64_t>(r1) - r0;
+  return n > p.max_new || n < 0 || (n > 0 && (r0 < 0 || r1 > p.n_rows || bad_len));
+}
+
 // WIDE: clusters of sixteen, for a few long sequences (their merge in the other kernel would cost it registers).
 template <bool DYN, bool WIDE>
 __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const PagedAttnParams p) {
@@ -142,8 +149,8 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
     const int l = pq::ld_dep(p.len + b_direct);
     len_direct = clip_len(l);
     const int r0 = pq::ld_dep(p.q_begin + b_direct), r1 = pq::ld_dep(p.q_begin + b_direct + 1);
-    if (threadIdx.x == 0 && (r1 - r0 > p.max_new || (l != len_direct && r1 > r0))) pq::report(p.status, PQ_ERR_SHAPE);
-    if (r1 - r0 != 1 || r0 < 0 || r0 >= p.n_rows) return leave();  // the whole cluster alike
+    if (threadIdx.x == 0 && odd_rows(p, r0, r1, l != len_direct)) pq::report(p.status, PQ_ERR_SHAPE);
+    if (!one_row(p, r0, r1)) return leave();  // the whole cluster alike
     row_direct = r0;
     u1 = max(1, (len_direct + DP_ROUND - 1) / DP_ROUND);
     __syncwarp();
@@ -152,10 +159,9 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
     for (int b = threadIdx.x; b < p.B; b += DP_THREADS) {
       const int l = pq::ld_dep(p.len + b), lc = clip_len(l);
       const int r0 = pq::ld_dep(p.q_begin + b), r1 = pq::ld_dep(p.q_begin + b + 1);
-      const bool mine = r1 - r0 == 1 && r0 >= 0 && r0 < p.n_rows;
-      odd |= r1 - r0 > p.max_new || (l != lc && r1 > r0);
+      odd |= odd_rows(p, r0, r1, l != lc);
       lens[b] = lc, rows[b] = r0;
-      scan[b] = mine ? max(1, (lc + DP_ROUND - 1) / DP_ROUND) : 0;
+      scan[b] = one_row(p, r0, r1) ? max(1, (lc + DP_ROUND - 1) / DP_ROUND) : 0;
     }
     __syncthreads();
     const int64_t total = pq::block_scan<DP_THREADS>(scan, p.B, part) * p.Hkv;

@@ -1,4 +1,5 @@
-"""Calls of the paged KV4 entry points that are easily got wrong: results that must not depend on which shapes a process ran before."""
+"""Calls of the paged KV4 entry points that are easily got wrong: row ranges outside the queries, and results that must not depend on which
+shapes a process ran before."""
 import hashlib
 import math
 import os
@@ -14,7 +15,42 @@ import paged_ref as ref
 from test_gpu_paged import i32
 
 pytestmark = pytest.mark.gpu
-D = 128
+D, DEV = 128, "cuda"
+PQ_ERR_SHAPE = 2
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = binding.Context()
+    yield c
+    c.check()
+    c.close()
+
+
+@pytest.mark.parametrize("max_new", [1, 3])
+@pytest.mark.parametrize("n_seqs", [3, 700])
+@pytest.mark.parametrize("begin", [[0, 1, 5], [-1, 0, 1], [2, 1, 2], [3, 4, 5], [0, 0, -1], [0, 2**31 - 1, 3], [-2**31, 2**31 - 1, 3]])
+def test_rows_outside_the_queries_are_reported_in_a_step_of_single_tokens_too(ctx, begin, n_seqs, max_new):
+    """Whatever bound the caller gives; the rows of sequences that are in order are computed, the others left out. With one worker to a pair (few
+    sequences) and in equal stretches (many)."""
+    lengths = [20, 40] + [100] * (n_seqs - 2)
+    cache = ref.make_cache(lengths[:2], 4, 2, 16, seed=8, width=8)
+    extra = n_seqs - 2  # sequences without rows behind the two
+    pg = cache.pages
+    table = torch.cat((pg.table, torch.zeros((extra, pg.max_pages), dtype=torch.int32, device=DEV)))
+    cache = binding.KV4PagedCache(binding.Pages(table, i32(lengths), pg.free_list, pg.n_free, 16), cache.prefix_k, cache.prefix_v, cache.codes, 4, s_k=cache.s_k,
+                                  s_v=cache.s_v)
+    q = ref.queries(4, 4)
+    ws = ctx.attn_kv4_paged_workspace(cache, 4, max_new)
+    out = torch.full((4, 4, D), 9.0, dtype=torch.bfloat16, device=DEV)
+    ctx.attn_kv4_paged(cache, q, i32(begin + [begin[-1]] * extra), max_new, 0.1, ws, out=out)
+    assert ctx.check_status() == PQ_ERR_SHAPE
+    good = [(b, begin[b]) for b in range(2) if begin[b + 1] - begin[b] == 1 and 0 <= begin[b] < 4]
+    want, tol = torch.full(out.shape, 9.0, dtype=torch.float64, device=DEV), torch.zeros(out.shape, dtype=torch.float64, device=DEV)
+    for b, r in good:
+        w, t = ref.attention(cache, q[r: r + 1], [0] * (b + 1) + [1] * (n_seqs - b), lengths[: b + 1] + [0] * (n_seqs - b - 1), 0.1)
+        want[r], tol[r] = w[0], t[0]
+    assert ((out.double() - want).abs() <= tol).all()
 
 
 # (sequences, tokens of each, query heads, KV heads), own steps but for the last: the shared memory of the first two differs by 3.6 KB, and with the larger one
