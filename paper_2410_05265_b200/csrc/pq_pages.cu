@@ -6,6 +6,8 @@
 // gives the same verdict on the step as the others, and writes its share of the rows and of the pages; the lengths and the count of free
 // pages, which every CTA reads, are written behind the cluster's barrier, so that they may be advanced in place. No atomics, no counter
 // that outlives the launch; the order of the pages is that of the definition whatever the shape of the launch.
+#include <atomic>
+
 #include "pq_paged.cuh"
 
 namespace {
@@ -157,10 +159,21 @@ __global__ void __launch_bounds__(PG_THREADS) page_release_kernel(const PlanPara
   if (tid == 0) *p.n_free_out = refused ? n_free : n_free + static_cast<int32_t>(total);
 }
 
-pq_status launch(void (*kern)(const PlanParams), const PlanParams& p, int64_t items, size_t smem, cudaStream_t st) {
-  if (smem > 48 * 1024 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess) {
-    cudaGetLastError();
-    return PQ_ERR_CUDA;
+// Bytes of dynamic shared memory of `arrays` arrays over the sequences, some of them one longer.
+constexpr size_t pg_smem_bytes(int64_t B, int arrays, int longer) { return (static_cast<size_t>(arrays) * B + longer) * sizeof(int32_t); }
+
+// The kernel's limit on shared memory belongs to the device, not to the call or the context: it is set once, to the most that any call takes, so that the calls of
+// another host thread never find it lower.
+pq_status launch(const pq_ctx* ctx, void (*kern)(const PlanParams), std::atomic<bool> (&limit_set)[64], const PlanParams& p, int64_t items, int arrays, int longer,
+                 cudaStream_t st) {
+  if (ctx->device < 0 || ctx->device >= 64) return PQ_ERR_UNSUPPORTED;
+  const size_t smem = pg_smem_bytes(p.B, arrays, longer);
+  if (!limit_set[ctx->device].load(std::memory_order_relaxed)) {
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(pg_smem_bytes(PQ_PAGED_MAX_SEQS, arrays, longer))) != cudaSuccess) {
+      cudaGetLastError();
+      return PQ_ERR_CUDA;
+    }
+    limit_set[ctx->device].store(true, std::memory_order_relaxed);
   }
   const int ctas = items > PG_ONE_CTA ? PG_CLUSTER : 1;
   return pq_launch_cluster_pdl(kern, dim3(ctas), PG_THREADS, smem, ctas, st, p);
@@ -187,7 +200,8 @@ extern "C" pq_status pq_page_plan(pq_ctx* ctx, const pq_pages* pages, const int3
   if (pq_misaligned16(slot) || pq_misaligned16(pos)) return PQ_ERR_ALIGN;
   PlanParams p = base_params(ctx, pages);
   p.n_new = n_new, p.pos0 = pos0, p.n_rows = n_rows, p.q_begin = q_begin, p.slot = slot, p.pos = pos, p.len_out = len_out, p.n_free_out = n_free_out;
-  return launch(page_plan_kernel, p, n_rows, (3 * static_cast<size_t>(p.B) + 2) * sizeof(int32_t), static_cast<cudaStream_t>(stream));
+  static std::atomic<bool> limit_set[64] = {};
+  return launch(ctx, page_plan_kernel, limit_set, p, n_rows, 3, 2, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" pq_status pq_page_release(pq_ctx* ctx, const pq_pages* pages, const int32_t* done, int32_t* len_out, int32_t* n_free_out, void* stream) {
@@ -197,5 +211,6 @@ extern "C" pq_status pq_page_release(pq_ctx* ctx, const pq_pages* pages, const i
   if (pages->B > 0 && (!done || !len_out)) return PQ_ERR_INVALID_ARG;
   PlanParams p = base_params(ctx, pages);
   p.n_new = done, p.len_out = len_out, p.n_free_out = n_free_out;
-  return launch(page_release_kernel, p, pages->n_pages, (2 * static_cast<size_t>(p.B) + 1) * sizeof(int32_t), static_cast<cudaStream_t>(stream));
+  static std::atomic<bool> limit_set[64] = {};
+  return launch(ctx, page_release_kernel, limit_set, p, pages->n_pages, 2, 1, static_cast<cudaStream_t>(stream));
 }

@@ -1,10 +1,12 @@
-"""Calls of the paged KV4 entry points that are easily got wrong: row ranges outside the queries, and results that must not depend on which
-shapes a process ran before."""
+"""Calls of the paged KV4 entry points that are easily got wrong: row ranges outside the queries, host threads with a context each, and results that must not
+depend on which shapes a process ran before."""
+import ctypes
 import hashlib
 import math
 import os
 import subprocess
 import sys
+import threading
 
 import pytest
 import torch
@@ -51,6 +53,36 @@ def test_rows_outside_the_queries_are_reported_in_a_step_of_single_tokens_too(ct
         w, t = ref.attention(cache, q[r: r + 1], [0] * (b + 1) + [1] * (n_seqs - b), lengths[: b + 1] + [0] * (n_seqs - b - 1), 0.1)
         want[r], tol[r] = w[0], t[0]
     assert ((out.double() - want).abs() <= tol).all()
+
+
+def test_host_threads_with_a_context_each_do_not_disturb_one_another():
+    """Plans and releases of batches whose shared memory differs and is above what a kernel gets by itself, from four host threads at once, each on a stream of its
+    own: all are launched. (The library is called directly, so that the threads meet in it.)"""
+    lib, page, n_calls, seen = binding.load_library(), 16, 10000, {}
+
+    def serve(B):
+        c, stream = binding.Context(), torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            z = lambda n, dtype=torch.int32: torch.zeros(n, dtype=dtype, device=DEV)
+            pg = binding.Pages(z(2 * B).view(B, 2), z(B), torch.arange(B, dtype=torch.int32, device=DEV), i32([B]), page)
+            n_new, done, out = z(B), z(B), [z(B + 1), z(4, torch.int64), z(4), z(B), z(1)]
+            n_new[0] = 1
+            torch.cuda.synchronize()
+            at, ref_pages, s = [t.data_ptr() for t in out], ctypes.byref(pg.struct), stream.cuda_stream
+            statuses = set()
+            for _ in range(n_calls):
+                statuses.add(lib.pq_page_plan(c.h, ref_pages, n_new.data_ptr(), 0, 4, *at, s))
+                statuses.add(lib.pq_page_release(c.h, ref_pages, done.data_ptr(), at[3], at[4], s))
+            statuses.add(c.check_status())
+            seen[B] = statuses
+        c.close()
+
+    threads = [threading.Thread(target=serve, args=(B,)) for B in (4200, 5000, 7000, 8192)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert seen == {B: {0} for B in (4200, 5000, 7000, 8192)}
 
 
 # (sequences, tokens of each, query heads, KV heads), own steps but for the last: the shared memory of the first two differs by 3.6 KB, and with the larger one
