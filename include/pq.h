@@ -352,7 +352,7 @@ pq_status pq_page_release(pq_ctx* ctx, const pq_pages* pages, const int32_t* don
  *             image: time, row, column)
  *   sections  host array of n_axes counts with sum 64: the first sections[0] frequencies follow axis 0, the next sections[1] axis 1, ..
  *             (null with n_axes = 1)
- *   y         bf16 [N, Hq + Hk, 128], ldy elements between rows; may be x (with ldy == ld)
+ *   y         bf16 [N, Hq + Hk, 128], ldy elements between rows; may be x (with ldy == ld where N > 1), else it must not overlap it
  * fp32 arithmetic, angles reduced in 64 bits, one rounding. D = 128; x, y, gq, gk 16-byte aligned; ld, ldy multiples of 8. Hk may be 0. */
 pq_status pq_qk_norm_rope(pq_ctx* ctx, const void* x, int64_t N, int32_t Hq, int32_t Hk, int32_t D, int64_t ld, const void* gq, const void* gk,
                           float eps, const int32_t* pos, int32_t n_axes, int64_t ld_pos, const int32_t* sections, double theta, int32_t rotate,
@@ -383,7 +383,7 @@ typedef struct pq_kv4_paged {
  * projection's bf16 value, and s is the head's static step or, with steps, max|y| / 7 of the vector (1 where max|y| < 2^-57), which is written
  * beside the codes.
  * Rows with a negative slot (padding) are neither read nor written; a slot past the cache is skipped and PQ_ERR_SHAPE reported. The slots of
- * a call are distinct. q_out may be qkv itself (with ldq == ld), else it must not overlap it. pos, sections, theta, rotate, gq, gk as above;
+ * a call are distinct. q_out may be qkv itself (with ldq == ld where N > 1), else it must not overlap it. pos, sections, theta, rotate, gq, gk as above;
  * qkv, q_out 16-byte aligned, ld, ldq multiples of 8. */
 pq_status pq_qk_norm_rope_kv4_paged_append(pq_ctx* ctx, const pq_kv4_paged* cache, const void* qkv, int64_t N, int64_t ld, const void* gq,
                                            const void* gk, float eps, const int32_t* pos, int32_t n_axes, int64_t ld_pos, const int32_t* sections,

@@ -383,7 +383,7 @@ pq_status rope_params(QkParams& p, const void* x, int64_t N, int32_t Hq, int32_t
   if (!x || !y || !pos || Hq < 0 || Hk < 0 || Hq + static_cast<int64_t>(Hk) <= 0 || (gq != nullptr) != (gk != nullptr)) return PQ_ERR_INVALID_ARG;
   if (!(theta > 0.0) || !isfinite(theta) || !(eps >= 0.0f)) return PQ_ERR_INVALID_ARG;
   if (n_axes < 1 || n_axes > 3 || (n_axes > 1 && (!sections || ld_pos < N))) return PQ_ERR_INVALID_ARG;
-  if (ld < n_cols || ldy < y_cols || (y == x && ldy != ld)) return PQ_ERR_INVALID_ARG;
+  if (ld < n_cols || ldy < y_cols || (y == x && ldy != ld && N > 1)) return PQ_ERR_INVALID_ARG;  // (of a single row the distance says nothing)
   if (Hq > 65536 || Hk > 65536) return PQ_ERR_SHAPE;
   int32_t sec[3] = {64, 0, 0};
   if (sections) {

@@ -1,5 +1,5 @@
-"""Calls of the paged KV4 entry points that are easily got wrong: row ranges outside the queries, host threads with a context each, and results that must not
-depend on which shapes a process ran before."""
+"""Calls of the paged KV4 entry points that are easily got wrong: row ranges outside the queries, one row appended in place, host threads with a context each, and
+results that must not depend on which shapes a process ran before."""
 import ctypes
 import hashlib
 import math
@@ -14,7 +14,7 @@ import torch
 from paper_2410_05265_b200 import binding
 
 import paged_ref as ref
-from test_gpu_paged import i32
+from test_gpu_paged import gains, heads, i32, positions
 
 pytestmark = pytest.mark.gpu
 D, DEV = 128, "cuda"
@@ -53,6 +53,21 @@ def test_rows_outside_the_queries_are_reported_in_a_step_of_single_tokens_too(ct
         w, t = ref.attention(cache, q[r: r + 1], [0] * (b + 1) + [1] * (n_seqs - b), lengths[: b + 1] + [0] * (n_seqs - b - 1), 0.1)
         want[r], tol[r] = w[0], t[0]
     assert ((out.double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("steps", ["head", "vector"])
+def test_one_row_is_appended_in_place(ctx, steps):
+    """The stride of a single row says nothing: the query heads may stay where the projection wrote them, as with several rows."""
+    Hq, Hkv = 4, 2
+    (gq, gk), pos, slot = gains(1), positions(1, 1, 5), torch.tensor([3], device=DEV)
+    qkv = heads(1, Hq + 2 * Hkv, 6).view(1, -1)
+    a, b = (ref.make_cache([20], Hq, Hkv, 32, steps, seed=1) for _ in range(2))
+    q = ctx.qk_norm_rope_kv4_paged_append(a, qkv, gq, gk, 1e-5, pos, slot, 500000.0)
+    rest = qkv[:, Hq * D:].clone()
+    ctx.qk_norm_rope_kv4_paged_append(b, qkv, gq, gk, 1e-5, pos, slot, 500000.0, q_out=qkv[:, : Hq * D].unflatten(1, (Hq, D)))
+    ctx.check()
+    assert torch.equal(qkv[:, : Hq * D].view(1, Hq, D), q) and torch.equal(qkv[:, Hq * D:], rest)
+    assert torch.equal(a.codes, b.codes) and (steps == "head" or torch.equal(a.steps, b.steps))
 
 
 def test_host_threads_with_a_context_each_do_not_disturb_one_another():

@@ -156,3 +156,11 @@ def test_workspace_of_nothing_is_nothing(lib, ctx):
     assert lib.pq_attn_kv4_paged_workspace_bytes(None, ctypes.byref(cache()), 4, 1) == 0
     assert lib.pq_attn_kv4_paged_workspace_bytes(ctx, ctypes.byref(cache(D=64)), 4, 1) == 0
     assert lib.pq_attn_kv4_paged_workspace_bytes(ctx, ctypes.byref(cache()), 0, 1) == 0
+
+
+def test_in_place_with_another_stride_is_refused_of_several_rows_only(lib, ctx):
+    """The distance of a single row says nothing: the next thing to refuse (here gains that are not aligned) is reached."""
+    assert append(lib, ctx, cache(), N=2, q_out=AT, gq=AT + 8) == INVALID
+    assert append(lib, ctx, cache(), N=1, q_out=AT, gq=AT + 8) == ALIGN
+    assert rope(lib, ctx, N=2, y=AT, ldy=8 * 128, gq=AT + 8) == INVALID
+    assert rope(lib, ctx, N=1, y=AT, ldy=8 * 128, gq=AT + 8) == ALIGN
