@@ -341,7 +341,8 @@ pq_status pq_page_plan(pq_ctx* ctx, const pq_pages* pages, const int32_t* n_new,
                        int32_t* pos, int32_t* len_out, int32_t* n_free_out, void* stream);
 /* The pages of the sequences with done[b] != 0 go back, sequence by sequence in the order of the table: they follow the free ids,
  * *n_free_out = *n_free + their number, len_out[b] = 0 (len[b] for the others). The table is left as it is. len_out and n_free_out may
- * be len and n_free. If the list cannot hold them (n_pages entries) or a length is no length, nothing changes and PQ_ERR_SHAPE is reported. */
+ * be len and n_free. If the list cannot hold them (n_pages entries), a length is no length or an id to go back is none, nothing changes and PQ_ERR_SHAPE is
+ * reported. */
 pq_status pq_page_release(pq_ctx* ctx, const pq_pages* pages, const int32_t* done, int32_t* len_out, int32_t* n_free_out, void* stream);
 
 /* Norm of every query and key head and rotary embedding in one pass over x bf16 [N, Hq + Hk, 128], ld elements between rows:

@@ -63,6 +63,15 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
+// The counterpart of a shared variable in CTA `rank` of the cluster.
+__device__ __forceinline__ int ld_cluster(const int* p, int rank) {
+  uint32_t a;
+  int v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+
 __device__ __forceinline__ int64_t ld_dep(const int64_t* p) {
   int64_t v;
   asm volatile("ld.global.b64 %0, [%1];" : "=l"(v) : "l"(p));

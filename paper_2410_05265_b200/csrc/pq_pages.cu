@@ -124,10 +124,10 @@ __global__ void __launch_bounds__(PG_THREADS) page_plan_kernel(const PlanParams 
 __global__ void __launch_bounds__(PG_THREADS) page_release_kernel(const PlanParams p) {
   extern __shared__ __align__(16) int32_t pg_smem[];
   __shared__ int64_t part[PG_THREADS / 32];
-  __shared__ int bad;
+  __shared__ int bad, no_id;
   int32_t *pages = pg_smem, *len = pages + p.B + 1;
   pq::pdl_wait();
-  if (threadIdx.x == 0) bad = 0;
+  if (threadIdx.x == 0) bad = no_id = 0;
   __syncthreads();
   const int32_t n_free = pq::ld_dep(p.n_free);
   const int64_t capacity = static_cast<int64_t>(p.max_pages) << p.page_log2;
@@ -141,13 +141,32 @@ __global__ void __launch_bounds__(PG_THREADS) page_release_kernel(const PlanPara
   }
   __syncthreads();
   const int64_t total = pq::block_scan<PG_THREADS>(pages, p.B, part);
-  const bool refused = bad || n_free < 0 || n_free + total > p.n_pages;
+  bool refused = bad || n_free < 0 || n_free + total > p.n_pages;
   const int n_ctas = gridDim.x, tid = blockIdx.x * PG_THREADS + threadIdx.x, n_threads = n_ctas * PG_THREADS;
+  auto page_id = [&](int64_t k) {  // the k-th page that goes back
+    const int b = pq::find_segment(pages, p.B, static_cast<int32_t>(k));
+    return pq::ld_dep(p.table + static_cast<int64_t>(b) * p.max_pages + (k - pages[b]));
+  };
+  // Are all of them ids? Every thread looks at its own (the first stays in a register), the CTAs tell one another.
+  int32_t first = 0;
   if (!refused) {
+    bool none = false;
     for (int64_t k = tid; k < total; k += n_threads) {
-      const int b = pq::find_segment(pages, p.B, static_cast<int32_t>(k));
-      p.free_list[n_free + k] = pq::ld_dep(p.table + static_cast<int64_t>(b) * p.max_pages + (k - pages[b]));
+      const int32_t id = page_id(k);
+      if (k == tid) first = id;
+      none |= id < 0 || id >= p.n_pages;
     }
+    if (none) no_id = 1;
+    if (n_ctas > 1) {
+      pq::cluster_sync();
+      refused = __syncthreads_or(threadIdx.x < n_ctas && pq::ld_cluster(&no_id, threadIdx.x));
+    } else {
+      __syncthreads();
+      refused = no_id;
+    }
+  }
+  if (!refused) {
+    for (int64_t k = tid; k < total; k += n_threads) p.free_list[n_free + k] = k == tid ? first : page_id(k);
   } else if (tid == 0) {
     pq::report(p.status, PQ_ERR_SHAPE);
   }

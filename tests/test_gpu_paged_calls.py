@@ -1,5 +1,5 @@
-"""Calls of the paged KV4 entry points that are easily got wrong: row ranges outside the queries, one row appended in place, host threads with a context each, and
-results that must not depend on which shapes a process ran before."""
+"""Calls of the paged KV4 entry points that are easily got wrong: row ranges outside the queries, one row appended in place, ids that are none given back, host
+threads with a context each, and results that must not depend on which shapes a process ran before."""
 import ctypes
 import hashlib
 import math
@@ -14,7 +14,7 @@ import torch
 from paper_2410_05265_b200 import binding
 
 import paged_ref as ref
-from test_gpu_paged import gains, heads, i32, positions
+from test_gpu_paged import gains, heads, i32, pages_of, positions
 
 pytestmark = pytest.mark.gpu
 D, DEV = 128, "cuda"
@@ -68,6 +68,27 @@ def test_one_row_is_appended_in_place(ctx, steps):
     ctx.check()
     assert torch.equal(qkv[:, : Hq * D].view(1, Hq, D), q) and torch.equal(qkv[:, Hq * D:], rest)
     assert torch.equal(a.codes, b.codes) and (steps == "head" or torch.equal(a.steps, b.steps))
+
+
+@pytest.mark.parametrize("n_pages", [12, 5000])
+@pytest.mark.parametrize("bad", [-1, 10**6, "n_pages"])
+def test_release_gives_no_ids_back_that_are_none(ctx, bad, n_pages):
+    """A page id outside the pool in the table of an ended request: nothing changes and it is reported, as with a length that is none. Ids of requests that
+    go on, and entries behind an ended one's pages, are not looked at. One CTA and a cluster of them."""
+    bad = n_pages if bad == "n_pages" else bad
+    free = [2, 4] + [9] * (n_pages - 2)
+    for table, done, refused in (([[3, bad, -1], [0, -1, -1]], [1, 1], True), ([[3, 1, -1], [bad, -1, -1]], [1, 1], True), ([[3, bad, -1], [0, -1, -1]], [0, 1], False),
+                                 ([[3, 1, bad], [0, bad, -1]], [1, 1], False)):
+        pg = pages_of(table, [20, 16], free, 2, 16)
+        ctx.page_release(pg, i32(done))
+        if refused:
+            assert ctx.check_status() == PQ_ERR_SHAPE
+            assert pg.length.tolist() == [20, 16] and pg.n_free.tolist() == [2] and pg.free_list.tolist() == free
+        else:
+            back = ([3, 1] if done[0] else []) + [0]
+            ctx.check()
+            assert pg.length.tolist() == [0 if d else n for d, n in zip(done, [20, 16])] and pg.n_free.tolist() == [2 + len(back)]
+            assert pg.free_list.tolist() == [2, 4] + back + free[2 + len(back):]
 
 
 def test_host_threads_with_a_context_each_do_not_disturb_one_another():
