@@ -248,6 +248,7 @@ class Pages:
         assert length.shape == (B,) and free_list.dim() == 1 and n_free.numel() == 1
         self.table, self.length, self.free_list, self.n_free = table, length, free_list, n_free
         self.B, self.max_pages, self.page, self.n_pages = B, max_pages, int(page), free_list.numel()
+        self.at = table.get_device()
         self.struct = PagesStruct(table.data_ptr(), length.data_ptr(), free_list.data_ptr(), n_free.data_ptr(), B, max_pages, self.page, self.n_pages)
 
 
@@ -668,17 +669,20 @@ class Context:
                                         1 if rotate else 0, _stream()), "pq_rope_kv4_append")
 
     # ---- paged KV4 cache ------------------------------------------------------------------------
-    def _here(self) -> int:
-        """The context's device, which is the current one: its current stream is the one that is used."""
+    def _here(self, pages: Pages | None = None) -> int:
+        """The context's device, which is the current one: its current stream is the one that is used. The block table (with which the whole cache
+        agrees) must lie there."""
         if torch._C._cuda_getDevice() != self.device:
             raise ValueError(f"cuda:{torch._C._cuda_getDevice()} is current in a call to a context of cuda:{self.device}")
+        if pages is not None and pages.at != self.device:
+            raise ValueError(f"the cache is on cuda:{pages.at} in a call to a context of cuda:{self.device}")
         return self.device
 
     def page_plan(self, pages: Pages, n_new: torch.Tensor, n_rows: int | None = None, pos0: int = 0, out=None, len_out=None, n_free_out=None):
         """Pages, slots and positions of a step in which sequence b gets n_new[b] tokens; n_rows is the number of rows of the (padded) step.
         Returns (q_begin int32 [B + 1], slot int64 [n_rows], pos int32 [n_rows]), which may be given as `out`. The lengths and the count
         of free pages advance in place unless len_out, n_free_out are given."""
-        here, B, s = self._here(), pages.B, pages.struct
+        here, B, s = self._here(pages), pages.B, pages.struct
         if out is None:
             out = (torch.empty((B + 1,), dtype=torch.int32, device=n_new.device), torch.empty((n_rows,), dtype=torch.int64, device=n_new.device),
                    torch.empty((n_rows,), dtype=torch.int32, device=n_new.device))
@@ -695,7 +699,7 @@ class Context:
 
     def page_release(self, pages: Pages, done: torch.Tensor, len_out=None, n_free_out=None) -> None:
         """The pages of the sequences with done[b] != 0 (int32 [B]) go back to the free list; lengths and count change in place by default."""
-        here, B, s = self._here(), pages.B, pages.struct
+        here, B, s = self._here(pages), pages.B, pages.struct
         _ok(self.lib.pq_page_release(self.h, ctypes.byref(s), _arr(done, torch.int32, (B,), here, "done"),
                                      s.len if len_out is None else _arr(len_out, torch.int32, (B,), here, "len_out"),
                                      s.n_free if n_free_out is None else _arr(n_free_out, torch.int32, (1,), here, "n_free_out"),
@@ -735,7 +739,7 @@ class Context:
                                       theta: float, sections=None, rotate: bool = False, q_out: torch.Tensor | None = None):
         """qk_norm_rope of a projection output qkv [N, (Hq + 2 Hkv) * 128]: the query heads to q_out [N, Hq, 128] (returned), the key and value
         heads, quantized, to the slots of the paged cache. Rows with slot -1 are neither read nor written."""
-        here = self._here()
+        here = self._here(cache.pages)
         N, cols = qkv.shape
         ld, one = qkv.stride()
         if qkv.dtype != torch.bfloat16 or qkv.get_device() != here or one != 1 or cols != (cache.Hq + 2 * cache.Hkv) * cache.D:
@@ -751,7 +755,7 @@ class Context:
 
     def kv4_paged_read(self, cache: KV4PagedCache, slot: torch.Tensor, out: torch.Tensor | None = None):
         """Keys and values at the given slots as a reader of the cache finds them, bf16 [N, 2, Hkv, 128]; rows with slot -1 keep what out holds."""
-        here, N = self._here(), slot.numel()
+        here, N = self._here(cache.pages), slot.numel()
         if out is None:
             out = torch.zeros((N, 2, cache.Hkv, cache.D), dtype=torch.bfloat16, device=slot.device)
         _ok(self.lib.pq_kv4_paged_read(self.h, ctypes.byref(cache.struct), _arr(slot, torch.int64, (N,), here, "slot"), N,
@@ -768,7 +772,7 @@ class Context:
         """Causal attention of the rows q [N, Hq, 128] of a ragged batch (sequence b: rows q_begin[b] .. q_begin[b + 1] - 1, its last tokens) over
         [prefix || paged cache]. max_new bounds the rows of a sequence, max_len (0: the capacity) the lengths; rows behind the last stay as they are.
         out may be q."""
-        here, N = self._here(), q.shape[0]
+        here, N = self._here(cache.pages), q.shape[0]
         q_at, ldq = _heads(q, N, cache.Hq, cache.D, here, "q")
         if out is None:
             out = torch.zeros((N, cache.Hq, cache.D), dtype=q.dtype, device=q.device)
