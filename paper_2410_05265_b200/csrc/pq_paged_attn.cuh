@@ -30,6 +30,11 @@ struct PagedAttnParams {
   int32_t workers;  // 0: one worker per (sequence, KV head)
 };
 
+// One mbarrier try_wait may suspend its thread for thousands of clocks (three of them on a barrier that nothing completes take 15700), in which an ordinary wait ends. A
+// limit below that is kept by forms of the two kernels that poll instead (POLL): with them a test makes waits run out. As a choice inside the kernels it
+// took 2 to 4 % of them.
+#define PQ_SUSPENDED_CLOCKS 16384
+
 // Tickets 0 .. 15 belong to the appends, those from PQ_N_TICKETS / 2 on to the one-launch decode step.
 #define PQ_PAGED_TICKET0 16
 #define PQ_PAGED_MAX_WORKERS 4096
@@ -71,6 +76,33 @@ __device__ __forceinline__ void bulk_load(uint32_t dst_smem, const void* src, ui
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst_smem), "l"(src), "r"(bytes),
                "r"(smem_u32(bar))
                : "memory");
+}
+// Is the phase over? Does not suspend.
+__device__ __forceinline__ bool mbar_test_wait(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+      "selp.u32 %0, 1, 0, p;\n"
+      "}\n"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+// One look at a wait, and a bounded wait.
+template <bool POLL>
+__device__ __forceinline__ bool mbar_look(uint64_t* bar, uint32_t parity) {
+  return POLL ? mbar_test_wait(bar, parity) : mbar_try_wait(bar, parity);
+}
+template <bool POLL>
+__device__ __forceinline__ bool mbar_look_for(uint64_t* bar, uint32_t parity, long long limit) {
+  if (!POLL) return mbar_wait_for(bar, parity, limit);
+  const long long t0 = clock64();
+  while (!mbar_test_wait(bar, parity))
+    if (clock64() - t0 > limit) return false;
+  return true;
 }
 __device__ __forceinline__ uint4 lds128(uint32_t a) {
   uint4 v;

@@ -98,7 +98,7 @@ __device__ __forceinline__ bool odd_rows(const PagedAttnParams& p, int r0, int r
 }
 
 // WIDE: clusters of sixteen, for a few long sequences (their merge in the other kernel would cost it registers).
-template <bool DYN, bool WIDE>
+template <bool DYN, bool WIDE, bool POLL>
 __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const PagedAttnParams p) {
   constexpr int SLOT = slot_bytes(DYN);
   extern __shared__ __align__(128) uint8_t dp_smem[];
@@ -374,8 +374,8 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
     const uint32_t v_off = (2 * t) * 64 + 8 * g;  // keys 2t, 2t+1, 2t+8, 2t+9: 16 codes at dims 16g..16g+15
     for (int key0 = x.r0 * DP_ROUND + first_key; key0 < kend; key0 += stride) {
       const int s = n_done % DP_SLOTS;
-      bool late = !__all_sync(0xffffffffu, pq::mbar_try_wait(&full[warp][s], (n_done / DP_SLOTS) & 1));
-      if (late) late = timed_out || n_done >= n_issued || __any_sync(0xffffffffu, !pq::mbar_wait_for(&full[warp][s], (n_done / DP_SLOTS) & 1, p.wait_clocks));
+      bool late = !__all_sync(0xffffffffu, pq::mbar_look<POLL>(&full[warp][s], (n_done / DP_SLOTS) & 1));
+      if (late) late = timed_out || n_done >= n_issued || __any_sync(0xffffffffu, !pq::mbar_look_for<POLL>(&full[warp][s], (n_done / DP_SLOTS) & 1, p.wait_clocks));
       if (late) {
         timed_out = true;  // nothing more is requested; the pieces run out without work
         is_ok = false;
@@ -666,9 +666,10 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
 
 constexpr int DP_CTAS_PER_SM = 4;
 
-void (*kernel_of(bool dyn, int csize))(const PagedAttnParams) {
-  if (csize > 8) return dyn ? paged_decode_kernel<true, true> : paged_decode_kernel<false, true>;
-  return dyn ? paged_decode_kernel<true, false> : paged_decode_kernel<false, false>;
+void (*kernel_of(bool dyn, int csize, bool poll))(const PagedAttnParams) {
+  if (poll) return dyn ? paged_decode_kernel<true, true, true> : paged_decode_kernel<false, true, true>;  // (any cluster size)
+  if (csize > 8) return dyn ? paged_decode_kernel<true, true, false> : paged_decode_kernel<false, true, false>;
+  return dyn ? paged_decode_kernel<true, false, false> : paged_decode_kernel<false, false, false>;
 }
 
 int most_ctas(const pq_ctx* ctx) { return DP_CTAS_PER_SM * ctx->sm_count; }
@@ -690,7 +691,7 @@ int resident_workers(const pq_ctx* ctx, bool dyn, int csize, size_t smem) {
   attr[0].val.clusterDim.x = csize, attr[0].val.clusterDim.y = 1, attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  if (cudaOccupancyMaxActiveClusters(&n, kernel_of(dyn, csize), &cfg) != cudaSuccess || n < 1) {
+  if (cudaOccupancyMaxActiveClusters(&n, kernel_of(dyn, csize, false), &cfg) != cudaSuccess || n < 1) {
     cudaGetLastError();
     n = csize > 8 ? 0 : ctx->sm_count / csize;  // (clusters of more than eight need not fit at all)
   }
@@ -706,17 +707,18 @@ size_t pq_paged_decode_ws_bytes(const pq_ctx* ctx, const pq_kv4_paged* c) {
 }
 
 pq_status pq_paged_decode_launch(pq_ctx* ctx, const pq_kv4_paged* c, PagedAttnParams p, int64_t max_len, void* ws, cudaStream_t st) {
-  const bool dyn = p.steps != nullptr;
+  const bool dyn = p.steps != nullptr, poll = p.wait_clocks < PQ_SUSPENDED_CLOCKS;
   // the largest there is, once per device and kernel
   static std::atomic<bool> attr_set[64][2] = {};
   if (ctx->device < 0 || ctx->device >= 64) return PQ_ERR_UNSUPPORTED;
   if (!attr_set[ctx->device][dyn].load(std::memory_order_relaxed)) {
     const int most = static_cast<int>(DP_MAX_KB * 1024);
-    if (cudaFuncSetAttribute(kernel_of(dyn, 1), cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess ||
-        cudaFuncSetAttribute(kernel_of(dyn, 16), cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess ||
-        cudaFuncSetAttribute(kernel_of(dyn, 16), cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
-      cudaGetLastError();
-      return PQ_ERR_CUDA;
+    for (auto* const kern : {kernel_of(dyn, 1, false), kernel_of(dyn, 16, false), kernel_of(dyn, 16, true)}) {
+      if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess ||
+          (kern != kernel_of(dyn, 1, false) && cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)) {
+        cudaGetLastError();
+        return PQ_ERR_CUDA;
+      }
     }
     attr_set[ctx->device][dyn].store(true, std::memory_order_relaxed);
   }
@@ -750,5 +752,5 @@ pq_status pq_paged_decode_launch(pq_ctx* ctx, const pq_kv4_paged* c, PagedAttnPa
   p.ws_o = static_cast<float*>(ws);
   p.ws_ml = p.ws_o + static_cast<size_t>(2) * p.workers * p.G * 128;
   const int64_t grid = (direct ? pairs : p.workers) * csize;
-  return pq_launch_cluster_pdl(kernel_of(dyn, p.csize), dim3(static_cast<unsigned>(grid)), DP_THREADS, smem, p.csize, st, p);
+  return pq_launch_cluster_pdl(kernel_of(dyn, p.csize, poll), dim3(static_cast<unsigned>(grid)), DP_THREADS, smem, p.csize, st, p);
 }

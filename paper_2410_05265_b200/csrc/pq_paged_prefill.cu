@@ -273,7 +273,7 @@ struct PpItem {
   int u;                // unit where this worker's share begins (an item is PP_ITEM_UNITS units and its tiles)
 };
 
-template <bool DYN>
+template <bool DYN, bool POLL>
 __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const PagedAttnParams p) {
   extern __shared__ uint8_t pp_raw[];
   uint8_t* smem = pp_raw + (-pq::smem_u32(pp_raw) & 1023u);  // (through an integer the compiler would lose sight of shared memory and use generic loads)
@@ -444,10 +444,10 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
 
   // Bounded wait; also gives up when another role of the CTA has raised the abort flag.
   auto wait = [&](uint64_t* bar, uint32_t parity) -> bool {
-    if (pq::mbar_try_wait(bar, parity)) return true;
+    if (pq::mbar_look<POLL>(bar, parity)) return true;
     const long long c0 = clock64();
     for (;;) {
-      if (pq::mbar_try_wait(bar, parity)) return true;
+      if (pq::mbar_look<POLL>(bar, parity)) return true;
       if (*abort_flag) return false;
       if (clock64() - c0 > p.wait_clocks) return false;
     }
@@ -1091,16 +1091,17 @@ size_t pq_paged_prefill_ws_bytes(const pq_ctx* ctx) {
 }
 
 pq_status pq_paged_prefill_launch(pq_ctx* ctx, PagedAttnParams p, void* ws, cudaStream_t st) {
-  const bool dyn = p.steps != nullptr;
-  void (*const kern)(const PagedAttnParams) = dyn ? paged_prefill_kernel<true> : paged_prefill_kernel<false>;
-  static std::atomic<bool> attr_set[64][2] = {};
+  const bool dyn = p.steps != nullptr, poll = p.wait_clocks < PQ_SUSPENDED_CLOCKS;
+  void (*const kern)(const PagedAttnParams) = poll ? (dyn ? paged_prefill_kernel<true, true> : paged_prefill_kernel<false, true>)
+                                                   : (dyn ? paged_prefill_kernel<true, false> : paged_prefill_kernel<false, false>);
+  static std::atomic<bool> attr_set[64][2][2] = {};
   if (ctx->device < 0 || ctx->device >= 64 || ctx->sm_count > PQ_PAGED_MAX_WORKERS) return PQ_ERR_UNSUPPORTED;
-  if (!attr_set[ctx->device][dyn].load(std::memory_order_relaxed)) {
+  if (!attr_set[ctx->device][dyn][poll].load(std::memory_order_relaxed)) {
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(PP_SMEM_BYTES)) != cudaSuccess) {
       cudaGetLastError();
       return PQ_ERR_CUDA;
     }
-    attr_set[ctx->device][dyn].store(true, std::memory_order_relaxed);
+    attr_set[ctx->device][dyn][poll].store(true, std::memory_order_relaxed);
   }
   p.ws_o = static_cast<float*>(ws);
   p.ws_ml = p.ws_o + static_cast<size_t>(2) * ctx->sm_count * PP_PARTIAL;
