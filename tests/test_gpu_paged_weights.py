@@ -118,3 +118,28 @@ def test_a_prefixed_key_that_draws_nearly_all_of_the_weight(ctx, lengths, new, H
             tol[r] = near[:, None].expand(-1, Hq // Hkv, -1).reshape(Hq, D) + (2.0**-11 + 2.0**-20) * (a + want[r].abs()) + 17 * 8 * 2.0**-23 * seen * p * unit + want[r].abs() * 2.0**-8 + 2.0**-125
     bad = ~((out.double() - want).abs() <= tol)
     assert not bad.any(), f"{int(bad.sum())} of {bad.numel()}; worst {float(((out.double() - want).abs() / tol).max())} of the tolerance"
+
+
+@pytest.mark.parametrize("steps", ["head", "vector"])
+@pytest.mark.parametrize("lengths,new,Hq,Hkv", [([1000, 40], [1, 1], 8, 2), ([700 + 13 * i for i in range(90)], [1] * 90, 8, 4), ([700, 300, 64], [300, 1, 64], 6, 2)])
+def test_infinities_and_nan_stay_in_their_row_and_head(ctx, lengths, new, Hq, Hkv, steps):
+    """Queries that are not finite, and steps and prefix keys that no row sees because they lie behind a sequence, leave every other row and head as it is, bit for bit."""
+    cache = ref.make_cache(lengths, Hq, Hkv, 16, steps, seed=3)
+    begin = [0]
+    for n in new:
+        begin.append(begin[-1] + n)
+    q = ref.queries(begin[-1], Hq)
+    ws = ctx.attn_kv4_paged_workspace(cache, begin[-1], max(new))
+    want = ctx.attn_kv4_paged(cache, q, i32(begin), max(new), 1 / math.sqrt(D), ws)
+    bad = torch.zeros(q.shape[:2], dtype=torch.bool, device=DEV)
+    for r, h, value in ((0, 1, math.nan), (begin[-1] - 1, Hq - 1, math.inf), (begin[-1] // 2, 0, -math.inf), (begin[-1] // 2, 2, math.nan)):
+        q[r, h, (r + h) % D] = value
+        bad[r, h] = True
+    if steps == "vector":
+        for b, n in enumerate(lengths):
+            if n % 16:
+                cache.steps[cache.pages.table[b, n // 16].long(), :, :, n % 16:] = math.nan
+    out = ctx.attn_kv4_paged(cache, q, i32(begin), max(new), 1 / math.sqrt(D), ws)
+    ctx.check()
+    assert torch.equal(out[~bad], want[~bad])
+    assert out[bad].isnan().any(-1).all()
