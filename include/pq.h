@@ -58,7 +58,8 @@ pq_status pq_check(pq_ctx* ctx, void* stream);
 
 /* Bound of the device-side waits (a consumer waiting for a copy or for a producer, a producer waiting for
  * a free buffer) of the kernels launched through this context from now on, in SM clocks; 0 restores the
- * default of 2^31 clocks (about a second). A wait that runs out makes its kernel wind down in an orderly
+ * default of 2^31 clocks (about a second). One hardware try of a wait may itself take some thousand clocks; pq_attn_kv4_paged keeps limits below 16384 clocks by
+ * polling. A wait that runs out makes its kernel wind down in an orderly
  * way (copies in flight are awaited, tensor memory is released) and leaves PQ_ERR_TIMEOUT in the status
  * word; the kernel's output is then undefined. Failure-detection tests set a bound of a few clocks so that
  * an ordinary wait runs out. */
@@ -308,7 +309,8 @@ pq_status pq_rope_kv4_append(pq_ctx* ctx, const pq_kv4_cache* cache, int32_t seq
 /* ---------------------------------------------------------------------------------------------
  * Paged KV4 cache (the cache of Sec. 4.2 for a server whose requests come and go: the paper has no counterpart of the paging).
  * Sequences take pages of `page` tokens from one pool; the pool's block table is shared by all layers, each layer has codes of
- * its own for every page. The same code, step and prefix rules as in the contiguous cache above hold.
+ * its own for every page. The same code, step and prefix rules as in the contiguous cache above hold, but for one: a key is not rounded to bf16 between its rotary
+ * position and its code, which pq_rope_kv4_append does (codes next to a border may differ between the two caches).
  *
  *   table      int32 [B, max_pages]  page ids of each sequence in order; entries behind its last page are neither read nor written
  *   len        int32 [B]             cached tokens of each sequence
@@ -354,7 +356,7 @@ pq_status pq_page_release(pq_ctx* ctx, const pq_pages* pages, const int32_t* don
  *   sections  host array of n_axes counts with sum 64: the first sections[0] frequencies follow axis 0, the next sections[1] axis 1, ..
  *             (null with n_axes = 1)
  *   y         bf16 [N, Hq + Hk, 128], ldy elements between rows; may be x (with ldy == ld where N > 1), else it must not overlap it
- * fp32 arithmetic, angles reduced in 64 bits, one rounding. D = 128; x, y, gq, gk 16-byte aligned; ld, ldy multiples of 8. Hk may be 0. */
+ * fp32 arithmetic (the squares of a head must not leave fp32: |x| < 2^60), angles reduced in 64 bits, one rounding. D = 128; x, y, gq, gk 16-byte aligned; ld, ldy multiples of 8. Hk may be 0. */
 pq_status pq_qk_norm_rope(pq_ctx* ctx, const void* x, int64_t N, int32_t Hq, int32_t Hk, int32_t D, int64_t ld, const void* gq, const void* gk,
                           float eps, const int32_t* pos, int32_t n_axes, int64_t ld_pos, const int32_t* sections, double theta, int32_t rotate,
                           void* y, int64_t ldy, void* stream);
@@ -402,9 +404,14 @@ pq_status pq_kv4_paged_read(pq_ctx* ctx, const pq_kv4_paged* cache, const int64_
  *   q_begin  int32 [B + 1], ascending, on the device; rows from q_begin[B] on (padding) are neither read nor written. Sequences with rows outside
  *            [0, n_rows), or that end before they begin, are left out and PQ_ERR_SHAPE is reported
  *   max_new  at least the largest n (a host bound); sequences with more rows are left out and PQ_ERR_SHAPE is reported
- *   max_len  at least the largest len (a host bound that only chooses how the work is split; 0: the capacity max_pages * page)
+ *   max_len  at least the largest len (a host bound that only chooses how the work of single tokens is split; 0: the capacity max_pages * page). With a table far wider
+ *            than the lengths a bound pays: 12000 tokens take 14.4 us with it and 20.5 without under a table of 131072, 16 x 8000 39 and 48
  *   ws       scratch of pq_attn_kv4_paged_workspace_bytes(ctx, cache, n_rows, max_new) bytes, 16-byte aligned
- *   sm_scale > 0. */
+ *   sm_scale > 0.
+ * Accumulation in fp32. What is held in fewer bits: the softmax weights that are multiplied with V are fp16 relative to a reference of the row, near its largest exponent so
+ * far (11 bits down to 2^-14 of the reference, multiples of 2^-24 of it below; with own steps the value's step is in the weight; a prefixed key that outweighs
+ * all cached ones does not set their reference); for single tokens the queries are fp16 after a power of two per head (elements below 2^-21 of the
+ * head's largest lose bits). */
 size_t pq_attn_kv4_paged_workspace_bytes(const pq_ctx* ctx, const pq_kv4_paged* cache, int64_t n_rows, int32_t max_new);
 pq_status pq_attn_kv4_paged(pq_ctx* ctx, const pq_kv4_paged* cache, const void* q, int64_t ldq, const int32_t* q_begin, int64_t n_rows,
                             int32_t max_new, int32_t max_len, void* out, float sm_scale, void* ws, size_t ws_bytes, void* stream);

@@ -35,7 +35,8 @@ struct PagedAttnParams {
 // took 2 to 4 % of them.
 #define PQ_SUSPENDED_CLOCKS 16384
 
-// Tickets 0 .. 15 belong to the appends, those from PQ_N_TICKETS / 2 on to the one-launch decode step.
+// Tickets 0 .. 15 belong to the appends, those from PQ_N_TICKETS / 2 on to the one-launch decode step. The decode attention of the contiguous cache counts from 16 on,
+// too: every call leaves its tickets at zero, and calls of a context are in stream order.
 #define PQ_PAGED_TICKET0 16
 #define PQ_PAGED_MAX_WORKERS 4096
 

@@ -27,8 +27,8 @@
 // Bound by the exponentials and the hand-overs between softmax and tensor core: a key tile of an item takes about 4300 clocks, of which the two products need
 // 2048 on the tensor core and the 32768 exponentials 2048 on the four special-function units; both row tiles' exponentials overlap (2100), then follow the
 // vote on the reference and the store of the weights (700) and the wait for the products (1500). An item costs 10000 clocks more (queries, first
-// scores, prefix, output). Measured: 2048 rows x 64 heads behind 21952 keys 1473 us, 0.65 of the measured bf16 rate on the products of visible pairs (own
-// steps 1752), 4096 rows x 64 heads 354, 2048 rows 132, 4 ragged prompts up to 2000 x 32 heads 160 (own steps 185), 515 rows 25.
+// scores, prefix, output). Measured: 2048 rows x 64 heads behind 21952 keys 1500 us, 0.62 of the measured bf16 rate (1651 TFLOP/s) on the products of visible pairs (own
+// steps 1815), 4096 rows x 64 heads 360 (453), 2048 rows 132 (154), 4 ragged prompts up to 2000 x 32 heads 162 (192), 515 rows 26 (29).
 // Tried and slower: a thread per row (own steps 2011 us: the constants of 64 keys per thread), half tiles of 64 keys with the scores of two in flight,
 // row tiles that form their weights in turn (1631; 1573 with half of the pass shared), queries of later items brought in by the expansion warps (the same),
 // eight expansion warps (their 48 registers spill).

@@ -4,7 +4,7 @@
 // Bound by HBM: a head is read once and written once (256 bytes each way, 64 bytes as codes). L lanes take a head, a warp 32 / L heads of a block of tokens; a
 // lane holds C = 64 / L dims of each half, t C .. t C + C - 1 and 64 + t C ..: both halves of a rotary pair and the lower stages of the Hadamard
 // transform are inside the lane, log2 L stages are shuffles, and the fp32 arithmetic runs on packed pairs. L = 4 for many tokens (with L = 16 the
-// kernel is bound by instruction issue: 4099 x 72 heads with R3 48.5 us, against 35.2 = 0.66 of the measured copy rate; L = 8 with a token's factors kept in
+// kernel is bound by instruction issue: 4099 x 72 heads with R3 48.5 us, against 35.4 = 0.65 of the measured copy rate; L = 8 with a token's factors kept in
 // registers and a warp's heads in a row, which takes half the load off the shared-memory pipe, 40.3, with two heads requested ahead 43.0), L = 16 for few, where
 // the chain of one head is the time. Angles are reduced in 64 bits as fractions of a turn (a position of 10^5 leaves an fp32 angle three digits).
 // The append of 6001 tokens x 80 heads with R3 and own steps takes 73 us.
