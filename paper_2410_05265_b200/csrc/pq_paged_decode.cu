@@ -19,7 +19,7 @@
 // CTA barrier stands in the key loop. The ring runs on across the pairs of a stretch.
 //   scores   S^T[key, head] with the fp16 MMA, keys on the 16-row side. code + 8 is taken as the fp16 number whose bits it is (a subnormal, (code + 8) 2^-24;
 //            the odd nibbles four bits up, with q / 16): one LOP3 for two codes, and 8 sum(q) is taken off each score. The offset is of
-//            the codes' own size, so fp32 sums lose nothing by it. The query is scaled by a power of two per head, so that every bf16
+//            the codes' own size, so that fp32 sums lose by it what sums of values of 8 steps lose. The query is scaled by a power of two per head, so that every bf16
 //            query fits fp16.
 //   softmax  in log2 units against a reference exponent per head that moves only when a score exceeds it by more than DP_HEADROOM
 //   output   O^T = V^T P^T with the fp16 MMA, head dims on the 16-row side, codes + 8 as above; one more MMA over codes of zero gives what the offset adds

@@ -56,9 +56,9 @@ constexpr int PP_ITEM_UNITS = 4;    // units of work that an item costs besides 
 constexpr int PP_SHORT = 8;         // an item of so many key tiles or fewer is not shared between workers
 constexpr float PP_LAZY = 15.0f;      // log2 units an exponent may exceed the reference before it is moved: weights stay inside fp16
 // A prefixed key may draw nearly all of the weight while its value is small: what the other weights keep of their bits is then what the output keeps. So where the
-// largest exponent of an item's second tile lies more than PP_LOW below the reference, the reference goes down to it, by PP_FAR at most (the sums, in fp32, grow by
-// that). Tried instead: the reference 8 or 10 below the largest exponent always, which moves again and again (4 ragged prompts 191 -> 226 and 242 us).
-constexpr float PP_LOW = 10.0f, PP_FAR = 40.0f;
+// largest exponent of an item's second tile lies more than PP_LOW below the reference, the reference goes down to it, by PP_FAR_.. at most (the sums, in fp32, grow by
+// that: of a prefix, whose values are fp16, to 2^102; of cached keys, whose denominators may be 2^60 already, to 2^107). Tried instead: the reference 8 or 10 below the largest exponent always, which moves again and again (4 ragged prompts 191 -> 226 and 242 us).
+constexpr float PP_LOW = 10.0f, PP_FAR_PREFIX = 80.0f, PP_FAR_CACHED = 40.0f;
 // Registers: 768 threads at 80; the softmax warpgroups take 96, the others leave 48 (512 x 96 + 256 x 48 = 768 x 80).
 constexpr int PP_REGS_SOFTMAX = 96, PP_REGS_OTHERS = 48;
 constexpr int PP_HALF_KEYS = PP_KEYS / 2;  // key columns of a softmax thread
@@ -679,7 +679,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
           for (int k = 0; k < 4; ++k) {
             const float most = fmaxf(top[k], *const_cast<const volatile float*>(&bars->row[i][set ^ 1][fr + 8 * k]));
             const bool first = m_ref[k] == -INFINITY, move = most > (first ? -INFINITY : PP_LAZY) || (most < -PP_LOW && most != -INFINITY && jt == 1 && x.j0 == 0);
-            const float m_new = move ? ceilf(first ? most : m_ref[k] + fmaxf(most, -PP_FAR)) : m_ref[k];
+            const float m_new = move ? ceilf(first ? most : m_ref[k] + fmaxf(most, has_prefix ? -PP_FAR_PREFIX : -PP_FAR_CACHED)) : m_ref[k];
             alpha[k] = move ? pq::ex2_approx(m_ref[k] - m_new) : 1.0f;  // 2^(-inf) = 0 for a row that had seen nothing
             l[k] = DYN && move ? pq::at_reference(l[k], m_ref[k] - m_new) : l[k] * alpha[k];
             m_ref[k] = m_new;

@@ -121,6 +121,33 @@ def test_a_prefixed_key_that_draws_nearly_all_of_the_weight(ctx, lengths, new, H
 
 
 @pytest.mark.parametrize("steps", ["head", "vector"])
+@pytest.mark.parametrize("step", [-60, -45, -20, 60])
+@pytest.mark.parametrize("above", [0.0, 15.0])
+@pytest.mark.parametrize("lengths,new,Hq,Hkv", [([1000], [1], 8, 2), ([700], [300], 8, 2), ([9000, 200, 40], [40, 200, 1], 8, 1)])
+def test_values_of_any_step_beside_a_prefix_without_values(ctx, lengths, new, Hq, Hkv, above, step, steps):
+    """The prefixed keys' values are zero, the cached ones' steps at the ends of their range: what comes out is theirs alone, in their own size. Bounds of
+    ref.attention, whose largest |v| is a cached one, times the share of the weights that the cached keys have."""
+    cache = cache_of(lengths, Hq, Hkv, steps, 2)
+    if steps == "vector":
+        cache.steps[:, :, 0], cache.steps[:, :, 1] = 2.0**-60, 2.0**step
+    else:
+        cache.codes[:, :, 0] = 0
+        cache.s_v.fill_(2.0**step)
+    cache.prefix_k.zero_(), cache.prefix_v.zero_()
+    cache.prefix_k[:, :, 0] = above
+    q, begin, out = attend(ctx, cache, new)
+    want, tol = ref.attention(cache, q, begin, lengths, LN2)
+    for b, n_keys in enumerate(lengths):
+        for t in range(new[b]):
+            r, seen = begin[b] + t, n_keys - new[b] + t + 1
+            share = seen / (seen + 2 * 2.0**above)
+            whole = want[r].abs() * 2.0**-8 + 2.0**-125
+            tol[r] = whole + (tol[r] - whole) * share
+    bad = ~((out.double() - want).abs() <= tol)
+    assert not bad.any(), f"{int(bad.sum())} of {bad.numel()}; worst {float(((out.double() - want).abs() / tol).max())} of the tolerance"
+
+
+@pytest.mark.parametrize("steps", ["head", "vector"])
 @pytest.mark.parametrize("lengths,new,Hq,Hkv", [([1000, 40], [1, 1], 8, 2), ([700 + 13 * i for i in range(90)], [1] * 90, 8, 4), ([700, 300, 64], [300, 1, 64], 6, 2)])
 def test_infinities_and_nan_stay_in_their_row_and_head(ctx, lengths, new, Hq, Hkv, steps):
     """Queries that are not finite, and steps and prefix keys that no row sees because they lie behind a sequence, leave every other row and head as it is, bit for bit."""
