@@ -416,6 +416,61 @@ size_t pq_attn_kv4_paged_workspace_bytes(const pq_ctx* ctx, const pq_kv4_paged* 
 pq_status pq_attn_kv4_paged(pq_ctx* ctx, const pq_kv4_paged* cache, const void* q, int64_t ldq, const int32_t* q_begin, int64_t n_rows,
                             int32_t max_new, int32_t max_len, void* out, float sm_scale, void* ws, size_t ws_bytes, void* stream);
 
+/* The same attention through a sliding window with first keys that stay visible (a layer with local attention; the prefixed tokens are the paper's own such keys
+ * and are seen whatever the window). The row of the token at cached place c (row t of n: c = len[b] - n + t) sees every prefixed key and the cached keys j <= c with
+ *     j > c - window   or   j < n_sink
+ *   window >= 1, n_sink >= 0; every other argument, the workspace and the limits as in pq_attn_kv4_paged, whose result a window of at least the capacity gives bit for
+ * bit. Work and memory traffic are those of the visible keys, rounded up to tiles. Pages that no new token of their sequence sees any key of are not read, and
+ * their table entries may hold anything. */
+pq_status pq_attn_kv4_paged_window(pq_ctx* ctx, const pq_kv4_paged* cache, const void* q, int64_t ldq, const int32_t* q_begin, int64_t n_rows,
+                                   int32_t max_new, int32_t max_len, int32_t window, int32_t n_sink, void* out, float sm_scale, void* ws, size_t ws_bytes,
+                                   void* stream);
+
+/* Drafted tokens (speculative decoding; the paper has no counterpart). The n = q_begin[b + 1] - q_begin[b] <= 128 new tokens of sequence b are a tree: row 0 is the
+ * root, the token that follows the cached ones; every other row continues the row of its sequence that it names as its parent. A step is
+ *     pq_page_plan (a slot to a draft), pq_tree_plan, the layers with pq_qk_norm_rope_kv4_paged_append and pq_attn_kv4_paged_tree, pq_tree_accept,
+ *     pq_page_keep, and pq_kv4_paged_keep of every layer's cache.
+ *
+ * pq_tree_plan: what a draft sees, and its position.
+ *   parent  int32 [n_rows]  row of the parent within the sequence, before the row's own (0 <= parent < t), or -1: no draft before it
+ *   mask    uint32 [n_rows, mask_words], n <= 32 * mask_words, mask_words <= 4: bit u of a row (bit u % 32 of word u / 32) is set when its sequence's row u is the row
+ *           itself or above it
+ *   pos     int32 [n_rows]: pos0 + (len[b] - n) + the number of rows above it (len as pq_page_plan left it: with the drafts)
+ * Rows behind the last sequence get mask 0 and position 0. A parent out of range counts as -1; a sequence whose rows do not lie in [0, n_rows), are too many, or are
+ * more than its cached tokens is left out (mask 0, position 0 of the latter); all of these report PQ_ERR_SHAPE. */
+pq_status pq_tree_plan(pq_ctx* ctx, const pq_pages* pages, const int32_t* parent, const int32_t* q_begin, int64_t n_rows, int32_t pos0, uint32_t* mask,
+                       int32_t mask_words, int32_t* pos, void* stream);
+
+/* Attention of drafts: row t sees every prefixed key, the cached keys before the n drafts, itself, and the drafts u with bit u of mask[row] set (any of them, not
+ * only rows before it; bits from n on say nothing).
+ *   window  0, or a window of at least max_new keys with n_sink first ones as above, where the place of a row is len[b] - n + (the drafts it sees) - 1
+ *   mask as pq_tree_plan writes it or the caller's own; max_new <= 128 and <= 32 * mask_words; the workspace is
+ *   pq_attn_kv4_paged_tree_workspace_bytes(ctx, cache, n_rows, max_new); every other argument as in pq_attn_kv4_paged. */
+size_t pq_attn_kv4_paged_tree_workspace_bytes(const pq_ctx* ctx, const pq_kv4_paged* cache, int64_t n_rows, int32_t max_new);
+pq_status pq_attn_kv4_paged_tree(pq_ctx* ctx, const pq_kv4_paged* cache, const void* q, int64_t ldq, const int32_t* q_begin, int64_t n_rows, int32_t max_new,
+                                 int32_t max_len, const uint32_t* mask, int32_t mask_words, int32_t window, int32_t n_sink, void* out, float sm_scale,
+                                 void* ws, size_t ws_bytes, void* stream);
+
+/* The accepted path of every tree: row 0 (its token is known), then from row r the first row c with parent[c] == r and draft[c] == target[r], until there is none.
+ *   draft, target  int32 [n_rows]: the token of a row, and the model's choice after it (draft of row 0 is not looked at)
+ *   kept    int32 [n_rows]  the rows of the path, within the sequence and ascending, in the first places of the sequence's rows; -1 behind them and behind the
+ *           last sequence
+ *   n_kept  int32 [B] their number (0 for a sequence without rows),  next int32 [B] the model's choice after the last of them (-1)
+ * A parent out of range belongs to no path; sequences with rows outside [0, n_rows) or more than 128 of them keep none; both report PQ_ERR_SHAPE. */
+pq_status pq_tree_accept(pq_ctx* ctx, const int32_t* q_begin, int32_t B, const int32_t* parent, const int32_t* draft, const int32_t* target, int64_t n_rows,
+                         int32_t* kept, int32_t* n_kept, int32_t* next, void* stream);
+/* Of the n = q_begin[b + 1] - q_begin[b] last cached tokens of every sequence the first n_kept[b] stay (by pq_tree_accept, or any other rule):
+ *     len_out[b] = len[b] - n + n_kept[b]
+ * The pages behind the new length go back, sequence by sequence in the order of the table: they follow the free ids, *n_free_out = *n_free + their number. The table is
+ * left as it is. len_out and n_free_out may be len and n_free. If a count or length is none (0 <= n_kept <= n <= len), the list cannot hold the pages or an id to go
+ * back is none, nothing changes and PQ_ERR_SHAPE is reported. */
+pq_status pq_page_keep(pq_ctx* ctx, const pq_pages* pages, const int32_t* q_begin, const int32_t* n_kept, int32_t* len_out, int32_t* n_free_out, void* stream);
+/* The moves of one layer's cache that belong to it, behind pq_page_keep (cache->pages.len holds the lengths it left) and before the pages that went back are written
+ * again: with base = len[b] - n_kept[b] the vectors (codes and, with own steps, steps) of the token at place base + kept[q_begin[b] + i] go to place base + i, for
+ * i < n_kept[b], as if all were read before any is written. kept need not ascend; what lies behind base + n_kept is undefined afterwards.
+ * Sequences whose counts, lengths or rows are none are left out, tokens whose kept is no row or whose table entry is no page stay; both report PQ_ERR_SHAPE. */
+pq_status pq_kv4_paged_keep(pq_ctx* ctx, const pq_kv4_paged* cache, const int32_t* q_begin, const int32_t* kept, const int32_t* n_kept, int64_t n_rows, void* stream);
+
 /* ---------------------------------------------------------------------------------------------
  * Decode attention for callers that may not allocate. (The paper has no counterpart: this is a
  * packaging variant of pq_decode_attn_kv4_prefix, same kernel, same arguments and result.)

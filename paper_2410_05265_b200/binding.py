@@ -32,6 +32,8 @@ EXPORTS = [
     "pq_swiglu_hadamard_quant_act", "pq_kv4_append_decode_attn", "pq_set_wait_limit", "pq_probe_i8_mma", "pq_grid_search_act_asym", "pq_grid_search_clip_dyn", "pq_rmsnorm_hadamard_quant_act", "pq_rope_kv4_append", "pq_selftest_wait",
     "pq_page_plan", "pq_page_release", "pq_qk_norm_rope", "pq_qk_norm_rope_kv4_paged_append", "pq_kv4_paged_read",
     "pq_attn_kv4_paged_workspace_bytes", "pq_attn_kv4_paged",
+    "pq_attn_kv4_paged_window", "pq_tree_plan", "pq_attn_kv4_paged_tree_workspace_bytes", "pq_attn_kv4_paged_tree", "pq_tree_accept", "pq_page_keep",
+    "pq_kv4_paged_keep",
 ]
 
 
@@ -150,9 +152,20 @@ def load_library() -> ctypes.CDLL:
     lib.pq_attn_kv4_paged_workspace_bytes.argtypes = [c_void_p, POINTER(KV4PagedStruct), c_int64, c_int32]
     lib.pq_attn_kv4_paged.argtypes = [c_void_p, POINTER(KV4PagedStruct), c_void_p, c_int64, c_void_p, c_int64, c_int32, c_int32, c_void_p, c_float,
                                       c_void_p, c_size_t, c_void_p]
+    lib.pq_attn_kv4_paged_window.argtypes = [c_void_p, POINTER(KV4PagedStruct), c_void_p, c_int64, c_void_p, c_int64, c_int32, c_int32, c_int32, c_int32,
+                                             c_void_p, c_float, c_void_p, c_size_t, c_void_p]
+    lib.pq_tree_plan.argtypes = [c_void_p, POINTER(PagesStruct), c_void_p, c_void_p, c_int64, c_int32, c_void_p, c_int32, c_void_p, c_void_p]
+    lib.pq_attn_kv4_paged_tree_workspace_bytes.restype = c_size_t
+    lib.pq_attn_kv4_paged_tree_workspace_bytes.argtypes = lib.pq_attn_kv4_paged_workspace_bytes.argtypes
+    lib.pq_attn_kv4_paged_tree.argtypes = [c_void_p, POINTER(KV4PagedStruct), c_void_p, c_int64, c_void_p, c_int64, c_int32, c_int32, c_void_p, c_int32, c_int32,
+                                           c_int32, c_void_p, c_float, c_void_p, c_size_t, c_void_p]
+    lib.pq_tree_accept.argtypes = [c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_void_p]
+    lib.pq_page_keep.argtypes = [c_void_p, POINTER(PagesStruct), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
+    lib.pq_kv4_paged_keep.argtypes = [c_void_p, POINTER(KV4PagedStruct), c_void_p, c_void_p, c_void_p, c_int64, c_void_p]
     for name in EXPORTS:
         getattr(lib, name)
-        if name not in ("pq_status_string", "pq_w4a4_gemm_workspace_bytes", "pq_decode_attn_workspace_bytes", "pq_attn_kv4_paged_workspace_bytes"):
+        if name not in ("pq_status_string", "pq_w4a4_gemm_workspace_bytes", "pq_decode_attn_workspace_bytes", "pq_attn_kv4_paged_workspace_bytes",
+                        "pq_attn_kv4_paged_tree_workspace_bytes"):
             getattr(lib, name).restype = c_int32
     _lib = lib
     return lib
@@ -781,6 +794,86 @@ class Context:
                                        int(max_new), int(max_len), _arr(out, torch.bfloat16, (N, cache.Hq, cache.D), here, "out"), float(sm_scale),
                                        _arr(ws, torch.uint8, (n_ws,), here, "ws"), n_ws, torch._C._cuda_getCurrentRawStream(here)), "pq_attn_kv4_paged")
         return out
+
+    def attn_kv4_paged_window(self, cache: KV4PagedCache, q: torch.Tensor, q_begin: torch.Tensor, max_new: int, window: int, sm_scale: float, ws: torch.Tensor,
+                              n_sink: int = 0, max_len: int = 0, out: torch.Tensor | None = None):
+        """attn_kv4_paged through a sliding window: a token at cached place c sees the prefix and the cached keys j <= c with j > c - window or j < n_sink.
+        The workspace is that of attn_kv4_paged."""
+        here, N = self._here(cache.pages), q.shape[0]
+        q_at, ldq = _heads(q, N, cache.Hq, cache.D, here, "q")
+        if out is None:
+            out = torch.zeros((N, cache.Hq, cache.D), dtype=q.dtype, device=q.device)
+        n_ws = ws.numel()
+        _ok(self.lib.pq_attn_kv4_paged_window(self.h, ctypes.byref(cache.struct), q_at, ldq, _arr(q_begin, torch.int32, (cache.pages.B + 1,), here, "q_begin"),
+                                              N, int(max_new), int(max_len), int(window), int(n_sink),
+                                              _arr(out, torch.bfloat16, (N, cache.Hq, cache.D), here, "out"), float(sm_scale),
+                                              _arr(ws, torch.uint8, (n_ws,), here, "ws"), n_ws, torch._C._cuda_getCurrentRawStream(here)),
+            "pq_attn_kv4_paged_window")
+        return out
+
+    # ---- drafted tokens --------------------------------------------------------------------------
+    def tree_plan(self, pages: Pages, parent: torch.Tensor, q_begin: torch.Tensor, words: int | None = None, pos0: int = 0, out=None):
+        """What every draft sees of its sequence's drafts (itself and the rows above it) and its position, behind page_plan. parent int32 [n_rows]: a row's parent
+        within its sequence, -1 for a root. Returns (mask int32 [n_rows, words], 32 drafts to a word; pos int32 [n_rows]), which may be given as `out`."""
+        here, N = self._here(pages), parent.numel()
+        if out is None:
+            out = (torch.empty((N, words), dtype=torch.int32, device=parent.device), torch.empty((N,), dtype=torch.int32, device=parent.device))
+        mask, pos = out
+        W = mask.shape[-1]
+        assert words is None or words == W, "words"
+        _ok(self.lib.pq_tree_plan(self.h, ctypes.byref(pages.struct), _arr(parent, torch.int32, (N,), here, "parent"),
+                                  _arr(q_begin, torch.int32, (pages.B + 1,), here, "q_begin"), N, int(pos0), _arr(mask, torch.int32, (N, W), here, "mask"), W,
+                                  _arr(pos, torch.int32, (N,), here, "pos"), torch._C._cuda_getCurrentRawStream(here)), "pq_tree_plan")
+        return out
+
+    def attn_kv4_paged_tree_workspace(self, cache: KV4PagedCache, n_rows: int, max_new: int) -> torch.Tensor:
+        n = int(self.lib.pq_attn_kv4_paged_tree_workspace_bytes(self.h, ctypes.byref(cache.struct), int(n_rows), int(max_new)))
+        return torch.empty((max(n, 16),), dtype=torch.uint8, device=cache.codes.device)
+
+    def attn_kv4_paged_tree(self, cache: KV4PagedCache, q: torch.Tensor, q_begin: torch.Tensor, max_new: int, mask: torch.Tensor, sm_scale: float,
+                            ws: torch.Tensor, window: int = 0, n_sink: int = 0, max_len: int = 0, out: torch.Tensor | None = None):
+        """Attention of drafted tokens: the rows of a sequence (its last cached tokens, 128 at most) see the prefix, the cached keys before them (through a window
+        of at least max_new keys, where one is given) and, of one another, what mask int32 [n_rows, words] says."""
+        here, N = self._here(cache.pages), q.shape[0]
+        q_at, ldq = _heads(q, N, cache.Hq, cache.D, here, "q")
+        if out is None:
+            out = torch.zeros((N, cache.Hq, cache.D), dtype=q.dtype, device=q.device)
+        n_ws, W = ws.numel(), mask.shape[-1]
+        _ok(self.lib.pq_attn_kv4_paged_tree(self.h, ctypes.byref(cache.struct), q_at, ldq, _arr(q_begin, torch.int32, (cache.pages.B + 1,), here, "q_begin"), N,
+                                            int(max_new), int(max_len), _arr(mask, torch.int32, (N, W), here, "mask"), W, int(window), int(n_sink),
+                                            _arr(out, torch.bfloat16, (N, cache.Hq, cache.D), here, "out"), float(sm_scale),
+                                            _arr(ws, torch.uint8, (n_ws,), here, "ws"), n_ws, torch._C._cuda_getCurrentRawStream(here)),
+            "pq_attn_kv4_paged_tree")
+        return out
+
+    def tree_accept(self, q_begin: torch.Tensor, parent: torch.Tensor, draft: torch.Tensor, target: torch.Tensor, out=None):
+        """The accepted path of every tree: from row 0 on the first child whose token draft[c] is the model's choice target[r] after its parent r. All int32 [n_rows].
+        Returns (kept int32 [n_rows]: the path's rows in the first places of the sequence's, n_kept int32 [B], next int32 [B]: the choice after the last)."""
+        here, N, B = self._here(), parent.numel(), q_begin.numel() - 1
+        if out is None:
+            out = tuple(torch.empty((n,), dtype=torch.int32, device=parent.device) for n in (N, B, B))
+        kept, n_kept, nxt = out
+        i32 = torch.int32
+        _ok(self.lib.pq_tree_accept(self.h, _arr(q_begin, i32, (B + 1,), here, "q_begin"), B, _arr(parent, i32, (N,), here, "parent"), _arr(draft, i32, (N,), here, "draft"),
+                                    _arr(target, i32, (N,), here, "target"), N, _arr(kept, i32, (N,), here, "kept"), _arr(n_kept, i32, (B,), here, "n_kept"),
+                                    _arr(nxt, i32, (B,), here, "next"), torch._C._cuda_getCurrentRawStream(here)), "pq_tree_accept")
+        return out
+
+    def page_keep(self, pages: Pages, q_begin: torch.Tensor, n_kept: torch.Tensor, len_out=None, n_free_out=None) -> None:
+        """Of every sequence's last tokens, as many as it has rows, the first n_kept[b] stay; pages behind the new length go back to the free list. Lengths and count
+        change in place by default."""
+        here, B, s = self._here(pages), pages.B, pages.struct
+        _ok(self.lib.pq_page_keep(self.h, ctypes.byref(s), _arr(q_begin, torch.int32, (B + 1,), here, "q_begin"), _arr(n_kept, torch.int32, (B,), here, "n_kept"),
+                                  s.len if len_out is None else _arr(len_out, torch.int32, (B,), here, "len_out"),
+                                  s.n_free if n_free_out is None else _arr(n_free_out, torch.int32, (1,), here, "n_free_out"),
+                                  torch._C._cuda_getCurrentRawStream(here)), "pq_page_keep")
+
+    def kv4_paged_keep(self, cache: KV4PagedCache, q_begin: torch.Tensor, kept: torch.Tensor, n_kept: torch.Tensor) -> None:
+        """The moves in one layer's cache behind page_keep: the token at place base + kept[q_begin[b] + i] goes to base + i, base = length - n_kept[b]."""
+        here, B, N = self._here(cache.pages), cache.pages.B, kept.numel()
+        _ok(self.lib.pq_kv4_paged_keep(self.h, ctypes.byref(cache.struct), _arr(q_begin, torch.int32, (B + 1,), here, "q_begin"),
+                                       _arr(kept, torch.int32, (N,), here, "kept"), _arr(n_kept, torch.int32, (B,), here, "n_kept"), N,
+                                       torch._C._cuda_getCurrentRawStream(here)), "pq_kv4_paged_keep")
 
     # ---- transformer-block glue -----------------------------------------------------------------
     def rmsnorm(self, x: torch.Tensor, g: torch.Tensor, eps: float = 1e-5, out: torch.Tensor | None = None):

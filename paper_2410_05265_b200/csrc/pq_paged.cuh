@@ -6,6 +6,7 @@
 #define PQ_PAGED_MAX_SEQS 8192
 #define PQ_PAGED_MAX_PREFIX 64
 #define PQ_PAGED_MAX_GROUP 8  // query heads per KV head
+#define PQ_TREE_MAX_ROWS 128  // drafts of a sequence
 
 static inline bool pq_misaligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
 

@@ -28,6 +28,10 @@ struct PagedAttnParams {
   int32_t n_rows, B, max_pages, page_log2, n_pages, Hq, Hkv, G, n_prefix, max_new;
   int32_t csize;    // decode: CTAs of a worker (one cluster)
   int32_t workers;  // 0: one worker per (sequence, KV head)
+  int32_t window;       // 0: none; else the cached keys at the places c - window + 1 .. c of a token at place c, and those before n_sink
+  int32_t n_sink;
+  const uint32_t* mask;  // null, or [n_rows][mask_words]: the drafts of its sequence that a row sees
+  int32_t mask_words;
 };
 
 // One mbarrier try_wait may suspend its thread for thousands of clocks (three of them on a barrier that nothing completes take 15700), in which an ordinary wait ends. A

@@ -97,8 +97,23 @@ __device__ __forceinline__ bool odd_rows(const PagedAttnParams& p, int r0, int r
   return n > p.max_new || n < 0 || (n > 0 && (r0 < 0 || r1 > p.n_rows || bad_len));
 }
 
-// WIDE: clusters of sixteen, for a few long sequences (their merge in the other kernel would cost it registers).
-template <bool DYN, bool WIDE, bool POLL>
+// The cached keys that a windowed token sees, in the kernel's numbering: n_sink first ones, rounded up to a group of 16 (the unit of a copy), then those from the
+// group on that holds the window's first key. What lies between is `skip` keys that are neither requested nor counted as work; the keys hid0 .. hid1 - 1
+// (fewer than 32, at the seam) are brought in and masked. Every group that is brought in holds a key the token sees.
+struct WindowView {
+  int len, skip, sink16, hid0, hid1;
+};
+__device__ __forceinline__ WindowView window_view(const PagedAttnParams& p, int len) {
+  const int lo = max(0, len - p.window);
+  WindowView v;
+  v.sink16 = (p.n_sink + 15) & ~15;
+  v.skip = max(0, lo - v.sink16) & ~15;
+  v.len = len - v.skip, v.hid0 = p.n_sink, v.hid1 = lo - v.skip;
+  return v;
+}
+
+// WIDE: clusters of sixteen, for a few long sequences (their merge in the other kernel would cost it registers). WIN: a window over the cached keys.
+template <bool DYN, bool WIDE, bool POLL, bool WIN>
 __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const PagedAttnParams p) {
   constexpr int SLOT = slot_bytes(DYN);
   extern __shared__ __align__(128) uint8_t dp_smem[];
@@ -152,7 +167,7 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
     if (threadIdx.x == 0 && odd_rows(p, r0, r1, l != len_direct)) pq::report(p.status, PQ_ERR_SHAPE);
     if (!one_row(p, r0, r1)) return leave();  // the whole cluster alike
     row_direct = r0;
-    u1 = max(1, (len_direct + DP_ROUND - 1) / DP_ROUND);
+    u1 = max(1, ((WIN ? window_view(p, len_direct).len : len_direct) + DP_ROUND - 1) / DP_ROUND);
     __syncwarp();
   } else {
     bool odd = false;
@@ -161,7 +176,7 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
       const int r0 = pq::ld_dep(p.q_begin + b), r1 = pq::ld_dep(p.q_begin + b + 1);
       odd |= odd_rows(p, r0, r1, l != lc);
       lens[b] = lc, rows[b] = r0;
-      scan[b] = one_row(p, r0, r1) ? max(1, (lc + DP_ROUND - 1) / DP_ROUND) : 0;
+      scan[b] = one_row(p, r0, r1) ? max(1, ((WIN ? window_view(p, lc).len : lc) + DP_ROUND - 1) / DP_ROUND) : 0;
     }
     __syncthreads();
     const int64_t total = pq::block_scan<DP_THREADS>(scan, p.B, part) * p.Hkv;
@@ -176,11 +191,20 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
   }
   struct Piece {
     int b, h, r0, r1, rounds, len;  // rounds r0 .. r1 - 1 of the `rounds` of the pair
+    int skip, hid1;                 // WIN, with len in the numbering of the window
+  };
+  auto set_len = [&](Piece& x, int len) {
+    x.len = len;
+    if (WIN) {
+      const WindowView v = window_view(p, len);
+      x.len = v.len, x.skip = v.skip, x.hid1 = v.hid1;
+    }
   };
   auto first_piece = [&]() {
     Piece x;
     if (direct) {
-      x.b = b_direct, x.h = h_direct, x.r0 = 0, x.r1 = x.rounds = u1, x.len = len_direct;
+      x.b = b_direct, x.h = h_direct, x.r0 = 0, x.r1 = x.rounds = u1;
+      set_len(x, len_direct);
       return x;
     }
     x.b = pq::find_segment(scan, p.B, u0 / p.Hkv);
@@ -190,7 +214,7 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
     x.h = rel / x.rounds;
     x.r0 = rel - x.h * x.rounds;
     x.r1 = min(x.rounds, x.r0 + (u1 - u0));
-    x.len = lens[x.b];
+    set_len(x, lens[x.b]);
     return x;
   };
   auto advance = [&](Piece& x, int u) {  // to the piece that begins at unit u < u1
@@ -199,7 +223,7 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
       do ++x.b;
       while (scan[x.b + 1] == scan[x.b]);
       x.rounds = scan[x.b + 1] - scan[x.b];
-      x.len = lens[x.b];
+      set_len(x, lens[x.b]);
     }
     x.r0 = 0, x.r1 = min(x.rounds, u1 - u);
   };
@@ -221,10 +245,12 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
   const int64_t page_bytes = static_cast<int64_t>(p.Hkv * 2 * cp_unit) << page_log2;
   const uint8_t* is_src = cp_base;  // the head's rows inside a page
   const int32_t* is_row = p.table;
+  const int sink16 = WIN ? (p.n_sink + 15) & ~15 : 0;
+  auto place_of = [&](int k) { return WIN && k >= sink16 ? k + is_piece.skip : k; };
   // The page of this lane's group of the cursor's block. An id that is none is reported and page 0 read in its place.
   auto fetch_id = [&]() {
     const int k = is_key + 16 * cp_group;
-    is_id = cp_lane && k < is_end ? pq::ld_dep(is_row + (k >> page_log2)) : -1;
+    is_id = cp_lane && k < is_end ? pq::ld_dep(is_row + (place_of(k) >> page_log2)) : -1;
   };
   auto next_piece = [&]() {
     is_ok = false;
@@ -254,7 +280,7 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
         pq::report(p.status, PQ_ERR_SHAPE);
         is_id = 0;
       }
-      pq::bulk_load(cp_dst + s * SLOT, is_src + is_id * page_bytes + (k & page_mask) * cp_unit, cp_bytes, bar);
+      pq::bulk_load(cp_dst + s * SLOT, is_src + is_id * page_bytes + (place_of(k) & page_mask) * cp_unit, cp_bytes, bar);
     }
     ++n_issued;
     is_key += stride;
@@ -389,7 +415,7 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
         // end has the score -inf
         const float* st = reinterpret_cast<const float*>(slot + DP_BLOCK * 128) + lane;
         const float k_step = st[0], v_step = st[DP_BLOCK];
-        const bool dead = key0 + lane >= kend;
+        const bool dead = key0 + lane >= kend || (WIN && key0 + lane >= p.n_sink && key0 + lane < x.hid1);
         sm_step[warp][lane] = dead ? make_float4(0.0f, -INFINITY, 0.0f, 0.0f) : make_float4(k_step, pq::lg2_approx(v_step), pq::rcp_approx(v_step) * pq::PQ_DOWN, 0.0f);
         __syncwarp();
       }
@@ -419,6 +445,14 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
         for (int v = 0; v < 2; ++v) {
           if (key0 + 16 * v + g >= kend) c[v][0] = c[v][1] = -INFINITY;
           if (key0 + 16 * v + 8 + g >= kend) c[v][2] = c[v][3] = -INFINITY;
+        }
+      }
+      if (WIN && !DYN && key0 < x.hid1 && key0 + DP_BLOCK > p.n_sink) {  // the seam between the first keys and the window
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          const int k = key0 + 16 * v + g;
+          if (k >= p.n_sink && k < x.hid1) c[v][0] = c[v][1] = -INFINITY;
+          if (k + 8 >= p.n_sink && k + 8 < x.hid1) c[v][2] = c[v][3] = -INFINITY;
         }
       }
       // maxima of heads 2t, 2t+1 over this lane's keys; a reference moves only when one exceeds it by more than the headroom (the first
@@ -666,20 +700,22 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
 
 constexpr int DP_CTAS_PER_SM = 4;
 
-void (*kernel_of(bool dyn, int csize, bool poll))(const PagedAttnParams) {
-  if (poll) return dyn ? paged_decode_kernel<true, true, true> : paged_decode_kernel<false, true, true>;  // (any cluster size)
-  if (csize > 8) return dyn ? paged_decode_kernel<true, true, false> : paged_decode_kernel<false, true, false>;
-  return dyn ? paged_decode_kernel<true, false, false> : paged_decode_kernel<false, false, false>;
+template <bool WIN>
+void (*kernel_of_form(bool dyn, int csize, bool poll))(const PagedAttnParams) {
+  if (poll) return dyn ? paged_decode_kernel<true, true, true, WIN> : paged_decode_kernel<false, true, true, WIN>;  // (any cluster size)
+  if (csize > 8) return dyn ? paged_decode_kernel<true, true, false, WIN> : paged_decode_kernel<false, true, false, WIN>;
+  return dyn ? paged_decode_kernel<true, false, false, WIN> : paged_decode_kernel<false, false, false, WIN>;
 }
+void (*kernel_of(bool dyn, bool win, int csize, bool poll))(const PagedAttnParams) { return win ? kernel_of_form<true>(dyn, csize, poll) : kernel_of_form<false>(dyn, csize, poll); }
 
 int most_ctas(const pq_ctx* ctx) { return DP_CTAS_PER_SM * ctx->sm_count; }
 
 // Clusters of csize CTAs that are resident at once: fewer than the CTAs alone would be, since a cluster stays inside a group of SMs. Asked once per
 // device, kernel, cluster size and size of the shared memory in whole KB: the answer, and with it how the work is split, follows from the call alone.
-int resident_workers(const pq_ctx* ctx, bool dyn, int csize, size_t smem) {
-  static std::atomic<uint16_t> known[64][2][5][DP_MAX_KB + 1] = {};  // one more than the answer
+int resident_workers(const pq_ctx* ctx, bool dyn, bool win, int csize, size_t smem) {
+  static std::atomic<uint16_t> known[64][2][2][5][DP_MAX_KB + 1] = {};  // one more than the answer
   const int ci = csize == 16 ? 4 : csize == 8 ? 3 : csize == 4 ? 2 : csize == 2 ? 1 : 0;
-  std::atomic<uint16_t>& slot = known[ctx->device][dyn][ci][smem_kb(smem)];
+  std::atomic<uint16_t>& slot = known[ctx->device][dyn][win][ci][smem_kb(smem)];
   int n = slot.load(std::memory_order_relaxed);
   if (n > 0) return n - 1;
   cudaLaunchConfig_t cfg = {};
@@ -691,7 +727,7 @@ int resident_workers(const pq_ctx* ctx, bool dyn, int csize, size_t smem) {
   attr[0].val.clusterDim.x = csize, attr[0].val.clusterDim.y = 1, attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  if (cudaOccupancyMaxActiveClusters(&n, kernel_of(dyn, csize, false), &cfg) != cudaSuccess || n < 1) {
+  if (cudaOccupancyMaxActiveClusters(&n, kernel_of(dyn, win, csize, false), &cfg) != cudaSuccess || n < 1) {
     cudaGetLastError();
     n = csize > 8 ? 0 : ctx->sm_count / csize;  // (clusters of more than eight need not fit at all)
   }
@@ -707,20 +743,21 @@ size_t pq_paged_decode_ws_bytes(const pq_ctx* ctx, const pq_kv4_paged* c) {
 }
 
 pq_status pq_paged_decode_launch(pq_ctx* ctx, const pq_kv4_paged* c, PagedAttnParams p, int64_t max_len, void* ws, cudaStream_t st) {
-  const bool dyn = p.steps != nullptr, poll = p.wait_clocks < PQ_SUSPENDED_CLOCKS;
+  const bool dyn = p.steps != nullptr, win = p.window > 0, poll = p.wait_clocks < PQ_SUSPENDED_CLOCKS;
+  if (win && max_len > static_cast<int64_t>(p.window) + p.n_sink + 30) max_len = static_cast<int64_t>(p.window) + p.n_sink + 30;  // (what window_view leaves at most)
   // the largest there is, once per device and kernel
-  static std::atomic<bool> attr_set[64][2] = {};
+  static std::atomic<bool> attr_set[64][2][2] = {};
   if (ctx->device < 0 || ctx->device >= 64) return PQ_ERR_UNSUPPORTED;
-  if (!attr_set[ctx->device][dyn].load(std::memory_order_relaxed)) {
+  if (!attr_set[ctx->device][dyn][win].load(std::memory_order_relaxed)) {
     const int most = static_cast<int>(DP_MAX_KB * 1024);
-    for (auto* const kern : {kernel_of(dyn, 1, false), kernel_of(dyn, 16, false), kernel_of(dyn, 16, true)}) {
+    for (auto* const kern : {kernel_of(dyn, win, 1, false), kernel_of(dyn, win, 16, false), kernel_of(dyn, win, 16, true)}) {
       if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess ||
-          (kern != kernel_of(dyn, 1, false) && cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)) {
+          (kern != kernel_of(dyn, win, 1, false) && cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)) {
         cudaGetLastError();
         return PQ_ERR_CUDA;
       }
     }
-    attr_set[ctx->device][dyn].store(true, std::memory_order_relaxed);
+    attr_set[ctx->device][dyn][win].store(true, std::memory_order_relaxed);
   }
   const int64_t pairs = static_cast<int64_t>(p.B) * p.Hkv, most = most_ctas(ctx);
   const int64_t rounds = (max_len + DP_ROUND - 1) / DP_ROUND;
@@ -736,8 +773,8 @@ pq_status pq_paged_decode_launch(pq_ctx* ctx, const pq_kv4_paged* c, PagedAttnPa
   int64_t one = csize;
   while (one > 1 && one > rounds) one >>= 1;
   // us with clusters of 8 / 16, 1 sequence of 2100 tokens (17 rounds) 8.3 / 8.9, 4000 10.7 / 9.7, 6000 12.3 / 11.1, 12000 18.9 / 15.0, 20000 27.1 / 20.0.
-  if (one == 8 && rounds >= 24 && pairs * 16 <= ctx->sm_count && pairs <= resident_workers(ctx, dyn, 16, smem_one)) one = 16;
-  bool direct = pairs <= resident_workers(ctx, dyn, static_cast<int>(one), smem_one);
+  if (one == 8 && rounds >= 24 && pairs * 16 <= ctx->sm_count && pairs <= resident_workers(ctx, dyn, win, 16, smem_one)) one = 16;
+  bool direct = pairs <= resident_workers(ctx, dyn, win, static_cast<int>(one), smem_one);
   if (direct) {
     const double sms = ctx->sm_count, per_sm = pairs * one > ctx->sm_count ? pairs * one / sms : 1.0;
     const double t_one = static_cast<double>((rounds + one - 1) / one) * (0.75 + 0.45 * per_sm) + 6.0;
@@ -747,10 +784,10 @@ pq_status pq_paged_decode_launch(pq_ctx* ctx, const pq_kv4_paged* c, PagedAttnPa
   if (direct) csize = one;
   const size_t smem = dynamic_smem(dyn, p.G, p.n_prefix, direct ? 0 : p.B);
   p.csize = static_cast<int32_t>(csize);
-  p.workers = direct ? 0 : resident_workers(ctx, dyn, p.csize, smem);
+  p.workers = direct ? 0 : resident_workers(ctx, dyn, win, p.csize, smem);
   if (p.workers > PQ_PAGED_MAX_WORKERS) p.workers = PQ_PAGED_MAX_WORKERS;
   p.ws_o = static_cast<float*>(ws);
   p.ws_ml = p.ws_o + static_cast<size_t>(2) * p.workers * p.G * 128;
   const int64_t grid = (direct ? pairs : p.workers) * csize;
-  return pq_launch_cluster_pdl(kernel_of(dyn, p.csize, poll), dim3(static_cast<unsigned>(grid)), DP_THREADS, smem, p.csize, st, p);
+  return pq_launch_cluster_pdl(kernel_of(dyn, win, p.csize, poll), dim3(static_cast<unsigned>(grid)), DP_THREADS, smem, p.csize, st, p);
 }

@@ -271,9 +271,45 @@ struct PpItem {
   int base;             // cached keys before the new rows: len - n
   int tiles, j0, j1;    // key tiles of the item (the prefix first), and this worker's
   int u;                // unit where this worker's share begins (an item is PP_ITEM_UNITS units and its tiles)
+  int skip, lo;         // MASKED: key tiles left out behind the first ones, and the first key of the window of any row
 };
 
-template <bool DYN, bool POLL>
+// The keys a .. b - 1 as bits of a word whose bit 0 is key `at`.
+__device__ __forceinline__ uint64_t key_bits(int a, int b, int at) {
+  const int from = max(a - at, 0), to = min(b - at, 64);
+  return from >= to ? 0 : (~0ull >> (64 - (to - from))) << from;
+}
+// Of a word whose bit i is column i of a row, those of the columns 2t, 2t + 1 of every eight: bits 2j, 2j + 1 are columns 8j + 2t, 8j + 2t + 1.
+__device__ __forceinline__ uint32_t own_columns(uint64_t v, int t) {
+  const uint32_t lo = static_cast<uint32_t>(v) >> (2 * t), hi = static_cast<uint32_t>(v >> 32) >> (2 * t);
+  uint32_t r = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) r |= ((lo >> (8 * j)) & 3u) << (2 * j) | ((hi >> (8 * j)) & 3u) << (8 + 2 * j);
+  return r;
+}
+
+// A row's mask: bit u is new row u of its sequence; the row itself is always seen, bits past the sequence's n rows say nothing.
+// Generations above a row: the rows it sees less itself.
+__device__ __forceinline__ int place_in_tree(const uint32_t* mask, int t, int n) {
+  int seen = 0;
+  for (int w = 0; w * 32 < n; ++w) {
+    uint32_t m = pq::ld_dep(mask + w) | (t >> 5 == w ? 1u << (t & 31) : 0u);
+    if (n - w * 32 < 32) m &= (1u << (n - w * 32)) - 1;
+    seen += __popc(m);
+  }
+  return seen - 1;
+}
+// 64 bits of the mask from bit `from` on (zeros outside the words).
+__device__ __forceinline__ uint64_t draft_bits(const uint32_t* mask, int t, int words, int from) {
+  auto word = [&](int w) { return w < 0 || w >= words ? 0u : pq::ld_dep(mask + w) | (t >> 5 == w ? 1u << (t & 31) : 0u); };
+  const int w = from >> 5, sh = from & 31;
+  const uint64_t lo = word(w), mid = word(w + 1), hi = word(w + 2);
+  const uint64_t v = lo | mid << 32;
+  return sh == 0 ? v : v >> sh | hi << (64 - sh);
+}
+
+// MASKED: a window over the cached keys with first keys that stay visible, and (p.mask) rows that see some of the new keys only.
+template <bool DYN, bool POLL, bool MASKED>
 __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const PagedAttnParams p) {
   extern __shared__ uint8_t pp_raw[];
   uint8_t* smem = pp_raw + (-pq::smem_u32(pp_raw) & 1023u);  // (through an integer the compiler would lose sight of shared memory and use generic loads)
@@ -329,10 +365,38 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     x.base = x.len - x.n;
     x.nt = (x.n + R - 1) / R;
   };
+  const bool tree = MASKED && p.mask != nullptr;  // rows see what their masks say of the new keys, each item all key tiles
+  const int first_tiles = MASKED ? (p.n_sink + PP_KEYS - 1) / PP_KEYS : 0;  // key tiles with keys that stay visible
+  // A row at place c sees the keys from c - window + 1 on. An item leaves out the key tiles between the first ones and the one that holds the window's begin of
+  // its first row: (skip_at + rt R) / 128 of them, where that is positive (for a tree, whose rows lie at the root's place or behind it: rt = 0).
+  auto skip_at = [&](const PpItem& x) { return static_cast<int64_t>(x.base) - p.window + 1 - static_cast<int64_t>(first_tiles) * PP_KEYS; };
+  auto skip_of = [&](const PpItem& x, int rt) {
+    if (!MASKED || p.window == 0) return 0;
+    const int64_t v = skip_at(x) + (tree ? 0 : static_cast<int64_t>(rt) * R);
+    return v > 0 ? static_cast<int>(v >> 7) : 0;
+  };
   // key tiles of row tile rt; an item with fewer cached keys than rows counts the tiles as if the keys began at zero
-  auto tiles_of = [&](const PpItem& x, int rt) { return has_prefix + (max(x.base, 0) + min(x.n, (rt + 1) * R) + PP_KEYS - 1) / PP_KEYS; };
+  auto tiles_of = [&](const PpItem& x, int rt) {
+    const int rows = MASKED && tree ? x.n : min(x.n, (rt + 1) * R);
+    return has_prefix + (max(x.base, 0) + rows + PP_KEYS - 1) / PP_KEYS - (MASKED ? skip_of(x, rt) : 0);
+  };
   auto units_before = [&](const PpItem& x, int rt) {  // of the row tiles 0 .. rt - 1, all of them full
-    return static_cast<int64_t>(rt) * (has_prefix + PP_ITEM_UNITS) + (rt > 0 ? floor_sum_128(rt, R, static_cast<int64_t>(max(x.base, 0)) + R + PP_KEYS - 1) : 0);
+    if (MASKED && tree) return static_cast<int64_t>(rt) * (tiles_of(x, 0) + PP_ITEM_UNITS);
+    int64_t u = static_cast<int64_t>(rt) * (has_prefix + PP_ITEM_UNITS) + (rt > 0 ? floor_sum_128(rt, R, static_cast<int64_t>(max(x.base, 0)) + R + PP_KEYS - 1) : 0);
+    if (MASKED && p.window > 0) {
+      const int64_t at = skip_at(x), i0 = at >= 0 ? 0 : (-at + R - 1) / R;  // the first row tile whose window begins behind the first tiles
+      if (rt > i0) u -= floor_sum_128(rt - i0, R, at + i0 * R);
+    }
+    return u;
+  };
+  auto key_of = [&](const PpItem& x, int jt) {  // first key of an item's tile jt
+    const int t = jt - has_prefix;
+    return (MASKED && t >= first_tiles ? t + x.skip : t) * PP_KEYS;
+  };
+  auto set_view = [&](PpItem& x) {
+    if (!MASKED) return;
+    x.skip = skip_of(x, x.rt);
+    x.lo = p.window > 0 ? max(0, static_cast<int>(x.base - p.window + 1 + (tree ? 0 : static_cast<int64_t>(x.rt) * R))) : 0;
   };
   int32_t* scan = reinterpret_cast<int32_t*>(kv_buf);
   __syncthreads();
@@ -419,6 +483,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     load_seq(x, odd);
     x.tiles = tiles_of(x, x.rt), x.j0 = start.j0, x.u = start.u0;
     x.j1 = min(x.tiles, x.j0 + (start.u1 - x.u) - (x.j0 == 0 ? PP_ITEM_UNITS : 0));
+    set_view(x);
     return x;
   };
   auto next_item = [&](PpItem& x) {  // false at the end of the stretch
@@ -437,9 +502,12 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     }
     x.tiles = tiles_of(x, x.rt), x.j0 = 0;
     x.j1 = min(x.tiles, start.u1 - x.u - PP_ITEM_UNITS);
+    set_view(x);
     return true;
   };
-  auto n_ctx_of = [&](const PpItem& x) { return min(x.len, max(x.base, 0) + min(x.n, (x.rt + 1) * R)); };  // cached keys a row of the item may see
+  auto n_ctx_of = [&](const PpItem& x) {  // cached keys a row of the item may see
+    return MASKED && tree ? x.len : min(x.len, max(x.base, 0) + min(x.n, (x.rt + 1) * R));
+  };
   auto second_tile = [&](const PpItem& x) { return x.n > x.rt * R + RT; };  // does the second row tile have rows
 
   // Bounded wait; also gives up when another role of the CTA has raised the abort flag.
@@ -547,13 +615,20 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
       }
       const float scale_ctx = s_k * p.scale2, log2_sv = DYN ? 0.0f : pq::lg2_approx(s_v), inv_sv = DYN ? 1.0f : 1.0f / s_v;
       const int n_ctx = n_ctx_of(x), tile_min_tok = t0 + i * RT;
+      uint32_t rel4 = tok4;  // MASKED: places of the four rows, from place0 on
+      const int place0 = MASKED && !tree ? x.base + t0 : x.base;
+      auto mask_of = [&](int k) { return p.mask + static_cast<int64_t>(x.row0 + min(t0 + static_cast<int>((tok4 >> (8 * k)) & 255u), x.n - 1)) * p.mask_words; };
+      if (MASKED && tree) {
+        rel4 = 0;
+        for (int k = 0; k < 4; ++k) rel4 |= static_cast<uint32_t>(place_in_tree(mask_of(k), min(t0 + static_cast<int>((tok4 >> (8 * k)) & 255u), x.n - 1), x.n)) << (8 * k);
+      }
       float m_ref[4], l[4];  // l: of this thread's columns
 #pragma unroll
       for (int k = 0; k < 4; ++k) m_ref[k] = -INFINITY, l[k] = 0.0f;
       for (int jt = x.j0; jt < x.j1; ++jt, ++c) {
         if (!active) continue;
         const bool is_pre = has_prefix && jt == 0;
-        const int key0 = (jt - has_prefix) * PP_KEYS;
+        const int key0 = key_of(x, jt);
         if (__any_sync(0xffffffffu, !wait(&bars->s_full[i], n_tiles_done & 1) || (DYN && !wait(&bars->v_full[c % PP_STAGES], (c / PP_STAGES) & 1)))) {
           leave();
           pair_any(true);  // the other warp of the rows comes to its vote and learns of it there
@@ -563,7 +638,42 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
         const int c0 = set * PP_HALF_KEYS;  // this thread's first column; the prefix tile has columns for the first set only
         const bool idle = is_pre && set == 1;
         const float scale = is_pre ? p.scale2 : scale_ctx, add = is_pre ? 0.0f : log2_sv;
-        const bool need_mask = is_pre ? p.n_prefix < pre_cols : (key0 + PP_KEYS > x.base + tile_min_tok + 1 || key0 + PP_KEYS > n_ctx);
+        bool need_mask = is_pre ? p.n_prefix < pre_cols : (key0 + PP_KEYS > x.base + (MASKED && tree ? -1 : tile_min_tok) + 1 || key0 + PP_KEYS > n_ctx);
+        uint32_t vis[2] = {~0u, ~0u};  // MASKED: the visible ones of this thread's 16 columns, of rows fr, fr + 8 (16 bits each), of rows fr + 16, fr + 24
+        bool lower = x.j0 == 0 && jt == 1;  // MASKED: differs from row to row
+        uint32_t lower4 = 0;
+        if (MASKED) {
+          // the last row's window begins behind this tile's first key, and the tile is not one of keys that stay visible
+          const int last_place = x.base + (tree ? x.n : min(x.n, tile_min_tok + RT)) - 1;
+          if (!is_pre && p.window > 0 && key0 < last_place - p.window + 1 && key0 + PP_KEYS > p.n_sink) need_mask = true;
+          if (need_mask) {
+            const int at = key0 + c0;
+            for (int k = 0; k < 4; ++k) {
+              uint64_t v;
+              if (is_pre) {
+                v = key_bits(0, p.n_prefix, c0);
+              } else {
+                const int place = min(place0 + static_cast<int>((rel4 >> (8 * k)) & 255u), x.base + x.n - 1), lo = p.window > 0 ? place - p.window + 1 : 0;
+                const int end = min(n_ctx, tree ? x.base : place + 1);  // of the keys that are visible but for the window
+                v = key_bits(max(lo, 0), end, at) | key_bits(0, min(p.n_sink, end), at);
+                if (tree && at + 64 > x.base)
+                  v |= draft_bits(mask_of(k), min(t0 + static_cast<int>((tok4 >> (8 * k)) & 255u), x.n - 1), p.mask_words, at - x.base) & key_bits(max(x.base, 0), x.len, at);
+              }
+              const uint32_t w = own_columns(v, ft) << (16 * (k & 1));
+              if (k & 1)
+                vis[k >> 1] |= w;
+              else
+                vis[k >> 1] = w;
+            }
+          }
+          if (x.j0 == 0 && !is_pre)  // is this the first tile (without a prefix the second) with cached keys that the row sees
+            for (int k = 0; k < 4; ++k) {
+              const int place = min(place0 + static_cast<int>((rel4 >> (8 * k)) & 255u), x.base + x.n - 1);
+              const int first = p.window > 0 && p.n_sink == 0 ? max(0, place - p.window + 1) : 0;
+              const int t = first / PP_KEYS, f = 1 + (t < first_tiles ? t : t - x.skip);
+              if (jt == f) lower4 |= 1u << k;
+            }
+        }
         const PpSteps* st = steps_buf + c % PP_STAGES;
         // w = 2^(exponent - m) against the reference so far, fp16, kept in registers until the whole tile has been looked at. Where an exponent is more than
         // PP_LAZY above the reference (or there is none yet), the reference is moved to a whole number, the sums and O_i are multiplied by the power
@@ -613,7 +723,17 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
                     else
                       ex[2 * n + y] = __ffma2_rn(v, scale2, off2);
                   }
-                if (need_mask) {
+                if (MASKED) {
+                  if (need_mask) {
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+#pragma unroll
+                      for (int n = 0; n < 2; ++n) {
+                        ex[2 * n + y].x = vis[hf] & (1u << (16 * y + 4 * cc + 2 * n)) ? ex[2 * n + y].x : -INFINITY;
+                        ex[2 * n + y].y = vis[hf] & (2u << (16 * y + 4 * cc + 2 * n)) ? ex[2 * n + y].y : -INFINITY;
+                      }
+                  }
+                } else if (need_mask) {
 #pragma unroll
                   for (int y = 0; y < 2; ++y) {
                     const int tk = min(t0 + static_cast<int>((tok4 >> (16 * hf + 8 * y)) & 255u), x.n - 1);
@@ -654,12 +774,12 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
             if (DYN) top[k] -= pq::PQ_UP;
             over |= top[k] > (m_ref[k] == -INFINITY ? -INFINITY : PP_LAZY);
           }
-          if (x.j0 == 0 && jt == 1)  // (of the row's columns of this set)
+          if (MASKED ? x.j0 == 0 && !is_pre : lower)  // (of the row's columns of this set)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               float t = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 1));
               t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
-              over |= t < -PP_LOW && t != -INFINITY;
+              over |= t < -PP_LOW && t != -INFINITY && (!MASKED || (lower4 >> k & 1));
             }
           if (!pair_any(over)) break;
           if (*pair_out) {
@@ -678,7 +798,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             const float most = fmaxf(top[k], *const_cast<const volatile float*>(&bars->row[i][set ^ 1][fr + 8 * k]));
-            const bool first = m_ref[k] == -INFINITY, move = most > (first ? -INFINITY : PP_LAZY) || (most < -PP_LOW && most != -INFINITY && jt == 1 && x.j0 == 0);
+            const bool first = m_ref[k] == -INFINITY, move = most > (first ? -INFINITY : PP_LAZY) || (most < -PP_LOW && most != -INFINITY && (MASKED ? (lower4 >> k & 1) != 0 : lower));
             const float m_new = move ? ceilf(first ? most : m_ref[k] + fmaxf(most, has_prefix ? -PP_FAR_PREFIX : -PP_FAR_CACHED)) : m_ref[k];
             alpha[k] = move ? pq::ex2_approx(m_ref[k] - m_new) : 1.0f;  // 2^(-inf) = 0 for a row that had seen nothing
             l[k] = DYN && move ? pq::at_reference(l[k], m_ref[k] - m_new) : l[k] * alpha[k];
@@ -912,8 +1032,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
           }
           if (DYN && kv) {  // thread j: key j of the tile. A key that no row sees adds nothing.
             const float* st = reinterpret_cast<const float*>(land + slot * PP_LAND + PP_KEYS * 64);
-            const int key = (jt - has_prefix) * PP_KEYS + tid_e;
-            const bool in = !is_pre && key < n_ctx;
+            const int key = key_of(x, jt) + tid_e;
+            const bool in = !is_pre && key < n_ctx && (!MASKED || key >= x.lo || key < p.n_sink);
             const float k_step = in ? st[tid_e] : 1.0f, v_step = in ? st[PP_KEYS + tid_e] : 1.0f;
             float* key_out = reinterpret_cast<float*>(&steps_buf[stage].key[tid_e >> 1]) + (tid_e & 1);
             key_out[0] = k_step * p.scale2, key_out[2] = pq::lg2_approx(v_step);
@@ -944,8 +1064,10 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
         const int n_ctx = n_ctx_of(x);
         const int32_t* row = p.table + static_cast<int64_t>(x.b) * p.max_pages;
         for (int jt = max(x.j0, has_prefix); jt < x.j1 && ok; ++jt) {
-          const int key0 = (jt - has_prefix) * PP_KEYS, n_here = min(pages, (n_ctx - key0 + page - 1) >> p.page_log2);  // pages with keys in them
-          const bool mine = pg < n_here && kind < (DYN ? 3 : 1);
+          const int key0 = key_of(x, jt), n_here = min(pages, (n_ctx - key0 + page - 1) >> p.page_log2);  // pages with keys in them
+          bool mine = pg < n_here && kind < (DYN ? 3 : 1);
+          if (MASKED) mine = mine && (key0 + ((pg + 1) << p.page_log2) > x.lo || key0 + (pg << p.page_log2) < p.n_sink);  // that some row sees
+          const uint32_t n_copies = MASKED ? __popc(__ballot_sync(0xffffffffu, mine && kind == 0)) : static_cast<uint32_t>(max(n_here, 0));
           int id = 0;
           if (mine) {
             id = pq::ld_dep(row + (key0 >> p.page_log2) + pg);
@@ -963,8 +1085,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
               break;
             }
             const uint32_t dst = pq::smem_u32(land + slot * PP_LAND);
-            const uint32_t n_pages = static_cast<uint32_t>(max(n_here, 0));
-            if (lane == 0) pq::mbar_arrive_expect_tx(&bars->land_full[slot], n_pages * page * (64 + (DYN && kv ? 8 : 0)));
+            if (lane == 0) pq::mbar_arrive_expect_tx(&bars->land_full[slot], n_copies * page * (64 + (DYN && kv ? 8 : 0)));
             __syncwarp();
             if (mine && kind == 0)
               pq::bulk_load(dst + pg * page * 64, p.codes + (vec + kv * page) * 64, page * 64, &bars->land_full[slot]);
@@ -1084,6 +1205,12 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
   }
 }
 
+template <bool MASKED>
+void (*kernel_of(bool dyn, bool poll))(const PagedAttnParams) {
+  if (poll) return dyn ? paged_prefill_kernel<true, true, MASKED> : paged_prefill_kernel<false, true, MASKED>;
+  return dyn ? paged_prefill_kernel<true, false, MASKED> : paged_prefill_kernel<false, false, MASKED>;
+}
+
 }  // namespace
 
 size_t pq_paged_prefill_ws_bytes(const pq_ctx* ctx) {
@@ -1091,17 +1218,16 @@ size_t pq_paged_prefill_ws_bytes(const pq_ctx* ctx) {
 }
 
 pq_status pq_paged_prefill_launch(pq_ctx* ctx, PagedAttnParams p, void* ws, cudaStream_t st) {
-  const bool dyn = p.steps != nullptr, poll = p.wait_clocks < PQ_SUSPENDED_CLOCKS;
-  void (*const kern)(const PagedAttnParams) = poll ? (dyn ? paged_prefill_kernel<true, true> : paged_prefill_kernel<false, true>)
-                                                   : (dyn ? paged_prefill_kernel<true, false> : paged_prefill_kernel<false, false>);
-  static std::atomic<bool> attr_set[64][2][2] = {};
+  const bool dyn = p.steps != nullptr, poll = p.wait_clocks < PQ_SUSPENDED_CLOCKS, masked = p.window > 0 || p.mask;
+  void (*const kern)(const PagedAttnParams) = masked ? kernel_of<true>(dyn, poll) : kernel_of<false>(dyn, poll);
+  static std::atomic<bool> attr_set[64][2][2][2] = {};
   if (ctx->device < 0 || ctx->device >= 64 || ctx->sm_count > PQ_PAGED_MAX_WORKERS) return PQ_ERR_UNSUPPORTED;
-  if (!attr_set[ctx->device][dyn][poll].load(std::memory_order_relaxed)) {
+  if (!attr_set[ctx->device][dyn][poll][masked].load(std::memory_order_relaxed)) {
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(PP_SMEM_BYTES)) != cudaSuccess) {
       cudaGetLastError();
       return PQ_ERR_CUDA;
     }
-    attr_set[ctx->device][dyn][poll].store(true, std::memory_order_relaxed);
+    attr_set[ctx->device][dyn][poll][masked].store(true, std::memory_order_relaxed);
   }
   p.ws_o = static_cast<float*>(ws);
   p.ws_ml = p.ws_o + static_cast<size_t>(2) * ctx->sm_count * PP_PARTIAL;

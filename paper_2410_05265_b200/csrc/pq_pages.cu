@@ -178,6 +178,61 @@ __global__ void __launch_bounds__(PG_THREADS) page_release_kernel(const PlanPara
   if (tid == 0) *p.n_free_out = refused ? n_free : n_free + static_cast<int32_t>(total);
 }
 
+// The last tokens of a sequence leave: of the rows q_begin[b] .. q_begin[b + 1] - 1, which are the last of the cached ones, the first n_kept[b] stay. Shared memory:
+// pages[B + 1], len[B] (after).
+__global__ void __launch_bounds__(PG_THREADS) page_keep_kernel(const PlanParams p) {
+  extern __shared__ __align__(16) int32_t pg_smem[];
+  __shared__ int64_t part[PG_THREADS / 32];
+  __shared__ int bad, no_id;
+  int32_t *pages = pg_smem, *len = pages + p.B + 1;
+  pq::pdl_wait();
+  if (threadIdx.x == 0) bad = no_id = 0;
+  __syncthreads();
+  const int32_t n_free = pq::ld_dep(p.n_free);
+  const int64_t capacity = static_cast<int64_t>(p.max_pages) << p.page_log2;
+  for (int b = threadIdx.x; b < p.B; b += PG_THREADS) {
+    const int64_t l = pq::ld_dep(p.len + b), k = pq::ld_dep(p.n_new + b), n = static_cast<int64_t>(pq::ld_dep(p.q_begin + b + 1)) - pq::ld_dep(p.q_begin + b);
+    const bool ok = l >= 0 && l <= capacity && k >= 0 && k <= n && n <= l;
+    if (!ok) bad = 1;
+    len[b] = ok ? static_cast<int32_t>(l - n + k) : 0;
+    pages[b] = ok ? pages_of(static_cast<int32_t>(l), p.page_log2) - pages_of(len[b], p.page_log2) : 0;
+  }
+  __syncthreads();
+  const int64_t total = pq::block_scan<PG_THREADS>(pages, p.B, part);
+  bool refused = bad || n_free < 0 || n_free + total > p.n_pages;
+  const int n_ctas = gridDim.x, tid = blockIdx.x * PG_THREADS + threadIdx.x, n_threads = n_ctas * PG_THREADS;
+  auto page_id = [&](int64_t k) {  // the k-th page that goes back
+    const int b = pq::find_segment(pages, p.B, static_cast<int32_t>(k));
+    return pq::ld_dep(p.table + static_cast<int64_t>(b) * p.max_pages + pages_of(len[b], p.page_log2) + (k - pages[b]));
+  };
+  int32_t first = 0;
+  if (!refused) {  // are all of them ids
+    bool none = false;
+    for (int64_t k = tid; k < total; k += n_threads) {
+      const int32_t id = page_id(k);
+      if (k == tid) first = id;
+      none |= id < 0 || id >= p.n_pages;
+    }
+    if (none) no_id = 1;
+    if (n_ctas > 1) {
+      pq::cluster_sync();
+      refused = __syncthreads_or(threadIdx.x < n_ctas && pq::ld_cluster(&no_id, threadIdx.x));
+    } else {
+      __syncthreads();
+      refused = no_id;
+    }
+  }
+  if (!refused) {
+    for (int64_t k = tid; k < total; k += n_threads) p.free_list[n_free + k] = k == tid ? first : page_id(k);
+  } else if (tid == 0) {
+    pq::report(p.status, PQ_ERR_SHAPE);
+  }
+  if (n_ctas > 1) pq::cluster_sync();  // every CTA has read the lengths and the count
+  __syncthreads();
+  for (int b = tid; b < p.B; b += n_threads) p.len_out[b] = refused ? pq::ld_dep(p.len + b) : len[b];
+  if (tid == 0) *p.n_free_out = refused ? n_free : n_free + static_cast<int32_t>(total);
+}
+
 // Bytes of dynamic shared memory of `arrays` arrays over the sequences, some of them one longer.
 constexpr size_t pg_smem_bytes(int64_t B, int arrays, int longer) { return (static_cast<size_t>(arrays) * B + longer) * sizeof(int32_t); }
 
@@ -232,4 +287,15 @@ extern "C" pq_status pq_page_release(pq_ctx* ctx, const pq_pages* pages, const i
   p.n_new = done, p.len_out = len_out, p.n_free_out = n_free_out;
   static std::atomic<bool> limit_set[64] = {};
   return launch(ctx, page_release_kernel, limit_set, p, pages->n_pages, 2, 1, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" pq_status pq_page_keep(pq_ctx* ctx, const pq_pages* pages, const int32_t* q_begin, const int32_t* n_kept, int32_t* len_out, int32_t* n_free_out, void* stream) {
+  if (!ctx || !n_free_out) return PQ_ERR_INVALID_ARG;
+  const pq_status st = pq_check_pages(pages);
+  if (st != PQ_OK) return st;
+  if (pages->B > 0 && (!q_begin || !n_kept || !len_out)) return PQ_ERR_INVALID_ARG;
+  PlanParams p = base_params(ctx, pages);
+  p.q_begin = const_cast<int32_t*>(q_begin), p.n_new = n_kept, p.len_out = len_out, p.n_free_out = n_free_out;
+  static std::atomic<bool> limit_set[64] = {};
+  return launch(ctx, page_keep_kernel, limit_set, p, pages->B, 2, 1, static_cast<cudaStream_t>(stream));
 }
