@@ -22,7 +22,7 @@ pq_status attention(pq_ctx* ctx, const pq_kv4_paged* c, const void* q, int64_t l
   if (!q || !out || !q_begin || ldq < static_cast<int64_t>(c->Hq) * 128) return PQ_ERR_INVALID_ARG;
   if (n_rows > 0x7fffffffll) return PQ_ERR_SHAPE;
   if (pq_misaligned16(q) || pq_misaligned16(out) || pq_misaligned16(ws) || ldq % 8 != 0) return PQ_ERR_ALIGN;
-  if (!ws || ws_bytes < pq_attn_kv4_paged_workspace_bytes(ctx, c, n_rows, max_new)) return PQ_ERR_WORKSPACE;
+  if (!ws || ws_bytes < (mask ? pq_attn_kv4_paged_tree_workspace_bytes : pq_attn_kv4_paged_workspace_bytes)(ctx, c, n_rows, max_new)) return PQ_ERR_WORKSPACE;
   PagedAttnParams p{};
   p.q = static_cast<const __nv_bfloat16*>(q), p.ldq = ldq, p.out = static_cast<__nv_bfloat16*>(out), p.q_begin = q_begin;
   p.len = c->pages.len, p.table = c->pages.table;
@@ -37,6 +37,7 @@ pq_status attention(pq_ctx* ctx, const pq_kv4_paged* c, const void* q, int64_t l
   // a window that holds every cache is none; numbers past any cache's end stay clear of the end of 32 bits
   p.window = window >= capacity ? 0 : window, p.n_sink = p.window == 0 ? 0 : n_sink < capacity ? n_sink : static_cast<int32_t>(capacity);
   p.mask = mask, p.mask_words = mask_words;
+  if (mask) return pq_paged_tree_launch(ctx, p, ws, static_cast<cudaStream_t>(stream));
   // The kernel for several rows takes whole SMs and goes first; the one for single tokens, whose CTAs are small, starts beside it on the SMs that it leaves.
   if (max_new > 1) {
     st = pq_paged_prefill_launch(ctx, p, static_cast<uint8_t*>(ws) + pq_paged_decode_ws_bytes(ctx, c), static_cast<cudaStream_t>(stream));
@@ -60,7 +61,8 @@ extern "C" pq_status pq_attn_kv4_paged_window(pq_ctx* ctx, const pq_kv4_paged* c
 }
 
 extern "C" size_t pq_attn_kv4_paged_tree_workspace_bytes(const pq_ctx* ctx, const pq_kv4_paged* cache, int64_t n_rows, int32_t max_new) {
-  return pq_attn_kv4_paged_workspace_bytes(ctx, cache, n_rows, max_new);
+  if (!ctx || pq_check_paged(cache) != PQ_OK || n_rows <= 0 || max_new <= 0) return 0;
+  return pq_paged_tree_ws_bytes(ctx);
 }
 
 extern "C" pq_status pq_attn_kv4_paged_tree(pq_ctx* ctx, const pq_kv4_paged* c, const void* q, int64_t ldq, const int32_t* q_begin, int64_t n_rows,

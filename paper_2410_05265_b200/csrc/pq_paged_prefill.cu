@@ -35,7 +35,7 @@
 #include <atomic>
 #include <type_traits>
 
-#include "pq_paged_attn.cuh"
+#include "pq_paged_mma.cuh"
 
 namespace {
 
@@ -94,100 +94,9 @@ constexpr size_t PP_SMEM_BYTES = 1024 /*alignment slack*/ + 2 * PP_TILE /*Q*/ + 
 static_assert(PP_SMEM_BYTES <= 227 * 1024, "shared memory budget");
 static_assert((PQ_PAGED_MAX_SEQS + 1) * 4 <= PP_STAGES * 2 * PP_TILE, "the prefix sums lie in the K and V buffers before the pipeline starts");
 
-__device__ __forceinline__ float max3f(float a, float b, float c) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
-__device__ __forceinline__ uint32_t hfma2_u32(uint32_t a, uint32_t b, uint32_t c) {
-  uint32_t d;
-  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-  return d;
-}
-__device__ __forceinline__ uint32_t bsub2_u32(uint32_t a, uint32_t b) {
-  uint32_t d;
-  asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-  return d;
-}
-// Eight codes of one packed word (nibble i = head dim i of the group) as exact fp16 integers in the order (0,4) (1,5) (2,6) (3,7): nibbles 0 and 4 under the
-// exponent of 1024 read 1032 + code, nibbles 1 and 5 stay four bits up and read 1152 + 16 * code; one fused multiply-add each removes the offset
-// (and the factor 16).
-__device__ __forceinline__ uint4 expand8_f16(uint32_t w) {
-  const uint32_t w8 = w >> 8;
-  const uint32_t ONE = 0x3C003C00u, SIXTEENTH = 0x2C002C00u;  // half2(1, 1), half2(1/16, 1/16)
-  const uint32_t M1032 = 0xE408E408u, M72 = 0xD480D480u;      // half2(-1032, -1032), half2(-72, -72)
-  uint4 o;
-  o.x = hfma2_u32(pq::and_xor<0x000F000Fu, 0x64086408u>(w), ONE, M1032);
-  o.y = hfma2_u32(pq::and_xor<0x00F000F0u, 0x64806480u>(w), SIXTEENTH, M72);
-  o.z = hfma2_u32(pq::and_xor<0x000F000Fu, 0x64086408u>(w8), ONE, M1032);
-  o.w = hfma2_u32(pq::and_xor<0x00F000F0u, 0x64806480u>(w8), SIXTEENTH, M72);
-  return o;
-}
-// The same as exact bf16 integers: under the exponent of 128 (bf16 has seven fraction bits) a nibble reads 136 + code.
-__device__ __forceinline__ uint4 expand8_bf16(uint32_t w) {
-  const uint32_t OFF = 0x43084308u;  // bf16x2(136, 136)
-  return make_uint4(bsub2_u32(pq::and_xor<0x000F000Fu, 0x43084308u>(w), OFF), bsub2_u32(pq::and_xor<0x000F000Fu, 0x43084308u>(w >> 4), OFF),
-                    bsub2_u32(pq::and_xor<0x000F000Fu, 0x43084308u>(w >> 8), OFF), bsub2_u32(pq::and_xor<0x000F000Fu, 0x43084308u>(w >> 12), OFF));
-}
-// Eight two-byte values (d0 .. d7 in four words) in the same order (0,4) (1,5) (2,6) (3,7).
-__device__ __forceinline__ uint4 permute8(const uint4& v) {
-  return make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
-}
-// Two fp16 values as two bf16 terms whose sum they are (8 + 8 of at most 11 significand bits): the first or the second.
-__device__ __forceinline__ uint32_t bf16_term(uint32_t h2, bool second) {
-  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h2));
-  __nv_bfloat162 b = __floats2bfloat162_rn(f.x, f.y);
-  if (second) {
-    const float2 hi = __bfloat1622float2(b);
-    b = __floats2bfloat162_rn(f.x - hi.x, f.y - hi.y);
-  }
-  return *reinterpret_cast<const uint32_t*>(&b);
-}
 // Byte offset of 16-byte chunk c16 (eight dims; 0..15) of row r inside a [rows][128] tile of two-byte values.
 __device__ __forceinline__ uint32_t tile_off(int r, int c16) {
   return static_cast<uint32_t>((c16 >> 3) * PP_HALF + r * 128 + (((c16 & 7) ^ (r & 7)) << 4));
-}
-__device__ __forceinline__ void sts128(uint32_t a, const uint4& v) {
-  asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-}
-
-// ---- tcgen05 forms used here (cta_group::1, kind::f16) ----------------------------------------------------
-// Instruction descriptor: A and B both fp16 or both bf16 -> fp32, A K-major (or in tensor memory), B K-major or MN-major.
-__host__ __device__ constexpr uint32_t idesc_16(int M, int N, bool bf16, bool b_mn_major) {
-  return (1u << 4) /*D = f32*/ | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (b_mn_major ? (1u << 16) : 0u) | (static_cast<uint32_t>(N >> 3) << 17) |
-         (static_cast<uint32_t>(M >> 4) << 24);
-}
-// Shared-memory descriptor of a 128-byte-swizzled operand whose rows are 128 bytes and whose 8-row groups are 1024 bytes apart. K-major use: rows =
-// M/N index, the row's bytes = 64 K elements (lbo unused). MN-major use: rows = K index, the row's bytes = 64 M/N elements, lbo = distance
-// to the next 64 M/N elements.
-__device__ __forceinline__ uint64_t desc_sw128(uint32_t smem_addr, uint32_t lbo_bytes) {
-  uint64_t d = 0;
-  d |= static_cast<uint64_t>((smem_addr >> 4) & 0x3FFF);
-  d |= static_cast<uint64_t>((lbo_bytes >> 4) & 0x3FFF) << 16;
-  d |= static_cast<uint64_t>(1024 >> 4) << 32;
-  d |= static_cast<uint64_t>(1) << 46;
-  d |= static_cast<uint64_t>(2) << 61;
-  return d;
-}
-__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n"
-      ".reg .pred p;\n"
-      "setp.ne.b32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
-      "}\n" ::"r"(d_tmem),
-      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n"
-      ".reg .pred p;\n"
-      "setp.ne.b32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
-      "}\n" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
-      : "memory");
 }
 constexpr int PP_CHUNK = 16;  // score columns of a step of the softmax
 // 16 rows x 16 columns as a matrix fragment: lane 4g + t gets columns 8n + 2t, 8n + 2t + 1 of row g (r[4n], r[4n + 1]) and of row g + 8 (r[4n + 2], r[4n + 3]).
@@ -204,24 +113,6 @@ __device__ __forceinline__ void tmem_ld_wait_frag(uint32_t (&r)[8]) {
                :
                : "memory");
 }
-// 16 rows x 32 words, the counterpart: lane 4g + t has word 4n + t of row g (r[2n]) and of row g + 8 (r[2n + 1]).
-__device__ __forceinline__ void tmem_st_frag(uint32_t taddr, const uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-      : "memory");
-}
-__device__ __forceinline__ void tmem_ld_32x16(uint32_t taddr, uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
-      "tcgen05.wait::ld.sync.aligned;"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
-        "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr)
-      : "memory");
-}
 // Exchanges between lanes l and l ^ m: the lane with the bit clear keeps a and receives the other's a as b, the other keeps b and receives b as a.
 __device__ __forceinline__ void swap_halves(uint4& a, uint4& b, bool bit, int m) {
   uint4 t = bit ? a : b;
@@ -232,15 +123,6 @@ __device__ __forceinline__ void swap_halves(uint4& a, uint4& b, bool bit, int m)
   else
     b = t;
 }
-__device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-      : "memory");
-}
-
 // sum_{i=0}^{n-1} floor((a i + b) / 128) for a, b >= 0, by the Euclidean reduction of the lattice points under a line (the first step is by shifts).
 __device__ int64_t floor_sum_128(int64_t n, int64_t a, int64_t b) {
   int64_t s = (a >> 7) * (n * (n - 1) / 2) + (b >> 7) * n;
@@ -271,7 +153,7 @@ struct PpItem {
   int base;             // cached keys before the new rows: len - n
   int tiles, j0, j1;    // key tiles of the item (the prefix first), and this worker's
   int u;                // unit where this worker's share begins (an item is PP_ITEM_UNITS units and its tiles)
-  int skip, lo;         // MASKED: key tiles left out behind the first ones, and the first key of the window of any row
+  int skip, lo;         // WIN: key tiles left out behind the first ones, and the first key of the window of any row
 };
 
 // The keys a .. b - 1 as bits of a word whose bit 0 is key `at`.
@@ -288,28 +170,8 @@ __device__ __forceinline__ uint32_t own_columns(uint64_t v, int t) {
   return r;
 }
 
-// A row's mask: bit u is new row u of its sequence; the row itself is always seen, bits past the sequence's n rows say nothing.
-// Generations above a row: the rows it sees less itself.
-__device__ __forceinline__ int place_in_tree(const uint32_t* mask, int t, int n) {
-  int seen = 0;
-  for (int w = 0; w * 32 < n; ++w) {
-    uint32_t m = pq::ld_dep(mask + w) | (t >> 5 == w ? 1u << (t & 31) : 0u);
-    if (n - w * 32 < 32) m &= (1u << (n - w * 32)) - 1;
-    seen += __popc(m);
-  }
-  return seen - 1;
-}
-// 64 bits of the mask from bit `from` on (zeros outside the words).
-__device__ __forceinline__ uint64_t draft_bits(const uint32_t* mask, int t, int words, int from) {
-  auto word = [&](int w) { return w < 0 || w >= words ? 0u : pq::ld_dep(mask + w) | (t >> 5 == w ? 1u << (t & 31) : 0u); };
-  const int w = from >> 5, sh = from & 31;
-  const uint64_t lo = word(w), mid = word(w + 1), hi = word(w + 2);
-  const uint64_t v = lo | mid << 32;
-  return sh == 0 ? v : v >> sh | hi << (64 - sh);
-}
-
-// MASKED: a window over the cached keys with first keys that stay visible, and (p.mask) rows that see some of the new keys only.
-template <bool DYN, bool POLL, bool MASKED>
+// WIN: a window over the cached keys with first keys that stay visible.
+template <bool DYN, bool POLL, bool WIN>
 __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const PagedAttnParams p) {
   extern __shared__ uint8_t pp_raw[];
   uint8_t* smem = pp_raw + (-pq::smem_u32(pp_raw) & 1023u);  // (through an integer the compiler would lose sight of shared memory and use generic loads)
@@ -365,25 +227,22 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     x.base = x.len - x.n;
     x.nt = (x.n + R - 1) / R;
   };
-  const bool tree = MASKED && p.mask != nullptr;  // rows see what their masks say of the new keys, each item all key tiles
-  const int first_tiles = MASKED ? (p.n_sink + PP_KEYS - 1) / PP_KEYS : 0;  // key tiles with keys that stay visible
+  const int first_tiles = WIN ? (p.n_sink + PP_KEYS - 1) / PP_KEYS : 0;  // key tiles with keys that stay visible
   // A row at place c sees the keys from c - window + 1 on. An item leaves out the key tiles between the first ones and the one that holds the window's begin of
-  // its first row: (skip_at + rt R) / 128 of them, where that is positive (for a tree, whose rows lie at the root's place or behind it: rt = 0).
+  // its first row: (skip_at + rt R) / 128 of them, where that is positive.
   auto skip_at = [&](const PpItem& x) { return static_cast<int64_t>(x.base) - p.window + 1 - static_cast<int64_t>(first_tiles) * PP_KEYS; };
   auto skip_of = [&](const PpItem& x, int rt) {
-    if (!MASKED || p.window == 0) return 0;
-    const int64_t v = skip_at(x) + (tree ? 0 : static_cast<int64_t>(rt) * R);
+    if (!WIN) return 0;
+    const int64_t v = skip_at(x) + static_cast<int64_t>(rt) * R;
     return v > 0 ? static_cast<int>(v >> 7) : 0;
   };
   // key tiles of row tile rt; an item with fewer cached keys than rows counts the tiles as if the keys began at zero
   auto tiles_of = [&](const PpItem& x, int rt) {
-    const int rows = MASKED && tree ? x.n : min(x.n, (rt + 1) * R);
-    return has_prefix + (max(x.base, 0) + rows + PP_KEYS - 1) / PP_KEYS - (MASKED ? skip_of(x, rt) : 0);
+    return has_prefix + (max(x.base, 0) + min(x.n, (rt + 1) * R) + PP_KEYS - 1) / PP_KEYS - skip_of(x, rt);
   };
   auto units_before = [&](const PpItem& x, int rt) {  // of the row tiles 0 .. rt - 1, all of them full
-    if (MASKED && tree) return static_cast<int64_t>(rt) * (tiles_of(x, 0) + PP_ITEM_UNITS);
     int64_t u = static_cast<int64_t>(rt) * (has_prefix + PP_ITEM_UNITS) + (rt > 0 ? floor_sum_128(rt, R, static_cast<int64_t>(max(x.base, 0)) + R + PP_KEYS - 1) : 0);
-    if (MASKED && p.window > 0) {
+    if (WIN) {
       const int64_t at = skip_at(x), i0 = at >= 0 ? 0 : (-at + R - 1) / R;  // the first row tile whose window begins behind the first tiles
       if (rt > i0) u -= floor_sum_128(rt - i0, R, at + i0 * R);
     }
@@ -391,12 +250,12 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
   };
   auto key_of = [&](const PpItem& x, int jt) {  // first key of an item's tile jt
     const int t = jt - has_prefix;
-    return (MASKED && t >= first_tiles ? t + x.skip : t) * PP_KEYS;
+    return (WIN && t >= first_tiles ? t + x.skip : t) * PP_KEYS;
   };
   auto set_view = [&](PpItem& x) {
-    if (!MASKED) return;
+    if (!WIN) return;
     x.skip = skip_of(x, x.rt);
-    x.lo = p.window > 0 ? max(0, static_cast<int>(x.base - p.window + 1 + (tree ? 0 : static_cast<int64_t>(x.rt) * R))) : 0;
+    x.lo = max(0, x.base - p.window + 1 + x.rt * R);
   };
   int32_t* scan = reinterpret_cast<int32_t*>(kv_buf);
   __syncthreads();
@@ -506,7 +365,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     return true;
   };
   auto n_ctx_of = [&](const PpItem& x) {  // cached keys a row of the item may see
-    return MASKED && tree ? x.len : min(x.len, max(x.base, 0) + min(x.n, (x.rt + 1) * R));
+    return min(x.len, max(x.base, 0) + min(x.n, (x.rt + 1) * R));
   };
   auto second_tile = [&](const PpItem& x) { return x.n > x.rt * R + RT; };  // does the second row tile have rows
 
@@ -615,13 +474,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
       }
       const float scale_ctx = s_k * p.scale2, log2_sv = DYN ? 0.0f : pq::lg2_approx(s_v), inv_sv = DYN ? 1.0f : 1.0f / s_v;
       const int n_ctx = n_ctx_of(x), tile_min_tok = t0 + i * RT;
-      uint32_t rel4 = tok4;  // MASKED: places of the four rows, from place0 on
-      const int place0 = MASKED && !tree ? x.base + t0 : x.base;
-      auto mask_of = [&](int k) { return p.mask + static_cast<int64_t>(x.row0 + min(t0 + static_cast<int>((tok4 >> (8 * k)) & 255u), x.n - 1)) * p.mask_words; };
-      if (MASKED && tree) {
-        rel4 = 0;
-        for (int k = 0; k < 4; ++k) rel4 |= static_cast<uint32_t>(place_in_tree(mask_of(k), min(t0 + static_cast<int>((tok4 >> (8 * k)) & 255u), x.n - 1), x.n)) << (8 * k);
-      }
+      auto place_of = [&](int k) { return x.base + min(t0 + static_cast<int>((tok4 >> (8 * k)) & 255u), x.n - 1); };  // of row fr + 8k
       float m_ref[4], l[4];  // l: of this thread's columns
 #pragma unroll
       for (int k = 0; k < 4; ++k) m_ref[k] = -INFINITY, l[k] = 0.0f;
@@ -638,27 +491,20 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
         const int c0 = set * PP_HALF_KEYS;  // this thread's first column; the prefix tile has columns for the first set only
         const bool idle = is_pre && set == 1;
         const float scale = is_pre ? p.scale2 : scale_ctx, add = is_pre ? 0.0f : log2_sv;
-        bool need_mask = is_pre ? p.n_prefix < pre_cols : (key0 + PP_KEYS > x.base + (MASKED && tree ? -1 : tile_min_tok) + 1 || key0 + PP_KEYS > n_ctx);
-        uint32_t vis[2] = {~0u, ~0u};  // MASKED: the visible ones of this thread's 16 columns, of rows fr, fr + 8 (16 bits each), of rows fr + 16, fr + 24
-        bool lower = x.j0 == 0 && jt == 1;  // MASKED: differs from row to row
+        bool need_mask = is_pre ? p.n_prefix < pre_cols : (key0 + PP_KEYS > x.base + tile_min_tok + 1 || key0 + PP_KEYS > n_ctx);
+        uint32_t vis[2] = {~0u, ~0u};  // WIN: the visible ones of this thread's 16 columns, of rows fr, fr + 8 (16 bits each), of rows fr + 16, fr + 24
+        // Is this the first tile (without a prefix the second) with cached keys that the row sees? With a window that differs from row to row.
+        const bool lower = x.j0 == 0 && jt == 1;
         uint32_t lower4 = 0;
-        if (MASKED) {
+        if (WIN) {
           // the last row's window begins behind this tile's first key, and the tile is not one of keys that stay visible
-          const int last_place = x.base + (tree ? x.n : min(x.n, tile_min_tok + RT)) - 1;
-          if (!is_pre && p.window > 0 && key0 < last_place - p.window + 1 && key0 + PP_KEYS > p.n_sink) need_mask = true;
+          const int last_place = x.base + min(x.n, tile_min_tok + RT) - 1;
+          if (!is_pre && key0 < last_place - p.window + 1 && key0 + PP_KEYS > p.n_sink) need_mask = true;
           if (need_mask) {
             const int at = key0 + c0;
             for (int k = 0; k < 4; ++k) {
-              uint64_t v;
-              if (is_pre) {
-                v = key_bits(0, p.n_prefix, c0);
-              } else {
-                const int place = min(place0 + static_cast<int>((rel4 >> (8 * k)) & 255u), x.base + x.n - 1), lo = p.window > 0 ? place - p.window + 1 : 0;
-                const int end = min(n_ctx, tree ? x.base : place + 1);  // of the keys that are visible but for the window
-                v = key_bits(max(lo, 0), end, at) | key_bits(0, min(p.n_sink, end), at);
-                if (tree && at + 64 > x.base)
-                  v |= draft_bits(mask_of(k), min(t0 + static_cast<int>((tok4 >> (8 * k)) & 255u), x.n - 1), p.mask_words, at - x.base) & key_bits(max(x.base, 0), x.len, at);
-              }
+              const int place = place_of(k), end = is_pre ? p.n_prefix : min(n_ctx, place + 1);
+              const uint64_t v = is_pre ? key_bits(0, end, c0) : key_bits(max(place - p.window + 1, 0), end, at) | key_bits(0, min(p.n_sink, end), at);
               const uint32_t w = own_columns(v, ft) << (16 * (k & 1));
               if (k & 1)
                 vis[k >> 1] |= w;
@@ -666,12 +512,10 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
                 vis[k >> 1] = w;
             }
           }
-          if (x.j0 == 0 && !is_pre)  // is this the first tile (without a prefix the second) with cached keys that the row sees
+          if (x.j0 == 0 && !is_pre)
             for (int k = 0; k < 4; ++k) {
-              const int place = min(place0 + static_cast<int>((rel4 >> (8 * k)) & 255u), x.base + x.n - 1);
-              const int first = p.window > 0 && p.n_sink == 0 ? max(0, place - p.window + 1) : 0;
-              const int t = first / PP_KEYS, f = 1 + (t < first_tiles ? t : t - x.skip);
-              if (jt == f) lower4 |= 1u << k;
+              const int first = p.n_sink == 0 ? max(0, place_of(k) - p.window + 1) : 0, t = first / PP_KEYS;
+              if (jt == 1 + (t < first_tiles ? t : t - x.skip)) lower4 |= 1u << k;
             }
         }
         const PpSteps* st = steps_buf + c % PP_STAGES;
@@ -723,7 +567,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
                     else
                       ex[2 * n + y] = __ffma2_rn(v, scale2, off2);
                   }
-                if (MASKED) {
+                if (WIN) {
                   if (need_mask) {
 #pragma unroll
                     for (int y = 0; y < 2; ++y)
@@ -774,12 +618,12 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
             if (DYN) top[k] -= pq::PQ_UP;
             over |= top[k] > (m_ref[k] == -INFINITY ? -INFINITY : PP_LAZY);
           }
-          if (MASKED ? x.j0 == 0 && !is_pre : lower)  // (of the row's columns of this set)
+          if (WIN ? x.j0 == 0 && !is_pre : lower)  // (of the row's columns of this set)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               float t = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 1));
               t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
-              over |= t < -PP_LOW && t != -INFINITY && (!MASKED || (lower4 >> k & 1));
+              over |= t < -PP_LOW && t != -INFINITY && (!WIN || (lower4 >> k & 1));
             }
           if (!pair_any(over)) break;
           if (*pair_out) {
@@ -798,7 +642,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             const float most = fmaxf(top[k], *const_cast<const volatile float*>(&bars->row[i][set ^ 1][fr + 8 * k]));
-            const bool first = m_ref[k] == -INFINITY, move = most > (first ? -INFINITY : PP_LAZY) || (most < -PP_LOW && most != -INFINITY && (MASKED ? (lower4 >> k & 1) != 0 : lower));
+            const bool first = m_ref[k] == -INFINITY, move = most > (first ? -INFINITY : PP_LAZY) || (most < -PP_LOW && most != -INFINITY && (WIN ? (lower4 >> k & 1) != 0 : lower));
             const float m_new = move ? ceilf(first ? most : m_ref[k] + fmaxf(most, has_prefix ? -PP_FAR_PREFIX : -PP_FAR_CACHED)) : m_ref[k];
             alpha[k] = move ? pq::ex2_approx(m_ref[k] - m_new) : 1.0f;  // 2^(-inf) = 0 for a row that had seen nothing
             l[k] = DYN && move ? pq::at_reference(l[k], m_ref[k] - m_new) : l[k] * alpha[k];
@@ -1033,7 +877,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
           if (DYN && kv) {  // thread j: key j of the tile. A key that no row sees adds nothing.
             const float* st = reinterpret_cast<const float*>(land + slot * PP_LAND + PP_KEYS * 64);
             const int key = key_of(x, jt) + tid_e;
-            const bool in = !is_pre && key < n_ctx && (!MASKED || key >= x.lo || key < p.n_sink);
+            const bool in = !is_pre && key < n_ctx && (!WIN || key >= x.lo || key < p.n_sink);
             const float k_step = in ? st[tid_e] : 1.0f, v_step = in ? st[PP_KEYS + tid_e] : 1.0f;
             float* key_out = reinterpret_cast<float*>(&steps_buf[stage].key[tid_e >> 1]) + (tid_e & 1);
             key_out[0] = k_step * p.scale2, key_out[2] = pq::lg2_approx(v_step);
@@ -1066,8 +910,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
         for (int jt = max(x.j0, has_prefix); jt < x.j1 && ok; ++jt) {
           const int key0 = key_of(x, jt), n_here = min(pages, (n_ctx - key0 + page - 1) >> p.page_log2);  // pages with keys in them
           bool mine = pg < n_here && kind < (DYN ? 3 : 1);
-          if (MASKED) mine = mine && (key0 + ((pg + 1) << p.page_log2) > x.lo || key0 + (pg << p.page_log2) < p.n_sink);  // that some row sees
-          const uint32_t n_copies = MASKED ? __popc(__ballot_sync(0xffffffffu, mine && kind == 0)) : static_cast<uint32_t>(max(n_here, 0));
+          if (WIN) mine = mine && (key0 + ((pg + 1) << p.page_log2) > x.lo || key0 + (pg << p.page_log2) < p.n_sink);  // that some row sees
+          const uint32_t n_copies = WIN ? __popc(__ballot_sync(0xffffffffu, mine && kind == 0)) : static_cast<uint32_t>(max(n_here, 0));
           int id = 0;
           if (mine) {
             id = pq::ld_dep(row + (key0 >> p.page_log2) + pg);
@@ -1205,10 +1049,10 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
   }
 }
 
-template <bool MASKED>
+template <bool WIN>
 void (*kernel_of(bool dyn, bool poll))(const PagedAttnParams) {
-  if (poll) return dyn ? paged_prefill_kernel<true, true, MASKED> : paged_prefill_kernel<false, true, MASKED>;
-  return dyn ? paged_prefill_kernel<true, false, MASKED> : paged_prefill_kernel<false, false, MASKED>;
+  if (poll) return dyn ? paged_prefill_kernel<true, true, WIN> : paged_prefill_kernel<false, true, WIN>;
+  return dyn ? paged_prefill_kernel<true, false, WIN> : paged_prefill_kernel<false, false, WIN>;
 }
 
 }  // namespace
@@ -1218,16 +1062,16 @@ size_t pq_paged_prefill_ws_bytes(const pq_ctx* ctx) {
 }
 
 pq_status pq_paged_prefill_launch(pq_ctx* ctx, PagedAttnParams p, void* ws, cudaStream_t st) {
-  const bool dyn = p.steps != nullptr, poll = p.wait_clocks < PQ_SUSPENDED_CLOCKS, masked = p.window > 0 || p.mask;
-  void (*const kern)(const PagedAttnParams) = masked ? kernel_of<true>(dyn, poll) : kernel_of<false>(dyn, poll);
+  const bool dyn = p.steps != nullptr, poll = p.wait_clocks < PQ_SUSPENDED_CLOCKS, win = p.window > 0;
+  void (*const kern)(const PagedAttnParams) = win ? kernel_of<true>(dyn, poll) : kernel_of<false>(dyn, poll);
   static std::atomic<bool> attr_set[64][2][2][2] = {};
   if (ctx->device < 0 || ctx->device >= 64 || ctx->sm_count > PQ_PAGED_MAX_WORKERS) return PQ_ERR_UNSUPPORTED;
-  if (!attr_set[ctx->device][dyn][poll][masked].load(std::memory_order_relaxed)) {
+  if (!attr_set[ctx->device][dyn][poll][win].load(std::memory_order_relaxed)) {
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(PP_SMEM_BYTES)) != cudaSuccess) {
       cudaGetLastError();
       return PQ_ERR_CUDA;
     }
-    attr_set[ctx->device][dyn][poll][masked].store(true, std::memory_order_relaxed);
+    attr_set[ctx->device][dyn][poll][win].store(true, std::memory_order_relaxed);
   }
   p.ws_o = static_cast<float*>(ws);
   p.ws_ml = p.ws_o + static_cast<size_t>(2) * ctx->sm_count * PP_PARTIAL;
