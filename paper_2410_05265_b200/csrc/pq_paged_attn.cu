@@ -37,7 +37,7 @@ pq_status attention(pq_ctx* ctx, const pq_kv4_paged* c, const void* q, int64_t l
   // a window that holds every cache is none; numbers past any cache's end stay clear of the end of 32 bits
   p.window = window >= capacity ? 0 : window, p.n_sink = p.window == 0 ? 0 : n_sink < capacity ? n_sink : static_cast<int32_t>(capacity);
   p.mask = mask, p.mask_words = mask_words;
-  if (mask) return pq_paged_tree_launch(ctx, p, ws, static_cast<cudaStream_t>(stream));
+  if (mask) return pq_paged_tree_launch(ctx, p, bound, ws, static_cast<cudaStream_t>(stream));
   // The kernel for several rows takes whole SMs and goes first; the one for single tokens, whose CTAs are small, starts beside it on the SMs that it leaves.
   if (max_new > 1) {
     st = pq_paged_prefill_launch(ctx, p, static_cast<uint8_t*>(ws) + pq_paged_decode_ws_bytes(ctx, c), static_cast<cudaStream_t>(stream));

@@ -156,18 +156,15 @@ struct PpItem {
   int skip, lo;         // WIN: key tiles left out behind the first ones, and the first key of the window of any row
 };
 
-// The keys a .. b - 1 as bits of a word whose bit 0 is key `at`.
-__device__ __forceinline__ uint64_t key_bits(int a, int b, int at) {
-  const int from = max(a - at, 0), to = min(b - at, 64);
-  return from >= to ? 0 : (~0ull >> (64 - (to - from))) << from;
+// Of 64 columns a thread has 16, 8j + 2t and 8j + 2t + 1 as bits 2j, 2j + 1: how many of them lie before column x (any x).
+__device__ __forceinline__ int columns_before(int x, int t) {
+  x = min(max(x, 0), 64);
+  return 2 * (x >> 3) + min(max((x & 7) - 2 * t, 0), 2);
 }
-// Of a word whose bit i is column i of a row, those of the columns 2t, 2t + 1 of every eight: bits 2j, 2j + 1 are columns 8j + 2t, 8j + 2t + 1.
-__device__ __forceinline__ uint32_t own_columns(uint64_t v, int t) {
-  const uint32_t lo = static_cast<uint32_t>(v) >> (2 * t), hi = static_cast<uint32_t>(v >> 32) >> (2 * t);
-  uint32_t r = 0;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) r |= ((lo >> (8 * j)) & 3u) << (2 * j) | ((hi >> (8 * j)) & 3u) << (8 + 2 * j);
-  return r;
+// Those of the columns a .. b - 1.
+__device__ __forceinline__ uint32_t own_columns(int a, int b, int t) {
+  const uint32_t below_a = (1u << columns_before(a, t)) - 1, below_b = (1u << columns_before(b, t)) - 1;
+  return below_b & ~below_a;
 }
 
 // WIN: a window over the cached keys with first keys that stay visible.
@@ -503,9 +500,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
           if (need_mask) {
             const int at = key0 + c0;
             for (int k = 0; k < 4; ++k) {
-              const int place = place_of(k), end = is_pre ? p.n_prefix : min(n_ctx, place + 1);
-              const uint64_t v = is_pre ? key_bits(0, end, c0) : key_bits(max(place - p.window + 1, 0), end, at) | key_bits(0, min(p.n_sink, end), at);
-              const uint32_t w = own_columns(v, ft) << (16 * (k & 1));
+              const int place = place_of(k), end = is_pre ? p.n_prefix - c0 : min(n_ctx, place + 1) - at;
+              const uint32_t v = own_columns(is_pre ? 0 : place - p.window + 1 - at, end, ft) | (is_pre ? 0u : own_columns(0, min(p.n_sink - at, end), ft)), w = v << (16 * (k & 1));
               if (k & 1)
                 vis[k >> 1] |= w;
               else

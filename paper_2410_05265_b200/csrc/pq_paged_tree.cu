@@ -29,7 +29,7 @@ namespace {
 
 constexpr int TK_KEYS = 128;
 constexpr int TK_COLS = 32;  // columns of a softmax thread
-constexpr int TK_ITEM_UNITS = 4;  // units that an item costs besides its key tiles
+constexpr int TK_ITEM_UNITS = 10;  // units that an item costs besides its key tiles
 constexpr int TK_SHORT = 8;       // an item of so many key tiles or fewer is not shared between workers
 constexpr float TK_LAZY = 15.0f;
 constexpr float TK_NONE = 3.0e38f;  // in place of -m of a column that has seen no key: whatever it sees first exceeds the reference
@@ -87,12 +87,14 @@ struct TkState {
   volatile int n_tiles;  // of this CTA, once the loader knows
   TkStart start;
   TkShared shared[2];
+  int n_shared;
   uint32_t out[Sh::SETS];  // a warp of the set has given up
   TkItem item[2];         // as the softmax warps read it, beside its queries; no tiles: there are no more
+  uint4 pre_key[8][32];   // prefixed keys as operand B
   alignas(16) float neg_m[Sh::SOFTMAX_WARPS][TK_COLS];  // -m of a column, TK_NONE while it has seen no key; every warp has its copy
   alignas(16) float moved[Sh::SOFTMAX_WARPS][2 * TK_COLS];  // 2^(m before its last move - m behind it), in two factors
   float red[Sh::GROUPS][4][NC];
-  int lo[2][PQ_TREE_MAX_ROWS];  // first key of the window of an item's tokens
+  int lo[2][NC];  // first key of the window of an item's tokens
 };
 
 template <int NC>
@@ -101,7 +103,7 @@ constexpr size_t tk_smem_bytes(bool dyn, int n_prefix) {
          sizeof(TkState<NC>) + static_cast<size_t>(NC) * ((n_prefix + 3) / 4 * 4) * 4;
 }
 static_assert(tk_smem_bytes<128>(true, PQ_PAGED_MAX_PREFIX) <= 227 * 1024, "shared memory budget");
-static_assert(tk_smem_bytes<64>(true, 16) <= 113 * 1024 && tk_smem_bytes<32>(true, 48) <= 113 * 1024, "shared memory of two CTAs (longer prefixes: of one)");
+static_assert(tk_smem_bytes<64>(true, 12) <= 113 * 1024 && tk_smem_bytes<32>(true, 12) <= 113 * 1024, "shared memory of two CTAs (longer prefixes: of one)");
 static_assert((PQ_PAGED_MAX_SEQS + 1) * 4 <= 3 * TK_LAND_CODES, "the prefix sums lie in the landing ring before the pipeline starts");
 
 // The landing ring's 64-byte swizzle: 16-byte piece c of row r (64 bytes a row, rows from a multiple of 512 bytes on).
@@ -109,6 +111,25 @@ __device__ __forceinline__ uint32_t land_off(uint32_t row_off, int c) { return r
 // Nibbles 0 and 4, nibbles 1 and 5 of a word as exact fp16 integers (the first half of expand8_f16).
 __device__ __forceinline__ uint2 expand2_f16(uint32_t w) {
   return make_uint2(hfma2_u32(pq::and_xor<0x000F000Fu, 0x64086408u>(w), 0x3C003C00u, 0xE408E408u), hfma2_u32(pq::and_xor<0x00F000F0u, 0x64806480u>(w), 0x2C002C00u, 0xD480D480u));
+}
+// 16 rows x 16 words: lane 4g + t has word 4n + t of row g (r[2n]) and of row g + 8 (r[2n + 1]).
+__device__ __forceinline__ void tmem_st_frag8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]),
+               "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st_cols(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]),
+               "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+__device__ __forceinline__ void ldmatrix_x4(uint32_t a, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void ldmatrix_x4_trans(uint32_t a, uint32_t* r) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
@@ -158,15 +179,6 @@ __device__ __forceinline__ float lane_join(float (&v)[N], int lane, const F& f) 
   if (N == 16) v[0] = f(v[0], __shfl_xor_sync(0xffffffffu, v[0], 16));
   return v[0];
 }
-// Four columns of the dims 4g + j (lane 8j + g of a quadrant) to column j of the dims 4g .. 4g + 3.
-__device__ __forceinline__ float4 gather_dims(float v0, float v1, float v2, float v3, int lane) {
-  const bool a = lane & 8, b = lane & 16;
-  const float x = __shfl_xor_sync(0xffffffffu, a ? v0 : v1, 8), y = __shfl_xor_sync(0xffffffffu, a ? v2 : v3, 8);
-  const float2 p = a ? make_float2(x, v1) : make_float2(v0, x), q = a ? make_float2(y, v3) : make_float2(v2, y);  // of column 0 or 1, of column 2 or 3
-  const float2 send = b ? p : q, keep = b ? q : p;
-  const float2 got = make_float2(__shfl_xor_sync(0xffffffffu, send.x, 16), __shfl_xor_sync(0xffffffffu, send.y, 16));
-  return b ? make_float4(got.x, got.y, keep.x, keep.y) : make_float4(keep.x, keep.y, got.x, got.y);
-}
 __device__ __forceinline__ uint2 pack_bf16x4(const float4& v) {
   const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x, v.y), hi = __floats2bfloat162_rn(v.z, v.w);
   return make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
@@ -206,7 +218,7 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
     for (int i = 0; i < Sh::SETS; ++i) st->out[i] = 0;
     pq::mbar_init(&st->pre_full, 1), pq::mbar_init(&st->pre_empty, TK_SOFTMAX_WARPS);
     pq::mbar_init(&st->drain[0], 1), pq::mbar_init(&st->drain[1], 1);
-    st->abort_flag = 0, st->n_tiles = 0x7fffffff;
+    st->abort_flag = 0, st->n_tiles = 0x7fffffff, st->n_shared = 0;
     pq::mbar_fence_init();
   }
   if (warp == Sh::WARP_QK) {
@@ -377,29 +389,40 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
       }
     pq::fence_proxy_async_smem();
   };
-  auto prefix_scores = [&](const TkItem& x, int buf, int tid, int threads) {  // from the queries in shared memory: a thread to a (column, key), neighbours share the key
-    const int cols = min(TI, x.n - x.it * TI) * G;
-    const uint8_t* q = q_buf + buf * NC * 256;
-    for (int i = tid; i < NC * pre_stride; i += threads) {
-      const int j = i / NC, col = i % NC;
-      if (col >= cols) continue;
-      float acc = 0.0f;
-      if (j < p.n_prefix) {
-        const uint4* kr = reinterpret_cast<const uint4*>(p.prefix_k + (static_cast<int64_t>(x.h) * p.n_prefix + j) * 128);
+  // scores of the prefixed keys, by one warp: columns on the 16-row side of the bf16 MMA (every query is exact), the fp16 keys as two bf16 terms
+  auto prefix_scores = [&](const TkItem& x, int buf) {
+    const int cols = min(TI, x.n - x.it * TI) * G, g = lane >> 2, t = lane & 3;
+    const uint32_t q = pq::smem_u32(q_buf + buf * NC * 256);
+    for (int j0 = 0; j0 < p.n_prefix; j0 += 8) {
+      // operand B of 16 dims: key j0 + g, in the order of the queries (0,4) (1,5) (2,6) (3,7) of every eight dims
+      const uint16_t* key = reinterpret_cast<const uint16_t*>(p.prefix_k) + (static_cast<int64_t>(x.h) * p.n_prefix + j0 + g) * 128 + t;
+      __syncwarp();
 #pragma unroll 4
-        for (int c16 = 0; c16 < 16; ++c16) {
-          const uint4 kv = permute8(pq::ld_dep(kr + c16));
-          const uint4 qv = *reinterpret_cast<const uint4*>(q + (c16 >> 3) * (NC * 128) + col * 128 + (((c16 & 7) ^ (col & 7)) << 4));
-          const uint32_t qw[4] = {qv.x, qv.y, qv.z, qv.w}, kw[4] = {kv.x, kv.y, kv.z, kv.w};
+      for (int kk = 0; kk < 8; ++kk) {
+        uint32_t w[2] = {0, 0};
+        if (j0 + g < p.n_prefix)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float2 kf = __half22float2(*reinterpret_cast<const __half2*>(&kw[e]));
-            acc = fmaf(__uint_as_float(qw[e] << 16), kf.x, acc);
-            acc = fmaf(__uint_as_float(qw[e] & 0xFFFF0000u), kf.y, acc);
-          }
+          for (int i = 0; i < 2; ++i) w[i] = __ldcg(key + kk * 16 + 8 * i) | static_cast<uint32_t>(__ldcg(key + kk * 16 + 8 * i + 4)) << 16;
+        st->pre_key[kk][lane] = make_uint4(bf16_term(w[0], false), bf16_term(w[1], false), bf16_term(w[0], true), bf16_term(w[1], true));
+      }
+      __syncwarp();
+      for (int col0 = 0; col0 < cols; col0 += 16) {
+        float c[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        const int row = col0 + (lane & 15);
+#pragma unroll 4
+        for (int kk = 0; kk < 8; ++kk) {
+          const int c16 = 2 * kk + (lane >> 4);
+          uint32_t a[4];
+          ldmatrix_x4(q + (c16 >> 3) * (NC * 128) + row * 128 + (((c16 & 7) ^ (row & 7)) << 4), a);
+          const uint4 b = st->pre_key[kk][lane];
+          mma_bf16(c, a, b.x, b.y), mma_bf16(c, a, b.z, b.w);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int j = j0 + 2 * t + (i & 1);
+          if (j < pre_stride) pre[(col0 + g + 8 * (i >> 1)) * pre_stride + j] = c[i] * p.scale2;
         }
       }
-      pre[col * pre_stride + j] = acc * p.scale2;
     }
   };
 
@@ -432,19 +455,14 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
     const uint32_t o_addr = tmem_base + lane_base + Sh::COL_O + group * NC + col0;
     const uint32_t p_row = pq::smem_u32(p_buf) + (col0 >> 6) * (TK_KEYS * 128) + in_set * Sh::P_ROW, p_turn = NC < 64 ? (in_set >> 1) & 3 : in_set & 7;
     const float* const step0 = reinterpret_cast<const float*>(land_steps) + ((in_set >> p.page_log2) << (p.page_log2 + 1)) + (in_set & ((1 << p.page_log2) - 1));
-    int c0 = 0, n_pre = 0, n_shared = 0;  // tiles before the item, items with the prefix, shared items
-    int k = 0;                            // this group's tiles so far
+    int n_pre = 0;  // items with the prefix
+    int k = 0;      // this group's tiles so far
     if (any) {
       const TkItem x = first_item();
       load_queries(x, 0, threadIdx.x, TK_SOFTMAX_WARPS * 32, std::integral_constant<int, NC / 8 / Sh::SETS>());
       if (threadIdx.x == 0) st->item[0] = x;
       all_sync();
       if (threadIdx.x == 0) pq::mbar_arrive(&st->q_full[0]);
-      if (x.j0 == 0 && p.n_prefix > 0) {
-        prefix_scores(x, 0, threadIdx.x, TK_SOFTMAX_WARPS * 32);
-        all_sync();
-        if (threadIdx.x == 0) pq::mbar_arrive(&st->pre_full);
-      }
     }
     if (any && !wait_warp(&st->q_full[0], 0)) leave();
     bool more = any;
@@ -459,15 +477,16 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
       for (int i = 0; i < TK_COLS / 2; ++i) l[i] = make_float2(0.0f, 0.0f);
       // Tiles that need masks: from the one with the first new key on (the cache ends there, too), and from the first that is not wholly of keys that stay visible to the
       // last in which a row's window begins.
-      int mask_from = (x.base < 0 ? 0 : x.base / TK_KEYS - x.skip) - x.j0, mask_a = 0, mask_b = 0;
+      const int mask_from = (x.base < 0 ? 0 : x.base / TK_KEYS - x.skip) - x.j0;
+      int mask_a = 0, mask_n = 0;
       if (p.window > 0) {
         const int tile_lo = (max(0, x.base + x.n - p.window) + TK_KEYS - 1) / TK_KEYS;
-        mask_a = p.n_sink / TK_KEYS - x.j0, mask_b = (tile_lo > first_tiles ? tile_lo - x.skip : tile_lo) - x.j0;
+        mask_a = p.n_sink / TK_KEYS, mask_n = max(0, (tile_lo > first_tiles ? tile_lo - x.skip : tile_lo) - mask_a), mask_a -= x.j0;
       }
       for (int i0 = turn; i0 < n_tiles; i0 += T, ++k) {
         const int buf = T > 1 ? group : k % NB, phase = T > 1 ? k & 1 : (k / NB) & 1;
         const uint32_t s_addr = tmem_base + lane_base + buf * NC + col0;
-        const bool need_mask = i0 >= mask_from || (i0 >= mask_a && i0 < mask_b);
+        const bool need_mask = i0 >= mask_from || static_cast<uint32_t>(i0 - mask_a) < static_cast<uint32_t>(mask_n);
         // what the key's score is multiplied by, log2 of the value's step PQ_UP octaves up, and what its weight counts in the denominator
         float a = scale, b = 0.0f, inv = 1.0f;
         if (DYN) {
@@ -568,9 +587,7 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
             tmem_ld_cols(o_addr + e, r);
 #pragma unroll
             for (int i = 0; i < 8; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * moved[e + i] * (DYN ? moved[TK_COLS + e + i] : 1.0f));
-            asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(o_addr + e), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]),
-                         "r"(r[5]), "r"(r[6]), "r"(r[7])
-                         : "memory");
+            tmem_st_cols(o_addr + e, r);
           }
           pq::tmem_st_wait();
         };
@@ -633,7 +650,7 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
         ++n_pre;
       }
       // the next item lies beside the other queries
-      const int next_turn = (group - c0 - n_tiles) & (T - 1);
+      const int next_turn = (turn - n_tiles) & (T - 1);
       const TkItem& y = st->item[(n_items + 1) & 1];
       if (ok && !wait_warp(&st->q_full[(n_items + 1) & 1], ((n_items + 1) >> 1) & 1)) leave();
       if (any_of(1, TK_SOFTMAX_WARPS * 32, !ok)) {
@@ -641,13 +658,19 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
         break;
       }
       pq::tc_fence_after();
+      float y4[4];  // a head dim of the first prefixed values
+      const int dim = 4 * (lane & 7) + (lane >> 3) + 32 * quad;
+      const __half* const pv = p.prefix_v + static_cast<int64_t>(x.h) * p.n_prefix * 128 + dim;
+      auto prefix_value = [&](int j) { return has_prefix && j < p.n_prefix ? __half2float(__ushort_as_half(__ldcg(reinterpret_cast<const unsigned short*>(pv + j * 128)))) : 0.0f; };
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y4[j] = prefix_value(j);
       const bool whole = x.j0 == 0 && x.j1 == x.tiles;
       const int64_t part = (2 * static_cast<int64_t>(blockIdx.x) + (x.j0 == 0 ? 1 : 0)) * NC;
       // A warp takes the head dims of its quadrant of PART = 32 / T columns; of group g and column c of them lane g PART + c.
       constexpr int PART = NC / Sh::SETS;
       static_assert(PART * T == 32, "a lane per group and column");
-      const int t0 = x.it * TI, cols = min(TI, x.n - t0) * G, dim = 4 * (lane & 7) + (lane >> 3) + 32 * quad;
-      float m, norm = 1.0f, fac;
+      const int t0 = x.it * TI, cols = min(TI, x.n - t0) * G;
+      float m, norm = 1.0f;
       {
         const int g = lane / PART, col = set * PART + lane % PART;
         const float neg = st->neg_m[(g * SETS + col / TK_COLS) * 4 + quad][col % TK_COLS], m_g = neg == TK_NONE ? -INFINITY : -neg;
@@ -669,8 +692,21 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
           norm = sum > 0.0f ? 1.0f / sum : sum == sum ? 0.0f : sum;  // (zero: a column that sees nothing)
         else if (quad == 0 && g == 0)
           *reinterpret_cast<float2*>(p.ws_ml + (part + col) * 2) = make_float2(m, sum);
-        fac = pq::ex2_approx(d) * norm * s_v;
+        moved[lane] = pq::ex2_approx(d) * norm * s_v;
       }
+      if (has_prefix) {  // scores to weights, a quarter of the columns to a warp
+        set_sync();
+        for (int e0 = quad * (PART / 4); e0 < (quad + 1) * (PART / 4); ++e0) {
+          const float m_c = __shfl_sync(0xffffffffu, m, e0), norm_c = __shfl_sync(0xffffffffu, norm, e0);
+          float* const e = pre + (set * PART + e0) * pre_stride;
+          for (int j = lane; j < p.n_prefix; j += 32) e[j] = pq::ex2_approx(e[j] - m_c) * norm_c;
+        }
+        set_sync();
+      }
+      __syncwarp();
+      // a head dim of eight columns at a time
+      int tok = set * PART / G, head = set * PART - tok * G;
+      int64_t at = whole ? (static_cast<int64_t>(x.row0 + t0 + tok) * p.Hq + x.h * G + head) * 128 + dim : (part + set * PART) * 128 + dim;
 #pragma unroll 1
       for (int e0 = 0; e0 < PART; e0 += 8) {
         const int first = set * PART + e0;  // column
@@ -680,51 +716,44 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
         for (int i = 0; i < 8; ++i) acc[i] = 0.0f;
 #pragma unroll
         for (int g = 0; g < T; ++g) {
-          if (((g - c0) & (T - 1)) >= n_tiles) continue;  // (the group had no tile: its columns hold another item's)
+          if (((g - group + turn) & (T - 1)) >= n_tiles) continue;  // (the group had no tile: its columns hold another item's)
           uint32_t r[8];
           tmem_ld_cols(tmem_base + lane_base + Sh::COL_O + g * NC + first, r);
+          const float4 f0 = *reinterpret_cast<const float4*>(moved + g * PART + e0), f1 = *reinterpret_cast<const float4*>(moved + g * PART + e0 + 4);
+          const float f[8] = {f0.x, f0.y, f0.z, f0.w, f1.x, f1.y, f1.z, f1.w};
 #pragma unroll
-          for (int i = 0; i < 8; ++i) acc[i] = fmaf(__uint_as_float(r[i]), __shfl_sync(0xffffffffu, fac, g * PART + e0 + i), acc[i]);
+          for (int i = 0; i < 8; ++i) acc[i] = fmaf(__uint_as_float(r[i]), f[i], acc[i]);
         }
-        if (has_prefix) {
-          const __half* pv = p.prefix_v + static_cast<int64_t>(x.h) * p.n_prefix * 128 + dim;
+        if (has_prefix)
           for (int j = 0; j < p.n_prefix; j += 4) {
-            float y4[4];
+            if (p.n_prefix > 4)
 #pragma unroll
-            for (int jj = 0; jj < 4; ++jj) y4[jj] = j + jj < p.n_prefix ? __half2float(__ushort_as_half(__ldcg(reinterpret_cast<const unsigned short*>(pv + (j + jj) * 128)))) : 0.0f;
-            // the weight of column lane / 4, key lane % 4
-            const float m_c = __shfl_sync(0xffffffffu, m, e0 + (lane >> 2)), norm_c = __shfl_sync(0xffffffffu, norm, e0 + (lane >> 2));
-            const float w = j + (lane & 3) < p.n_prefix ? pq::ex2_approx(pre[(first + (lane >> 2)) * pre_stride + j + (lane & 3)] - m_c) * norm_c : 0.0f;
+              for (int jj = 0; jj < 4; ++jj) y4[jj] = prefix_value(j + jj);
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-#pragma unroll
-              for (int jj = 0; jj < 4; ++jj) acc[i] = fmaf(__shfl_sync(0xffffffffu, w, 4 * i + jj), y4[jj], acc[i]);
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 8; i += 4) {
-          const float4 o = gather_dims(acc[i], acc[i + 1], acc[i + 2], acc[i + 3], lane);
-          const int col = first + i + (lane >> 3), d0 = 32 * quad + 4 * (lane & 7);
-          if (col < cols) {
-            if (whole) {
-              const int tok = col / G;
-              *reinterpret_cast<uint2*>(p.out + (static_cast<int64_t>(x.row0 + t0 + tok) * p.Hq + x.h * G + (col - tok * G)) * 128 + d0) = pack_bf16x4(o);
-            } else {
-              *reinterpret_cast<float4*>(p.ws_o + (part + col) * 128 + d0) = o;
+            for (int i = 0; i < 8; ++i) {
+              const float4 e = *reinterpret_cast<const float4*>(pre + (first + i) * pre_stride + j);
+              acc[i] = fmaf(e.x, y4[0], fmaf(e.y, y4[1], fmaf(e.z, y4[2], fmaf(e.w, y4[3], acc[i]))));
             }
           }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (first + i < cols) {
+            if (whole)
+              p.out[at] = __float2bfloat16_rn(acc[i]);
+            else
+              p.ws_o[at] = acc[i];
+          }
+          at += 128;
+          if (whole && ++head == G) head = 0, at += static_cast<int64_t>(p.Hq - G) * 128;
         }
       }
-      if (!whole) {
-        if (threadIdx.x == 0) {
-          const int u = x.j0 == 0 ? x.u + TK_ITEM_UNITS : x.u - x.j0;  // of the item's first tile
-          // (exact: the quotient is a whole number or at least 2^-31 from one)
-          auto worker_of = [&](int unit) { return static_cast<int>((static_cast<double>(unit + 1ll) * start.workers - 1.0) / start.U); };
-          st->shared[n_shared & 1] = TkShared{worker_of(u), worker_of(u + x.tiles - 1), x.b, x.h, x.it, x.row0, x.n};
-        }
-        ++n_shared;
+      if (!whole && threadIdx.x == 0) {
+        const int u = x.j0 == 0 ? x.u + TK_ITEM_UNITS : x.u - x.j0;  // of the item's first tile
+        // (exact: the quotient is a whole number or at least 2^-31 from one)
+        auto worker_of = [&](int unit) { return static_cast<int>((static_cast<double>(unit + 1ll) * start.workers - 1.0) / start.U); };
+        st->shared[st->n_shared++] = TkShared{worker_of(u), worker_of(u + x.tiles - 1), x.b, x.h, x.it, x.row0, x.n};
       }
-      c0 += n_tiles, turn = next_turn;
+      turn = next_turn;
       more = y.j1 > y.j0;
       pq::tc_fence_before();
       all_sync();  // sums and references are used again, and the groups' O is written again
@@ -738,7 +767,7 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
     __threadfence();
     all_sync();
     if (threadIdx.x < 2) {
-      const bool go = !st->abort_flag && static_cast<int>(threadIdx.x) < n_shared;
+      const bool go = !st->abort_flag && static_cast<int>(threadIdx.x) < st->n_shared;  // (its first item and its last)
       const TkShared sh = st->shared[threadIdx.x];
       st->merge[threadIdx.x] = go && atomicAdd(p.tickets + TK_TICKET0 + sh.w0, 1u) == static_cast<uint32_t>(sh.w1 - sh.w0) ? 1 : 0;
     }
@@ -811,14 +840,17 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
         if (!last) {
           pq::tc_fence_after();
           const uint32_t at = land0 + slot * TK_LAND_CODES + k_row;
-#pragma unroll 2
-          for (int i = 0; i < 4; ++i) {
-            const uint4 w = pq::lds128(at + ((i << 4) ^ k_turn));
-            const uint4 e[4] = {expand8_bf16(w.x), expand8_bf16(w.y), expand8_bf16(w.z), expand8_bf16(w.w)};
-            uint32_t r[16];
+          uint4 w[2] = {pq::lds128(at + k_turn)};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) r[4 * j] = e[j].x, r[4 * j + 1] = e[j].y, r[4 * j + 2] = e[j].z, r[4 * j + 3] = e[j].w;
-            tmem_st_32x16(k_dst + 16 * i, r);
+          for (int i = 0; i < 4; ++i) {  // 32 head dims
+            if (i < 3) w[(i + 1) & 1] = pq::lds128(at + (((i + 1) << 4) ^ k_turn));
+            const uint32_t(&ww)[4] = reinterpret_cast<const uint32_t(&)[4]>(w[i & 1]);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const uint4 e = expand8_bf16(ww[2 * j]), f = expand8_bf16(ww[2 * j + 1]);
+              const uint32_t r[8] = {e.x, e.y, e.z, e.w, f.x, f.y, f.z, f.w};
+              tmem_st_cols(k_dst + 16 * i + 8 * j, r);
+            }
           }
           pq::tmem_st_wait();
           pq::tc_fence_before();
@@ -833,19 +865,20 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
           }
           pq::tc_fence_after();
           const uint32_t at = v_slot * TK_LAND_CODES;
+          uint32_t w[2][4];
+          ldmatrix_x4_trans(v_off[0] + at, w[0]);
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {  // 64 keys
-            uint32_t w[8];
-            ldmatrix_x4_trans(v_off[2 * i] + at, w), ldmatrix_x4_trans(v_off[2 * i + 1] + at, w + 4);
+          for (int i = 0; i < 4; ++i) {  // 32 keys, the next ones' rows on their way
+            if (i < 3) ldmatrix_x4_trans(v_off[i + 1] + at, w[(i + 1) & 1]);
 #pragma unroll
             for (int j = 0; j < 2; ++j) {  // dims 4g, 4g + 1 (lanes 0 .. 15), dims 4g + 2, 4g + 3
-              uint32_t r[16];
+              uint32_t r[8];
 #pragma unroll
-              for (int n = 0; n < 8; ++n) {
-                const uint2 e = expand2_f16(j ? w[n] >> 8 : w[n]);
+              for (int n = 0; n < 4; ++n) {
+                const uint2 e = expand2_f16(j ? w[i & 1][n] >> 8 : w[i & 1][n]);
                 r[2 * n] = e.x, r[2 * n + 1] = e.y;
               }
-              tmem_st_frag(v_dst + (static_cast<uint32_t>(16 * j) << 16) + 32 * i, r);
+              tmem_st_frag8(v_dst + (static_cast<uint32_t>(16 * j) << 16) + 16 * i, r);
             }
           }
           pq::tmem_st_wait();
@@ -860,6 +893,7 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
     } else if (warp == Sh::WARP_LOAD) {
       // ================================================================== loader: lanes 0 .. 7 the pages of a tile
       const int pages = TK_KEYS >> p.page_log2, page = 1 << p.page_log2, pg = lane & 7;
+      const bool leader = pq::elect_one();
       bool ok = true;
       int slot = 0, slot_phase = 1;
       TkItem x;
@@ -888,13 +922,20 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
             pq::report(p.status, PQ_ERR_SHAPE);
             id = 0;
           }
-          const uint32_t n_copies = __popc(__ballot_sync(0xffffffffu, mine));
+          const uint32_t copies = __ballot_sync(0xffffffffu, mine);
           if (!wait_warp(&st->land_empty[slot], slot_phase)) {
             ok = false;
             break;
           }
-          if (lane == 0) pq::mbar_arrive_expect_tx(&st->land_full[slot], n_copies * page * 128);
+          const int row = id * p.Hkv + x.h;
+          if (leader) pq::mbar_arrive_expect_tx(&st->land_full[slot], __popc(copies) * page * 128);
           __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {  // (a lane at a time would take three times as long)
+            if (i >= pages) break;
+            const int row_i = __shfl_sync(0xffffffffu, row, i);
+            if (leader && ((copies >> i) & 1)) tma_load_3d(pq::smem_u32(land + slot * TK_LAND_CODES) + i * page * 128, &map, 0, 0, row_i, &st->land_full[slot]);
+          }
           if (DYN) {  // own steps, 16 bytes to a lane and copy
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -906,7 +947,6 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
             }
             cp_async_arrive(&st->land_full[slot]);
           }
-          if (mine) tma_load_3d(pq::smem_u32(land + slot * TK_LAND_CODES) + pg * page * 128, &map, 0, 0, id * p.Hkv + x.h, &st->land_full[slot]);
           ++lands_issued;
           if (++slot == LANDS) slot = 0, slot_phase ^= 1;
         }
@@ -976,37 +1016,35 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
       __syncwarp();
       pq::mbar_wait(&st->drain[scores ? 0 : 1], 0);
     } else if (warp == Sh::WARP_HELP) {
-      // ================================================================== helper: queries and prefix scores of the items behind the first
+      // ================================================================== helper: queries of the items behind the first, prefix scores of all
       bool ok = true;
-      int item = 1, n_pre = 0;
+      int n_pre = 0;
       TkItem x;
+      if (any) x = first_item();
       bool more = any;
-      if (any) {
-        x = first_item();
-        n_pre = x.j0 == 0 && p.n_prefix > 0 ? 1 : 0;
-        more = next_item(x);
-      }
-      for (; any; more = next_item(x), ++item) {
+      for (int item = 0; any; more = next_item(x), ++item) {
         const int buf = item & 1;
-        if (!wait_warp(&st->q_empty[buf], ((item >> 1) & 1) ^ 1)) {
-          ok = false;
-          break;
+        if (item > 0) {
+          if (!wait_warp(&st->q_empty[buf], ((item >> 1) & 1) ^ 1)) {
+            ok = false;
+            break;
+          }
+          if (more) load_queries(x, buf, lane, 32, std::integral_constant<int, 4>());
+          if (lane == 0) {
+            if (!more) x.j1 = x.j0;  // (no more)
+            st->item[buf] = x;
+          }
+          __syncwarp();
+          if (lane == 0) pq::mbar_arrive(&st->q_full[buf]);
+          if (!more) break;
         }
-        if (more) load_queries(x, buf, lane, 32, std::integral_constant<int, 4>());
-        if (lane == 0) {
-          if (!more) x.j1 = x.j0;  // (no more)
-          st->item[buf] = x;
-        }
-        __syncwarp();
-        if (lane == 0) pq::mbar_arrive(&st->q_full[buf]);
-        if (!more) break;
         if (x.j0 == 0 && p.n_prefix > 0) {
-          if (!wait_warp(&st->pre_empty, (n_pre & 1) ^ 1)) {
+          if ((item == 0 && !wait_warp(&st->q_full[0], 0)) || !wait_warp(&st->pre_empty, (n_pre & 1) ^ 1)) {
             ok = false;
             break;
           }
           ++n_pre;
-          prefix_scores(x, buf, lane, 32);
+          prefix_scores(x, buf);
           __syncwarp();
           if (lane == 0) pq::mbar_arrive(&st->pre_full);
         }
@@ -1039,10 +1077,22 @@ TkForm form(bool dyn, int n_prefix) {
   return {dyn ? paged_tree_kernel<NC, true, POLL> : paged_tree_kernel<NC, false, POLL>, NC, TkShape<NC>::CTAS, TkShape<NC>::THREADS, tk_smem_bytes<NC>(dyn, n_prefix),
           tk_smem_bytes<NC>(dyn, PQ_PAGED_MAX_PREFIX)};
 }
-// The fewest columns that hold a sequence's rows, or items of 128. Short wait limits take the polling form, of 128 columns whatever the rows.
-TkForm form_of(bool dyn, int columns, int n_prefix, bool poll) {
-  if (poll) return form<128, true>(dyn, n_prefix);
-  return columns <= 32 ? form<32, false>(dyn, n_prefix) : columns <= 64 ? form<64, false>(dyn, n_prefix) : form<128, false>(dyn, n_prefix);
+// How many columns: by an estimate for B sequences of max_new rows and max_len cached keys. A key tile of an SM takes 0.9 us with 32 columns, 1.15 with 64 and 1.5 with 128
+// (own steps: 1.1, 1.6, 2.1), so that wide items are cheaper by the column; but a stretch is no shorter than a short item, whose tiles one CTA takes one after another, and
+// narrow items are more. us with 32 / 64 / 128 columns, 32 heads on 8: 1 x 26 rows at 1021 keys 19 / 23 / 25, at 4000 25 / 32 / 34; 1 x 128 at 20000 106 / 85 / 76;
+// 16 x 16 at 4000 66 / 56 / 65, 64 x 8 at 6000 151 / 180 / 257, 32 x 30 at 4000 226 / 148 / 131. Short wait limits take the polling form, of 128 columns whatever the rows.
+TkForm form_of(const pq_ctx* ctx, const PagedAttnParams& p, int64_t max_len) {
+  const bool dyn = p.steps != nullptr;
+  if (p.wait_clocks < PQ_SUSPENDED_CLOCKS) return form<128, true>(dyn, p.n_prefix);
+  const double tiles = static_cast<double>(max_len < TK_KEYS ? 1 : (max_len + TK_KEYS - 1) / TK_KEYS), least = (tiles < TK_SHORT ? tiles : TK_SHORT) + TK_ITEM_UNITS;
+  auto estimate = [&](int nc, double busy, double alone) {
+    const int per_item = nc / p.G;
+    const double work = static_cast<double>(p.B) * p.Hkv * ((p.max_new + per_item - 1) / per_item) * (tiles + TK_ITEM_UNITS) / ctx->sm_count * busy;
+    return work > least * alone ? work : least * alone;
+  };
+  const double t32 = estimate(32, 0.9, 0.95), t64 = estimate(64, 1.15, 1.3), t128 = estimate(128, 1.5, 1.45);
+  if (t32 <= t64 && t32 <= t128) return form<32, false>(dyn, p.n_prefix);
+  return t64 <= t128 ? form<64, false>(dyn, p.n_prefix) : form<128, false>(dyn, p.n_prefix);
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
@@ -1052,9 +1102,10 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
 
 size_t pq_paged_tree_ws_bytes(const pq_ctx* ctx) { return static_cast<size_t>(2) * ctx->sm_count * 128 * (128 + 2) * sizeof(float); }
 
-pq_status pq_paged_tree_launch(pq_ctx* ctx, PagedAttnParams p, void* ws, cudaStream_t st) {
+pq_status pq_paged_tree_launch(pq_ctx* ctx, PagedAttnParams p, int64_t max_len, void* ws, cudaStream_t st) {
   const bool dyn = p.steps != nullptr, poll = p.wait_clocks < PQ_SUSPENDED_CLOCKS;
-  const TkForm f = form_of(dyn, p.max_new * p.G, p.n_prefix, poll);
+  if (p.window > 0 && max_len > static_cast<int64_t>(p.window) + p.n_sink + 3 * TK_KEYS) max_len = static_cast<int64_t>(p.window) + p.n_sink + 3 * TK_KEYS;  // (about what a window leaves)
+  const TkForm f = form_of(ctx, p, max_len);
   if (ctx->device < 0 || ctx->device >= 64 || 2 * ctx->sm_count > PQ_PAGED_MAX_WORKERS) return PQ_ERR_UNSUPPORTED;
   static std::atomic<bool> attr_set[64][2][4] = {};  // the largest there is, once per device and kernel
   std::atomic<bool>& set = attr_set[ctx->device][dyn][poll ? 3 : f.nc >> 6];
