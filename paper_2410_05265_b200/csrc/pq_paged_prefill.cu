@@ -153,7 +153,7 @@ struct PpItem {
   int base;             // cached keys before the new rows: len - n
   int tiles, j0, j1;    // key tiles of the item (the prefix first), and this worker's
   int u;                // unit where this worker's share begins (an item is PP_ITEM_UNITS units and its tiles)
-  int skip, lo;         // WIN: key tiles left out behind the first ones, and the first key of the window of any row
+  int skip, n_window, lo;  // WIN: key tiles left out behind the first ones, those behind them, and the first key of the window of any row
 };
 
 // Of 64 columns a thread has 16, 8j + 2t and 8j + 2t + 1 as bits 2j, 2j + 1: how many of them lie before column x (any x).
@@ -245,13 +245,17 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     }
     return u;
   };
-  auto key_of = [&](const PpItem& x, int jt) {  // first key of an item's tile jt
-    const int t = jt - has_prefix;
-    return (WIN && t >= first_tiles ? t + x.skip : t) * PP_KEYS;
+  // With a window an item takes its key tiles in another order: those of the window, the first ones, the prefix. Keys that stay visible often outweigh the others while
+  // their values are small; behind the others they move the reference of sums in fp32, in which those have kept their bits.
+  auto pre_tile = [&](const PpItem& x, int jt) { return has_prefix && jt == (WIN ? x.tiles - 1 : 0); };
+  auto key_of = [&](const PpItem& x, int jt) {  // first key of an item's tile jt, which is not the prefix
+    if (!WIN) return (jt - has_prefix) * PP_KEYS;
+    return (jt < x.n_window ? first_tiles + x.skip + jt : jt - x.n_window) * PP_KEYS;
   };
   auto set_view = [&](PpItem& x) {
     if (!WIN) return;
     x.skip = skip_of(x, x.rt);
+    x.n_window = max(0, x.tiles - has_prefix - first_tiles);
     x.lo = max(0, x.base - p.window + 1 + x.rt * R);
   };
   int32_t* scan = reinterpret_cast<int32_t*>(kv_buf);
@@ -477,7 +481,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
       for (int k = 0; k < 4; ++k) m_ref[k] = -INFINITY, l[k] = 0.0f;
       for (int jt = x.j0; jt < x.j1; ++jt, ++c) {
         if (!active) continue;
-        const bool is_pre = has_prefix && jt == 0;
+        const bool is_pre = pre_tile(x, jt);
         const int key0 = key_of(x, jt);
         if (__any_sync(0xffffffffu, !wait(&bars->s_full[i], n_tiles_done & 1) || (DYN && !wait(&bars->v_full[c % PP_STAGES], (c / PP_STAGES) & 1)))) {
           leave();
@@ -490,9 +494,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
         const float scale = is_pre ? p.scale2 : scale_ctx, add = is_pre ? 0.0f : log2_sv;
         bool need_mask = is_pre ? p.n_prefix < pre_cols : (key0 + PP_KEYS > x.base + tile_min_tok + 1 || key0 + PP_KEYS > n_ctx);
         uint32_t vis[2] = {~0u, ~0u};  // WIN: the visible ones of this thread's 16 columns, of rows fr, fr + 8 (16 bits each), of rows fr + 16, fr + 24
-        // Is this the first tile (without a prefix the second) with cached keys that the row sees? With a window that differs from row to row.
-        const bool lower = x.j0 == 0 && jt == 1;
-        uint32_t lower4 = 0;
+        const bool lower = !WIN && x.j0 == 0 && jt == 1;
         if (WIN) {
           // the last row's window begins behind this tile's first key, and the tile is not one of keys that stay visible
           const int last_place = x.base + min(x.n, tile_min_tok + RT) - 1;
@@ -508,11 +510,6 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
                 vis[k >> 1] = w;
             }
           }
-          if (x.j0 == 0 && !is_pre)
-            for (int k = 0; k < 4; ++k) {
-              const int first = p.n_sink == 0 ? max(0, place_of(k) - p.window + 1) : 0, t = first / PP_KEYS;
-              if (jt == 1 + (t < first_tiles ? t : t - x.skip)) lower4 |= 1u << k;
-            }
         }
         const PpSteps* st = steps_buf + c % PP_STAGES;
         // w = 2^(exponent - m) against the reference so far, fp16, kept in registers until the whole tile has been looked at. Where an exponent is more than
@@ -563,17 +560,15 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
                     else
                       ex[2 * n + y] = __ffma2_rn(v, scale2, off2);
                   }
-                if (WIN) {
-                  if (need_mask) {
+                if (WIN && need_mask) {
 #pragma unroll
-                    for (int y = 0; y < 2; ++y)
+                  for (int y = 0; y < 2; ++y)
 #pragma unroll
-                      for (int n = 0; n < 2; ++n) {
-                        ex[2 * n + y].x = vis[hf] & (1u << (16 * y + 4 * cc + 2 * n)) ? ex[2 * n + y].x : -INFINITY;
-                        ex[2 * n + y].y = vis[hf] & (2u << (16 * y + 4 * cc + 2 * n)) ? ex[2 * n + y].y : -INFINITY;
-                      }
-                  }
-                } else if (need_mask) {
+                    for (int n = 0; n < 2; ++n) {
+                      ex[2 * n + y].x = vis[hf] & (1u << (16 * y + 4 * cc + 2 * n)) ? ex[2 * n + y].x : -INFINITY;
+                      ex[2 * n + y].y = vis[hf] & (2u << (16 * y + 4 * cc + 2 * n)) ? ex[2 * n + y].y : -INFINITY;
+                    }
+                } else if (!WIN && need_mask) {
 #pragma unroll
                   for (int y = 0; y < 2; ++y) {
                     const int tk = min(t0 + static_cast<int>((tok4 >> (16 * hf + 8 * y)) & 255u), x.n - 1);
@@ -614,12 +609,12 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
             if (DYN) top[k] -= pq::PQ_UP;
             over |= top[k] > (m_ref[k] == -INFINITY ? -INFINITY : PP_LAZY);
           }
-          if (WIN ? x.j0 == 0 && !is_pre : lower)  // (of the row's columns of this set)
+          if (lower)  // (of the row's columns of this set)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               float t = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 1));
               t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
-              over |= t < -PP_LOW && t != -INFINITY && (!WIN || (lower4 >> k & 1));
+              over |= t < -PP_LOW && t != -INFINITY;
             }
           if (!pair_any(over)) break;
           if (*pair_out) {
@@ -638,7 +633,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             const float most = fmaxf(top[k], *const_cast<const volatile float*>(&bars->row[i][set ^ 1][fr + 8 * k]));
-            const bool first = m_ref[k] == -INFINITY, move = most > (first ? -INFINITY : PP_LAZY) || (most < -PP_LOW && most != -INFINITY && (WIN ? (lower4 >> k & 1) != 0 : lower));
+            const bool first = m_ref[k] == -INFINITY, move = most > (first ? -INFINITY : PP_LAZY) || (most < -PP_LOW && most != -INFINITY && lower);
             const float m_new = move ? ceilf(first ? most : m_ref[k] + fmaxf(most, has_prefix ? -PP_FAR_PREFIX : -PP_FAR_CACHED)) : m_ref[k];
             alpha[k] = move ? pq::ex2_approx(m_ref[k] - m_new) : 1.0f;  // 2^(-inf) = 0 for a row that had seen nothing
             l[k] = DYN && move ? pq::at_reference(l[k], m_ref[k] - m_new) : l[k] * alpha[k];
@@ -827,7 +822,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
       const int n_ctx = n_ctx_of(x);
       for (int jt = x.j0; jt < x.j1 && ok; ++jt, ++c) {
         const int stage = c % PP_STAGES;
-        const bool is_pre = has_prefix && jt == 0;
+        const bool is_pre = pre_tile(x, jt);
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {  // keys, then values
           const int slot = lc % PP_LANDS;
@@ -903,7 +898,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
       for (bool more = any; more && ok; more = next_item(x)) {
         const int n_ctx = n_ctx_of(x);
         const int32_t* row = p.table + static_cast<int64_t>(x.b) * p.max_pages;
-        for (int jt = max(x.j0, has_prefix); jt < x.j1 && ok; ++jt) {
+        for (int jt = x.j0; jt < x.j1 && ok; ++jt) {
+          if (pre_tile(x, jt)) continue;
           const int key0 = key_of(x, jt), n_here = min(pages, (n_ctx - key0 + page - 1) >> p.page_log2);  // pages with keys in them
           bool mine = pg < n_here && kind < (DYN ? 3 : 1);
           if (WIN) mine = mine && (key0 + ((pg + 1) << p.page_log2) > x.lo || key0 + (pg << p.page_log2) < p.n_sink);  // that some row sees
@@ -984,13 +980,13 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
           ++n_q[i];
           pq::tc_fence_after();
           if (leader) {
-            issue_s(i, c, has_prefix && x.j0 == 0);
+            issue_s(i, c, pre_tile(x, x.j0));
             if (i == groups - 1) pq::mma_commit(&bars->k_empty[c % PP_STAGES]);
           }
           __syncwarp();
         }
         for (int jt = x.j0; jt < x.j1 && ok; ++jt, ++c) {
-          const bool is_pre = has_prefix && jt == 0, last = jt + 1 == x.j1;
+          const bool is_pre = pre_tile(x, jt), last = jt + 1 == x.j1;
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             if (i >= groups) break;
@@ -1012,7 +1008,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
               }
               pq::tc_fence_after();
               if (leader) {
-                issue_s(i, c + 1, false);
+                issue_s(i, c + 1, WIN && pre_tile(x, jt + 1));
                 if (i == groups - 1) pq::mma_commit(&bars->k_empty[(c + 1) % PP_STAGES]);
               }
             } else if (leader) {
