@@ -31,6 +31,7 @@ constexpr int TK_KEYS = 128;
 constexpr int TK_COLS = 32;  // columns of a softmax thread
 constexpr int TK_ITEM_UNITS = 10;  // units that an item costs besides its key tiles
 constexpr int TK_SHORT = 8;       // an item of so many key tiles or fewer is not shared between workers
+constexpr int TK_PIECE = 15;      // units that cutting an item costs
 constexpr float TK_LAZY = 15.0f;
 constexpr float TK_NONE = 3.0e38f;  // in place of -m of a column that has seen no key: whatever it sees first exceeds the reference
 constexpr int TK_TICKET0 = PQ_PAGED_TICKET0 + PQ_PAGED_MAX_WORKERS;
@@ -87,7 +88,7 @@ struct TkState {
   volatile int n_tiles;  // of this CTA, once the loader knows
   TkStart start;
   TkShared shared[2];
-  int n_shared;
+  int n_shared, most_units;
   uint32_t out[Sh::SETS];  // a warp of the set has given up
   TkItem item[2];         // as the softmax warps read it, beside its queries; no tiles: there are no more
   uint4 pre_key[8][32];   // prefixed keys as operand B
@@ -104,7 +105,8 @@ constexpr size_t tk_smem_bytes(bool dyn, int n_prefix) {
 }
 static_assert(tk_smem_bytes<128>(true, PQ_PAGED_MAX_PREFIX) <= 227 * 1024, "shared memory budget");
 static_assert(tk_smem_bytes<64>(true, 12) <= 113 * 1024 && tk_smem_bytes<32>(true, 12) <= 113 * 1024, "shared memory of two CTAs (longer prefixes: of one)");
-static_assert((PQ_PAGED_MAX_SEQS + 1) * 4 <= 3 * TK_LAND_CODES, "the prefix sums lie in the landing ring before the pipeline starts");
+static_assert(2 * (PQ_PAGED_MAX_SEQS + 1) * 4 <= 16 * 1024 + 16 * 1024 + 4 * TK_LAND_CODES && 2 * (PQ_PAGED_MAX_SEQS + 1) * 4 <= 32 * 1024 + 16 * 1024 + 3 * TK_LAND_CODES,
+              "the prefix sums lie in the buffers of Q, P and the packed rows before the pipeline starts");
 
 // The landing ring's 64-byte swizzle: 16-byte piece c of row r (64 bytes a row, rows from a multiple of 512 bytes on).
 __device__ __forceinline__ uint32_t land_off(uint32_t row_off, int c) { return row_off + ((c ^ ((row_off >> 7) & 3)) << 4); }
@@ -218,7 +220,7 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
     for (int i = 0; i < Sh::SETS; ++i) st->out[i] = 0;
     pq::mbar_init(&st->pre_full, 1), pq::mbar_init(&st->pre_empty, TK_SOFTMAX_WARPS);
     pq::mbar_init(&st->drain[0], 1), pq::mbar_init(&st->drain[1], 1);
-    st->abort_flag = 0, st->n_tiles = 0x7fffffff, st->n_shared = 0;
+    st->abort_flag = 0, st->n_tiles = 0x7fffffff, st->n_shared = 0, st->most_units = 0;
     pq::mbar_fence_init();
   }
   if (warp == Sh::WARP_QK) {
@@ -246,7 +248,7 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
     x.tiles = max(1, (x.len + TK_KEYS - 1) / TK_KEYS - x.skip);
   };
   auto key_of = [&](const TkItem& x, int jt) { return (jt >= first_tiles ? jt + x.skip : jt) * TK_KEYS; };
-  int32_t* scan = reinterpret_cast<int32_t*>(land);
+  int32_t *scan = reinterpret_cast<int32_t*>(smem), *items = scan + p.B + 1;  // units and items of one KV head before a sequence
   __syncthreads();
   for (int b = threadIdx.x; b < p.B; b += TK_THREADS) {
     TkItem x;
@@ -256,15 +258,20 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
     const int64_t t = static_cast<int64_t>(x.nt) * (x.tiles + TK_ITEM_UNITS);
     if (odd || t * p.Hkv > 0x7fffffffll) pq::report(p.status, PQ_ERR_SHAPE);
     scan[b] = t * p.Hkv > 0x7fffffffll ? 0 : static_cast<int32_t>(t);
+    items[b] = scan[b] > 0 ? x.nt : 0;
+    if (scan[b] > 0) atomicMax(&st->most_units, x.tiles + TK_ITEM_UNITS);
   }
   __syncthreads();
-  const int64_t total = pq::block_scan<TK_THREADS>(scan, p.B, st->part) * p.Hkv;
+  const int64_t total = pq::block_scan<TK_THREADS>(scan, p.B, st->part) * p.Hkv, n_items = pq::block_scan<TK_THREADS>(items, p.B, st->part) * p.Hkv;
+  // An item to a worker where there are enough workers and no item is much longer than an equal share: pieces of items cost their ends and the merge. (16 x 33 rows, window
+  // 2048: 66 -> 48 us.)
+  const bool direct = n_items <= gridDim.x && static_cast<int64_t>(st->most_units - TK_PIECE) * gridDim.x <= total;
   if (warp < 2) {  // the two borders of this CTA's stretch, a warp each
     const bool too_many = total > 0x7fffffffll;
     if (too_many && threadIdx.x == 0) pq::report(p.status, PQ_ERR_SHAPE);
     TkStart s{};
     s.U = too_many ? 0 : static_cast<int>(total);
-    s.workers = min(static_cast<int>(gridDim.x), max(1, s.U / (TK_ITEM_UNITS + 1)));
+    s.workers = direct ? static_cast<int>(n_items) : min(static_cast<int>(gridDim.x), max(1, s.U / (TK_ITEM_UNITS + 1)));
     int u = 0;
     if (s.U > 0 && static_cast<int>(blockIdx.x) < s.workers) {
       int tiles = 0, at = 0;
@@ -280,7 +287,11 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
       // inside a short item, or among an item's own units, an end of the item is taken, so that no partials are left for a few tiles
       const int w = blockIdx.x + warp;
       u = static_cast<int>(static_cast<int64_t>(s.U) * w / s.workers);
-      if (w < s.workers) {
+      if (direct && w < s.workers) {
+        const int b = pq::find_segment(items, p.B, w / p.Hkv), nt = items[b + 1] - items[b], rel = w - items[b] * p.Hkv;
+        s.b = b, s.h = rel / nt, s.it = rel % nt, s.j0 = 0;
+        u = scan[b] * p.Hkv + rel * ((scan[b + 1] - scan[b]) / nt);
+      } else if (w < s.workers) {
         locate(u);
         int to = u;
         if (s.j0 == 0)
