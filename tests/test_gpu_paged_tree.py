@@ -468,3 +468,123 @@ def test_a_drafted_step_leaves_the_cache_of_plain_decoding(ctx, steps, captured)
         taken = sum(paged_ref.up(n, page) for n in now)
         assert int(cache.pages.n_free) + taken == cache.pages.n_pages
     assert ctx.check_status() == 0
+
+
+# ---- what the calls allow ------------------------------------------------------------------------------------
+@pytest.mark.parametrize("n_prefix", [0, 4])
+@pytest.mark.parametrize("steps", ["head", "vector"])
+def test_fewer_cached_keys_than_drafts(ctx, n_prefix, steps):
+    """The first drafts have no place: nobody sees them, and a row that sees nothing else (and no prefix) is zero."""
+    check(ctx, [3, 0, 40], see([5, 4, 40], 2), n_prefix=n_prefix, steps=steps)
+
+
+def test_rows_strides_and_output_over_the_queries(ctx):
+    lengths, new = [500, 300, 2000], [9, 40, 17]
+    cache = paged_ref.make_cache(lengths, 8, 2, 16, seed=9)
+    begin, trees = begins(new), see(new, 3)
+    wide = paged_ref.queries(begin[-1], 12, seed=9)
+    q, mask = wide[:, :8], ref.words_of(trees, 2, begin[-1])
+    want, tol = ref.attention(cache, q, begin, lengths, 128**-0.5, trees=trees)
+    assert torch.all((call(ctx, cache, q, begin, 40, mask).double() - want).abs() <= tol)
+    dense = q.contiguous()
+    call(ctx, cache, dense, begin, 40, mask, out=dense)
+    assert torch.all((dense.double() - want).abs() <= tol)
+    assert ctx.check_status() == 0
+
+
+@pytest.mark.parametrize("steps", ["head", "vector"])
+def test_a_cache_of_more_than_four_gigabytes(ctx, steps):
+    """Pages whose codes lie beyond 2^32 bytes."""
+    Hkv, page, n_pages = 8, 128, 36000
+    lengths, new = [300, 140], [10, 3]
+    codes = torch.zeros((n_pages, Hkv, 2, page, 64), dtype=torch.uint8, device="cuda")
+    assert codes.numel() > 2**32
+    ids = [n_pages - 1 - 7 * i for i in range(5)]
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for i in ids:
+        codes[i] = torch.randint(0, 256, codes[i].shape, generator=g, device="cuda", dtype=torch.uint8)
+    pages = binding.Pages(i32([ids[:3], ids[3:] + [-1]]), i32(lengths), torch.zeros(n_pages, dtype=torch.int32, device="cuda"), i32([0]), page)
+    own = torch.rand((n_pages, Hkv, 2, page), generator=g, device="cuda") + 0.3 if steps == "vector" else None
+    s = torch.full((Hkv,), 0.5, device="cuda")
+    cache = binding.KV4PagedCache(pages, None, None, codes, 2 * Hkv, s_k=s, s_v=s, steps=own)
+    begin, trees = begins(new), see(new, 2)
+    q = paged_ref.queries(13, 2 * Hkv)
+    want, tol = ref.attention(cache, q, begin, lengths, 128**-0.5, trees=trees)
+    assert torch.all((call(ctx, cache, q, begin, 10, ref.words_of(trees, 1, 13)).double() - want).abs() <= tol)
+    want, tol = ref.attention(cache, q, begin, lengths, 128**-0.5, 50, 3)
+    ws = ctx.attn_kv4_paged_workspace(cache, 13, 10)
+    out = ctx.attn_kv4_paged_window(cache, q, i32(begin), 10, 50, 128**-0.5, ws, n_sink=3)
+    assert torch.all((out.double() - want).abs() <= tol)
+    before = codes[ids[0], :, :, :3].clone()
+    kept = i32([0, 9, 8] + [-1] * 7 + [0, -1, -1])
+    pages.length.copy_(i32([293, 138]))  # 3 of 10, 1 of 3 stay
+    ctx.kv4_paged_keep(cache, i32(begin), kept, i32([3, 1]))
+    last = codes[ids[2], :, :, 34:44]  # places 290 .. 299
+    assert ctx.check_status() == 0 and torch.equal(last[:, :, 1], last[:, :, 9]) and torch.equal(codes[ids[0], :, :, :3], before)
+
+
+def test_two_contexts_on_two_streams(ctx):
+    """Trees of few and of many columns and windowed prompts side by side, again and again: each gives what it gives alone."""
+    other = binding.Context()
+    try:
+        jobs = []
+        for c, seed in ((ctx, 1), (other, 2)):
+            lengths, new = ([3000, 700, 90], [5, 8, 3]) if seed == 1 else ([2500, 900], [100, 64])
+            cache = paged_ref.make_cache(lengths, 8, 2, 16, steps="vector", seed=seed)
+            begin, q = begins(new), paged_ref.queries(sum(new), 8, seed=seed)
+            mask, qb, ws = ref.words_of(see(new, 3), 4, sum(new)), i32(begin), c.attn_kv4_paged_tree_workspace(cache, sum(new), max(new))
+            ws2, out, out2 = c.attn_kv4_paged_workspace(cache, sum(new), max(new)), torch.zeros_like(q), torch.zeros_like(q)
+
+            def run(c=c, cache=cache, q=q, qb=qb, mask=mask, ws=ws, ws2=ws2, out=out, out2=out2, most=max(new)):
+                c.attn_kv4_paged_tree(cache, q, qb, most, mask, 128**-0.5, ws, out=out)
+                c.attn_kv4_paged_window(cache, q, qb, most, 300, 128**-0.5, ws2, out=out2)
+                return out, out2
+
+            jobs.append((run, [t.clone() for t in run()], torch.cuda.Stream(), c))
+        torch.cuda.synchronize()
+        for _ in range(20):
+            for run, _, stream, _ in jobs:
+                with torch.cuda.stream(stream):
+                    run()
+        torch.cuda.synchronize()
+        for run, want, stream, c in jobs:
+            with torch.cuda.stream(stream):
+                assert all(torch.equal(a, b) for a, b in zip(run(), want)) and c.check_status() == 0
+    finally:
+        other.close()
+
+
+def test_two_captured_graphs_share_a_workspace(ctx):
+    lengths, new = [3000, 700], [9, 40]
+    cache = paged_ref.make_cache(lengths, 8, 2, 16, seed=3)
+    begin, q = begins(new), paged_ref.queries(49, 8, seed=3)
+    qb, mask = i32(begin), ref.words_of(see(new, 3), 2, 49)
+    ws = ctx.attn_kv4_paged_tree_workspace(cache, 49, 40)
+    outs, graphs = [torch.zeros_like(q) for _ in range(2)], []
+    calls = [lambda: ctx.attn_kv4_paged_tree(cache, q, qb, 40, mask, 128**-0.5, ws, out=outs[0]),
+             lambda: ctx.attn_kv4_paged_tree(cache, q, qb, 40, mask, 128**-0.5, ws, window=400, n_sink=5, out=outs[1])]
+    want = [f().clone() for f in calls]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        for f in calls:
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[-1], stream=s):
+                f()
+        for k in range(6):
+            for o in outs:
+                o.zero_()
+            graphs[k & 1].replay()
+            graphs[1 - (k & 1)].replay()
+            s.synchronize()
+            assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
+    torch.cuda.synchronize()
+    assert ctx.check_status() == 0
+
+
+@pytest.mark.parametrize("steps", ["head", "vector"])
+def test_every_number_of_columns(ctx, steps):
+    """Rows of 32, 64 and 128 columns, by the size of the call; a token's heads on both sides of a warp's 32 columns."""
+    for B, n, ctx_len, Hq, Hkv in ((40, 8, 300, 8, 2), (60, 13, 400, 10, 2), (80, 16, 500, 4, 1), (60, 18, 600, 14, 2), (40, 30, 700, 8, 2)):
+        new = [n - b % 3 for b in range(B)]
+        check(ctx, [ctx_len + 7 * b for b in range(B)], see(new, 4), Hq=Hq, Hkv=Hkv, steps=steps, hide=False)

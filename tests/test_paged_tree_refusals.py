@@ -120,11 +120,11 @@ def test_writers_of_lengths_and_caches_never_trigger(source, name):
 
 
 @pytest.mark.parametrize("source,name", [("pq_pages.cu", "page_keep_kernel"), ("pq_tree.cu", "kv4_paged_keep_kernel"), ("pq_tree.cu", "tree_plan_kernel"),
-                                         ("pq_tree.cu", "tree_accept_kernel")])
+                                         ("pq_tree.cu", "tree_accept_kernel"), ("pq_paged_tree.cu", "paged_tree_kernel")])
 def test_the_wait_comes_before_every_read_and_before_the_trigger(source, name):
     body = kernel_body(source, name)
     wait = body.index("pdl_wait")
-    assert wait < re.search(r"ld_dep|tree_rows|padding_rows|report\(", body).start()
+    assert wait < re.search(r"ld_dep|__ldcg|tma_load|cp_async|tree_rows|padding_rows|report\(", body).start()
     trigger = TRIGGER.search(body)
     assert trigger is None or wait < trigger.start()
     assert "__ldg(" not in body and "ld.global.nc" not in body
