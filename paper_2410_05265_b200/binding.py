@@ -816,6 +816,7 @@ class Context:
         """What every draft sees of its sequence's drafts (itself and the rows above it) and its position, behind page_plan. parent int32 [n_rows]: a row's parent
         within its sequence, -1 for a root. Returns (mask int32 [n_rows, words], 32 drafts to a word; pos int32 [n_rows]), which may be given as `out`."""
         here, N = self._here(pages), parent.numel()
+        assert words is not None or out is not None, "words"
         if out is None:
             out = (torch.empty((N, words), dtype=torch.int32, device=parent.device), torch.empty((N,), dtype=torch.int32, device=parent.device))
         mask, pos = out

@@ -872,7 +872,9 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
             const float k_step = in ? st[tid_e] : 1.0f, v_step = in ? st[PP_KEYS + tid_e] : 1.0f;
             float* key_out = reinterpret_cast<float*>(&steps_buf[stage].key[tid_e >> 1]) + (tid_e & 1);
             key_out[0] = k_step * p.scale2, key_out[2] = pq::lg2_approx(v_step);
-            reinterpret_cast<float*>(steps_buf[stage].inv)[tid_e] = pq::rcp_approx(v_step) * pq::PQ_DOWN;
+            const float inv = pq::rcp_approx(v_step) * pq::PQ_DOWN;
+            // (WIN: a step that is no number is in the exponents of the rows that see the key; the others' weights are zero)
+            reinterpret_cast<float*>(steps_buf[stage].inv)[tid_e] = WIN && !(inv < INFINITY) ? 0.0f : inv;
           }
           pq::fence_proxy_async_smem();  // generic-proxy writes -> visible to the tensor core's async proxy
           __syncwarp();

@@ -517,6 +517,7 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
           const int key = key_of(x, x.j0 + i0) + in_set, u = key - x.base, tok0 = col0 / G, tok_end = min(n_tok, (col0 + TK_COLS - 1) / G + 1);
           const bool seen = key < x.len && (key >= x.lo || key < p.n_sink), new_key = seen && u >= 0;  // by any row of the sequence
           if (DYN && !seen) a = 0.0f, b = 0.0f, inv = 0.0f;  // (its steps may be anything)
+          if (DYN && !(inv < INFINITY)) inv = 0.0f;          // (a draft's that is no number is in the exponents of those who see it; the others' weights are zero)
           const uint32_t* word = p.mask + static_cast<int64_t>(x.row0 + t0) * p.mask_words + (new_key ? u >> 5 : 0);
 #pragma unroll 1
           for (int tok = tok0; tok < tok_end; tok += 4) {

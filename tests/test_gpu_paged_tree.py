@@ -588,3 +588,25 @@ def test_every_number_of_columns(ctx, steps):
     for B, n, ctx_len, Hq, Hkv in ((40, 8, 300, 8, 2), (60, 13, 400, 10, 2), (80, 16, 500, 4, 1), (60, 18, 600, 14, 2), (40, 30, 700, 8, 2)):
         new = [n - b % 3 for b in range(B)]
         check(ctx, [ctx_len + 7 * b for b in range(B)], see(new, 4), Hq=Hq, Hkv=Hkv, steps=steps, hide=False)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), 0.0])
+@pytest.mark.parametrize("n", [7, 40, 120])
+def test_a_draft_without_numbers_stays_in_its_branch(ctx, n, bad):
+    """Own steps that are no number, of a draft: rows that do not see it keep their results."""
+    lengths = [300, 64 + n]
+    cache = paged_ref.make_cache(lengths, 8, 2, 16, steps="vector", seed=5)
+    begin, trees = [0, n, 2 * n], see([n, n], 3, seed=5)
+    q = paged_ref.queries(2 * n, 8, seed=5)
+    want, tol = ref.attention(cache, q, begin, lengths, 128**-0.5, trees=trees)
+    table = cache.pages.table.tolist()
+    for b, u in ((0, 2), (1, n - 2)):
+        c = lengths[b] - n + u
+        cache.steps[table[b][c // 16], :, :, c % 16] = bad
+    out = call(ctx, cache, q, begin, n, ref.words_of(trees, 4, 2 * n))
+    apart = torch.tensor([not row[u] for b, u in ((0, 2), (1, n - 2)) for row in trees[b]], device="cuda")
+    assert 0 < apart.sum() < 2 * n
+    assert torch.all((out.double() - want).abs()[apart] <= tol[apart])
+    if bad != bad:
+        assert torch.all(out[~apart].isnan())
+    assert ctx.check_status() == 0

@@ -188,3 +188,21 @@ def test_an_id_that_is_none_inside_the_window_is_reported(ctx):
     assert ctx.check_status() == 2
     call(ctx, cache, q, [0, 1], [1], 12, 0)  # keys 288 .. 299 lie on the page behind it
     assert ctx.check_status() == 0
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), 0.0])
+def test_a_key_without_numbers_leaves_with_the_window(ctx, bad):
+    """Own steps that are no number, of a cached key: rows whose window has left it keep their results, and so do the rows before it."""
+    lengths, begin, window = [400], [0, 300], 60
+    cache = paged_ref.make_cache(lengths, 8, 2, 16, steps="vector", seed=5)
+    q = paged_ref.queries(300, 8, seed=5)
+    want, tol = ref.attention(cache, q, begin, lengths, 128**-0.5, window, 4)
+    table, at = cache.pages.table.tolist(), 250
+    cache.steps[table[0][at // 16], :, :, at % 16] = bad
+    out = call(ctx, cache, q, begin, [300], window, 4)
+    place = torch.arange(300, device="cuda") + 100
+    sees = (place >= at) & (place < at + window)
+    assert torch.all((out.double() - want).abs()[~sees] <= tol[~sees])
+    if bad != bad:
+        assert torch.all(out[sees].isnan())
+    assert ctx.check_status() == 0
