@@ -58,7 +58,8 @@ pq_status pq_check(pq_ctx* ctx, void* stream);
 
 /* Bound of the device-side waits (a consumer waiting for a copy or for a producer, a producer waiting for
  * a free buffer) of the kernels launched through this context from now on, in SM clocks; 0 restores the
- * default of 2^31 clocks (about a second). One hardware try of a wait may itself take some thousand clocks; pq_attn_kv4_paged keeps limits below 16384 clocks by
+ * default of 2^31 clocks (about a second). One hardware try of a wait may itself take some thousand clocks; pq_attn_kv4_paged, its windowed form and
+ * pq_attn_kv4_paged_tree keep limits below 16384 clocks by
  * polling. A wait that runs out makes its kernel wind down in an orderly
  * way (copies in flight are awaited, tensor memory is released) and leaves PQ_ERR_TIMEOUT in the status
  * word; the kernel's output is then undefined. Failure-detection tests set a bound of a few clocks so that

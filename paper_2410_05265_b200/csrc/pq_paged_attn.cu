@@ -1,7 +1,8 @@
-// Attention over [full-precision prefix || paged 4-bit cache] for a ragged batch (pq_attn_kv4_paged).
+// Attention over [full-precision prefix || paged 4-bit cache] for a ragged batch (pq_attn_kv4_paged), through a window (pq_attn_kv4_paged_window) and of drafted trees
+// (pq_attn_kv4_paged_tree).
 //
-// Sequences with one new row (decode) and those with several (prompts, chunks) have a kernel each; which sequences are whose is found on the device, from
-// q_begin. A batch whose host bound says one row needs the first launch only.
+// Sequences with one new row (decode) and those with several (prompts, chunks) have a kernel each, with a form for windows; which sequences are whose is found on the
+// device, from q_begin. A batch whose host bound says one row needs the first launch only. Drafted trees have a kernel of their own, whatever their rows.
 #include "pq_paged_attn.cuh"
 
 extern "C" size_t pq_attn_kv4_paged_workspace_bytes(const pq_ctx* ctx, const pq_kv4_paged* cache, int64_t n_rows, int32_t max_new) {

@@ -1,5 +1,5 @@
-// Parameters and small device helpers of the two kernels behind pq_attn_kv4_paged: the one for single tokens (pq_paged_decode.cu) and
-// the one for sequences of several rows (pq_paged_prefill.cu).
+// Parameters and small device helpers of the kernels of paged attention: for single tokens (pq_paged_decode.cu), for sequences of several rows
+// (pq_paged_prefill.cu), both with a form for windows, and for drafted trees (pq_paged_tree.cu).
 #pragma once
 
 #include <math.h>
@@ -35,7 +35,7 @@ struct PagedAttnParams {
 };
 
 // One mbarrier try_wait may suspend its thread for thousands of clocks (three of them on a barrier that nothing completes take 15700), in which an ordinary wait ends. A
-// limit below that is kept by forms of the two kernels that poll instead (POLL): with them a test makes waits run out. As a choice inside the kernels it
+// limit below that is kept by forms of the kernels that poll instead (POLL): with them a test makes waits run out. As a choice inside the kernels it
 // took 2 to 4 % of them.
 #define PQ_SUSPENDED_CLOCKS 16384
 

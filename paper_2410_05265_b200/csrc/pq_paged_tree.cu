@@ -1,25 +1,40 @@
 // Attention of drafted trees: up to 128 new rows of a sequence, each of which sees the prefix, the cached keys before the new ones (through a window, where there is
 // one) and, of the new ones, what its mask says.
 //
-// Bound by HBM in principle while rows x heads of a KV head are few (128 bytes of codes for 256 D flops a column), by the tensor core and the special-function units
-// from 128 columns on. Few rows do not fill the 128 rows of an MMA, so the products are transposed: the keys, of which there are many, are the MMA's rows, a column is
-// a (token, query head) pair, and both products cost what the columns are:
+// Few rows do not fill the 128 rows of an MMA, so the products are transposed: the keys, of which there are many, are the MMA's rows, a column is a (token, query head)
+// pair, and both products cost what the columns are:
 //     S^T[key, column] = K Q^T        O^T[dim, column] = V^T P^T
 // The 4-bit codes are expanded into tensor memory, never into shared memory: K as exact bf16 integers (lane = key), V^T as exact fp16 integers (lane = head dim), each the
 // A operand of its product. What passes through shared memory is the packed rows, Q and P (the B operands): at 64 columns 640 clocks of its bandwidth per key
 // tile in place of 1660 with both operands there.
 //
-// An item is (sequence, KV head, floor(NC / G) tokens): NC = 32, 64 or 128 columns, the fewest that hold the call's rows. Work is counted in key tiles of 128 and a few
-// more for every item; a CTA per SM takes an equal stretch of the units of all items laid end to end. An item inside one stretch is final, one that several share
-// leaves partials in the workspace, and the last CTA to finish merges them in the order of the CTAs.
-//   loader warp       a TMA box per page (K and V rows of a head, 64-byte-swizzled so that both readers meet no bank twice) into a ring of key tiles
-//   K, V warps        four each: a warp expands its 32 keys, or its 32 head dims of all keys (transposed matrix loads; lane 8j + g of a quadrant is dim 4g + j)
-//   MMA warp          S^T of tile c + 1 is issued before O^T of tile c: the scores are double-buffered
-//   softmax warps     eight: a thread is a key, a set of four warps has half of the columns. Own steps are then constants of the thread; masks are a bit per column. A
-//                     column's reference exponent m lies in shared memory and moves only when a score exceeds it by more than 15 (one vote of the set per tile):
-//                     w = 2^(s + log2 step - m) goes to P in fp16, the denominator (sum of w / step, fp32) stays in the thread until the item ends.
-//   helper warps      queries of the next item into shared memory; scores of the prefixed keys, in fp32, which join at the item's end (they never set a reference)
+// An item is (sequence, KV head, floor(NC / G) tokens): NC = 32, 64 or 128 columns, by an estimate of the time (form_of). Work is counted in key tiles of 128 and ten more for
+// every item. Where there are as many workers as items, and the items are of about one length, a worker takes an item; else every worker takes an equal stretch of the units
+// of all items laid end to end. An item inside one stretch is final, one that several share leaves partials in the workspace, and the last CTA to finish merges them
+// in the order of the CTAs. Up to 64 columns two CTAs share an SM, so that one's first and last tiles of an item go beside the other's work.
+//   loader warp       a TMA box per page (K and V rows of a head, 64-byte-swizzled so that both readers meet no bank twice) into a ring of key tiles; own steps by
+//                     asynchronous copies of 16 bytes, a lane to a copy
+//   expansion warps   four: a warp expands its 32 keys of a tile, then its 32 head dims of all keys of the tile before (transposed matrix loads; lane 8j + g of a quadrant is
+//                     dim 4g + j)
+//   two MMA warps     S^T of a tile as soon as K and a buffer are there, O^T as soon as V and P are
+//   softmax warps     eight (to 64 columns) or sixteen. A thread is a key, a set of four warps has 32 columns; with 32 columns two sets take the tiles in turn, each with sums
+//                     and an O^T of its own, joined at the item's end. Own steps are constants of the thread; masks are a bit per column. A column's reference
+//                     exponent m lies in shared memory and moves only when a score exceeds it by more than 15 (one vote of the set per tile): w = 2^(s + log2 step - m) goes
+//                     to P in fp16, the denominator (sum of w / step, fp32) stays in the thread until the item ends.
+//   helper warp       queries and description of the next item; scores of the prefixed keys (bf16 MMA, the fp16 keys as two terms, fp32 sums), which join at the item's end
+//                     and never set a reference
 // Roundings to fewer bits: w to fp16 (2^-11; below 2^-14 in steps of 2^-24 of the reference's weight), the result to bf16. Every wait is bounded.
+//
+// What bounds it. In principle HBM while rows x heads of a KV head are few (128 bytes of codes for 256 D flops a column), the tensor core and the special-function units at
+// 128 columns. In practice the instructions of the expansion and the softmax: a key tile takes 0.9 us of an SM with 32 columns, 1.15 with 64, 1.5 with 128 (own steps 1.1,
+// 1.6, 2.1); issue slots are 43 - 60 % busy, and with 32 columns warps wait for instructions (3.3 of 15 clocks between two of a warp) as long as for anything else, which is why
+// loops here are rolled where that costs nothing. 48 x 5 rows at 6000 keys, own steps, 32 heads on 8: 87 us, 2.2 TB/s of codes; 12 x 64 rows at 16000 keys, 64 heads on 8:
+// 290 us, 720 TFLOP/s of visible pairs, 0.43 of the measured bf16 rate; 16 x 33 rows through a window of 2048: 44; 1 x 26 rows at 1021 keys: 17, of which half are the
+// sums and first loads (2.9 us), the first tile (3) and the end of an item (4).
+// In place of this kernel: the prompts' kernel with these masks takes 30, 258, 331 and 75 us for 1 x 26, 48 x 5, 12 x 64 and the windowed 16 x 33 rows.
+// Tried and not kept: the softmax warps expand V for 32 columns (48 x 5: 99 us against 97), boxes issued by a lane each (three times as long), steps loaded by the
+// softmax threads, one loop over both prefix sums (no difference), the first reference from a key of every warp in place of the largest of all (static 0.2 us less, own steps 2 %
+// more), the packed rows read ahead of the waits for tensor memory (no difference).
 #include <atomic>
 #include <type_traits>
 
@@ -57,9 +72,6 @@ struct TkShape {
   static constexpr int REGS_SOFTMAX = NC < 128 ? 88 : 96, REGS_OTHERS = NC < 128 ? 40 : 48;
 };
 
-struct TkStart {  // where a worker's stretch begins
-  int b, h, it, j0, u0, U, workers;
-};
 struct TkShared {  // an item that several workers share
   int w0, w1, b, h, it, row0, n;
 };
@@ -71,6 +83,10 @@ struct TkItem {
   int tiles, j0, j1;         // key tiles of the item, and this worker's
   int u;                     // unit where this worker's share begins
   int skip, lo;              // key tiles left out behind the first ones, and the first key of any row's window
+};
+struct TkStart {  // where a worker's stretch begins
+  TkItem x;
+  int U, workers;
 };
 
 template <int NC>
@@ -233,13 +249,15 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
   // ---- the sequences: units of work of all groups of one KV head, prefix sums, and where this worker's stretch begins
   const int64_t capacity = static_cast<int64_t>(p.max_pages) << p.page_log2;
   const int first_tiles = (p.n_sink + TK_KEYS - 1) / TK_KEYS;  // key tiles with keys that stay visible
-  auto load_seq = [&](TkItem& x, bool& odd) {  // n = 0 for a sequence that is left out
+  auto load_rows = [&](TkItem& x) {  // n = 0 for a sequence that is left out; false: something about it is odd
     const int r0 = pq::ld_dep(p.q_begin + x.b), r1 = pq::ld_dep(p.q_begin + x.b + 1), l = pq::ld_dep(p.len + x.b);
     const int64_t n = static_cast<int64_t>(r1) - r0;
     x.row0 = r0;
     x.len = l < 0 ? 0 : l > capacity ? static_cast<int>(capacity) : l;
-    odd = n > p.max_new || n < 0 || (n > 0 && (r0 < 0 || r1 > p.n_rows || l != x.len));
     x.n = n >= 1 && n <= p.max_new && r0 >= 0 && r1 <= p.n_rows ? static_cast<int>(n) : 0;
+    return !(n > p.max_new || n < 0 || (n > 0 && (r0 < 0 || r1 > p.n_rows || l != x.len)));
+  };
+  auto lay_out = [&](TkItem& x) {  // what follows from rows and length
     x.base = x.len - x.n;
     x.nt = (x.n + TI - 1) / TI;
     // rows lie at the root's place, `base`, or behind it: what all windows leave out
@@ -247,25 +265,62 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
     x.skip = max(0, x.lo - first_tiles * TK_KEYS) / TK_KEYS;
     x.tiles = max(1, (x.len + TK_KEYS - 1) / TK_KEYS - x.skip);
   };
+  auto load_seq = [&](TkItem& x) {
+    load_rows(x);
+    lay_out(x);
+  };
   auto key_of = [&](const TkItem& x, int jt) { return (jt >= first_tiles ? jt + x.skip : jt) * TK_KEYS; };
   int32_t *scan = reinterpret_cast<int32_t*>(smem), *items = scan + p.B + 1;  // units and items of one KV head before a sequence
-  __syncthreads();
-  for (int b = threadIdx.x; b < p.B; b += TK_THREADS) {
-    TkItem x;
-    x.b = b;
-    bool odd;
-    load_seq(x, odd);
+  auto units_of = [&](const TkItem& x, bool fine) {
     const int64_t t = static_cast<int64_t>(x.nt) * (x.tiles + TK_ITEM_UNITS);
-    if (odd || t * p.Hkv > 0x7fffffffll) pq::report(p.status, PQ_ERR_SHAPE);
-    scan[b] = t * p.Hkv > 0x7fffffffll ? 0 : static_cast<int32_t>(t);
-    items[b] = scan[b] > 0 ? x.nt : 0;
-    if (scan[b] > 0) atomicMax(&st->most_units, x.tiles + TK_ITEM_UNITS);
+    const bool too_many = t * p.Hkv > 0x7fffffffll;
+    if (!fine || too_many) pq::report(p.status, PQ_ERR_SHAPE);
+    return too_many ? 0 : static_cast<int>(t);
+  };
+  // Up to 32 sequences are a lane each, of the two warps that need the sums: no barrier, and the sequence of the first item comes from a lane (1 x 26 rows at 1021 keys
+  // 20 -> 17.5 us, with the end of the kernel that is left out where no item is shared).
+  const bool few = p.B <= 32;
+  TkItem mine;
+  mine.b = lane, mine.n = mine.len = mine.row0 = 0;
+  int64_t total = 0, n_items = 0;
+  int most_units = 0;
+  if (!few) {
+    __syncthreads();
+    for (int b = threadIdx.x; b < p.B; b += TK_THREADS) {
+      TkItem x;
+      x.b = b;
+      const bool fine = load_rows(x);
+      lay_out(x);
+      scan[b] = units_of(x, fine);
+      items[b] = scan[b] > 0 ? x.nt : 0;
+      if (scan[b] > 0) atomicMax(&st->most_units, x.tiles + TK_ITEM_UNITS);
+    }
+    __syncthreads();
+    total = pq::block_scan<TK_THREADS>(scan, p.B, st->part) * p.Hkv, n_items = pq::block_scan<TK_THREADS>(items, p.B, st->part) * p.Hkv;
+    most_units = st->most_units;
+  } else if (warp < 2) {
+    const bool fine = lane < p.B ? load_rows(mine) : true;
+    lay_out(mine);
+    const int units = units_of(mine, fine || warp > 0), nt = units > 0 ? mine.nt : 0;
+    int64_t units_to = units;
+    int items_to = nt;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t u = __shfl_up_sync(0xffffffffu, units_to, d);
+      const int v = __shfl_up_sync(0xffffffffu, items_to, d);
+      if (lane >= d) units_to += u, items_to += v;
+    }
+    total = __shfl_sync(0xffffffffu, units_to, 31) * p.Hkv, n_items = static_cast<int64_t>(__shfl_sync(0xffffffffu, items_to, 31)) * p.Hkv;
+    most_units = __reduce_max_sync(0xffffffffu, units > 0 ? mine.tiles + TK_ITEM_UNITS : 0);
+    if (lane < p.B) {  // (both warps write the same)
+      if (lane == 0) scan[0] = items[0] = 0;
+      scan[lane + 1] = static_cast<int32_t>(units_to), items[lane + 1] = items_to;
+    }
+    __syncwarp();
   }
-  __syncthreads();
-  const int64_t total = pq::block_scan<TK_THREADS>(scan, p.B, st->part) * p.Hkv, n_items = pq::block_scan<TK_THREADS>(items, p.B, st->part) * p.Hkv;
   // An item to a worker where there are enough workers and no item is much longer than an equal share: pieces of items cost their ends and the merge. (16 x 33 rows, window
   // 2048: 66 -> 48 us.)
-  const bool direct = n_items <= gridDim.x && static_cast<int64_t>(st->most_units - TK_PIECE) * gridDim.x <= total;
+  const bool direct = n_items <= gridDim.x && static_cast<int64_t>(most_units - TK_PIECE) * gridDim.x <= total;
   if (warp < 2) {  // the two borders of this CTA's stretch, a warp each
     const bool too_many = total > 0x7fffffffll;
     if (too_many && threadIdx.x == 0) pq::report(p.status, PQ_ERR_SHAPE);
@@ -273,39 +328,47 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
     s.U = too_many ? 0 : static_cast<int>(total);
     s.workers = direct ? static_cast<int>(n_items) : min(static_cast<int>(gridDim.x), max(1, s.U / (TK_ITEM_UNITS + 1)));
     int u = 0;
+    TkItem& x = s.x;
     if (s.U > 0 && static_cast<int>(blockIdx.x) < s.workers) {
-      int tiles = 0, at = 0;
+      int at = 0;
+      auto sequence = [&](int b) {
+        x.b = b;
+        if (few)
+          x.n = __shfl_sync(0xffffffffu, mine.n, b), x.len = __shfl_sync(0xffffffffu, mine.len, b), x.row0 = __shfl_sync(0xffffffffu, mine.row0, b);
+        else
+          load_rows(x);
+        lay_out(x);
+      };
       auto locate = [&](int v) {
-        TkItem x;
-        x.b = pq::find_segment(scan, p.B, v / p.Hkv);
-        bool odd;
-        load_seq(x, odd);
+        sequence(pq::find_segment(scan, p.B, v / p.Hkv));
         const int per_head = scan[x.b + 1] - scan[x.b], per = x.tiles + TK_ITEM_UNITS, rel = v - scan[x.b] * p.Hkv;
-        s.b = x.b, s.h = rel / per_head, s.it = rel % per_head / per;
-        at = rel % per_head % per, tiles = x.tiles, s.j0 = max(0, at - TK_ITEM_UNITS);
+        x.h = rel / per_head, x.it = rel % per_head / per;
+        at = rel % per_head % per, x.j0 = max(0, at - TK_ITEM_UNITS);
       };
       // inside a short item, or among an item's own units, an end of the item is taken, so that no partials are left for a few tiles
       const int w = blockIdx.x + warp;
       u = static_cast<int>(static_cast<int64_t>(s.U) * w / s.workers);
       if (direct && w < s.workers) {
-        const int b = pq::find_segment(items, p.B, w / p.Hkv), nt = items[b + 1] - items[b], rel = w - items[b] * p.Hkv;
-        s.b = b, s.h = rel / nt, s.it = rel % nt, s.j0 = 0;
-        u = scan[b] * p.Hkv + rel * ((scan[b + 1] - scan[b]) / nt);
+        sequence(pq::find_segment(items, p.B, w / p.Hkv));
+        const int rel = w - items[x.b] * p.Hkv;
+        x.h = rel / x.nt, x.it = rel % x.nt, x.j0 = 0;
+        u = scan[x.b] * p.Hkv + rel * (x.tiles + TK_ITEM_UNITS);
       } else if (w < s.workers) {
         locate(u);
         int to = u;
-        if (s.j0 == 0)
+        if (x.j0 == 0)
           to = u - at;
-        else if (tiles <= TK_SHORT)
-          to = 2 * s.j0 < tiles ? u - at : u + tiles - s.j0;
+        else if (x.tiles <= TK_SHORT)
+          to = 2 * x.j0 < x.tiles ? u - at : u + x.tiles - x.j0;
         if (to > u && to < s.U) locate(to);
-        if (to < u) s.j0 = 0;
+        if (to < u) x.j0 = 0;
         u = to;
       }
     }
     if (lane == 0) {
+      x.u = u;
       if (warp == 0)
-        st->start = s, st->start.u0 = u;
+        st->start = s;
       else
         st->border = u;
     }
@@ -314,16 +377,12 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
   pq::tc_fence_before();
   __syncthreads();
   pq::tc_fence_after();
-  const TkStart start = st->start;
   const int u_end = st->border;
   const uint32_t tmem_base = __shfl_sync(0xffffffffu, st->tmem_base, 0);
 
   auto first_item = [&]() {
-    TkItem x;
-    x.b = start.b, x.h = start.h, x.it = start.it;
-    bool odd;
-    load_seq(x, odd);
-    x.j0 = start.j0, x.u = start.u0;
+    TkItem x = st->start.x;
+    if (DYN) load_seq(x);  // (the same once more: with the copy alone the compiler's loops come out slower, 48 x 5 rows at 6000 keys 102 us for 91)
     x.j1 = min(x.tiles, x.j0 + (u_end - x.u) - (x.j0 == 0 ? TK_ITEM_UNITS : 0));
     return x;
   };
@@ -334,10 +393,9 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
       x.it = 0;
       if (++x.h == p.Hkv) {
         x.h = 0;
-        bool odd;
         do {
           ++x.b;
-          load_seq(x, odd);
+          load_seq(x);
         } while (x.n == 0);
       }
     }
@@ -364,7 +422,7 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
     st->abort_flag = 1;
     pq::report(p.status, PQ_ERR_TIMEOUT);
   };
-  const bool any = start.u0 < u_end;
+  const bool any = st->start.x.u < u_end;
   int lands_issued = 0;  // loader only
 
   // Queries of an item into shared memory, and the first keys of its tokens' windows; scores of the prefixed keys in fp32. The first item's by the softmax warps, which have
@@ -518,23 +576,28 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
           const bool seen = key < x.len && (key >= x.lo || key < p.n_sink), new_key = seen && u >= 0;  // by any row of the sequence
           if (DYN && !seen) a = 0.0f, b = 0.0f, inv = 0.0f;  // (its steps may be anything)
           if (DYN && !(inv < INFINITY)) inv = 0.0f;          // (a draft's that is no number is in the exponents of those who see it; the others' weights are zero)
-          const uint32_t* word = p.mask + static_cast<int64_t>(x.row0 + t0) * p.mask_words + (new_key ? u >> 5 : 0);
-#pragma unroll 1
-          for (int tok = tok0; tok < tok_end; tok += 4) {
-            uint32_t m[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) m[i] = pq::ld_dep(word + static_cast<int64_t>(min(tok + i, n_tok - 1)) * p.mask_words);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int at = (tok + i) * G - col0;
-              bool see = seen && tok + i < tok_end;
-              if (new_key)
-                see = see && (u == t0 + tok + i || ((m[i] >> (u & 31)) & 1));
-              else if (p.window > 0)
-                see = see && (key < p.n_sink || key >= st->lo[n_items & 1][min(tok + i, n_tok - 1)]);
-              const uint32_t heads = (1u << G) - 1;
-              if (see) vis |= at >= 0 ? heads << at : heads >> -at;
+          // a lane per token: what it sees of the warp's 32 keys, which lie in two words at most
+          uint32_t sees = 0;
+          if (__any_sync(0xffffffffu, new_key)) {
+            const int u0 = u - lane, w = u0 >> 5;
+            if (tok0 + lane < tok_end) {
+              const uint32_t* word = p.mask + static_cast<int64_t>(x.row0 + t0 + tok0 + lane) * p.mask_words;
+              sees = __funnelshift_r(w >= 0 ? pq::ld_dep(word + w) : 0u, (w + 1) * 32 < x.n ? pq::ld_dep(word + w + 1) : 0u, u0 & 31);
+              const int own = t0 + tok0 + lane - u0;
+              if (static_cast<uint32_t>(own) < 32) sees |= 1u << own;
             }
+          }
+#pragma unroll 1
+          for (int tok = tok0; tok < tok_end; ++tok) {
+            const uint32_t new_keys = __shfl_sync(0xffffffffu, sees, tok - tok0);
+            bool see = seen;
+            if (new_key)
+              see = (new_keys >> lane) & 1;
+            else if (p.window > 0)
+              see = seen && (key < p.n_sink || key >= st->lo[n_items & 1][tok]);
+            const uint32_t heads = (1u << G) - 1;
+            const int at = tok * G - col0;
+            if (see) vis |= at >= 0 ? heads << at : heads >> -at;
           }
         }
         if (ok && !wait_warp(&st->s_full[buf], phase)) leave();
@@ -623,7 +686,7 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
             }
             move(fresh);
           }
-        } else {  // (two copies: in that form 12 x 64 rows at 16000 keys took 326 us, in this 298)
+        } else {  // (two copies: in that form 12 x 64 rows at 16000 keys took 326 us, in this 298 then)
           if (i0 == turn) move(true);
           if (overflow()) {
             stop = *out_flag != 0;
@@ -782,7 +845,7 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
       if (!whole && threadIdx.x == 0) {
         const int u = x.j0 == 0 ? x.u + TK_ITEM_UNITS : x.u - x.j0;  // of the item's first tile
         // (exact: the quotient is a whole number or at least 2^-31 from one)
-        auto worker_of = [&](int unit) { return static_cast<int>((static_cast<double>(unit + 1ll) * start.workers - 1.0) / start.U); };
+        auto worker_of = [&](int unit) { return static_cast<int>((static_cast<double>(unit + 1ll) * st->start.workers - 1.0) / st->start.U); };
         st->shared[st->n_shared++] = TkShared{worker_of(u), worker_of(u + x.tiles - 1), x.b, x.h, x.it, x.row0, x.n};
       }
       turn = next_turn;
@@ -796,56 +859,59 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
     }
     // ---- the last of the workers w0 .. w1 of a shared item to come here merges their partials, in that order
     if (!ok && lane == 0) give_up();
-    __threadfence();
     all_sync();
-    if (threadIdx.x < 2) {
-      const bool go = !st->abort_flag && static_cast<int>(threadIdx.x) < st->n_shared;  // (its first item and its last)
-      const TkShared sh = st->shared[threadIdx.x];
-      st->merge[threadIdx.x] = go && atomicAdd(p.tickets + TK_TICKET0 + sh.w0, 1u) == static_cast<uint32_t>(sh.w1 - sh.w0) ? 1 : 0;
-    }
-    all_sync();
-    __threadfence();
-    for (int i = 0; i < 2; ++i) {
-      if (!st->merge[i]) continue;
-      const TkShared sh = st->shared[i];
-      const int t0 = sh.it * TI, cols = min(TI, sh.n - t0) * G;
-      for (int col = warp; col < cols; col += TK_SOFTMAX_WARPS) {
-        float m = -INFINITY, sum = 0.0f;
-        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int w0 = sh.w0; w0 <= sh.w1; w0 += 32) {  // a lane per partial for the weights, then the partials in turn
-          const int nw = min(32, sh.w1 - w0 + 1);
-          auto slot_of = [&](int w) { return (2 * static_cast<int64_t>(w) + (w == sh.w0 ? 1 : 0)) * NC + col; };
-          const float2 ml = lane < nw ? __ldcg(reinterpret_cast<const float2*>(p.ws_ml) + slot_of(w0 + lane)) : make_float2(-INFINITY, 0.0f);
-          float4 o[4];  // the first partials are on their way while the weights are formed
-          auto load = [&](int i) { return i < nw ? __ldcg(reinterpret_cast<const float4*>(p.ws_o + slot_of(w0 + i) * 128) + lane) : make_float4(0.0f, 0.0f, 0.0f, 0.0f); };
-#pragma unroll
-          for (int i = 0; i < 4; ++i) o[i] = load(i);
-          float mc = ml.x;
-#pragma unroll
-          for (int d = 1; d < 32; d <<= 1) mc = fmaxf(mc, __shfl_xor_sync(0xffffffffu, mc, d));
-          const float mn = fmaxf(m, mc), keep = m == -INFINITY ? 0.0f : pq::ex2_approx(m - mn);
-          const float w = ml.x == -INFINITY ? 0.0f : pq::ex2_approx(ml.x - mn);
-          float lw = ml.y != ml.y ? ml.y : ml.x == -INFINITY ? 0.0f : DYN ? pq::at_reference(ml.y, ml.x - mn) : ml.y * w;
-#pragma unroll
-          for (int d = 1; d < 32; d <<= 1) lw += __shfl_xor_sync(0xffffffffu, lw, d);
-          sum = (m == -INFINITY ? 0.0f : DYN ? pq::at_reference(sum, m - mn) : sum * keep) + lw;
-          m = mn;
-          acc.x *= keep, acc.y *= keep, acc.z *= keep, acc.w *= keep;
-          for (int i0 = 0; i0 < nw; i0 += 4) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float wi = __shfl_sync(0xffffffffu, w, (i0 + i) & 31);
-              acc.x = fmaf(o[i].x, wi, acc.x), acc.y = fmaf(o[i].y, wi, acc.y), acc.z = fmaf(o[i].z, wi, acc.z), acc.w = fmaf(o[i].w, wi, acc.w);
-              o[i] = load(i0 + 4 + i);
+    if (st->n_shared > 0) {
+      __threadfence();
+      all_sync();
+      if (threadIdx.x < 2) {
+        const bool go = !st->abort_flag && static_cast<int>(threadIdx.x) < st->n_shared;  // (its first item and its last)
+        const TkShared sh = st->shared[threadIdx.x];
+        st->merge[threadIdx.x] = go && atomicAdd(p.tickets + TK_TICKET0 + sh.w0, 1u) == static_cast<uint32_t>(sh.w1 - sh.w0) ? 1 : 0;
+      }
+      all_sync();
+      __threadfence();
+      for (int i = 0; i < 2; ++i) {
+        if (!st->merge[i]) continue;
+        const TkShared sh = st->shared[i];
+        const int t0 = sh.it * TI, cols = min(TI, sh.n - t0) * G;
+        for (int col = warp; col < cols; col += TK_SOFTMAX_WARPS) {
+          float m = -INFINITY, sum = 0.0f;
+          float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          for (int w0 = sh.w0; w0 <= sh.w1; w0 += 32) {  // a lane per partial for the weights, then the partials in turn
+            const int nw = min(32, sh.w1 - w0 + 1);
+            auto slot_of = [&](int w) { return (2 * static_cast<int64_t>(w) + (w == sh.w0 ? 1 : 0)) * NC + col; };
+            const float2 ml = lane < nw ? __ldcg(reinterpret_cast<const float2*>(p.ws_ml) + slot_of(w0 + lane)) : make_float2(-INFINITY, 0.0f);
+            float4 o[4];  // the first partials are on their way while the weights are formed
+            auto load = [&](int i) { return i < nw ? __ldcg(reinterpret_cast<const float4*>(p.ws_o + slot_of(w0 + i) * 128) + lane) : make_float4(0.0f, 0.0f, 0.0f, 0.0f); };
+  #pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = load(i);
+            float mc = ml.x;
+  #pragma unroll
+            for (int d = 1; d < 32; d <<= 1) mc = fmaxf(mc, __shfl_xor_sync(0xffffffffu, mc, d));
+            const float mn = fmaxf(m, mc), keep = m == -INFINITY ? 0.0f : pq::ex2_approx(m - mn);
+            const float w = ml.x == -INFINITY ? 0.0f : pq::ex2_approx(ml.x - mn);
+            float lw = ml.y != ml.y ? ml.y : ml.x == -INFINITY ? 0.0f : DYN ? pq::at_reference(ml.y, ml.x - mn) : ml.y * w;
+  #pragma unroll
+            for (int d = 1; d < 32; d <<= 1) lw += __shfl_xor_sync(0xffffffffu, lw, d);
+            sum = (m == -INFINITY ? 0.0f : DYN ? pq::at_reference(sum, m - mn) : sum * keep) + lw;
+            m = mn;
+            acc.x *= keep, acc.y *= keep, acc.z *= keep, acc.w *= keep;
+            for (int i0 = 0; i0 < nw; i0 += 4) {
+  #pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float wi = __shfl_sync(0xffffffffu, w, (i0 + i) & 31);
+                acc.x = fmaf(o[i].x, wi, acc.x), acc.y = fmaf(o[i].y, wi, acc.y), acc.z = fmaf(o[i].z, wi, acc.z), acc.w = fmaf(o[i].w, wi, acc.w);
+                o[i] = load(i0 + 4 + i);
+              }
             }
           }
+          const float norm = sum > 0.0f ? 1.0f / sum : sum == sum ? 0.0f : sum;
+          const int tok = col / G;
+          *reinterpret_cast<uint2*>(p.out + (static_cast<int64_t>(sh.row0 + t0 + tok) * p.Hq + sh.h * G + (col - tok * G)) * 128 + 4 * lane) =
+              pack_bf16x4(make_float4(acc.x * norm, acc.y * norm, acc.z * norm, acc.w * norm));
         }
-        const float norm = sum > 0.0f ? 1.0f / sum : sum == sum ? 0.0f : sum;
-        const int tok = col / G;
-        *reinterpret_cast<uint2*>(p.out + (static_cast<int64_t>(sh.row0 + t0 + tok) * p.Hq + sh.h * G + (col - tok * G)) * 128 + 4 * lane) =
-            pack_bf16x4(make_float4(acc.x * norm, acc.y * norm, acc.z * norm, acc.w * norm));
+        if (threadIdx.x == 0) p.tickets[TK_TICKET0 + sh.w0] = 0;
       }
-      if (threadIdx.x == 0) p.tickets[TK_TICKET0 + sh.w0] = 0;
     }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Sh::REGS_OTHERS));
