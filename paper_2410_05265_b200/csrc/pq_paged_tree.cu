@@ -1175,20 +1175,23 @@ TkForm form(bool dyn, int n_prefix) {
   return {dyn ? paged_tree_kernel<NC, true, POLL> : paged_tree_kernel<NC, false, POLL>, NC, TkShape<NC>::CTAS, TkShape<NC>::THREADS, tk_smem_bytes<NC>(dyn, n_prefix),
           tk_smem_bytes<NC>(dyn, PQ_PAGED_MAX_PREFIX)};
 }
-// How many columns: by an estimate for B sequences of max_new rows and max_len cached keys. A key tile of an SM takes 0.9 us with 32 columns, 1.15 with 64 and 1.5 with 128
-// (own steps: 1.1, 1.6, 2.1), so that wide items are cheaper by the column; but a stretch is no shorter than a short item, whose tiles one CTA takes one after another, and
-// narrow items are more. us with 32 / 64 / 128 columns, 32 heads on 8: 1 x 26 rows at 1021 keys 19 / 23 / 25, at 4000 25 / 32 / 34; 1 x 128 at 20000 106 / 85 / 76;
-// 16 x 16 at 4000 66 / 56 / 65, 64 x 8 at 6000 151 / 180 / 257, 32 x 30 at 4000 226 / 148 / 131. Short wait limits take the polling form, of 128 columns whatever the rows.
+// How many columns: by an estimate for B sequences of max_new rows and max_len cached keys, fitted to 176 ragged batches of 1 to 48 sequences (on their average 1 % above the
+// best of the three, 35 % at most). An item costs its key tiles and 4 to 6 more of 1.5 us with 32 columns, 2.2 with 64 (two CTAs share the SM) and 1.9 with 128; short items are
+// not cut, so that CTAs walk whole rounds of them; and with long ones a stretch is no shorter than a short item. us with 32 / 64 / 128 columns, 32 heads on 8: 1 x 26
+// rows at 1021 keys 18 / 22 / 24, at 4000 23 / 30 / 33; 1 x 128 at 20000 106 / 82 / 74; 16 x 16 at 4000 55 / 52 / 56, 64 x 8 at 6000 139 / 170 / 250, 32 x 30 at 4000
+// 185 / 136 / 123. Short wait limits take the polling form, of 128 columns whatever the rows.
 TkForm form_of(const pq_ctx* ctx, const PagedAttnParams& p, int64_t max_len) {
   const bool dyn = p.steps != nullptr;
   if (p.wait_clocks < PQ_SUSPENDED_CLOCKS) return form<128, true>(dyn, p.n_prefix);
-  const double tiles = static_cast<double>(max_len < TK_KEYS ? 1 : (max_len + TK_KEYS - 1) / TK_KEYS), least = (tiles < TK_SHORT ? tiles : TK_SHORT) + TK_ITEM_UNITS;
-  auto estimate = [&](int nc, double busy, double alone) {
+  const double tiles = static_cast<double>(max_len < TK_KEYS ? 1 : (max_len + TK_KEYS - 1) / TK_KEYS);
+  auto estimate = [&](int nc, int ctas, double fixed, double more, double tile) {
     const int per_item = nc / p.G;
-    const double work = static_cast<double>(p.B) * p.Hkv * ((p.max_new + per_item - 1) / per_item) * (tiles + TK_ITEM_UNITS) / ctx->sm_count * busy;
-    return work > least * alone ? work : least * alone;
+    const int64_t items = static_cast<int64_t>(p.B) * p.Hkv * ((p.max_new + per_item - 1) / per_item), workers = static_cast<int64_t>(ctas) * ctx->sm_count;
+    const double least = TK_SHORT + more, share = static_cast<double>(items) / workers * (tiles + more);
+    const double units = tiles <= TK_SHORT ? static_cast<double>((items + workers - 1) / workers) * (tiles + more) : share > least ? share : least;
+    return fixed + units * tile;
   };
-  const double t32 = estimate(32, 0.9, 0.95), t64 = estimate(64, 1.15, 1.3), t128 = estimate(128, 1.5, 1.45);
+  const double t32 = estimate(32, 2, 3.0, 5.0, 1.5), t64 = estimate(64, 2, 2.0, 4.0, 2.2), t128 = estimate(128, 1, 0.0, 6.0, 1.9);
   if (t32 <= t64 && t32 <= t128) return form<32, false>(dyn, p.n_prefix);
   return t64 <= t128 ? form<64, false>(dyn, p.n_prefix) : form<128, false>(dyn, p.n_prefix);
 }
