@@ -47,6 +47,7 @@ constexpr int TK_COLS = 32;  // columns of a softmax thread
 constexpr int TK_ITEM_UNITS = 10;  // units that an item costs besides its key tiles
 constexpr int TK_SHORT = 8;       // an item of so many key tiles or fewer is not shared between workers
 constexpr int TK_PIECE = 15;      // units that cutting an item costs
+constexpr int TK_LEAST = 5;       // units of a stretch at least (eleven, an item of one tile: 3 x 26 rows at 1513 keys 23 us for 18, 2 x 18 at 3723 24 for 19)
 constexpr float TK_LAZY = 15.0f;
 constexpr float TK_NONE = 3.0e38f;  // in place of -m of a column that has seen no key: whatever it sees first exceeds the reference
 constexpr int TK_TICKET0 = PQ_PAGED_TICKET0 + PQ_PAGED_MAX_WORKERS;
@@ -326,7 +327,7 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
     if (too_many && threadIdx.x == 0) pq::report(p.status, PQ_ERR_SHAPE);
     TkStart s{};
     s.U = too_many ? 0 : static_cast<int>(total);
-    s.workers = direct ? static_cast<int>(n_items) : min(static_cast<int>(gridDim.x), max(1, s.U / (TK_ITEM_UNITS + 1)));
+    s.workers = direct ? static_cast<int>(n_items) : min(static_cast<int>(gridDim.x), max(1, s.U / TK_LEAST));
     int u = 0;
     TkItem& x = s.x;
     if (s.U > 0 && static_cast<int>(blockIdx.x) < s.workers) {
