@@ -445,6 +445,7 @@ pq_status pq_tree_plan(pq_ctx* ctx, const pq_pages* pages, const int32_t* parent
 /* Attention of drafts: row t sees every prefixed key, the cached keys before the n drafts, itself, and the drafts u with bit u of mask[row] set (any of them, not
  * only rows before it; bits from n on say nothing).
  *   window  0, or a window of at least max_new keys with n_sink first ones as above, where the place of a row is len[b] - n + (the drafts it sees) - 1
+ *           (pages whose keys all lie before len[b] - n - window + 1 and behind the first n_sink are not read; their table entries may hold anything)
  *   mask as pq_tree_plan writes it or the caller's own; max_new <= 128 and <= 32 * mask_words; the workspace is
  *   pq_attn_kv4_paged_tree_workspace_bytes(ctx, cache, n_rows, max_new); every other argument as in pq_attn_kv4_paged (max_len chooses how many rows share a
  *   key tile: 1 x 26 rows at 1021 keys take 17 us with it and 23 without under a table of 131072 tokens).

@@ -610,3 +610,15 @@ def test_a_draft_without_numbers_stays_in_its_branch(ctx, n, bad):
     if bad != bad:
         assert torch.all(out[~apart].isnan())
     assert ctx.check_status() == 0
+
+
+@pytest.mark.parametrize("steps", ["head", "vector"])
+@pytest.mark.parametrize("window", [64, 130, 500])
+def test_own_masks_through_a_window(ctx, window, steps):
+    """Any mask, not only a tree's: the place of a row, and with it its window, follows from how many drafts it sees. No key before every row's window is read."""
+    rng, new, lengths = random.Random(window), [64, 33, 1], [900, 40, 333]
+    trees = [[[rng.random() < 0.5 for _ in range(n)] for _ in range(n)] for n in new]
+    check(ctx, lengths, trees, steps=steps, window=window, n_sink=3, hide=False)
+    for row in trees:
+        row[0] = [True] + [False] * (len(row) - 1)  # a row that sees itself alone has the earliest window
+    check(ctx, lengths, trees, steps=steps, window=window, n_sink=3)
