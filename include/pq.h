@@ -467,8 +467,9 @@ pq_status pq_tree_accept(pq_ctx* ctx, const int32_t* q_begin, int32_t B, const i
  *     len_out[b] = len[b] - n + n_kept[b]
  * The pages behind the new length go back, sequence by sequence in the order of the table: they follow the free ids, *n_free_out = *n_free + their number. The table is
  * left as it is. len_out and n_free_out may be len and n_free. If a count or length is none (0 <= n_kept <= n <= len), the list cannot hold the pages or an id to go
- * back is none, nothing changes and PQ_ERR_SHAPE is reported. */
-pq_status pq_page_keep(pq_ctx* ctx, const pq_pages* pages, const int32_t* q_begin, const int32_t* n_kept, int32_t* len_out, int32_t* n_free_out, void* stream);
+ * back is none, no page and no length changes, PQ_ERR_SHAPE is reported, and every n_kept becomes -1, so that the pq_kv4_paged_keep calls of the step, which belong to the
+ * lengths this call would have left, move nothing in any sequence. */
+pq_status pq_page_keep(pq_ctx* ctx, const pq_pages* pages, const int32_t* q_begin, int32_t* n_kept, int32_t* len_out, int32_t* n_free_out, void* stream);
 /* The moves of one layer's cache that belong to it, behind pq_page_keep (cache->pages.len holds the lengths it left) and before the pages that went back are written
  * again: with base = len[b] - n_kept[b] the vectors (codes and, with own steps, steps) of the token at place base + kept[q_begin[b] + i] go to place base + i, for
  * i < n_kept[b], as if all were read before any is written. kept need not ascend; what lies behind base + n_kept is undefined afterwards.

@@ -862,7 +862,7 @@ class Context:
 
     def page_keep(self, pages: Pages, q_begin: torch.Tensor, n_kept: torch.Tensor, len_out=None, n_free_out=None) -> None:
         """Of every sequence's last tokens, as many as it has rows, the first n_kept[b] stay; pages behind the new length go back to the free list. Lengths and count
-        change in place by default."""
+        change in place by default. Where the call is refused (see check) n_kept becomes -1 everywhere, and the moves of kv4_paged_keep do nothing."""
         here, B, s = self._here(pages), pages.B, pages.struct
         _ok(self.lib.pq_page_keep(self.h, ctypes.byref(s), _arr(q_begin, torch.int32, (B + 1,), here, "q_begin"), _arr(n_kept, torch.int32, (B,), here, "n_kept"),
                                   s.len if len_out is None else _arr(len_out, torch.int32, (B,), here, "len_out"),

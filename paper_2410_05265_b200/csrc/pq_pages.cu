@@ -21,7 +21,8 @@ struct PlanParams {
   const int32_t* len;
   int32_t* free_list;
   const int32_t* n_free;
-  const int32_t* n_new;  // plan: new tokens; release: flags
+  const int32_t* n_new;  // plan: new tokens; release: flags; keep: how many stay
+  int32_t* n_kept;       // keep: the same array, -1 everywhere after a refusal
   int32_t* q_begin;
   int64_t* slot;
   int32_t* pos;
@@ -179,7 +180,8 @@ __global__ void __launch_bounds__(PG_THREADS) page_release_kernel(const PlanPara
 }
 
 // The last tokens of a sequence leave: of the rows q_begin[b] .. q_begin[b + 1] - 1, which are the last of the cached ones, the first n_kept[b] stay. Shared memory:
-// pages[B + 1], len[B] (after).
+// pages[B + 1], len[B] (after). The moves that follow in every layer's cache see the lengths and the counts alone, and a refusal for one sequence, for the list or for an id
+// leaves the lengths of all as they were: the counts are then set to -1, which no move follows.
 __global__ void __launch_bounds__(PG_THREADS) page_keep_kernel(const PlanParams p) {
   extern __shared__ __align__(16) int32_t pg_smem[];
   __shared__ int64_t part[PG_THREADS / 32];
@@ -227,9 +229,12 @@ __global__ void __launch_bounds__(PG_THREADS) page_keep_kernel(const PlanParams 
   } else if (tid == 0) {
     pq::report(p.status, PQ_ERR_SHAPE);
   }
-  if (n_ctas > 1) pq::cluster_sync();  // every CTA has read the lengths and the count
+  if (n_ctas > 1) pq::cluster_sync();  // every CTA has read the lengths and the counts
   __syncthreads();
-  for (int b = tid; b < p.B; b += n_threads) p.len_out[b] = refused ? pq::ld_dep(p.len + b) : len[b];
+  for (int b = tid; b < p.B; b += n_threads) {
+    p.len_out[b] = refused ? pq::ld_dep(p.len + b) : len[b];
+    if (refused) p.n_kept[b] = -1;
+  }
   if (tid == 0) *p.n_free_out = refused ? n_free : n_free + static_cast<int32_t>(total);
 }
 
@@ -289,13 +294,13 @@ extern "C" pq_status pq_page_release(pq_ctx* ctx, const pq_pages* pages, const i
   return launch(ctx, page_release_kernel, limit_set, p, pages->n_pages, 2, 1, static_cast<cudaStream_t>(stream));
 }
 
-extern "C" pq_status pq_page_keep(pq_ctx* ctx, const pq_pages* pages, const int32_t* q_begin, const int32_t* n_kept, int32_t* len_out, int32_t* n_free_out, void* stream) {
+extern "C" pq_status pq_page_keep(pq_ctx* ctx, const pq_pages* pages, const int32_t* q_begin, int32_t* n_kept, int32_t* len_out, int32_t* n_free_out, void* stream) {
   if (!ctx || !n_free_out) return PQ_ERR_INVALID_ARG;
   const pq_status st = pq_check_pages(pages);
   if (st != PQ_OK) return st;
   if (pages->B > 0 && (!q_begin || !n_kept || !len_out)) return PQ_ERR_INVALID_ARG;
   PlanParams p = base_params(ctx, pages);
-  p.q_begin = const_cast<int32_t*>(q_begin), p.n_new = n_kept, p.len_out = len_out, p.n_free_out = n_free_out;
+  p.q_begin = const_cast<int32_t*>(q_begin), p.n_new = p.n_kept = n_kept, p.len_out = len_out, p.n_free_out = n_free_out;
   static std::atomic<bool> limit_set[64] = {};
   return launch(ctx, page_keep_kernel, limit_set, p, pages->B, 2, 1, static_cast<cudaStream_t>(stream));
 }
