@@ -425,7 +425,8 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
     pq::report(p.status, PQ_ERR_TIMEOUT);
   };
   const bool any = st->start.x.u < u_end;
-  int lands_issued = 0;  // loader only
+  int lands_issued = 0;   // loader only
+  bool said_all = false;  // loader only: a slot more than those holds its word that this was all
 
   // Queries of an item into shared memory, and the first keys of its tokens' windows; scores of the prefixed keys in fp32. The first item's by the softmax warps, which have
   // nothing else to do yet, later ones' by the helper.
@@ -1057,6 +1058,7 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
         __threadfence_block();
         for (int i = 0; i < (DYN ? 33 : 1); ++i) pq::mbar_arrive(&st->land_full[slot]);
       }
+      said_all = ok;
       if (!ok && lane == 0) give_up();
     } else if (warp == Sh::WARP_QK || warp == Sh::WARP_PV) {
       // ================================================================== MMA issuers, a warp for each product: the whole warp runs the loop, the elected lane issues
@@ -1156,8 +1158,9 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
   pq::tc_fence_before();
   __syncthreads();
   if (warp == Sh::WARP_LOAD && lane == 0 && st->abort_flag) {
-    // copies that nobody consumed must have landed before the CTA may exit
-    for (int c = max(0, lands_issued - LANDS); c < lands_issued; ++c) pq::mbar_wait(&st->land_full[c % LANDS], (c / LANDS) & 1);
+    // Copies that nobody consumed must have landed before the CTA may exit. The slot with the loader's word has gone on by a phase, in which it has the parity that would be
+    // waited for; its copies have been read (the loader waited for that before it gave its word).
+    for (int c = max(0, lands_issued - LANDS + (said_all ? 1 : 0)); c < lands_issued; ++c) pq::mbar_wait(&st->land_full[c % LANDS], (c / LANDS) & 1);
   }
   __syncthreads();
   if (warp == Sh::WARP_QK) {
