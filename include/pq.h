@@ -449,7 +449,9 @@ pq_status pq_tree_plan(pq_ctx* ctx, const pq_pages* pages, const int32_t* parent
  *   mask as pq_tree_plan writes it or the caller's own; max_new <= 128 and <= 32 * mask_words; the workspace is
  *   pq_attn_kv4_paged_tree_workspace_bytes(ctx, cache, n_rows, max_new); every other argument as in pq_attn_kv4_paged (max_len chooses how many rows share a
  *   key tile: 1 x 26 rows at 1021 keys take 17 us with it and 23 without under a table of 131072 tokens).
- * Weights are held in fp16 as there, queries and keys exactly; prefixed keys are weighed in fp32. */
+ * Queries and keys are held exactly, weights in fp16 as there, prefixed keys are weighed in fp32. What draws most of the weight is often a first key whose value is small:
+ * neither a prefixed key nor a cached one among the first n_sink (n_sink 0: the first 128) takes bits of the other keys' weights, but for those beside it in its key tile of
+ * 128, which keep 11 bits down to 2^-27 of its weight and multiples of 2^-37 of it below. */
 size_t pq_attn_kv4_paged_tree_workspace_bytes(const pq_ctx* ctx, const pq_kv4_paged* cache, int64_t n_rows, int32_t max_new);
 pq_status pq_attn_kv4_paged_tree(pq_ctx* ctx, const pq_kv4_paged* cache, const void* q, int64_t ldq, const int32_t* q_begin, int64_t n_rows, int32_t max_new,
                                  int32_t max_len, const uint32_t* mask, int32_t mask_words, int32_t window, int32_t n_sink, void* out, float sm_scale,

@@ -21,6 +21,7 @@
 //                     and an O^T of its own, joined at the item's end. Own steps are constants of the thread; masks are a bit per column. A column's reference
 //                     exponent m lies in shared memory and moves only when a score exceeds it by more than 15 (one vote of the set per tile): w = 2^(s + log2 step - m) goes
 //                     to P in fp16, the denominator (sum of w / step, fp32) stays in the thread until the item ends.
+//                     The tiles of an item are walked from the one behind the first keys on, those of the first keys last (TK_LIFT).
 //   helper warp       queries and description of the next item; scores of the prefixed keys (bf16 MMA, the fp16 keys as two terms, fp32 sums), which join at the item's end
 //                     and never set a reference
 // Roundings to fewer bits: w to fp16 (2^-11; below 2^-14 in steps of 2^-24 of the reference's weight), the result to bf16. Every wait is bounded.
@@ -36,6 +37,8 @@
 // softmax threads, one loop over both prefix sums (no difference), the first reference from a key of every warp in place of the largest of all (static 0.2 us less, own steps 2 %
 // more), the packed rows read ahead of the waits for tensor memory (no difference), partials merged four columns at a time through a ring of asynchronous copies (large calls 2 to 3 %
 // less, small ones up to 5 % more).
+#include <limits.h>
+
 #include <atomic>
 #include <type_traits>
 
@@ -50,6 +53,10 @@ constexpr int TK_SHORT = 8;       // an item of so many key tiles or fewer is no
 constexpr int TK_PIECE = 15;      // units that cutting an item costs
 constexpr int TK_LEAST = 5;       // units of a stretch at least (eleven, an item of one tile: 3 x 26 rows at 1513 keys 23 us for 18, 2 x 18 at 3723 24 for 19)
 constexpr float TK_LAZY = 15.0f;
+// A first cached key often draws most of the weight and has a small value: what the others' weights keep of their bits is then what the output keeps. So the tiles of first
+// keys are an item's last, and a reference that moves to a key so far above the others, or is set by a group's last tile, stays TK_LIFT below it: nothing higher is
+// expected, and the other keys of that tile keep all their bits to 2^-27 of its weight and multiples of 2^-37 of it below.
+constexpr float TK_LIFT = 14.0f;
 constexpr float TK_NONE = 3.0e38f;  // in place of -m of a column that has seen no key: whatever it sees first exceeds the reference
 constexpr int TK_TICKET0 = PQ_PAGED_TICKET0 + PQ_PAGED_MAX_WORKERS;
 constexpr int TK_LAND_CODES = TK_KEYS * 128;  // a key tile's packed rows of K and V
@@ -271,7 +278,13 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
     load_rows(x);
     lay_out(x);
   };
-  auto key_of = [&](const TkItem& x, int jt) { return (jt >= first_tiles ? jt + x.skip : jt) * TK_KEYS; };
+  // First key of an item's tile jt: the tiles behind the first ones, then those (without keys that stay visible the cache's first, where it is not left out).
+  auto first_of = [&](const TkItem& x) { return min(x.tiles, first_tiles > 0 ? first_tiles : x.skip == 0 ? 1 : 0); };
+  auto key_of = [&](const TkItem& x, int jt) {
+    int at = jt + first_of(x);
+    if (at >= x.tiles) at -= x.tiles;
+    return (at >= first_tiles ? at + x.skip : at) * TK_KEYS;
+  };
   int32_t *scan = reinterpret_cast<int32_t*>(smem), *items = scan + p.B + 1;  // units and items of one KV head before a sequence
   auto units_of = [&](const TkItem& x, bool fine) {
     const int64_t t = static_cast<int64_t>(x.nt) * (x.tiles + TK_ITEM_UNITS);
@@ -547,18 +560,23 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
       float2 l[TK_COLS / 2];  // of this thread's keys
 #pragma unroll
       for (int i = 0; i < TK_COLS / 2; ++i) l[i] = make_float2(0.0f, 0.0f);
-      // Tiles that need masks: from the one with the first new key on (the cache ends there, too), and from the first that is not wholly of keys that stay visible to the
-      // last in which a row's window begins.
-      const int mask_from = (x.base < 0 ? 0 : x.base / TK_KEYS - x.skip) - x.j0;
-      int mask_a = 0, mask_n = 0;
-      if (p.window > 0) {
-        const int tile_lo = (max(0, x.base + x.n - p.window) + TK_KEYS - 1) / TK_KEYS;
-        mask_a = p.n_sink / TK_KEYS, mask_n = max(0, (tile_lo > first_tiles ? tile_lo - x.skip : tile_lo) - mask_a), mask_a -= x.j0;
+      // Tiles that need no masks: from the begin of the last row's window to the first new key (the cache ends behind it), and the first keys' at the end, where all rows see
+      // all of them.
+      int clear_a = 0, clear_n, clear_from = x.tiles - first_of(x) - x.j0;
+      {
+        const int first = first_of(x), tile_new = x.base < 0 ? 0 : x.base / TK_KEYS - x.skip;
+        if (p.window > 0) {
+          const int tile_lo = (max(0, x.base + x.n - p.window) + TK_KEYS - 1) / TK_KEYS - x.skip;
+          clear_a = max(0, tile_lo - first);
+          if (p.n_sink / TK_KEYS < min(tile_lo, first)) clear_from = INT_MAX;
+        }
+        clear_n = max(0, tile_new - first - clear_a), clear_a -= x.j0;
+        if (tile_new < first) clear_from = INT_MAX;
       }
       for (int i0 = turn; i0 < n_tiles; i0 += T, ++k) {
         const int buf = T > 1 ? group : k % NB, phase = T > 1 ? k & 1 : (k / NB) & 1;
         const uint32_t s_addr = tmem_base + lane_base + buf * NC + col0;
-        const bool need_mask = i0 >= mask_from || static_cast<uint32_t>(i0 - mask_a) < static_cast<uint32_t>(mask_n);
+        const bool need_mask = static_cast<uint32_t>(i0 - clear_a) >= static_cast<uint32_t>(clear_n) && i0 < clear_from;
         // what the key's score is multiplied by, log2 of the value's step PQ_UP octaves up, and what its weight counts in the denominator
         float a = scale, b = 0.0f, inv = 1.0f;
         if (DYN) {
@@ -579,28 +597,32 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
           const bool seen = key < x.len && (key >= x.lo || key < p.n_sink), new_key = seen && u >= 0;  // by any row of the sequence
           if (DYN && !seen) a = 0.0f, b = 0.0f, inv = 0.0f;  // (its steps may be anything)
           if (DYN && !(inv < INFINITY)) inv = 0.0f;          // (a draft's that is no number is in the exponents of those who see it; the others' weights are zero)
-          // a lane per token: what it sees of the warp's 32 keys, which lie in two words at most
-          uint32_t sees = 0;
-          if (__any_sync(0xffffffffu, new_key)) {
-            const int u0 = u - lane, w = u0 >> 5;
-            if (tok0 + lane < tok_end) {
-              const uint32_t* word = p.mask + static_cast<int64_t>(x.row0 + t0 + tok0 + lane) * p.mask_words;
-              sees = __funnelshift_r(w >= 0 ? pq::ld_dep(word + w) : 0u, (w + 1) * 32 < x.n ? pq::ld_dep(word + w + 1) : 0u, u0 & 31);
-              const int own = t0 + tok0 + lane - u0;
-              if (static_cast<uint32_t>(own) < 32) sees |= 1u << own;
+          if (key - in_set + TK_KEYS <= x.lo) {  // first keys alone, which all rows see
+            vis = seen ? ~0u : 0u;
+          } else {
+            // a lane per token: what it sees of the warp's 32 keys, which lie in two words at most
+            uint32_t sees = 0;
+            if (__any_sync(0xffffffffu, new_key)) {
+              const int u0 = u - lane, w = u0 >> 5;
+              if (tok0 + lane < tok_end) {
+                const uint32_t* word = p.mask + static_cast<int64_t>(x.row0 + t0 + tok0 + lane) * p.mask_words;
+                sees = __funnelshift_r(w >= 0 ? pq::ld_dep(word + w) : 0u, (w + 1) * 32 < x.n ? pq::ld_dep(word + w + 1) : 0u, u0 & 31);
+                const int own = t0 + tok0 + lane - u0;
+                if (static_cast<uint32_t>(own) < 32) sees |= 1u << own;
+              }
             }
-          }
 #pragma unroll 1
-          for (int tok = tok0; tok < tok_end; ++tok) {
-            const uint32_t new_keys = __shfl_sync(0xffffffffu, sees, tok - tok0);
-            bool see = seen;
-            if (new_key)
-              see = (new_keys >> lane) & 1;
-            else if (p.window > 0)
-              see = seen && (key < p.n_sink || key >= st->lo[n_items & 1][tok]);
-            const uint32_t heads = (1u << G) - 1;
-            const int at = tok * G - col0;
-            if (see) vis |= at >= 0 ? heads << at : heads >> -at;
+            for (int tok = tok0; tok < tok_end; ++tok) {
+              const uint32_t new_keys = __shfl_sync(0xffffffffu, sees, tok - tok0);
+              bool see = seen;
+              if (new_key)
+                see = (new_keys >> lane) & 1;
+              else if (p.window > 0)
+                see = seen && (key < p.n_sink || key >= st->lo[n_items & 1][tok]);
+              const uint32_t heads = (1u << G) - 1;
+              const int at = tok * G - col0;
+              if (see) vis |= at >= 0 ? heads << at : heads >> -at;
+            }
           }
         }
         if (ok && !wait_warp(&st->s_full[buf], phase)) leave();
@@ -624,7 +646,8 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
               v[i].y = vis & (2u << (2 * i)) ? v[i].y : -INFINITY;
             }
         };
-        // The references go to the whole number above the columns' largest exponents over the set's keys where one lies more than TK_LAZY above, or there is none yet.
+        // The references go to the whole number above the columns' largest exponents over the set's keys (or TK_LIFT below it) where one lies more than TK_LAZY above, or there
+        // is none yet.
         auto move = [&](bool first) {
 #pragma unroll 1
           for (int e = 0; e < TK_COLS; e += 16) {
@@ -641,7 +664,7 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
           const int col = col0 + lane;  // a lane per column, all four warps alike
           const float top_c = fmaxf(fmaxf(red[0][col], red[1][col]), fmaxf(red[2][col], red[3][col])) - (DYN ? pq::PQ_UP : 0.0f), neg = first ? TK_NONE : neg_m[lane];
           const bool none = neg == TK_NONE, up = none ? top_c > -INFINITY : top_c + neg > TK_LAZY;
-          const float m_new = ceilf(top_c);
+          const float m_new = ceilf(top_c) - (none && i0 + T < n_tiles ? 0.0f : TK_LIFT);
           if (!first) {  // 2^d for the sums; those of own steps, whose references may lie further apart than fp32 reaches, take it in two factors
             const float d = up ? (none ? -INFINITY : -neg - m_new) : 0.0f;
             moved[lane] = pq::ex2_approx(DYN ? fmaxf(d, -120.0f) : d);
