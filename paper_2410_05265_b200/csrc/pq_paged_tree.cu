@@ -54,8 +54,8 @@ constexpr int TK_PIECE = 15;      // units that cutting an item costs
 constexpr int TK_LEAST = 5;       // units of a stretch at least (eleven, an item of one tile: 3 x 26 rows at 1513 keys 23 us for 18, 2 x 18 at 3723 24 for 19)
 constexpr float TK_LAZY = 15.0f;
 // A first cached key often draws most of the weight and has a small value: what the others' weights keep of their bits is then what the output keeps. So the tiles of first
-// keys are an item's last, and a reference that moves to a key so far above the others, or is set by a group's last tile, stays TK_LIFT below it: nothing higher is
-// expected, and the other keys of that tile keep all their bits to 2^-27 of its weight and multiples of 2^-37 of it below.
+// keys are an item's last, and a reference that moves to a key so far above the others, or is set by a group's last tile or by one of first keys, stays TK_LIFT below
+// it: nothing higher is expected, and the other keys of that tile keep all their bits to 2^-27 of its weight and multiples of 2^-37 of it below.
 constexpr float TK_LIFT = 14.0f;
 constexpr float TK_NONE = 3.0e38f;  // in place of -m of a column that has seen no key: whatever it sees first exceeds the reference
 constexpr int TK_TICKET0 = PQ_PAGED_TICKET0 + PQ_PAGED_MAX_WORKERS;
@@ -664,7 +664,7 @@ __global__ void __launch_bounds__(TkShape<NC>::THREADS, TkShape<NC>::CTAS) paged
           const int col = col0 + lane;  // a lane per column, all four warps alike
           const float top_c = fmaxf(fmaxf(red[0][col], red[1][col]), fmaxf(red[2][col], red[3][col])) - (DYN ? pq::PQ_UP : 0.0f), neg = first ? TK_NONE : neg_m[lane];
           const bool none = neg == TK_NONE, up = none ? top_c > -INFINITY : top_c + neg > TK_LAZY;
-          const float m_new = ceilf(top_c) - (none && i0 + T < n_tiles ? 0.0f : TK_LIFT);
+          const float m_new = ceilf(top_c) - (none && i0 + T < n_tiles && x.j0 + i0 + first_of(x) < x.tiles ? 0.0f : TK_LIFT);
           if (!first) {  // 2^d for the sums; those of own steps, whose references may lie further apart than fp32 reaches, take it in two factors
             const float d = up ? (none ? -INFINITY : -neg - m_new) : 0.0f;
             moved[lane] = pq::ex2_approx(DYN ? fmaxf(d, -120.0f) : d);

@@ -52,3 +52,19 @@ def test_several_first_keys_share_the_weight(ctx):
         out = ctx.attn_kv4_paged_tree(cache, q, i32(begin), 20, ref.words_of(trees, 1, 20), first_keys.LN2, ws)
         assert ctx.check_status() == 0
         first_keys.assert_within(out, want, tol, 20)
+
+
+@pytest.mark.parametrize("steps", ["head", "vector"])
+@pytest.mark.parametrize("above", [20.0, 26.0])
+@pytest.mark.parametrize("lengths,new,Hq,Hkv", [([2900], [40], 8, 2), ([5000, 1700], [100, 30], 5, 1), ([1500] * 40, [30] * 40, 8, 2)])
+def test_several_tiles_of_first_keys(ctx, lengths, new, Hq, Hkv, above, steps):
+    """Some of them begin a worker's share of an item: what sets the reference there is the heavy key's tile, and others follow."""
+    window, n_sink, where = 300, 900, 3
+    cache = first_keys.make(lengths, Hq, Hkv, steps, 0, above, where)
+    begin, trees = begins(new), see(new, 3)
+    q, N = first_keys.ones(begin[-1], Hq), begin[-1]
+    want, tol = first_keys.bounds(cache, q, begin, lengths, above, where, window, n_sink, trees)
+    ws = ctx.attn_kv4_paged_tree_workspace(cache, N, max(new))
+    out = ctx.attn_kv4_paged_tree(cache, q, i32(begin), max(new), ref.words_of(trees, 4, N), first_keys.LN2, ws, window=window, n_sink=n_sink, max_len=max(lengths))
+    assert ctx.check_status() == 0
+    first_keys.assert_within(out, want, tol, N)
