@@ -64,6 +64,9 @@ constexpr float PP_LAZY = 15.0f;      // log2 units an exponent may exceed the r
 // largest exponent of an item's second tile lies more than PP_LOW below the reference, the reference goes down to it, by PP_FAR_.. at most (the sums, in fp32, grow by
 // that: of a prefix, whose values are fp16, to 2^102; of cached keys, whose denominators may be 2^60 already, to 2^107). Tried instead: the reference 8 or 10 below the largest exponent always, which moves again and again (4 ragged prompts 191 -> 226 and 242 us).
 constexpr float PP_LOW = 10.0f, PP_FAR_PREFIX = 80.0f, PP_FAR_CACHED = 40.0f;
+// Through a window the reference that moves to a key so far above the others, or is set by a tile of first keys, stays PP_LIFT below it: the other keys of that tile keep all
+// their bits to 2^-27 of its weight and multiples of 2^-37 of it below.
+constexpr float PP_LIFT = 14.0f;
 // Registers: 768 threads at 80; the softmax warpgroups take 96, the others leave 48 (512 x 96 + 256 x 48 = 768 x 80).
 constexpr int PP_REGS_SOFTMAX = 96, PP_REGS_OTHERS = 48;
 constexpr int PP_HALF_KEYS = PP_KEYS / 2;  // key columns of a softmax thread
@@ -158,7 +161,7 @@ struct PpItem {
   int base;             // cached keys before the new rows: len - n
   int tiles, j0, j1;    // key tiles of the item (the prefix first), and this worker's
   int u;                // unit where this worker's share begins (an item is PP_ITEM_UNITS units and its tiles)
-  int skip, n_window, lo;  // WIN: key tiles left out behind the first ones, those behind them, and the first key of the window of any row
+  int front, skip, n_window, lo;  // WIN: the window's first key tile, key tiles left out behind the first ones, those behind them, and the first key of the window of any row
 };
 
 // Of 64 columns a thread has 16, 8j + 2t and 8j + 2t + 1 as bits 2j, 2j + 1: how many of them lie before column x (any x).
@@ -250,17 +253,20 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
     }
     return u;
   };
-  // With a window an item takes its key tiles in another order: those of the window, the first ones, the prefix. Keys that stay visible often outweigh the others while
-  // their values are small; behind the others they move the reference of sums in fp32, in which those have kept their bits.
+  // With a window an item takes its key tiles in another order: those of the window, the first ones (without keys that stay visible the cache's first, where it is not left
+  // out), the prefix. First keys often outweigh the others while their values are small; behind the others they move the reference of sums in fp32, in which those have
+  // kept their bits.
   auto pre_tile = [&](const PpItem& x, int jt) { return has_prefix && jt == (WIN ? x.tiles - 1 : 0); };
+  auto front_of = [&](const PpItem& x) { return first_tiles > 0 ? first_tiles : x.skip == 0 ? 1 : 0; };
   auto key_of = [&](const PpItem& x, int jt) {  // first key of an item's tile jt, which is not the prefix
     if (!WIN) return (jt - has_prefix) * PP_KEYS;
-    return (jt < x.n_window ? first_tiles + x.skip + jt : jt - x.n_window) * PP_KEYS;
+    return (jt < x.n_window ? x.front + jt : jt - x.n_window) * PP_KEYS;
   };
   auto set_view = [&](PpItem& x) {
     if (!WIN) return;
     x.skip = skip_of(x, x.rt);
-    x.n_window = max(0, x.tiles - has_prefix - first_tiles);
+    x.n_window = max(0, x.tiles - has_prefix - front_of(x));
+    x.front = x.skip + front_of(x);
     x.lo = max(0, x.base - p.window + 1 + x.rt * R);
   };
   int32_t* scan = reinterpret_cast<int32_t*>(kv_buf);
@@ -639,7 +645,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prefill_kernel(const Page
           for (int k = 0; k < 4; ++k) {
             const float most = fmaxf(top[k], *const_cast<const volatile float*>(&bars->row[i][set ^ 1][fr + 8 * k]));
             const bool first = m_ref[k] == -INFINITY, move = most > (first ? -INFINITY : PP_LAZY) || (most < -PP_LOW && most != -INFINITY && lower);
-            const float m_new = move ? ceilf(first ? most : m_ref[k] + fmaxf(most, has_prefix ? -PP_FAR_PREFIX : -PP_FAR_CACHED)) : m_ref[k];
+            const float low = !WIN || (first && jt < x.n_window && jt + 1 < x.j1) ? 0.0f : PP_LIFT;
+            const float m_new = move ? ceilf(first ? most : m_ref[k] + fmaxf(most, has_prefix ? -PP_FAR_PREFIX : -PP_FAR_CACHED)) - low : m_ref[k];
             alpha[k] = move ? pq::ex2_approx(m_ref[k] - m_new) : 1.0f;  // 2^(-inf) = 0 for a row that had seen nothing
             l[k] = DYN && move ? pq::at_reference(l[k], m_ref[k] - m_new) : l[k] * alpha[k];
             m_ref[k] = m_new;
