@@ -422,9 +422,9 @@ pq_status pq_attn_kv4_paged(pq_ctx* ctx, const pq_kv4_paged* cache, const void* 
  *     j > c - window   or   j < n_sink
  *   window >= 1, n_sink >= 0; every other argument, the workspace and the limits as in pq_attn_kv4_paged, whose result a window of at least the capacity gives bit for
  * bit. Work and memory traffic are those of the visible keys, rounded up to tiles. Pages that no new token of their sequence sees any key of are not read, and
- * their table entries may hold anything. What draws most of the weight is often a first key whose value is small: in sequences of several rows a key among the first n_sink
- * (n_sink 0: the first 128) takes no bits of the other keys' weights, but for those beside it in its key tile of 128, which keep 11 bits down to 2^-27 of its weight and
- * multiples of 2^-37 of it below. */
+ * their table entries may hold anything. What draws most of the weight is often a first key whose value is small: a key among the first n_sink (in sequences of several
+ * rows and with n_sink 0, the first 128) takes no bits of the other keys' weights, but for those beside it in its key tile of 128 (for single tokens: the other first keys),
+ * which keep 11 bits down to 2^-27 of its weight and multiples of 2^-37 of it below. */
 pq_status pq_attn_kv4_paged_window(pq_ctx* ctx, const pq_kv4_paged* cache, const void* q, int64_t ldq, const int32_t* q_begin, int64_t n_rows,
                                    int32_t max_new, int32_t max_len, int32_t window, int32_t n_sink, void* out, float sm_scale, void* ws, size_t ws_bytes,
                                    void* stream);

@@ -5,8 +5,8 @@
 // slots). A long cache streams at 0.72 of the measured copy rate and a call costs 20 - 26 us besides (prefix sums 2, first blocks 3.5, a stretch's
 // pieces merged 2 - 6 each, the joined pairs 2, CTAs of an SM that end one after another). 48 ragged sequences to 6000 tokens, 32 heads on 8: 64 us
 // (own steps), 56 (static); 5 ragged to 50000, 64 heads: 60; one of 1021: 6.7.
-// Through a window (WIN) the keys between the first ones that stay visible and the window are left out in groups of 16, the unit of a copy, and the rest is numbered on, so that
-// work, stretches and blocks are those of the visible keys; one block has the seam and masks it. 64 ragged sequences to 16000 tokens, window 4096, own steps: 87 us for
+// Through a window (WIN) the keys between the first ones that stay visible and the window are left out in groups of 16, the unit of a copy, and the rest is numbered on, the
+// first keys behind the window's (window_view), so that work, stretches and blocks are those of the visible keys; the window's first and last blocks are masked. 64 ragged sequences to 16000 tokens, window 4096, own steps: 87 us for
 // 286 MB, as a cache of that length without a window; one of 30000 tokens, window 4096: 7.4.
 // Tried: rings of three and four blocks, five CTAs to an SM (no difference), multiplications for the shifts (slower), clusters of 1, 2 and 4 where 8 are
 // taken (2 % either way), longer stretches for the CTAs that an SM favours (2 - 5 % faster with eight heads to a group of four, 3 % slower with more).
@@ -42,6 +42,9 @@ constexpr int DP_ROWS = 8;     // query heads per KV head the MMA tile carries
 constexpr int DP_SO_STRIDE = 136;
 constexpr float DP_HEADROOM = 15.0f;  // log2 units: weights stay below 2^16, inside fp16
 constexpr int DP_SLOTS = 2;           // staged blocks per warp
+constexpr float DP_LIFT = 14.0f;      // a reference that moves to a first key stays so far below it: the others of its block keep multiples of 2^-38 of its weight
+// Forms: without a window, through one, through one with first keys that stay visible.
+constexpr int PLAIN = 0, WINDOW = 1, WINDOW_FIRST = 2;
 
 // Bytes of a staging slot: 32 rows of keys, 32 rows of values, with own steps 32 + 32 floats.
 __host__ __device__ constexpr int slot_bytes(bool dyn) { return DP_BLOCK * 128 + (dyn ? DP_BLOCK * 8 : 0); }
@@ -61,6 +64,14 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1,
 // Two codes of a word as (code + 8) 2^-24 (nibbles 0 and 4) and (code + 8) 2^-20 (nibbles 1 and 5), fp16 subnormals: their bits are the numbers.
 __device__ __forceinline__ uint32_t codes_lo(uint32_t w) { return pq::and_xor<0x000F000Fu, 0x00080008u>(w); }
 __device__ __forceinline__ uint32_t codes_hi(uint32_t w) { return pq::and_xor<0x00F000F0u, 0x00800080u>(w); }
+// The same without the offset: code 2^-24 and code 2^-20.
+__device__ __forceinline__ uint32_t less_f16(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint32_t exact_lo(uint32_t w) { return less_f16(codes_lo(w), 0x00080008u); }
+__device__ __forceinline__ uint32_t exact_hi(uint32_t w) { return less_f16(codes_hi(w), 0x00800080u); }
 __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t a) {
   uint32_t d;
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
@@ -100,23 +111,26 @@ __device__ __forceinline__ bool odd_rows(const PagedAttnParams& p, int r0, int r
   return n > p.max_new || n < 0 || (n > 0 && (r0 < 0 || r1 > p.n_rows || bad_len));
 }
 
-// The cached keys that a windowed token sees, in the kernel's numbering: n_sink first ones, rounded up to a group of 16 (the unit of a copy), then those from the
-// group on that holds the window's first key. What lies between is `skip` keys that are neither requested nor counted as work; the keys hid0 .. hid1 - 1
-// (fewer than 32, at the seam) are brought in and masked. Every group that is brought in holds a key the token sees.
+// The cached keys that a windowed token sees, in the kernel's numbering: those of the window (but for the first n_sink), from the group of 16 (the unit of a copy) on that
+// holds the first of them, then, from a whole block on, the first n_sink ones. What lies between is neither requested nor counted as work; a group at the border that both
+// parts need is brought in twice. First keys often outweigh the others while their values are small: they come last and in blocks of their own, where the reference may
+// move to them and the values are taken without the offset, so that the sums so far keep their bits.
 struct WindowView {
-  int len, skip, sink16, hid0, hid1;
+  int len, lo, n;  // keys in all; place of the window's first key, and keys from its group on
 };
+__device__ __forceinline__ int whole_blocks(int n) { return (n + DP_BLOCK - 1) & ~(DP_BLOCK - 1); }
+template <int WIN>
 __device__ __forceinline__ WindowView window_view(const PagedAttnParams& p, int len) {
-  const int lo = max(0, len - p.window);
+  const int n_first = WIN == WINDOW_FIRST ? p.n_sink : 0;
   WindowView v;
-  v.sink16 = (p.n_sink + 15) & ~15;
-  v.skip = max(0, lo - v.sink16) & ~15;
-  v.len = len - v.skip, v.hid0 = p.n_sink, v.hid1 = lo - v.skip;
+  v.lo = max(len - p.window, n_first);
+  v.n = len > n_first ? len - (v.lo & ~15) : 0;
+  v.len = WIN == WINDOW_FIRST ? whole_blocks(v.n) + min(len, n_first) : v.n;
   return v;
 }
 
-// WIDE: clusters of sixteen, for a few long sequences (their merge in the other kernel would cost it registers). WIN: a window over the cached keys.
-template <bool DYN, bool WIDE, bool POLL, bool WIN>
+// WIDE: clusters of sixteen, for a few long sequences (their merge in the other kernel would cost it registers). WIN: the form.
+template <bool DYN, bool WIDE, bool POLL, int WIN>
 __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const PagedAttnParams p) {
   constexpr int SLOT = slot_bytes(DYN);
   extern __shared__ __align__(128) uint8_t dp_smem[];
@@ -170,7 +184,7 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
     if (threadIdx.x == 0 && odd_rows(p, r0, r1, l != len_direct)) pq::report(p.status, PQ_ERR_SHAPE);
     if (!one_row(p, r0, r1)) return leave();  // the whole cluster alike
     row_direct = r0;
-    u1 = max(1, ((WIN ? window_view(p, len_direct).len : len_direct) + DP_ROUND - 1) / DP_ROUND);
+    u1 = max(1, ((WIN != PLAIN ? window_view<WIN>(p, len_direct).len : len_direct) + DP_ROUND - 1) / DP_ROUND);
     __syncwarp();
   } else {
     bool odd = false;
@@ -179,7 +193,7 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
       const int r0 = pq::ld_dep(p.q_begin + b), r1 = pq::ld_dep(p.q_begin + b + 1);
       odd |= odd_rows(p, r0, r1, l != lc);
       lens[b] = lc, rows[b] = r0;
-      scan[b] = one_row(p, r0, r1) ? max(1, ((WIN ? window_view(p, lc).len : lc) + DP_ROUND - 1) / DP_ROUND) : 0;
+      scan[b] = one_row(p, r0, r1) ? max(1, ((WIN != PLAIN ? window_view<WIN>(p, lc).len : lc) + DP_ROUND - 1) / DP_ROUND) : 0;
     }
     __syncthreads();
     const int64_t total = pq::block_scan<DP_THREADS>(scan, p.B, part) * p.Hkv;
@@ -194,13 +208,13 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
   }
   struct Piece {
     int b, h, r0, r1, rounds, len;  // rounds r0 .. r1 - 1 of the `rounds` of the pair
-    int skip, hid1;                 // WIN, with len in the numbering of the window
+    int lo, n;                      // through a window, with len in its numbering
   };
   auto set_len = [&](Piece& x, int len) {
     x.len = len;
-    if (WIN) {
-      const WindowView v = window_view(p, len);
-      x.len = v.len, x.skip = v.skip, x.hid1 = v.hid1;
+    if (WIN != PLAIN) {
+      const WindowView v = window_view<WIN>(p, len);
+      x.len = v.len, x.lo = v.lo, x.n = v.n;
     }
   };
   auto first_piece = [&]() {
@@ -248,12 +262,16 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
   const int64_t page_bytes = static_cast<int64_t>(p.Hkv * 2 * cp_unit) << page_log2;
   const uint8_t* is_src = cp_base;  // the head's rows inside a page
   const int32_t* is_row = p.table;
-  const int sink16 = WIN ? (p.n_sink + 15) & ~15 : 0;
-  auto place_of = [&](int k) { return WIN && k >= sink16 ? k + is_piece.skip : k; };
+  auto place_of = [&](int k) {
+    if (WIN == WINDOW_FIRST && k >= is_piece.n) return k - whole_blocks(is_piece.n);
+    return WIN != PLAIN ? (is_piece.lo & ~15) + k : k;
+  };
+  // Is the group of 16 at k requested: not what fills up the window's last block.
+  auto wanted = [&](int k) { return k < is_end && (WIN != WINDOW_FIRST || k < is_piece.n || k >= whole_blocks(is_piece.n)); };
   // The page of this lane's group of the cursor's block. An id that is none is reported and page 0 read in its place.
   auto fetch_id = [&]() {
     const int k = is_key + 16 * cp_group;
-    is_id = cp_lane && k < is_end ? pq::ld_dep(is_row + (place_of(k) >> page_log2)) : -1;
+    is_id = cp_lane && wanted(k) ? pq::ld_dep(is_row + (place_of(k) >> page_log2)) : -1;
   };
   auto next_piece = [&]() {
     is_ok = false;
@@ -276,9 +294,9 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
     if (!is_ok) return;
     const int s = n_issued % DP_SLOTS, k = is_key + 16 * cp_group;
     uint64_t* bar = &full[warp][s];
-    const bool both = is_key + 16 < is_end;
+    const bool both = wanted(is_key + 16);
     if (lane == 0) pq::mbar_arrive_expect_tx(bar, (both ? 2u : 1u) * (2 * 1024 + (DYN ? 2 * 64 : 0)));
-    if (cp_lane && k < is_end) {
+    if (cp_lane && wanted(k)) {
       if (static_cast<uint32_t>(is_id) >= static_cast<uint32_t>(p.n_pages)) {
         pq::report(p.status, PQ_ERR_SHAPE);
         is_id = 0;
@@ -397,7 +415,7 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
     float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    float den0 = 0.0f, den1 = 0.0f;  // DYN: this lane's shares of the denominators of heads 2t, 2t+1
+    float den0 = 0.0f, den1 = 0.0f;  // this lane's shares of the denominators of heads 2t, 2t+1: DYN of all keys, else of first keys
 
     const uint32_t k_off = g * 64 + 16 * t;      // key g (and g + 8): 32 codes at dims 32t..32t+31
     const uint32_t v_off = (2 * t) * 64 + 8 * g;  // keys 2t, 2t+1, 2t+8, 2t+9: 16 codes at dims 16g..16g+15
@@ -418,7 +436,7 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
         // end has the score -inf
         const float* st = reinterpret_cast<const float*>(slot + DP_BLOCK * 128) + lane;
         const float k_step = st[0], v_step = st[DP_BLOCK];
-        const bool dead = key0 + lane >= kend || (WIN && key0 + lane >= p.n_sink && key0 + lane < x.hid1);
+        const bool dead = key0 + lane >= kend || (WIN != PLAIN && key0 < x.n && (key0 + lane < (x.lo & 15) || key0 + lane >= x.n));
         sm_step[warp][lane] = dead ? make_float4(0.0f, -INFINITY, 0.0f, 0.0f) : make_float4(k_step, pq::lg2_approx(v_step), pq::rcp_approx(v_step) * pq::PQ_DOWN, 0.0f);
         __syncwarp();
       }
@@ -450,12 +468,12 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
           if (key0 + 16 * v + 8 + g >= kend) c[v][2] = c[v][3] = -INFINITY;
         }
       }
-      if (WIN && !DYN && key0 < x.hid1 && key0 + DP_BLOCK > p.n_sink) {  // the seam between the first keys and the window
+      if (WIN != PLAIN && !DYN && key0 < x.n && (key0 == 0 || (WIN == WINDOW_FIRST && key0 + DP_BLOCK > x.n))) {  // the window's first block, its last
 #pragma unroll
         for (int v = 0; v < 2; ++v) {
           const int k = key0 + 16 * v + g;
-          if (k >= p.n_sink && k < x.hid1) c[v][0] = c[v][1] = -INFINITY;
-          if (k + 8 >= p.n_sink && k + 8 < x.hid1) c[v][2] = c[v][3] = -INFINITY;
+          if (k < (x.lo & 15) || k >= x.n) c[v][0] = c[v][1] = -INFINITY;
+          if (k + 8 < (x.lo & 15) || k + 8 >= x.n) c[v][2] = c[v][3] = -INFINITY;
         }
       }
       // maxima of heads 2t, 2t+1 over this lane's keys; a reference moves only when one exceeds it by more than the headroom (the first
@@ -467,12 +485,12 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
           x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, d));
           x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, d));
         }
-        const float n0 = fmaxf(m0, x0), n1 = fmaxf(m1, x1);
+        const float lift = WIN == WINDOW_FIRST && key0 >= x.n ? DP_LIFT : 0.0f, n0 = fmaxf(m0, x0 - lift), n1 = fmaxf(m1, x1 - lift);
         const float d_lo = n0 == -INFINITY ? 0.0f : m0 - n0, d_hi = n1 == -INFINITY ? 0.0f : m1 - n1;
         const float a_lo = pq::ex2_approx(d_lo), a_hi = pq::ex2_approx(d_hi);
         m0 = n0, m1 = n1;
         zero[0] *= a_lo, zero[1] *= a_hi, zero[2] *= a_lo, zero[3] *= a_hi;
-        if (DYN) den0 = pq::at_reference(den0, d_lo), den1 = pq::at_reference(den1, d_hi);
+        if (DYN || WIN == WINDOW_FIRST) den0 = pq::at_reference(den0, d_lo), den1 = pq::at_reference(den1, d_hi);
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[i][0] *= a_lo, o[i][1] *= a_hi, o[i][2] *= a_lo, o[i][3] *= a_hi;
         z0 = m0 == -INFINITY ? 0.0f : m0, z1 = m1 == -INFINITY ? 0.0f : m1;
@@ -490,6 +508,18 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
         if (DYN) {
           den0 = fmaf(w0, rs[v][0], den0), den1 = fmaf(w1, rs[v][0], den1);
           den0 = fmaf(w2, rs[v][1], den0), den1 = fmaf(w3, rs[v][1], den1);
+        }
+        if (WIN == WINDOW_FIRST && key0 >= x.n) {  // first keys: without the offset
+          if (!DYN) den0 += w0 + w2, den1 += w1 + w3;
+#pragma unroll
+          for (int q4 = 0; q4 < 4; ++q4) {
+            const uint32_t sel = (q4 & 1) ? 0x7632u : 0x5410u;
+            const uint32_t ya = __byte_perm(q4 < 2 ? vc0.x : vc0.y, q4 < 2 ? vc1.x : vc1.y, sel);
+            const uint32_t yb = __byte_perm(q4 < 2 ? vc2.x : vc2.y, q4 < 2 ? vc3.x : vc3.y, sel);
+            mma_f16(o[2 * q4], exact_lo(ya), exact_hi(ya), exact_lo(yb), exact_hi(yb), pb0, pb1);
+            mma_f16(o[2 * q4 + 1], exact_lo(ya >> 8), exact_hi(ya >> 8), exact_lo(yb >> 8), exact_hi(yb >> 8), pb0, pb1);
+          }
+          continue;
         }
         mma_f16(zero, codes_lo(0u), codes_hi(0u), codes_lo(0u), codes_hi(0u), pb0, pb1);
         // ---- O^T += V^T P^T. A merged word pairs the same four dims of two neighbouring keys; nibbles 1 and 3 (16 x) are the rows g + 8 of the tile.
@@ -529,15 +559,14 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
           *reinterpret_cast<float2*>(sm_o + (warp * G + head) * DP_SO_STRIDE + 16 * m + 2 * g) = make_float2((o[m][hh] - zero[hh]) * 16777216.0f, (o[m][2 + hh] - zero[2 + hh]) * 1048576.0f);
       }
     }
-    if (DYN) {
+    if (DYN || WIN == WINDOW_FIRST) {
 #pragma unroll
       for (int d = 4; d < 32; d <<= 1) {
         den0 += __shfl_xor_sync(0xffffffffu, den0, d);
         den1 += __shfl_xor_sync(0xffffffffu, den1, d);
       }
-    } else {
-      den0 = zero[0] * 2097152.0f, den1 = zero[1] * 2097152.0f;  // 2^24 / 8
     }
+    if (!DYN) den0 += zero[0] * 2097152.0f, den1 += zero[1] * 2097152.0f;  // 2^24 / 8
     if (g == 0) {
       if (2 * t < G) sm_ml[warp][2 * t][0] = m0, sm_ml[warp][2 * t][1] = den0;
       if (2 * t + 1 < G) sm_ml[warp][2 * t + 1][0] = m1, sm_ml[warp][2 * t + 1][1] = den1;
@@ -703,20 +732,22 @@ __global__ void __launch_bounds__(DP_THREADS, 4) paged_decode_kernel(const Paged
 
 constexpr int DP_CTAS_PER_SM = 4;
 
-template <bool WIN>
+template <int WIN>
 void (*kernel_of_form(bool dyn, int csize, bool poll))(const PagedAttnParams) {
   if (poll) return dyn ? paged_decode_kernel<true, true, true, WIN> : paged_decode_kernel<false, true, true, WIN>;  // (any cluster size)
   if (csize > 8) return dyn ? paged_decode_kernel<true, true, false, WIN> : paged_decode_kernel<false, true, false, WIN>;
   return dyn ? paged_decode_kernel<true, false, false, WIN> : paged_decode_kernel<false, false, false, WIN>;
 }
-void (*kernel_of(bool dyn, bool win, int csize, bool poll))(const PagedAttnParams) { return win ? kernel_of_form<true>(dyn, csize, poll) : kernel_of_form<false>(dyn, csize, poll); }
+void (*kernel_of(bool dyn, int win, int csize, bool poll))(const PagedAttnParams) {
+  return (win == PLAIN ? kernel_of_form<PLAIN> : win == WINDOW ? kernel_of_form<WINDOW> : kernel_of_form<WINDOW_FIRST>)(dyn, csize, poll);
+}
 
 int most_ctas(const pq_ctx* ctx) { return DP_CTAS_PER_SM * ctx->sm_count; }
 
 // Clusters of csize CTAs that are resident at once: fewer than the CTAs alone would be, since a cluster stays inside a group of SMs. Asked once per
 // device, kernel, cluster size and size of the shared memory in whole KB: the answer, and with it how the work is split, follows from the call alone.
-int resident_workers(const pq_ctx* ctx, bool dyn, bool win, int csize, size_t smem) {
-  static std::atomic<uint16_t> known[64][2][2][5][DP_MAX_KB + 1] = {};  // one more than the answer
+int resident_workers(const pq_ctx* ctx, bool dyn, int win, int csize, size_t smem) {
+  static std::atomic<uint16_t> known[64][2][3][5][DP_MAX_KB + 1] = {};  // one more than the answer
   const int ci = csize == 16 ? 4 : csize == 8 ? 3 : csize == 4 ? 2 : csize == 2 ? 1 : 0;
   std::atomic<uint16_t>& slot = known[ctx->device][dyn][win][ci][smem_kb(smem)];
   int n = slot.load(std::memory_order_relaxed);
@@ -746,10 +777,12 @@ size_t pq_paged_decode_ws_bytes(const pq_ctx* ctx, const pq_kv4_paged* c) {
 }
 
 pq_status pq_paged_decode_launch(pq_ctx* ctx, const pq_kv4_paged* c, PagedAttnParams p, int64_t max_len, void* ws, cudaStream_t st) {
-  const bool dyn = p.steps != nullptr, win = p.window > 0, poll = p.wait_clocks < PQ_SUSPENDED_CLOCKS;
-  if (win && max_len > static_cast<int64_t>(p.window) + p.n_sink + 30) max_len = static_cast<int64_t>(p.window) + p.n_sink + 30;  // (what window_view leaves at most)
+  const bool dyn = p.steps != nullptr, poll = p.wait_clocks < PQ_SUSPENDED_CLOCKS;
+  const int win = p.window == 0 ? PLAIN : p.n_sink == 0 ? WINDOW : WINDOW_FIRST;
+  const int64_t most_seen = static_cast<int64_t>(p.window) + p.n_sink + 46;  // (what window_view leaves at most)
+  if (win != PLAIN && max_len > most_seen) max_len = most_seen;
   // the largest there is, once per device and kernel
-  static std::atomic<bool> attr_set[64][2][2] = {};
+  static std::atomic<bool> attr_set[64][2][3] = {};
   if (ctx->device < 0 || ctx->device >= 64) return PQ_ERR_UNSUPPORTED;
   if (!attr_set[ctx->device][dyn][win].load(std::memory_order_relaxed)) {
     const int most = static_cast<int>(DP_MAX_KB * 1024);

@@ -33,14 +33,15 @@ def ones(rows, Hq):
     return q
 
 
-def bounds(cache, q, begin, lengths, above, where, window=0, n_sink=0, trees=None, n=1, near_keys=128, near=2.0**-38, near_prefix=False):
+def bounds(cache, q, begin, lengths, above, where, window=0, n_sink=0, trees=None, n=1, near_keys=128, near=2.0**-38, near_prefix=False, code8=False):
     """(outputs in 64 bits, tolerance).
 
     A relative error e of the weights moves the quotient by at most e (sum p |v| + |out|), p the softmax in 64 bits: e is 2^-11 for a weight's rounding to fp16 and 2^-17 for
     its exponent (a score of at most 32 is a product of three factors rounded to fp32 and a difference: 4 x 2^-24 x 32 ln 2, and 2^-22 of 2^x). The keys that share the
     heavy key's tile, the first `near_keys` ones, may be rounded against its reference instead, in multiples of 2^-24: each off by 2^-25 of it, `near` of the heavy key's
-    weight where the reference lies 13 octaves below that (times its value's step, which the exponents carry); with `near_prefix` so may the prefixed ones. The store
-    rounds by 2^-8."""
+    weight where the reference lies 13 octaves below that (times its value's step, which the exponents carry); with `near_prefix` so may the prefixed ones.
+    With `code8` (single tokens) the keys but the heavy ones are multiplied as code + 8 and 8 sum(p) is taken off, in fp32 sums of equal terms: each of the 16 products of a
+    step and the sum so far is off by 2^-23 of 8 p per key. The store rounds by 2^-8."""
     want, _ = ref.attention(cache, q, begin, lengths, LN2, window, n_sink, trees)
     tol, pages, G = torch.zeros_like(want), cache.pages, cache.Hq // cache.Hkv
     table = pages.table.tolist()
@@ -67,6 +68,8 @@ def bounds(cache, q, begin, lengths, above, where, window=0, n_sink=0, trees=Non
                 here = near * 2.0**above * p * step * (codes[seen & (torch.arange(n_keys, device=want.device) < near_keys)].sum(0) + (pre if near_prefix else 0.0))
             wide = lambda x: x[:, None].expand(-1, G, -1).reshape(cache.Hq, 128)
             r = begin[b] + t
+            if code8:
+                here = here + 17 * 8 * 2.0**-23 * others * p * unit.max()
             tol[r] = (2.0**-11 + 2.0**-17) * (wide(a) + want[r].abs()) + wide(here) + want[r].abs() * 2.0**-8 + 2.0**-125
     return want, tol
 
