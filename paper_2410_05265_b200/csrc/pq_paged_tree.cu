@@ -43,13 +43,14 @@
 #include <type_traits>
 
 #include "pq_paged_mma.cuh"
+#include "pq_tree_form.cuh"
 
 namespace {
 
-constexpr int TK_KEYS = 128;
+constexpr int TK_KEYS = pq_tree::KEYS;
 constexpr int TK_COLS = 32;  // columns of a softmax thread
 constexpr int TK_ITEM_UNITS = 10;  // units that an item costs besides its key tiles
-constexpr int TK_SHORT = 8;       // an item of so many key tiles or fewer is not shared between workers
+constexpr int TK_SHORT = pq_tree::SHORT;
 constexpr int TK_PIECE = 15;      // units that cutting an item costs
 constexpr int TK_LEAST = 5;       // units of a stretch at least (eleven, an item of one tile: 3 x 26 rows at 1513 keys 23 us for 18, 2 x 18 at 3723 24 for 19)
 constexpr float TK_LAZY = 15.0f;
@@ -129,7 +130,12 @@ constexpr size_t tk_smem_bytes(bool dyn, int n_prefix) {
          sizeof(TkState<NC>) + static_cast<size_t>(NC) * ((n_prefix + 3) / 4 * 4) * 4;
 }
 static_assert(tk_smem_bytes<128>(true, PQ_PAGED_MAX_PREFIX) <= 227 * 1024, "shared memory budget");
-static_assert(tk_smem_bytes<64>(true, 12) <= 113 * 1024 && tk_smem_bytes<32>(true, 12) <= 113 * 1024, "shared memory of two CTAs (longer prefixes: of one)");
+// Two CTAs of an SM have 113 KB each: as long a prefix as the rule says, and none longer.
+template <int NC, bool DYN>
+constexpr bool tk_two_ctas() {
+  return tk_smem_bytes<NC>(DYN, pq_tree::two_ctas_prefix(NC, DYN)) <= 113 * 1024 && tk_smem_bytes<NC>(DYN, pq_tree::two_ctas_prefix(NC, DYN) + 1) > 113 * 1024;
+}
+static_assert(tk_two_ctas<32, false>() && tk_two_ctas<32, true>() && tk_two_ctas<64, false>() && tk_two_ctas<64, true>(), "CTAs of an SM");
 static_assert(2 * (PQ_PAGED_MAX_SEQS + 1) * 4 <= 16 * 1024 + 16 * 1024 + 4 * TK_LAND_CODES && 2 * (PQ_PAGED_MAX_SEQS + 1) * 4 <= 32 * 1024 + 16 * 1024 + 3 * TK_LAND_CODES,
               "the prefix sums lie in the buffers of Q, P and the packed rows before the pipeline starts");
 
@@ -1200,28 +1206,15 @@ struct TkForm {
 };
 template <int NC, bool POLL>
 TkForm form(bool dyn, int n_prefix) {
-  return {dyn ? paged_tree_kernel<NC, true, POLL> : paged_tree_kernel<NC, false, POLL>, NC, TkShape<NC>::CTAS, TkShape<NC>::THREADS, tk_smem_bytes<NC>(dyn, n_prefix),
+  return {dyn ? paged_tree_kernel<NC, true, POLL> : paged_tree_kernel<NC, false, POLL>, NC, pq_tree::ctas_of_sm(NC, dyn, n_prefix), TkShape<NC>::THREADS, tk_smem_bytes<NC>(dyn, n_prefix),
           tk_smem_bytes<NC>(dyn, PQ_PAGED_MAX_PREFIX)};
 }
-// How many columns: by an estimate for B sequences of max_new rows and max_len cached keys, fitted to 176 ragged batches of 1 to 48 sequences (on their average 1 % above the
-// best of the three, 35 % at most). An item costs its key tiles and 4 to 6 more of 1.5 us with 32 columns, 2.2 with 64 (two CTAs share the SM) and 1.9 with 128; short items are
-// not cut, so that CTAs walk whole rounds of them; and with long ones a stretch is no shorter than a short item. us with 32 / 64 / 128 columns, 32 heads on 8: 1 x 26
-// rows at 1021 keys 18 / 22 / 24, at 4000 23 / 30 / 33; 1 x 128 at 20000 106 / 82 / 74; 16 x 16 at 4000 55 / 52 / 56, 64 x 8 at 6000 139 / 170 / 250, 32 x 30 at 4000
-// 185 / 136 / 123. Short wait limits take the polling form, of 128 columns whatever the rows.
+// Short wait limits take the polling form, of 128 columns whatever the rows.
 TkForm form_of(const pq_ctx* ctx, const PagedAttnParams& p, int64_t max_len) {
   const bool dyn = p.steps != nullptr;
   if (p.wait_clocks < PQ_SUSPENDED_CLOCKS) return form<128, true>(dyn, p.n_prefix);
-  const double tiles = static_cast<double>(max_len < TK_KEYS ? 1 : (max_len + TK_KEYS - 1) / TK_KEYS);
-  auto estimate = [&](int nc, int ctas, double fixed, double more, double tile) {
-    const int per_item = nc / p.G;
-    const int64_t items = static_cast<int64_t>(p.B) * p.Hkv * ((p.max_new + per_item - 1) / per_item), workers = static_cast<int64_t>(ctas) * ctx->sm_count;
-    const double least = TK_SHORT + more, share = static_cast<double>(items) / workers * (tiles + more);
-    const double units = tiles <= TK_SHORT ? static_cast<double>((items + workers - 1) / workers) * (tiles + more) : share > least ? share : least;
-    return fixed + units * tile;
-  };
-  const double t32 = estimate(32, 2, 3.0, 5.0, 1.5), t64 = estimate(64, 2, 2.0, 4.0, 2.2), t128 = estimate(128, 1, 0.0, 6.0, 1.9);
-  if (t32 <= t64 && t32 <= t128) return form<32, false>(dyn, p.n_prefix);
-  return t64 <= t128 ? form<64, false>(dyn, p.n_prefix) : form<128, false>(dyn, p.n_prefix);
+  const int columns = pq_tree::columns_of(dyn, p.n_prefix, ctx->sm_count, p.B, p.Hkv, p.G, p.max_new, max_len, p.window, p.n_sink);
+  return columns == 32 ? form<32, false>(dyn, p.n_prefix) : columns == 64 ? form<64, false>(dyn, p.n_prefix) : form<128, false>(dyn, p.n_prefix);
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
@@ -1233,7 +1226,6 @@ size_t pq_paged_tree_ws_bytes(const pq_ctx* ctx) { return static_cast<size_t>(2)
 
 pq_status pq_paged_tree_launch(pq_ctx* ctx, PagedAttnParams p, int64_t max_len, void* ws, cudaStream_t st) {
   const bool dyn = p.steps != nullptr, poll = p.wait_clocks < PQ_SUSPENDED_CLOCKS;
-  if (p.window > 0 && max_len > static_cast<int64_t>(p.window) + p.n_sink + 3 * TK_KEYS) max_len = static_cast<int64_t>(p.window) + p.n_sink + 3 * TK_KEYS;  // (about what a window leaves)
   const TkForm f = form_of(ctx, p, max_len);
   if (ctx->device < 0 || ctx->device >= 64 || 2 * ctx->sm_count > PQ_PAGED_MAX_WORKERS) return PQ_ERR_UNSUPPORTED;
   static std::atomic<bool> attr_set[64][2][4] = {};  // the largest there is, once per device and kernel
