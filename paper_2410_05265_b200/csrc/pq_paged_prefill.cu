@@ -31,8 +31,8 @@
 // steps 1815), 4096 rows x 64 heads 360 (453), 2048 rows 132 (154), 4 ragged prompts up to 2000 x 32 heads 162 (192), 515 rows 26 (29).
 // Through a window (WIN) an item walks the key tiles from the one with the first key of any row's window on, then those with keys that stay visible, then the prefix: the few keys
 // that may draw much weight come last, so that references rise to them and need not come down. A thread's visible columns are 16 bits a row, formed once for a tile that a
-// border crosses. 4 ragged prompts to 2900 rows, window 1000, 4 first keys, 32 heads, own steps: 340 us (with the first keys' and the prefix's tiles first, and masks by
-// comparisons, 404); 2048 rows behind 29952 keys, window 4096, 64 heads: 352, 0.46 of the measured bf16 rate on visible pairs; short items cost more of it (three of eleven
+// border crosses. 4 ragged prompts to 2900 rows, window 1000, 4 first keys, 32 heads, own steps: 335 us (with the first keys' and the prefix's tiles first, and masks by
+// comparisons, 404); 2048 rows behind 29952 keys, window 4096, 64 heads: 340, 0.48 of the measured bf16 rate on visible pairs; short items cost more of it (three of eleven
 // tiles are the prefix, the first keys and the border, and the item's own 10000 clocks are the time of two more).
 // Tried and slower: a thread per row (own steps 2011 us: the constants of 64 keys per thread), half tiles of 64 keys with the scores of two in flight,
 // row tiles that form their weights in turn (1631; 1573 with half of the pass shared), queries of later items brought in by the expansion warps (the same),

@@ -21,7 +21,8 @@
 //                     and an O^T of its own, joined at the item's end. Own steps are constants of the thread; masks are a bit per column. A column's reference
 //                     exponent m lies in shared memory and moves only when a score exceeds it by more than 15 (one vote of the set per tile): w = 2^(s + log2 step - m) goes
 //                     to P in fp16, the denominator (sum of w / step, fp32) stays in the thread until the item ends.
-//                     The tiles of an item are walked from the one behind the first keys on, those of the first keys last (TK_LIFT).
+//                     The tiles of an item are walked from the one behind the first keys on, those of the first keys last (TK_LIFT). What decides of
+//                     masks is formed once per item (the item's fields read in shared memory for every tile: 12 x 64 rows 311 -> 346 us).
 //   helper warp       queries and description of the next item; scores of the prefixed keys (bf16 MMA, the fp16 keys as two terms, fp32 sums), which join at the item's end
 //                     and never set a reference
 // Roundings to fewer bits: w to fp16 (2^-11; below 2^-14 in steps of 2^-24 of the reference's weight), the result to bf16. Every wait is bounded.
@@ -29,9 +30,11 @@
 // What bounds it. In principle HBM while rows x heads of a KV head are few (128 bytes of codes for 256 D flops a column), the tensor core and the special-function units at
 // 128 columns. In practice the instructions of the expansion and the softmax: a key tile takes 0.9 us of an SM with 32 columns, 1.15 with 64, 1.5 with 128 (own steps 1.1,
 // 1.6, 2.1); issue slots are 43 - 60 % busy, and with 32 columns warps wait for instructions (3.3 of 15 clocks between two of a warp) as long as for anything else, which is why
-// loops here are rolled where that costs nothing. 48 x 5 rows at 6000 keys, own steps, 32 heads on 8: 87 us, 2.2 TB/s of codes; 12 x 64 rows at 16000 keys, 64 heads on 8:
-// 290 us, 720 TFLOP/s of visible pairs, 0.43 of the measured bf16 rate; 16 x 33 rows through a window of 2048: 44; 1 x 26 rows at 1021 keys: 17, of which half are the
-// sums and first loads (2.9 us), the first tile (3) and the end of an item (4).
+// loops here are rolled where that costs nothing. 48 ragged x 5 rows at 6000 keys, own steps, 32 heads on 8: 90 us, 2.1 TB/s of codes; 12 ragged x 64 rows at 16000 keys,
+// 64 heads on 8: 294 to 310 us, 675 to 710 TFLOP/s of visible pairs, 0.40 to 0.42 of the measured bf16 rate; 16 ragged x 33 rows through a window of 2048: 45; 1 x 26 rows at
+// 1021 keys: 16.6 (17 rows 16.4), of which half are the sums and first loads (2.9 us), the first tile (3) and the end of an item (4); its eight tiles in turn are what keeps
+// it there, since an item so short is not cut and 24 to 32 CTAs have all the work.
+// The tiles of first keys behind the others, and references below a heavy first key, cost 1 to 3 %.
 // In place of this kernel: the prompts' kernel with these masks takes 30, 258, 331 and 75 us for 1 x 26, 48 x 5, 12 x 64 and the windowed 16 x 33 rows.
 // Tried and not kept: the softmax warps expand V for 32 columns (48 x 5: 99 us against 97), boxes issued by a lane each (three times as long), steps loaded by the
 // softmax threads, one loop over both prefix sums (no difference), the first reference from a key of every warp in place of the largest of all (static 0.2 us less, own steps 2 %
