@@ -7,8 +7,8 @@
 // (own steps), 56 (static); 5 ragged to 50000, 64 heads: 60; one of 1021: 6.7.
 // Through a window (WIN) the keys between the first ones that stay visible and the window are left out in groups of 16, the unit of a copy, and the rest is numbered on, the
 // first keys behind the window's (window_view), so that work, stretches and blocks are those of the visible keys; the window's first and last blocks are masked. 64 ragged
-// sequences to 16000 tokens, window 4096, own steps: 87 us for 286 MB, as a cache of that length without a window; one of 30000 tokens, window 1024: 7.1. One form for
-// windows with and without first keys took 95 us for the former.
+// sequences to 16000 tokens, window 4096, own steps: 87 us for 286 MB, as a cache of that length without a window; one of 30000 tokens, window 1024: 7.1. With four
+// first keys 90 (static steps 77.5, without them 73); one form for windows with and without first keys took 95 us for the former.
 // Tried: rings of three and four blocks, five CTAs to an SM (no difference), multiplications for the shifts (slower), clusters of 1, 2 and 4 where 8 are
 // taken (2 % either way), longer stretches for the CTAs that an SM favours (2 - 5 % faster with eight heads to a group of four, 3 % slower with more).
 //
